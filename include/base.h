@@ -120,7 +120,13 @@ enum {
     /* the same values permuted by base_pack_experts so that every MFMA
      * operand fragment of the FFN is one contiguous 1 KiB block and each
      * wavefront of the FFN reads one contiguous stream (bf16 only) */
-    BASE_W_PACKED = 1
+    BASE_W_PACKED = 1,
+    /* microscaled 4-bit weights (E2M1 codes, one E8M0 scale per 32 elements of a
+     * row), in the layout base_mx_pack_experts or base_mx_quantize_experts
+     * writes: base_mx_w13_bytes and base_mx_w2_bytes bytes.  x, y and the
+     * products' sums are those of a bf16 layer (dtype BASE_BF16) whose weights
+     * have these values. */
+    BASE_W_MXFP4 = 4
 };
 
 /* One MoE layer.  Host struct holding device pointers. */
@@ -141,8 +147,8 @@ typedef struct base_layer {
                                correction folded in, App. A), or log mu_u
                                for BASE_SCORE_STATIC; not read by the
                                router-only rules */
-    const void *w13;        /* [E][2I][d]: rows 0..I-1 gate, I..2I-1 up;
-                               16-B aligned */
+    const void *w13;        /* [E][2I][d]: rows 0..I-1 gate, I..2I-1 up, in
+                               layout w_layout; 16-B aligned */
     const void *w2;         /* [E][d][I] down projection; 16-B aligned */
     /* Shared experts: always active for every token, outside the budget
      * and the selection (the paper leaves them out of its notation, Sec.
@@ -314,6 +320,59 @@ base_status base_decode_layer_noalloc(const base_layer *L, const void *x, int32_
  * Returns BASE_ERR_DTYPE for fp32 layers. */
 base_status base_pack_experts(const base_layer *L, void *w13_packed,
                               void *w2_packed, void *stream);
+
+/* Microscaled 4-bit floating point.  A row is cut into blocks of 32
+ * consecutive elements; element i of a block stands for e2m1(code_i) *
+ * 2^(s - 127) with the block's scale byte s (E8M0) and a 4-bit code (E2M1: sign,
+ * then 0, 0.5, 1, 1.5, 2, 3, 4, 6).  Quantising a block takes
+ *   s = max(floor(log2 max |v|) - 2 + 127, 0)  (0 for a block of zeros),
+ *   code_i = v_i / 2^(s - 127) to the nearest E2M1 value, ties to the even code,
+ *   magnitudes beyond 6 to 6;
+ * a block that holds NaN or an infinity gets s = 255 and codes 0, and s = 255
+ * stands for NaN in all of the block's elements.  A row-major matrix [rows]
+ * [cols] (cols a multiple of 32) is held as codes [rows][cols / 2], the lower
+ * four bits of a byte the element of even index, and scales [rows][cols / 32]. */
+#define BASE_MX_MAX_ROWS 0x7FFFFFFFLL
+#define BASE_MX_MAX_COLS (1 << 24)
+#define BASE_MX_MAX_LD (1LL << 40)
+
+/*   src     [rows][cols] of `dtype`, rows src_ld >= cols elements apart
+ *   codes   out, 16-B aligned; scales out
+ * Any element-aligned src and src_ld; 16-byte accesses where both allow them.
+ * BASE_ERR_SHAPE for rows, cols or a stride outside the limits above. */
+base_status base_mx_quantize(int32_t dtype, const void *src, int64_t rows, int32_t cols,
+                             int64_t src_ld, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* The values, exactly (in bf16 too; a value of 2^128 or more is an infinity), as
+ * [rows][cols] of `dtype` with rows dst_ld >= cols elements apart; elements
+ * between the rows are not touched. */
+base_status base_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows,
+                               int32_t cols, int32_t dtype, void *dst, int64_t dst_ld,
+                               void *stream);
+
+/* Bytes of the BASE_W_MXFP4 form of L's w13 and w2 (L->E, d and I are read; 0 if
+ * they are outside the limits). */
+size_t base_mx_w13_bytes(const base_layer *L);
+size_t base_mx_w2_bytes(const base_layer *L);
+
+/* Expert weights into the BASE_W_MXFP4 layout, once when a model is loaded:
+ * from codes and scales as above (w13 as [E][2I] rows of d, w2 as [E][d] rows of
+ * I), or from the row-major 16- or 32-bit weights of L, quantised as
+ * base_mx_quantize does.  L: a row-major layer (else BASE_ERR_SHAPE); its K and
+ * n_shared are not read, and the shared experts are packed by a call of their
+ * own with E = n_shared.
+ *   w13_mx  [base_mx_w13_bytes(L)] out, w2_mx [base_mx_w2_bytes(L)] out, 16-B
+ *           aligned; may not overlap the inputs
+ * Layout: each matrix as 16-row tiles (w13: gate rows 16 r .., up rows I + 16 r
+ * .., next r; w2: rows 16 t ..), a tile as chunks of four steps of 128 contraction
+ * elements: 64 x 4 bytes of scales (lane l, byte j: block l / 16 of step j of row
+ * l % 16), then 1 KiB of codes per step (lane l: the same block's 16 bytes); a
+ * last chunk has the steps there are, and blocks past I are zeros. */
+base_status base_mx_pack_experts(const base_layer *L, const uint8_t *w13_codes,
+                                 const uint8_t *w13_scales, const uint8_t *w2_codes,
+                                 const uint8_t *w2_scales, void *w13_mx, void *w2_mx,
+                                 void *stream);
+base_status base_mx_quantize_experts(const base_layer *L, void *w13_mx, void *w2_mx, void *stream);
 
 /* Calibration statistics of the predictor (Sec. 3.4; App. A "Calibration
  * Details"), accumulated batch by batch on the device; the fit is

@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "_lib", "libbase.so")
 
 BASE_F32, BASE_BF16 = 0, 1
-W_ROWMAJOR, W_PACKED = 0, 1
+W_ROWMAJOR, W_PACKED, W_MXFP4 = 0, 1, 4
 GATE_PAPER, GATE_RENORM = 0, 1
 FILL_BACKFILL, FILL_DROP = 0, 2
 SCORE_BASE, SCORE_TOP1, SCORE_WEIGHT, SCORE_WEIGHT_SQ, SCORE_STATIC = 0, 1, 2, 3, 4
@@ -26,7 +26,9 @@ EXPORTS = ("base_workspace_bytes", "base_route", "base_predict_cost",
            "base_pack_experts", "base_set_stage_events", "base_layer_stages",
            "base_status_string",
            "base_calib_stats_bytes", "base_calib_ws_bytes", "base_calib_reset",
-           "base_calib_accumulate")
+           "base_calib_accumulate",
+           "base_mx_quantize", "base_mx_dequantize", "base_mx_w13_bytes", "base_mx_w2_bytes",
+           "base_mx_pack_experts", "base_mx_quantize_experts")
 CALIB_LIB_PATH = os.path.join(HERE, "_lib", "libbase_calib.so")
 N_STAGES = 9     # one kernel each; base_set_stage_events takes 2 events per stage
 STAGES = ("scores", "tail", "select", "backfill", "compact", "gather",
@@ -34,6 +36,7 @@ STAGES = ("scores", "tail", "select", "backfill", "compact", "gather",
 
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
+_i64 = ctypes.c_int64
 
 
 class base_layer(ctypes.Structure):
@@ -119,6 +122,17 @@ def load(path: str = LIB_PATH):
     L.base_calib_accumulate.restype = _i32
     L.base_calib_accumulate.argtypes = [ctypes.POINTER(base_layer), _vp, _i32, _vp, _vp,
                                         ctypes.c_size_t, _vp]
+    L.base_mx_quantize.restype = _i32
+    L.base_mx_quantize.argtypes = [_i32, _vp, _i64, _i32, _i64, _vp, _vp, _vp]
+    L.base_mx_dequantize.restype = _i32
+    L.base_mx_dequantize.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _i64, _vp]
+    for f in (L.base_mx_w13_bytes, L.base_mx_w2_bytes):
+        f.restype = ctypes.c_size_t
+        f.argtypes = [ctypes.POINTER(base_layer)]
+    L.base_mx_pack_experts.restype = _i32
+    L.base_mx_pack_experts.argtypes = [ctypes.POINTER(base_layer)] + [_vp] * 7
+    L.base_mx_quantize_experts.restype = _i32
+    L.base_mx_quantize_experts.argtypes = [ctypes.POINTER(base_layer)] + [_vp] * 3
     _lib = L
     return L
 
@@ -191,6 +205,23 @@ class Layer:
         self.shared = shared
         self._desc = None
 
+    @classmethod
+    def mxfp4(cls, w_router, b_router, pred_a, pred_b, w13, w2, I: int, norm_topk: int = 1,
+              score_rule: int = 0, shared=None):
+        """A layer of 4-bit experts: w13, w2 (and the shared ones) are the byte
+        tensors base_mx_pack_experts / base_mx_quantize_experts wrote; shared:
+        (w13_shared, w2_shared, gate or None, how many)."""
+        import torch
+        self = cls.__new__(cls)
+        self.tensors = (w_router, b_router, pred_a, pred_b, w13, w2)
+        self.dtype, self.torch_dtype = BASE_BF16, torch.bfloat16
+        self.E, self.d = w_router.shape
+        self.I, self.K = I, None
+        self.norm_topk, self.w_layout, self.score_rule = norm_topk, W_MXFP4, score_rule
+        self.shared = shared
+        self._desc = None
+        return self
+
     def desc(self, K: int) -> base_layer:
         w_router, b_router, pred_a, pred_b, w13, w2 = self.tensors
         return base_layer(self.d, self.E, K, self.I, self.dtype,
@@ -202,8 +233,9 @@ class Layer:
     def _shared_fields(self):
         if self.shared is None:
             return (0, None, None, None)
-        w13s, w2s, gate = self.shared
-        return (int(w13s.shape[0]), _ptr(w13s), _ptr(w2s), _ptr(gate))
+        w13s, w2s, gate = self.shared[:3]
+        n = self.shared[3] if self.w_layout == W_MXFP4 else w13s.shape[0]
+        return (int(n), _ptr(w13s), _ptr(w2s), _ptr(gate))
 
 
 def base_workspace_bytes(desc: base_layer, B: int, budget: int) -> int:
@@ -291,6 +323,135 @@ def packed_layer(layer: "Layer", K: int, stream=None) -> "Layer":
         shared = (w13sp, w2sp, gate)
     return Layer(w_router, b_router, pred_a, pred_b, w13p, w2p,
                  layer.norm_topk, W_PACKED, layer.score_rule, shared)
+
+
+def _on_device(t, what):
+    """The launches go to the current GPU, so the tensors have to lie there."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: on the current GPU, not {t.device}")
+
+
+# Microscaled 4-bit floating point (E2M1 codes, an E8M0 scale per 32 elements)
+def _rows(t, what):
+    """(dtype, rows, cols, row stride) of a 2-D tensor with adjacent columns."""
+    import torch
+    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{what}: a 2-D fp32 or bf16 tensor")
+    _on_device(t, what)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: adjacent columns")
+    return (BASE_BF16 if t.dtype == torch.bfloat16 else BASE_F32, rows, cols,
+            t.stride(0) if rows > 1 else cols)
+
+
+def mx_quantize(src, codes=None, scales=None, stream=None):
+    """codes [rows, cols / 2] and scales [rows, cols / 32] (uint8) of src
+    [rows, cols]; the rows may lie inside wider ones."""
+    import torch
+    dt, rows, cols, ld = _rows(src, "src")
+    if codes is None:
+        codes = torch.empty(rows, cols // 2, dtype=torch.uint8, device=src.device)
+    if scales is None:
+        scales = torch.empty(rows, cols // 32, dtype=torch.uint8, device=src.device)
+    _mx_shapes(codes, scales, rows, cols)
+    _check(load().base_mx_quantize(dt, _ptr(src), rows, cols, ld, _ptr(codes), _ptr(scales),
+                                   _stream(stream)))
+    return codes, scales
+
+
+def mx_dequantize(codes, scales, dtype=None, out=None, stream=None):
+    """The values [rows, cols] as `dtype` (bf16), or into `out`."""
+    import torch
+    rows, cols = codes.shape[0], 2 * codes.shape[1]
+    _mx_shapes(codes, scales, rows, cols)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=dtype or torch.bfloat16, device=codes.device)
+    dt, r, c, ld = _rows(out, "out")
+    if (r, c) != (rows, cols):
+        raise ValueError("out: the codes' rows and columns")
+    _check(load().base_mx_dequantize(_ptr(codes), _ptr(scales), rows, cols, dt, _ptr(out), ld,
+                                     _stream(stream)))
+    return out
+
+
+def _mx_shapes(codes, scales, rows, cols):
+    import torch
+    for t, n, what in ((codes, cols // 2, "codes"), (scales, cols // 32, "scales")):
+        want = (*(rows if isinstance(rows, tuple) else (rows,)), n)
+        if t.dtype != torch.uint8 or tuple(t.shape) != want or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous uint8 {list(want)}")
+        _on_device(t, what)
+
+
+def _mx_desc(E, d, I, dtype=BASE_BF16, w13=None, w2=None):
+    return base_layer(d, E, 1, I, dtype, 1, W_ROWMAJOR, 0, None, None, None, None, _ptr(w13),
+                      _ptr(w2), 0, None, None, None)
+
+
+def _mx_out(desc, device):
+    import torch
+    n13, n2 = (int(f(ctypes.byref(desc))) for f in (load().base_mx_w13_bytes,
+                                                    load().base_mx_w2_bytes))
+    if n13 == 0:
+        raise BaseError(-2, status_string(-2))
+    return (torch.empty(n13, dtype=torch.uint8, device=device),
+            torch.empty(n2, dtype=torch.uint8, device=device))
+
+
+def mx_quantize_experts(w13, w2, stream=None):
+    """Row-major experts w13 [E, 2I, d], w2 [E, d, I] (bf16 or fp32) as the byte
+    tensors of a W_MXFP4 layer."""
+    import torch
+    E, d, I = w2.shape
+    if tuple(w13.shape) != (E, 2 * I, d) or w13.dtype != w2.dtype or not (
+            w13.is_contiguous() and w2.is_contiguous()):
+        raise ValueError("w13 [E, 2I, d] and w2 [E, d, I], contiguous, of one dtype")
+    desc = _mx_desc(E, d, I, BASE_BF16 if w13.dtype == torch.bfloat16 else BASE_F32, w13, w2)
+    out = _mx_out(desc, w13.device)
+    _check(load().base_mx_quantize_experts(ctypes.byref(desc), _ptr(out[0]), _ptr(out[1]),
+                                           _stream(stream)))
+    return out
+
+
+def mx_pack_experts(w13, w2, stream=None):
+    """The same from (codes, scales) pairs: w13 [E, 2I, d / 2] and [E, 2I, d / 32],
+    w2 [E, d, I / 2] and [E, d, I / 32]."""
+    E, d = w2[0].shape[:2]
+    I = 2 * w2[0].shape[2]
+    _mx_shapes(*w13, (E, 2 * I), d)
+    _mx_shapes(*w2, (E, d), I)
+    desc = _mx_desc(E, d, I)
+    out = _mx_out(desc, w13[0].device)
+    _check(load().base_mx_pack_experts(ctypes.byref(desc), *(_ptr(t) for t in (*w13, *w2, *out)),
+                                       _stream(stream)))
+    return out
+
+
+def mx_layer(layer: "Layer", stream=None) -> "Layer":
+    """A W_MXFP4 Layer with a row-major layer's experts quantised, sharing its
+    router and predictor tensors (one-time, on the device)."""
+    w_router, b_router, pred_a, pred_b, w13, w2 = layer.tensors
+    if layer.w_layout != W_ROWMAJOR:
+        raise ValueError("row-major experts")
+    shared = None
+    if layer.shared is not None:
+        w13s, w2s, gate = layer.shared
+        shared = (*mx_quantize_experts(w13s, w2s, stream), gate, int(w13s.shape[0]))
+    return Layer.mxfp4(w_router, b_router, pred_a, pred_b, *mx_quantize_experts(w13, w2, stream),
+                       layer.I, layer.norm_topk, layer.score_rule, shared)
+
+
+def mx_layer_from_codes(w_router, b_router, pred_a, pred_b, w13, w2, norm_topk: int = 1,
+                        score_rule: int = 0, shared=None, stream=None) -> "Layer":
+    """A W_MXFP4 Layer from experts held as (codes, scales) pairs (mx_pack_experts);
+    shared: None or (w13 pair, w2 pair, gate or None)."""
+    if shared is not None:
+        w13s, w2s, gate = shared
+        shared = (*mx_pack_experts(w13s, w2s, stream), gate, int(w13s[0].shape[0]))
+    return Layer.mxfp4(w_router, b_router, pred_a, pred_b, *mx_pack_experts(w13, w2, stream),
+                       2 * w2[0].shape[2], norm_topk, score_rule, shared)
 
 
 def base_set_stage_events(events):

@@ -10,6 +10,7 @@
 
 #include "../../include/base.h"
 #include "internal.hpp"
+#include "mx.hpp"
 
 namespace {
 
@@ -39,8 +40,10 @@ base_status check_layer(const base_layer *L, int32_t B, bool need_router,
   if (L->K < 1 || L->K > MAX_K || L->E < L->K || L->E > MAX_E) return BASE_ERR_SHAPE;
   if (L->I < 64 || L->I > 32768 || L->I % 64) return BASE_ERR_SHAPE;
   if (L->norm_topk != 0 && L->norm_topk != 1) return BASE_ERR_SHAPE;
-  if (L->w_layout != BASE_W_ROWMAJOR && L->w_layout != BASE_W_PACKED) return BASE_ERR_SHAPE;
-  if (L->w_layout == BASE_W_PACKED && L->dtype != BASE_BF16) return BASE_ERR_DTYPE;
+  if (L->w_layout != BASE_W_ROWMAJOR && L->w_layout != BASE_W_PACKED &&
+      L->w_layout != BASE_W_MXFP4)
+    return BASE_ERR_SHAPE;
+  if (L->w_layout != BASE_W_ROWMAJOR && L->dtype != BASE_BF16) return BASE_ERR_DTYPE;
   if (need_router) {
     if (!L->w_router) return BASE_ERR_NULL;
     if (!aligned(L->w_router, 16)) return BASE_ERR_ALIGN;
@@ -69,6 +72,8 @@ base_status check_layer(const base_layer *L, int32_t B, bool need_router,
   return BASE_OK;
 }
 
+bool mx_layer(const base_layer *L) { return L->w_layout == BASE_W_MXFP4; }
+
 // the shared-expert gate vector (only with shared experts)
 const float *shared_gate(const base_layer *L) {
   return L->n_shared > 0 ? L->shared_gate : nullptr;
@@ -91,9 +96,10 @@ base_status check_ptr(const void *p, size_t a) {
   } while (0)
 
 // Workspace layout: every array starts on a 256-byte boundary.  split: the FFN
-// takes its split kernels (bf16).
+// works on records (its split kernels, bf16, or 4-bit experts), nrec of them.
 struct Layout {
   bool split;
+  int nrec;
   size_t logits, gdot, topk_ids, topk_w, cost, scores, counts, sel_ids, n_sel,
       slot_of, exec_ids, exec_gates, offsets, pair_tok, pair_gate, pair_of, order, ex,
       den, hdr, units_gu, units_dn, tokoff, sprec, H, pairbuf, total;
@@ -137,6 +143,7 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc, bool split) {
   // the FFN's part tables and their header (bf16)
   const bool bf = L->dtype == BASE_BF16;
   // (one header per die; every die's run of units written on that die)
+  o.nrec = !split ? 0 : mx_layer(L) ? mx_records(B, L->K, bc, ns) : bc + ns;
   const bool units = bf && !split;
   const size_t ug = units ? (size_t)ffn_units_bound_gu(B, L->K, bc, ns, L->I) : 0;
   const size_t ud = units ? (size_t)ffn_units_bound_dn(B, L->K, bc, ns, L->d) : 0;
@@ -144,7 +151,7 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc, bool split) {
   o.units_gu = take(ug * sizeof(FfnUnit));
   o.units_dn = take(ud * sizeof(FfnUnit));
   o.tokoff = take(ug * FFN_GU_TOK * 4);
-  o.sprec = take(split ? N_XCD * ((size_t)bc + ns) * sizeof(SpRec) : 0);
+  o.sprec = take(N_XCD * (size_t)o.nrec * sizeof(SpRec));
   if (L->dtype == BASE_BF16) {
     // fragment-ordered SwiGLU activations (16-pair tiles)
     const size_t tiles = (size_t)ffn_max_tiles(B, L->K, bc, ns);
@@ -168,6 +175,7 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc, bool split) {
 // results are base_decode_layer's, takes it too.
 Layout layout(const base_layer *L, int32_t B, int32_t bc) {
   const bool bf = L->dtype == BASE_BF16;
+  if (mx_layer(L)) return layout(L, B, bc, true);
   const Layout s = layout(L, B, bc, bf && ffn_small(B, L->I));
   if (!s.split || ffn_split(B, L->K, L->d, L->I, bc, L->n_shared)) return s;
   const Layout u = layout(L, B, bc, false);
@@ -178,7 +186,7 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc) {
 // also where only those take the unit kernels and their tables.
 size_t workspace_bytes(const base_layer *L, int32_t B, int32_t bc) {
   const Layout o = layout(L, B, bc);
-  if (!o.split) return o.total;
+  if (!o.split || mx_layer(L)) return o.total;
   for (int32_t b = bc - 1; b >= 1; --b) {
     const Layout u = layout(L, B, b);
     if (!u.split) return std::max(o.total, u.total);
@@ -255,6 +263,46 @@ T *at(void *ws, size_t off) {
   return reinterpret_cast<T *>(static_cast<char *>(ws) + off);
 }
 
+// the part records a compaction of this layer writes (0: the slots')
+int part_records(const base_layer *L, int32_t B, const Layout &o) {
+  return mx_layer(L) && mx_parts(B) ? o.nrec : 0;
+}
+
+// gate/up and down of the plan in the workspace (stages 6 and 7), on at most
+// `slots` kept slots
+base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, int32_t slots,
+                    const int32_t *sel_ids, const int32_t *n_sel, void *ws, const Layout &o,
+                    hipStream_t st) {
+  const bool bf16 = L->dtype == BASE_BF16, packed = L->w_layout == BASE_W_PACKED;
+  const int ns = L->n_shared, n_cu = device_cus();
+  const int32_t *offsets = at<int32_t>(ws, o.offsets);
+  const int32_t *sptok = at<int32_t>(ws, o.pairbuf);
+  const FfnHdr *hdr = at<FfnHdr>(ws, o.hdr);
+  const SpRec *rec = o.split ? at<SpRec>(ws, o.sprec) : nullptr;
+  const float *pair_gate = at<float>(ws, o.pair_gate);
+  void *H = at<void>(ws, o.H);
+  stage(6, st);
+  if (mx_layer(L))
+    HIP_TRY(launch_mx_gateup(x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13, L->w13_shared,
+                             rec, sptok, H, st));
+  else
+    HIP_TRY(launch_gateup(bf16, packed, x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13,
+                          L->w13_shared, sel_ids, n_sel, offsets, at<int32_t>(ws, o.pair_tok), hdr,
+                          at<FfnUnit>(ws, o.units_gu), n_cu, at<uint32_t>(ws, o.tokoff), rec, sptok,
+                          H, st));
+  stage_end(st);
+  stage(7, st);
+  if (mx_layer(L))
+    HIP_TRY(launch_mx_down(B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2, L->w2_shared, rec,
+                           pair_gate, H, at<float>(ws, o.pairbuf), st));
+  else
+    HIP_TRY(launch_down(bf16, packed, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2,
+                        L->w2_shared, sel_ids, n_sel, offsets, hdr, at<FfnUnit>(ws, o.units_dn),
+                        rec, n_cu, pair_gate, H, at<float>(ws, o.pairbuf), st));
+  stage_end(st);
+  return BASE_OK;
+}
+
 // backfill (unless done with the selection) + compaction (unless planned:
 // done with both) + FFN + combine, on plan arrays already in place
 base_status run_forward(const base_layer *L, const void *x, int32_t B,
@@ -289,24 +337,13 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
     HIP_TRY(launch_compact(B, L->K, L->E, bc, ns, exec_ids, exec_gates, slot_of, n_sel,
                            shared_gate(L) ? at<float>(ws, o.gdot) : nullptr, offsets,
                            pair_tok, pair_gate, pair_of, sel_ids, bf16 && !o.split, L->d, L->I, tokoff, hdr,
-                           units_gu, units_dn, rec, sptok, n_cu, st));
+                           units_gu, units_dn, rec, sptok, part_records(L, B, o), n_cu, st));
   stage_end(st);
   stage(5, st);   // no launch of its own: gate/up gathers its tokens itself
   stage_end(st);
-  stage(6, st);
-  const bool packed = L->w_layout == BASE_W_PACKED;
   // the fused layer's kept set is part of its own batch's union; a caller of
   // base_moe_forward may bring any
-  const int slots = backfilled ? std::min(bc, B * L->K) : bc;
-  HIP_TRY(launch_gateup(bf16, packed, x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13,
-                        L->w13_shared, sel_ids, n_sel, offsets, pair_tok, hdr, units_gu, n_cu,
-                        tokoff, rec, sptok, at<void>(ws, o.H), st));
-  stage_end(st);
-  stage(7, st);
-  HIP_TRY(launch_down(bf16, packed, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2,
-                      L->w2_shared, sel_ids, n_sel, offsets, hdr, units_dn, rec, n_cu, pair_gate,
-                      at<void>(ws, o.H), at<float>(ws, o.pairbuf), st));
-  stage_end(st);
+  BASE_TRY(run_ffn(L, x, B, bc, backfilled ? std::min(bc, B * L->K) : bc, sel_ids, n_sel, ws, o, st));
   stage(8, st);
   HIP_TRY(launch_combine(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf),
                          residual, y, st));
@@ -314,9 +351,10 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
   return BASE_OK;
 }
 
-// the fused layer's plan in one launch: the split kernels' records (bf16), or
-// nothing but the plan (fp32)
+// the fused layer's plan in one launch: the slots' records (bf16 and 4-bit
+// experts), or nothing but the plan (fp32)
 bool one_plan(const base_layer *L, int32_t B, const Layout &o) {
+  if (mx_layer(L)) return !mx_parts(B);
   return L->dtype == BASE_BF16 ? o.split : ffn_small(B, L->I);
 }
 
@@ -603,14 +641,8 @@ base_status base_calib_accumulate(const base_layer *L, const void *z, int32_t B,
                          at<float>(ws, o.exec_gates), slot, nsel, nullptr, offsets, pair_tok,
                          at<float>(ws, o.pair_gate), at<int32_t>(ws, o.pair_of), sel,
                          bf16 && !o.split, C.d, C.I, at<uint32_t>(ws, o.tokoff), hdr, units_gu, units_dn,
-                         rec, sptok, n_cu, st));
-  const bool packed = C.w_layout == BASE_W_PACKED;
-  HIP_TRY(launch_gateup(bf16, packed, z, B, C.d, C.I, C.E, C.K, bc, std::min(bc, B * C.K), 0, C.w13, nullptr, sel,
-                        nsel, offsets, pair_tok, hdr, units_gu, n_cu, at<uint32_t>(ws, o.tokoff),
-                        rec, sptok, at<void>(ws, o.H), st));
-  HIP_TRY(launch_down(bf16, packed, B, C.d, C.I, C.E, C.K, bc, std::min(bc, B * C.K), 0, C.w2, nullptr, sel, nsel,
-                      offsets, hdr, units_dn, rec, n_cu, at<float>(ws, o.pair_gate),
-                      at<void>(ws, o.H), at<float>(ws, o.pairbuf), st));
+                         rec, sptok, part_records(&C, B, o), n_cu, st));
+  BASE_TRY(run_ffn(&C, z, B, bc, std::min(bc, B * C.K), sel, nsel, ws, o, st));
   double *inv = at<double>(ws, o.total);
   double *y = at<double>(ws, o.total + up256((size_t)B * 8));
   float *zbuf = at<float>(ws, o.total + up256((size_t)B * 8) + up256((size_t)B * C.K * 8));
@@ -635,6 +667,89 @@ base_status base_pack_experts(const base_layer *L, void *w13_packed,
   BASE_TRY(check_ptr(w2_packed, 16));
   HIP_TRY(launch_pack(L->w13, L->w2, w13_packed, w2_packed, L->E, L->d, L->I,
                       (hipStream_t)stream));
+  return BASE_OK;
+}
+
+// ------------------------------------------------------- 4-bit experts --
+// the expert matrices of L (E, d, I; K and n_shared are not read) and their
+// 16- or 32-bit type
+static base_status check_mx_experts(const base_layer *L) {
+  if (!L) return BASE_ERR_NULL;
+  if (L->w_layout != BASE_W_ROWMAJOR) return BASE_ERR_SHAPE;
+  base_layer C = *L;
+  C.K = 1;
+  C.n_shared = 0;
+  return check_layer(&C, 1, false, false, false);
+}
+
+size_t base_mx_w13_bytes(const base_layer *L) {
+  if (!L || L->E < 1 || L->E > MAX_E || L->d < 256 || L->d > 16384 || L->d % 256 || L->I < 64 ||
+      L->I > 32768 || L->I % 64)
+    return 0;
+  return (size_t)L->E * (L->I / 8) * mx_tile_bytes(L->d);
+}
+
+size_t base_mx_w2_bytes(const base_layer *L) {
+  if (base_mx_w13_bytes(L) == 0) return 0;
+  return (size_t)L->E * (L->d / 16) * mx_tile_bytes(L->I);
+}
+
+base_status base_mx_pack_experts(const base_layer *L, const uint8_t *w13_codes,
+                                 const uint8_t *w13_scales, const uint8_t *w2_codes,
+                                 const uint8_t *w2_scales, void *w13_mx, void *w2_mx,
+                                 void *stream) {
+  BASE_TRY(check_mx_experts(L));
+  BASE_TRY(check_ptr(w13_codes, 16));
+  BASE_TRY(check_ptr(w13_scales, 1));
+  BASE_TRY(check_ptr(w2_codes, 16));
+  BASE_TRY(check_ptr(w2_scales, 1));
+  BASE_TRY(check_ptr(w13_mx, 16));
+  BASE_TRY(check_ptr(w2_mx, 16));
+  HIP_TRY(launch_mx_pack(w13_codes, w13_scales, w2_codes, w2_scales, L->E, L->d, L->I, w13_mx,
+                         w2_mx, (hipStream_t)stream));
+  return BASE_OK;
+}
+
+base_status base_mx_quantize_experts(const base_layer *L, void *w13_mx, void *w2_mx, void *stream) {
+  BASE_TRY(check_mx_experts(L));
+  BASE_TRY(check_ptr(L->w13, 16));
+  BASE_TRY(check_ptr(L->w2, 16));
+  BASE_TRY(check_ptr(w13_mx, 16));
+  BASE_TRY(check_ptr(w2_mx, 16));
+  HIP_TRY(launch_mx_quantize_experts(L->dtype == BASE_BF16, L->w13, L->w2, L->E, L->d, L->I, w13_mx,
+                                     w2_mx, (hipStream_t)stream));
+  return BASE_OK;
+}
+
+// rows of `cols` elements with a stride of `ld`
+static base_status check_mx_rows(int32_t dtype, int64_t rows, int32_t cols, int64_t ld) {
+  if (dtype != BASE_F32 && dtype != BASE_BF16) return BASE_ERR_DTYPE;
+  if (rows < 1 || rows > BASE_MX_MAX_ROWS || cols < 32 || cols > BASE_MX_MAX_COLS || cols % 32 ||
+      ld < cols || ld > BASE_MX_MAX_LD)
+    return BASE_ERR_SHAPE;
+  return BASE_OK;
+}
+
+base_status base_mx_quantize(int32_t dtype, const void *src, int64_t rows, int32_t cols,
+                             int64_t src_ld, uint8_t *codes, uint8_t *scales, void *stream) {
+  BASE_TRY(check_mx_rows(dtype, rows, cols, src_ld));
+  BASE_TRY(check_ptr(src, elem_bytes(dtype)));
+  BASE_TRY(check_ptr(codes, 16));
+  BASE_TRY(check_ptr(scales, 1));
+  HIP_TRY(launch_mx_quantize(dtype == BASE_BF16, src, rows, cols, src_ld, codes, scales,
+                             (hipStream_t)stream));
+  return BASE_OK;
+}
+
+base_status base_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows,
+                               int32_t cols, int32_t dtype, void *dst, int64_t dst_ld,
+                               void *stream) {
+  BASE_TRY(check_mx_rows(dtype, rows, cols, dst_ld));
+  BASE_TRY(check_ptr(codes, 16));
+  BASE_TRY(check_ptr(scales, 1));
+  BASE_TRY(check_ptr(dst, elem_bytes(dtype)));
+  HIP_TRY(launch_mx_dequantize(dtype == BASE_BF16, codes, scales, rows, cols, dst, dst_ld,
+                               (hipStream_t)stream));
   return BASE_OK;
 }
 

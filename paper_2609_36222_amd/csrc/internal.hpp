@@ -157,6 +157,20 @@ struct alignas(16) SpRec {
   int32_t u, p0, n, pad;
 };
 
+// 4-bit experts (ffn_mx.hip) take records for every batch: up to FFN_SPLIT_B
+// tokens the slots' (above; a slot's pairs fit MX_NT 16-pair tiles), beyond it
+// one per part of at most MX_NT tiles of a slot, the shared slots' parts first,
+// `pad` the slot's number in that order, and empty ones up to mx_records.
+constexpr int MX_NT = 4;
+static_assert(FFN_SPLIT_B <= 16 * MX_NT, "a slot of a small batch is one part");
+inline bool mx_parts(int B) { return B > FFN_SPLIT_B; }
+// slots' records, or an upper bound of the parts: the sum over slots of
+// ceil(tiles / MX_NT) is at most (tiles + (MX_NT - 1) slots) / MX_NT
+inline int mx_records(int B, int K, int budget, int ns) {
+  if (!mx_parts(B)) return budget + ns;
+  return (ffn_max_tiles(B, K, budget, ns) + (MX_NT - 1) * (budget + ns)) / MX_NT;
+}
+
 // A unit: expert u (u >= E: shared expert u - E), the part's first 16-pair
 // tile, its tile count, its first pair in the compacted order and its pair
 // count, and the unit's row group (gate/up: hdr.rp_gu row-pair tiles;
@@ -287,8 +301,8 @@ hipError_t launch_compact(int B, int K, int E, int budget, int ns, const int32_t
                           int32_t *pair_tok, float *pair_gate,
                           int32_t *pair_of, const int32_t *sel_ids, bool tables, int d,
                           int I, uint32_t *tokoff, FfnHdr *hdr, FfnUnit *units_gu,
-                          FfnUnit *units_dn, SpRec *rec, int32_t *sptok, int n_cu,
-                          hipStream_t st);
+                          FfnUnit *units_dn, SpRec *rec, int32_t *sptok, int nparts,
+                          int n_cu, hipStream_t st);   // nparts > 0: that many part records (mx_records)
 hipError_t launch_pack(const void *w13, const void *w2, void *w13p, void *w2p,
                        int E, int d, int I, hipStream_t st);
 // slots: at most this many kept slots (budget, or fewer where the kept set is
@@ -308,6 +322,25 @@ hipError_t launch_down(bool bf16, bool packed, int B, int d, int I, int E, int K
                        const int32_t *n_sel, const int32_t *offsets,
                        const FfnHdr *hdr, const FfnUnit *units, const SpRec *rec, int n_cu,
                        const float *pair_gate, const void *H, float *pairbuf, hipStream_t st);
+// the same on 4-bit weights; rec / sptok: see mx_records
+hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, int budget, int slots,
+                            int ns, const void *w13, const void *w13s, const SpRec *rec,
+                            const int32_t *sptok, void *H, hipStream_t st);
+hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
+                          const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
+                          const void *H, float *pairbuf, hipStream_t st);
+// rows [rows][cols] (row stride ld) to codes [rows][cols / 2] and scales [rows]
+// [cols / 32] and back; experts into the packed 4-bit layout (mx.hpp) from codes
+// and scales or from 16- or 32-bit weights
+hipError_t launch_mx_quantize(bool bf16, const void *src, long long rows, int cols, long long ld,
+                              void *codes, uint8_t *scales, hipStream_t st);
+hipError_t launch_mx_dequantize(bool bf16, const void *codes, const uint8_t *scales, long long rows,
+                                int cols, void *dst, long long ld, hipStream_t st);
+hipError_t launch_mx_pack(const uint8_t *w13c, const uint8_t *w13s, const uint8_t *w2c,
+                          const uint8_t *w2s, int E, int d, int I, void *w13, void *w2,
+                          hipStream_t st);
+hipError_t launch_mx_quantize_experts(bool bf16, const void *w13, const void *w2, int E, int d,
+                                      int I, void *w13m, void *w2m, hipStream_t st);
 // kc: columns of pair_of (K routed + the shared experts)
 hipError_t launch_combine(bool bf16, int B, int d, int kc,
                           const int32_t *pair_of, const float *pairbuf,

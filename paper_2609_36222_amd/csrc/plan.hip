@@ -688,8 +688,9 @@ constexpr int CP_PAIRS = MAX_B * MAX_K;   // routed pairs at most
 // die, each making the whole sort (the same arithmetic, so the same result
 // everywhere) and writing its die's header, units and token rows, which the
 // FFN's workgroups on that die then read from their own L2; workgroup 0
-// alone writes the plan.  With the split kernels' records (rec) the same, each
-// workgroup writing its die's records and token list; with neither, one workgroup.
+// alone writes the plan.  With records (rec: a slot's, or with nparts a part's)
+// the same, each workgroup writing its die's records and token list; with
+// neither, one workgroup.
 // The routed pairs are taken in flat order q = t K + j, so sorting by (slot,
 // q) is sorting by (slot, token, rank).  Wavefront w owns the pairs w 64 PPT
 // + r 64 + lane (r = 0 .. PPT - 1, PPT pairs per thread, PPT * CP_THREADS >=
@@ -745,7 +746,7 @@ void k_compact(int B, int K, uint64_t kmul, int E, int budget, int ns,
                const int32_t *__restrict__ sel_ids, int tables, int d, int I,
                uint32_t *__restrict__ tokoff, FfnHdr *__restrict__ hdr,
                FfnUnit *__restrict__ units_gu, FfnUnit *__restrict__ units_dn,
-               SpRec *__restrict__ rec, int32_t *__restrict__ sptok, int n_cu) {
+               SpRec *__restrict__ rec, int32_t *__restrict__ sptok, int nparts, int n_cu) {
   // cw[w][s]: pairs of slot s in wavefront w, then their first rank in slot s
   __shared__ int cw[CP_WAVES][MAX_E];
   __shared__ int cnt[SCAN_N];
@@ -1032,9 +1033,29 @@ void k_compact(int B, int K, uint64_t kmul, int E, int budget, int ns,
   }
   if (rec) {
     // the split kernels' records and token list, this die's copy
-    SpRec *rx = rec + (size_t)blockIdx.x * (budget + ns);
+    SpRec *rx = rec + (size_t)blockIdx.x * (nparts > 0 ? nparts : budget + ns);
     int32_t *tx = sptok + (size_t)blockIdx.x * B * kc;
-    for (int s = tid; s < budget + ns; s += CP_THREADS) {
+    if (nparts > 0) {   // one record per part of MX_NT tiles, the shared slots first
+      for (int j = tid; j < SCAN_N; j += CP_THREADS) {
+        const int s = j < ns ? n_sel + j : j - ns;
+        np_gu[j] = j < nslot ? (tb[s + 1] - tb[s] + MX_NT - 1) / MX_NT : 0;
+      }
+      __syncthreads();
+      if (wv == 0) wave_scan_counts(np_gu, pre_gu);
+      __syncthreads();
+      for (int j = wv; j < nslot; j += CP_WAVES) {
+        const int s = j < ns ? n_sel + j : j - ns;
+        const int u = s < n_sel ? sel_s[s] : E + (s - n_sel);
+        const bool run = u >= 0 && u < E + ns;
+        for (int q = lane; q < np_gu[j]; q += WAVE) {
+          const int c = 16 * MX_NT * q;
+          rx[pre_gu[j] + q] = SpRec{run ? u : 0, run ? off[s] + c : 0,
+                                    run ? min(16 * MX_NT, cnt[s] - c) : 0, j};
+        }
+      }
+      for (int i = pre_gu[SCAN_N] + tid; i < nparts; i += CP_THREADS) rx[i] = SpRec{0, 0, 0, 0};
+    }
+    for (int s = tid; nparts <= 0 && s < budget + ns; s += CP_THREADS) {
       const int q = s < budget ? s : n_sel + (s - budget);
       const bool kept = s >= budget || s < n_sel;
       const int u = s < budget ? (kept ? sel_s[s] : 0) : E + (s - budget);
@@ -1420,15 +1441,16 @@ hipError_t launch_compact(int B, int K, int E, int budget, int ns, const int32_t
                           int32_t *pair_tok, float *pair_gate,
                           int32_t *pair_of, const int32_t *sel_ids, bool tables, int d,
                           int I, uint32_t *tokoff, FfnHdr *hdr, FfnUnit *units_gu,
-                          FfnUnit *units_dn, SpRec *rec, int32_t *sptok, int n_cu,
-                          hipStream_t st) {
+                          FfnUnit *units_dn, SpRec *rec, int32_t *sptok, int nparts,
+                          int n_cu, hipStream_t st) {
   const int ppt = (B * K + CP_THREADS - 1) / CP_THREADS;
   const uint64_t kmul = ((1ull << 32) + (uint64_t)K - 1) / (uint64_t)K;
   const unsigned blocks = tables || rec ? N_XCD : 1u;   // one workgroup per die
 #define BASE_COMPACT(P)                                                                    \
   launch_k(k_compact<P>, dim3(blocks), dim3(CP_THREADS), 0, st, B, K, kmul, E, budget, ns, \
            exec_ids, exec_gates, slot_of, n_sel, gdot, offsets, pair_tok, pair_gate,      \
-           pair_of, sel_ids, (int)tables, d, I, tokoff, hdr, units_gu, units_dn, rec, sptok, n_cu)
+           pair_of, sel_ids, (int)tables, d, I, tokoff, hdr, units_gu, units_dn, rec, sptok, nparts,\
+           n_cu)
   if (ppt <= 1) BASE_COMPACT(1);
   else if (ppt <= 2) BASE_COMPACT(2);
   else if (ppt <= 4) BASE_COMPACT(4);

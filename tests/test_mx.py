@@ -1,0 +1,141 @@
+"""4-bit experts without a GPU: the oracle's own format, the sizes the library
+reports, and every refusal of the calls (nothing is enqueued by any of them)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import mx
+from paper_2609_36222_amd import binding as bd
+from test_abi import (ALIGN, BUDGET, DTYPE, FAKE, NULL, OK, SHAPE, WS,  # noqa: F401
+                      decode, layer, lib)
+
+MXL = dict(w_layout=4)
+
+
+def test_oracle_rounds_to_the_nearest_code_and_even_on_ties():
+    grid = np.concatenate([-mx.E2M1[::-1], mx.E2M1])
+    t = np.linspace(-7.99, 7.99, 3197)
+    v = np.zeros((len(t), 32))
+    v[:, 0], v[:, 1] = 6.0, t          # 6 (or t itself, below 8) fixes the scale at 2^0
+    codes, scales = mx.quantize(v)
+    assert (scales == 127).all()
+    got = mx.dequantize(codes, scales)[:, 1]
+    best = np.abs(grid[None] - np.clip(t, -6, 6)[:, None]).min(1)
+    assert np.allclose(np.abs(got - np.clip(t, -6, 6)), best, atol=1e-12)
+    ties = {0.25: 0.0, 0.75: 1.0, 1.25: 1.0, 1.75: 2.0, 2.5: 2.0, 3.5: 4.0, 5.0: 4.0}
+    for a, b in ties.items():
+        v = np.zeros((2, 32))
+        v[:, 0], v[0, 1], v[1, 1] = 4.0, a, -a
+        assert mx.dequantize(*mx.quantize(v))[:, 1].tolist() == [b, -b]
+
+
+def test_oracle_special_blocks():
+    v = np.zeros((5, 32))
+    v[1, 3], v[2, 5], v[3, 0], v[4, 1] = np.nan, -np.inf, 2.0 ** -140, 3.0e38
+    codes, scales = mx.quantize(v)
+    assert scales.ravel().tolist() == [0, 255, 255, 0, 127 + 127 - 2]
+    assert (codes[:3] == 0).all() and np.isnan(mx.dequantize(codes, scales)[1:3]).all()
+
+
+@pytest.mark.parametrize("E,d,I", [(1, 256, 64), (3, 512, 192), (60, 2048, 1408), (8, 4096, 14336)])
+def test_bytes(lib, E, d, I):
+    L = layer(E=E, K=1, d=d, I=I)
+    per = lambda rows, K: rows // 16 * (-(-K // 512) * 256 + -(-K // 128) * 1024)  # noqa: E731
+    assert lib.base_mx_w13_bytes(ctypes.byref(L)) == E * per(2 * I, d)
+    assert lib.base_mx_w2_bytes(ctypes.byref(L)) == E * per(d, I)
+
+
+@pytest.mark.parametrize("kw", [dict(E=0), dict(E=257), dict(d=128), dict(d=300), dict(d=16640),
+                                dict(I=0), dict(I=100), dict(I=32832)])
+def test_bytes_of_a_bad_shape(lib, kw):
+    assert lib.base_mx_w13_bytes(ctypes.byref(layer(**kw))) == 0
+    assert lib.base_mx_w2_bytes(ctypes.byref(layer(**kw))) == 0
+
+
+def test_bytes_null(lib):
+    assert lib.base_mx_w13_bytes(None) == 0 and lib.base_mx_w2_bytes(None) == 0
+
+
+def test_layer_layout(lib):
+    assert decode(lib, layer(dtype=0, **MXL), nbytes=1 << 40) == DTYPE
+    L = layer(**MXL)
+    n = lib.base_workspace_bytes(ctypes.byref(L), 16, 4)
+    assert n > 0
+    assert decode(lib, L, nbytes=n - 1) == WS
+    assert decode(lib, layer(w13=0, **MXL)) == NULL
+    assert decode(lib, layer(w2=FAKE + 8, **MXL)) == ALIGN
+    assert decode(lib, L, budget=0, nbytes=n) == BUDGET
+    assert lib.base_pack_experts(ctypes.byref(L), FAKE, FAKE, None) == SHAPE
+    for w in (2, 3, 5):
+        assert decode(lib, layer(w_layout=w), nbytes=1 << 40) == SHAPE
+
+
+@pytest.mark.parametrize("B", [1, 64, 65, 1024])
+def test_workspace_covers_smaller_budgets(lib, B):
+    """Sized for one budget it holds every smaller one."""
+    L = layer(E=256, K=8, n_shared=3, w13_shared=FAKE, w2_shared=FAKE, **MXL)
+    n = [lib.base_workspace_bytes(ctypes.byref(L), B, b) for b in (1, 2, 7, 64, 65, 255, 256, 999)]
+    assert n == sorted(n) and n[-1] == n[-2] and n[0] > 0
+
+
+def test_quantize_refusals(lib):
+    def q(dtype=1, src=FAKE, rows=4, cols=64, ld=64, codes=FAKE, scales=FAKE):
+        return lib.base_mx_quantize(dtype, src, rows, cols, ld, codes, scales, None)
+    assert q(dtype=2) == DTYPE
+    for kw in (dict(rows=0), dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=48),
+               dict(cols=-32), dict(cols=(1 << 24) + 32, ld=1 << 25), dict(ld=63), dict(ld=0),
+               dict(ld=-64), dict(ld=(1 << 40) + 1)):
+        assert q(**kw) == SHAPE, kw
+    assert q(src=0) == NULL and q(codes=0) == NULL and q(scales=0) == NULL
+    assert q(src=FAKE + 1) == ALIGN and q(src=FAKE + 2, dtype=0) == ALIGN
+    assert q(codes=FAKE + 8) == ALIGN
+
+
+def test_dequantize_refusals(lib):
+    def q(dtype=1, dst=FAKE, rows=4, cols=64, ld=64, codes=FAKE, scales=FAKE):
+        return lib.base_mx_dequantize(codes, scales, rows, cols, dtype, dst, ld, None)
+    assert q(dtype=-1) == DTYPE
+    for kw in (dict(rows=0), dict(cols=31), dict(ld=32)):
+        assert q(**kw) == SHAPE, kw
+    assert q(dst=0) == NULL and q(codes=0) == NULL and q(scales=0) == NULL
+    assert q(dst=FAKE + 1) == ALIGN and q(dst=FAKE + 2, dtype=0) == ALIGN
+
+
+def test_pack_refusals(lib):
+    def p(L, *ptr):
+        return lib.base_mx_pack_experts(ctypes.byref(L), *(ptr or [FAKE] * 6), None)
+    ok = [FAKE] * 6
+    for i in range(6):
+        assert p(layer(), *[0 if j == i else v for j, v in enumerate(ok)]) == NULL
+    for i in (0, 2, 4, 5):
+        assert p(layer(), *[v + 8 if j == i else v for j, v in enumerate(ok)]) == ALIGN
+    assert p(layer(w_layout=1)) == SHAPE and p(layer(**MXL)) == SHAPE
+    assert p(layer(I=96)) == SHAPE and p(layer(d=128)) == SHAPE and p(layer(dtype=3)) == DTYPE
+    assert lib.base_mx_pack_experts(None, *ok, None) == NULL
+
+
+def test_quantize_experts_refusals(lib):
+    def p(L, a=FAKE, b=FAKE):
+        return lib.base_mx_quantize_experts(ctypes.byref(L), a, b, None)
+    assert p(layer(), a=0) == NULL and p(layer(), b=FAKE + 4) == ALIGN
+    assert p(layer(w13=0)) == NULL and p(layer(w2=FAKE + 4)) == ALIGN
+    assert p(layer(w_layout=1)) == SHAPE and p(layer(**MXL)) == SHAPE
+    assert lib.base_mx_quantize_experts(None, FAKE, FAKE, None) == NULL
+
+
+def test_calibration_takes_the_layout(lib):
+    L = layer(**MXL)
+    n = lib.base_calib_ws_bytes(ctypes.byref(L), 300)
+    assert n > 0
+    assert lib.base_calib_accumulate(ctypes.byref(L), FAKE, 300, FAKE, FAKE, n - 1, None) == WS
+
+
+def test_binding_refuses_host_tensors():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        bd.mx_quantize(torch.zeros(2, 64))
+    with pytest.raises(ValueError):
+        bd.mx_quantize(torch.zeros(2, 64, dtype=torch.float16))
+    with pytest.raises(ValueError):
+        bd.mx_dequantize(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 3, dtype=torch.uint8))
