@@ -273,6 +273,52 @@ base_status base_decode_layer(const base_layer *L, const void *x, int32_t B,
                               base_plan *plan_out, void *ws, size_t ws_bytes,
                               void *stream);
 
+/* Norms before and after a block, fused with the block's gate and the scale of
+ * the residual stream.  For rows of d elements, with n(v) = v / sqrt(mean v^2 +
+ * eps) (0 where mean v^2 + eps = 0):
+ *   h' = res_scale h + gate * (post_gain * n(y))   (y itself if post_gain is NULL)
+ *   x' = pre_gain * n(h')
+ * in fp32, h' and x' each rounded to `dtype` once (x' is made from h' before its
+ * rounding). */
+typedef struct base_norms {
+    int32_t d;              /* row length, 1 .. BASE_NORM_MAX_D */
+    int32_t dtype;          /* base_dtype of y, h, h_out and x_out */
+    float eps;              /* >= 0 */
+    float res_scale;        /* finite */
+    const float *post_gain; /* [d] fp32, or NULL: y is not normalised */
+    const float *gate;      /* fp32, or NULL: 1 */
+    int64_t gate_ld;        /* 0: one gate [d] for every row; else elements (>= d)
+                               from a row's gate to the next's */
+    const float *pre_gain;  /* [d] fp32; needed for x_out */
+} base_norms;
+#define BASE_NORM_MAX_D 16384
+#define BASE_NORM_MAX_ROWS 0x7FFFFFFFLL
+
+/*   y      the block's output, or NULL: h' = h (the norm before the first block;
+ *          res_scale, gate and post_gain are not read, and h_out must be NULL)
+ *   h      the residual stream
+ *   h_out  h', or NULL;  x_out  x', or NULL (not both)
+ * Each is rows x d with its own row stride (>= d elements); elements between the
+ * rows are not touched.  Element alignment suffices; 16-byte accesses are used
+ * where d, every stride and every pointer allow them.  h_out may be h or y, and
+ * x_out may be y or h, with the same stride; otherwise they must not overlap.
+ * BASE_ERR_SHAPE: d, rows, a stride, eps or res_scale outside the above;
+ * BASE_ERR_FLAGS: h_out without y, h_out the same as x_out, or another stride in
+ * place. */
+base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y, int64_t y_ld,
+                               const void *h, int64_t h_ld, void *h_out, int64_t h_out_ld,
+                               void *x_out, int64_t x_out_ld, void *stream);
+
+/* A decode block's tail in the layer's last launch: base_decode_layer without
+ * a residual, then base_norm_residual on its output y and the residual stream h,
+ * bit for bit, without y in memory.  h, h_out, x_out: [B][d], rows d elements
+ * apart, 16-B aligned, as are the gains and the gate (gate_ld a multiple of 4);
+ * h_out may be h, and x_out may be x (the layer's input, read before).  N->d and
+ * N->dtype are the layer's. */
+base_status base_decode_block(const base_layer *L, const base_norms *N, const void *x, int32_t B,
+                              int32_t budget, int32_t flags, const void *h, void *h_out, void *x_out,
+                              base_plan *plan_out, void *ws, size_t ws_bytes, void *stream);
+
 /* For callers that cannot allocate device memory (code under stream
  * capture, tight serving loops, harnesses that forbid allocation): the same
  * layer as base_decode_layer, with the workspace replaced by a fixed scratch

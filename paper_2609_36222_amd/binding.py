@@ -28,7 +28,8 @@ EXPORTS = ("base_workspace_bytes", "base_route", "base_predict_cost",
            "base_calib_stats_bytes", "base_calib_ws_bytes", "base_calib_reset",
            "base_calib_accumulate",
            "base_mx_quantize", "base_mx_dequantize", "base_mx_w13_bytes", "base_mx_w2_bytes",
-           "base_mx_pack_experts", "base_mx_quantize_experts")
+           "base_mx_pack_experts", "base_mx_quantize_experts",
+           "base_norm_residual", "base_decode_block")
 CALIB_LIB_PATH = os.path.join(HERE, "_lib", "libbase_calib.so")
 N_STAGES = 9     # one kernel each; base_set_stage_events takes 2 events per stage
 STAGES = ("scores", "tail", "select", "backfill", "compact", "gather",
@@ -55,6 +56,12 @@ _PLAN_FIELDS = ["logits", "topk_ids", "topk_w", "cost", "scores", "counts",
 
 class base_plan(ctypes.Structure):
     _fields_ = [(f, _vp) for f in _PLAN_FIELDS]
+
+
+class base_norms(ctypes.Structure):
+    _fields_ = [("d", _i32), ("dtype", _i32), ("eps", ctypes.c_float),
+                ("res_scale", ctypes.c_float), ("post_gain", _vp), ("gate", _vp),
+                ("gate_ld", _i64), ("pre_gain", _vp)]
 
 
 class BaseError(RuntimeError):
@@ -133,6 +140,13 @@ def load(path: str = LIB_PATH):
     L.base_mx_pack_experts.argtypes = [ctypes.POINTER(base_layer)] + [_vp] * 7
     L.base_mx_quantize_experts.restype = _i32
     L.base_mx_quantize_experts.argtypes = [ctypes.POINTER(base_layer)] + [_vp] * 3
+    L.base_norm_residual.restype = _i32
+    L.base_norm_residual.argtypes = [ctypes.POINTER(base_norms), _i64, _vp, _i64, _vp, _i64, _vp,
+                                     _i64, _vp, _i64, _vp]
+    L.base_decode_block.restype = _i32
+    L.base_decode_block.argtypes = [ctypes.POINTER(base_layer), ctypes.POINTER(base_norms), _vp,
+                                    _i32, _i32, _i32, _vp, _vp, _vp, ctypes.POINTER(base_plan),
+                                    _vp, ctypes.c_size_t, _vp]
     _lib = L
     return L
 
@@ -452,6 +466,80 @@ def mx_layer_from_codes(w_router, b_router, pred_a, pred_b, w13, w2, norm_topk: 
         shared = (*mx_pack_experts(w13s, w2s, stream), gate, int(w13s[0].shape[0]))
     return Layer.mxfp4(w_router, b_router, pred_a, pred_b, *mx_pack_experts(w13, w2, stream),
                        2 * w2[0].shape[2], norm_topk, score_rule, shared)
+
+
+class Norms:
+    """The parameters of the norms around a block (base_norms): fp32 gains [d], a
+    gate [d] (every row's) or [rows, d] (each row its own), the residual scale."""
+
+    def __init__(self, d, dtype, post_gain=None, gate=None, pre_gain=None, res_scale=1.0, eps=1e-6):
+        import torch
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("dtype: fp32 or bf16")
+        for t, what in ((post_gain, "post_gain"), (pre_gain, "pre_gain"), (gate, "gate")):
+            if t is None:
+                continue
+            if (t.dtype != torch.float32 or t.shape[-1] != d or t.dim() > (2 if what == "gate" else 1)
+                    or (d > 1 and t.stride(-1) != 1)):
+                raise ValueError(f"{what}: fp32, {d} adjacent elements a row")
+            _on_device(t, what)
+        self.tensors = (post_gain, gate, pre_gain)
+        self.d, self.torch_dtype = d, dtype
+        self.gate_rows = gate.shape[0] if gate is not None and gate.dim() == 2 else None
+        ld = 0 if self.gate_rows is None else (gate.stride(0) if self.gate_rows > 1 else d)
+        self.desc = base_norms(d, BASE_BF16 if dtype == torch.bfloat16 else BASE_F32, eps, res_scale,
+                               _ptr(post_gain), _ptr(gate), ld, _ptr(pre_gain))
+
+    def _check_rows(self, rows, *tensors):
+        if self.gate_rows not in (None, rows):
+            raise ValueError(f"gate: one row, or {rows}")
+        for t, what in tensors:
+            if t is None:
+                continue
+            if t.dtype != self.torch_dtype or tuple(t.shape) != (rows, self.d):
+                raise ValueError(f"{what}: {self.torch_dtype} [{rows}, {self.d}]")
+            _rows(t, what)
+
+
+def base_norm_residual(norms: Norms, y, h, h_out=None, x_out=None, stream=None):
+    """h_out = res_scale h + gate (post_gain n(y)), x_out = pre_gain n(h_out); [rows, d]
+    tensors whose rows may lie inside wider ones; y None: x_out = pre_gain n(h)."""
+    rows = h.shape[0]
+    norms._check_rows(rows, (y, "y"), (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
+    a = []
+    for t in (y, h, h_out, x_out):
+        a += [_ptr(t), 0 if t is None else _rows(t, "rows")[3]]
+    _check(load().base_norm_residual(ctypes.byref(norms.desc), rows, *a, _stream(stream)))
+
+
+def norm_residual(h, y=None, post_gain=None, gate=None, pre_gain=None, res_scale=1.0, eps=1e-6,
+                  h_out=None, x_out=None, stream=None):
+    """base_norm_residual with the parameters given here; returns (h_out, x_out), new
+    tensors where they are not given (None where there is nothing to write)."""
+    import torch
+    n = Norms(h.shape[1], h.dtype, post_gain, gate, pre_gain, res_scale, eps)
+    if h_out is None and y is not None:
+        h_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    if x_out is None and pre_gain is not None:
+        x_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    base_norm_residual(n, y, h, h_out, x_out, stream)
+    return h_out, x_out
+
+
+def base_decode_block(desc, norms: Norms, x, B, budget, flags, h, ws, h_out=None, x_out=None,
+                      plan=None, stream=None):
+    """base_decode_layer, then base_norm_residual on its output, in the layer's
+    launches; returns the filled base_plan (device pointers into ws)."""
+    plan = base_plan() if plan is None else plan
+    norms._check_rows(B, (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
+    for t, what in ((h, "h"), (h_out, "h_out"), (x_out, "x_out")):
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous rows")
+    _check(load().base_decode_block(
+        ctypes.byref(desc), ctypes.byref(norms.desc), _ptr(x), B, budget, flags, _ptr(h),
+        _ptr(h_out), _ptr(x_out), ctypes.byref(plan), _ptr(ws), ws.numel() * ws.element_size(),
+        _stream(stream)))
+    return plan
 
 
 def base_set_stage_events(events):

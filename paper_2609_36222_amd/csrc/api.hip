@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "../../include/base.h"
 #include "internal.hpp"
@@ -303,13 +304,23 @@ base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, i
   return BASE_OK;
 }
 
+// What follows the layer's experts: y = residual + sum, or (norms) the norm of
+// the sum into the residual stream h (base_decode_block).
+struct Tail {
+  const void *residual;
+  void *y;
+  const base_norms *norms = nullptr;
+  const void *h = nullptr;
+  void *h_out = nullptr, *x_out = nullptr;
+};
+
 // backfill (unless done with the selection) + compaction (unless planned:
 // done with both) + FFN + combine, on plan arrays already in place
 base_status run_forward(const base_layer *L, const void *x, int32_t B,
                         const float *logits, const int32_t *ids,
                         const int32_t *sel_ids, const int32_t *n_sel,
                         const int32_t *slot_of, int32_t bc, int32_t flags,
-                        const void *residual, void *y, void *ws,
+                        const Tail &tail, void *ws,
                         const Layout &o, hipStream_t st, bool backfilled = false,
                         bool planned = false) {
   const bool bf16 = L->dtype == BASE_BF16;
@@ -345,8 +356,13 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
   // base_moe_forward may bring any
   BASE_TRY(run_ffn(L, x, B, bc, backfilled ? std::min(bc, B * L->K) : bc, sel_ids, n_sel, ws, o, st));
   stage(8, st);
-  HIP_TRY(launch_combine(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf),
-                         residual, y, st));
+  if (const base_norms *N = tail.norms)
+    HIP_TRY(launch_combine_norm(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf), N->eps,
+                                N->res_scale, N->post_gain, N->gate, N->gate_ld, N->pre_gain, tail.h,
+                                tail.h_out, tail.x_out, st));
+  else
+    HIP_TRY(launch_combine(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf),
+                           tail.residual, tail.y, st));
   stage_end(st);
   return BASE_OK;
 }
@@ -483,23 +499,16 @@ base_status base_moe_forward(const base_layer *L, const void *x, int32_t B,
     HIP_TRY(launch_scores(L->dtype == BASE_BF16, x, B, L->d, nullptr, nullptr, 0,
                           shared_gate(L), nullptr, at<float>(ws, o.gdot), (hipStream_t)stream));
   BASE_TRY(run_forward(L, x, B, logits, topk_ids, sel_ids, n_sel,
-                       slot_of_expert, bc, flags, residual, y, ws, o,
+                       slot_of_expert, bc, flags, Tail{residual, y}, ws, o,
                        (hipStream_t)stream));
   fill_plan(plan_out, ws, o, false);
   return BASE_OK;
 }
 
-base_status base_decode_layer(const base_layer *L, const void *x, int32_t B,
-                              int32_t budget, int32_t flags,
-                              const void *residual, void *y,
-                              base_plan *plan_out, void *ws, size_t ws_bytes,
-                              void *stream) {
-  BASE_TRY(check_layer(L, B, true, true, true));
-  if (budget < 1) return BASE_ERR_BUDGET;
-  if (flags & ~3) return BASE_ERR_FLAGS;
-  BASE_TRY(check_ptr(x, 16));
-  BASE_TRY(check_ptr(y, 16));
-  if (residual && !aligned(residual, 16)) return BASE_ERR_ALIGN;
+// the whole layer, arguments checked
+static base_status decode_layer(const base_layer *L, const void *x, int32_t B, int32_t budget,
+                                int32_t flags, const Tail &tail, base_plan *plan_out, void *ws,
+                                size_t ws_bytes, void *stream) {
   const int32_t bc = budget < L->E ? budget : L->E;
   BASE_TRY(check_ws(L, B, bc, ws, ws_bytes));
   const Layout o = layout(L, B, bc);
@@ -545,9 +554,80 @@ base_status base_decode_layer(const base_layer *L, const void *x, int32_t B,
                                    device_cus(), st));
   stage_end(st);
   BASE_TRY(run_forward(L, x, B, logits, ids, sel, nsel, slot, bc, flags,
-                       residual, y, ws, o, st, true, joined));
+                       tail, ws, o, st, true, joined));
   fill_plan(plan_out, ws, o, true);
   return BASE_OK;
+}
+
+base_status base_decode_layer(const base_layer *L, const void *x, int32_t B,
+                              int32_t budget, int32_t flags,
+                              const void *residual, void *y,
+                              base_plan *plan_out, void *ws, size_t ws_bytes,
+                              void *stream) {
+  BASE_TRY(check_layer(L, B, true, true, true));
+  if (budget < 1) return BASE_ERR_BUDGET;
+  if (flags & ~3) return BASE_ERR_FLAGS;
+  BASE_TRY(check_ptr(x, 16));
+  BASE_TRY(check_ptr(y, 16));
+  if (residual && !aligned(residual, 16)) return BASE_ERR_ALIGN;
+  return decode_layer(L, x, B, budget, flags, Tail{residual, y}, plan_out, ws, ws_bytes, stream);
+}
+
+// rows, the outputs asked for and the parameters they need
+static base_status check_norms(const base_norms *N, int64_t rows, bool has_y, const void *h,
+                               const void *h_out, const void *x_out) {
+  if (!N || !h || (!h_out && !x_out)) return BASE_ERR_NULL;
+  if (N->dtype != BASE_F32 && N->dtype != BASE_BF16) return BASE_ERR_DTYPE;
+  if (N->d < 1 || N->d > BASE_NORM_MAX_D || rows < 1 || rows > BASE_NORM_MAX_ROWS)
+    return BASE_ERR_SHAPE;
+  if (!(N->eps >= 0.0f) || !std::isfinite(N->eps) || !std::isfinite(N->res_scale))
+    return BASE_ERR_SHAPE;
+  if (N->gate && N->gate_ld != 0 && (N->gate_ld < N->d || N->gate_ld > BASE_MX_MAX_LD))
+    return BASE_ERR_SHAPE;
+  if (x_out && !N->pre_gain) return BASE_ERR_NULL;
+  if (!has_y && h_out) return BASE_ERR_FLAGS;   // nothing to add: h' is h
+  if (h_out && h_out == x_out) return BASE_ERR_FLAGS;
+  for (const float *p : {N->post_gain, N->gate, N->pre_gain})
+    if (p && !aligned(p, 4)) return BASE_ERR_ALIGN;
+  return BASE_OK;
+}
+
+base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y, int64_t y_ld,
+                               const void *h, int64_t h_ld, void *h_out, int64_t h_out_ld,
+                               void *x_out, int64_t x_out_ld, void *stream) {
+  BASE_TRY(check_norms(N, rows, y != nullptr, h, h_out, x_out));
+  const struct { const void *p; int64_t ld; } rs[] = {{y, y_ld}, {h, h_ld}, {h_out, h_out_ld}, {x_out, x_out_ld}};
+  for (const auto &r : rs) {
+    if (!r.p) continue;
+    if (r.ld < N->d || r.ld > BASE_MX_MAX_LD) return BASE_ERR_SHAPE;
+    if (!aligned(r.p, elem_bytes(N->dtype))) return BASE_ERR_ALIGN;
+  }
+  // in place only row by row
+  if ((h_out == h && h_out_ld != h_ld) || (x_out && x_out == y && x_out_ld != y_ld) ||
+      (x_out == h && x_out_ld != h_ld) || (y && h_out == y && h_out_ld != y_ld))
+    return BASE_ERR_FLAGS;
+  HIP_TRY(launch_norm(N->dtype == BASE_BF16, N->d, N->eps, N->res_scale, N->post_gain, N->gate,
+                      N->gate_ld, N->pre_gain, rows, y, y_ld, h, h_ld, h_out, h_out_ld, x_out,
+                      x_out_ld, (hipStream_t)stream));
+  return BASE_OK;
+}
+
+base_status base_decode_block(const base_layer *L, const base_norms *N, const void *x, int32_t B,
+                              int32_t budget, int32_t flags, const void *h, void *h_out, void *x_out,
+                              base_plan *plan_out, void *ws, size_t ws_bytes, void *stream) {
+  BASE_TRY(check_layer(L, B, true, true, true));
+  if (budget < 1) return BASE_ERR_BUDGET;
+  if (flags & ~3) return BASE_ERR_FLAGS;
+  BASE_TRY(check_ptr(x, 16));
+  BASE_TRY(check_norms(N, B, true, h, h_out, x_out));
+  if (N->d != L->d) return BASE_ERR_SHAPE;
+  if (N->dtype != L->dtype) return BASE_ERR_DTYPE;
+  for (const void *p : {h, (const void *)h_out, (const void *)x_out, (const void *)N->post_gain,
+                        (const void *)N->gate, (const void *)N->pre_gain})
+    if (p && !aligned(p, 16)) return BASE_ERR_ALIGN;
+  if (N->gate && N->gate_ld % 4) return BASE_ERR_ALIGN;
+  return decode_layer(L, x, B, budget, flags, Tail{nullptr, nullptr, N, h, h_out, x_out}, plan_out, ws,
+                      ws_bytes, stream);
 }
 
 base_status base_decode_layer_noalloc(const base_layer *L, const void *x, int32_t B,

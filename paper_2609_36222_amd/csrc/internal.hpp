@@ -346,6 +346,20 @@ hipError_t launch_combine(bool bf16, int B, int d, int kc,
                           const int32_t *pair_of, const float *pairbuf,
                           const void *residual, void *y, hipStream_t st);
 
+// h' = scale h + gate (post n(y)), x' = pre n(h') (norm.hip): rows of d elements
+// with the strides given; y null: h' = h (ho must be null), post / gate null: left
+// out, gate_ld 0: one gate row; ho, xo null: not written
+hipError_t launch_norm(bool bf16, int d, float eps, float scale, const float *post, const float *gate,
+                       long long gate_ld, const float *pre, long long rows, const void *y,
+                       long long y_ld, const void *h, long long h_ld, void *ho, long long ho_ld,
+                       void *xo, long long xo_ld, hipStream_t st);
+// the combine (no residual) and the same on its output, d a multiple of 256; every
+// pointer 16-byte aligned, gate_ld a multiple of four
+hipError_t launch_combine_norm(bool bf16, int B, int d, int kc, const int32_t *pair_of,
+                               const float *pairbuf, float eps, float scale, const float *post,
+                               const float *gate, long long gate_ld, const float *pre, const void *h,
+                               void *ho, void *xo, hipStream_t st);
+
 // Calibration statistics (per expert u): head[u] = (n, sum y, sum y^2, 0)
 // fp64, sz[u][d] and q[u][d] fp64, G[u][d][d] fp32; each array 256-byte
 // aligned in the caller's buffer, in this order.
