@@ -310,8 +310,8 @@ base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y,
                                void *x_out, int64_t x_out_ld, void *stream);
 
 /* A decode block's tail in the layer's last launch: base_decode_layer without
- * a residual, then base_norm_residual on its output y and the residual stream h,
- * bit for bit, without y in memory.  h, h_out, x_out: [B][d], rows d elements
+ * a residual, then base_norm_residual on its output y and the residual stream h
+ * (16-byte aligned rows), bit for bit, without y in memory.  h, h_out, x_out: [B][d], rows d elements
  * apart, 16-B aligned, as are the gains and the gate (gate_ld a multiple of 4);
  * h_out may be h, and x_out may be x (the layer's input, read before).  N->d and
  * N->dtype are the layer's. */

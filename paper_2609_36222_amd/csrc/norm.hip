@@ -190,6 +190,19 @@ void k_combine_norm(NormArgs a, int kc, const int32_t *__restrict__ pair_of,
       h + (size_t)t * d, ho ? ho + (size_t)t * d : nullptr, xo ? xo + (size_t)t * d : nullptr, red);
 }
 
+// The shapes of a row by its length, LAUNCH(threads a row, elements a thread, rows a
+// workgroup).  k_norm and k_combine_norm take the same ones, so that their sums
+// have the same order and the block call the bits of its parts.
+#define BASE_NORM_SHAPES(d, LAUNCH)       \
+  do {                                    \
+    if ((d) <= 512) LAUNCH(64, 8, 4);     \
+    else if ((d) <= 1024) LAUNCH(64, 16, 4); \
+    else if ((d) <= 2048) LAUNCH(256, 8, 1); \
+    else if ((d) <= 4096) LAUNCH(256, 16, 1); \
+    else if ((d) <= 8192) LAUNCH(512, 16, 1); \
+    else LAUNCH(1024, 16, 1);             \
+  } while (0)
+
 namespace {
 constexpr long long NORM_BLOCKS = 1 << 22;   // workgroups at most; they stride over the rows
 
@@ -205,12 +218,7 @@ hipError_t norm_launch(const NormArgs &a, long long rows, const void *y, long lo
              0, st, a, rows, (const T *)y, y_ld, (const T *)h, h_ld, (T *)ho, ho_ld, (T *)xo, \
              xo_ld);                                                                          \
   } while (0)
-  if (a.d <= 512) BASE_NORM(64, 8, 4);
-  else if (a.d <= 1024) BASE_NORM(64, 16, 4);
-  else if (a.d <= 2048) BASE_NORM(256, 8, 1);
-  else if (a.d <= 4096) BASE_NORM(256, 16, 1);
-  else if (a.d <= 8192) BASE_NORM(512, 16, 1);
-  else BASE_NORM(1024, 16, 1);
+  BASE_NORM_SHAPES(a.d, BASE_NORM);
 #undef BASE_NORM
   return hipGetLastError();
 }
@@ -239,19 +247,16 @@ hipError_t launch_combine_norm(bool bf16, int B, int d, int kc, const int32_t *p
                                const float *gate, long long gate_ld, const float *pre, const void *h,
                                void *ho, void *xo, hipStream_t st) {
   const NormArgs a{d, eps, scale, post, gate, pre, gate_ld};
-#define BASE_CN(T, TPR, EPT, V)                                                                     \
-  launch_k(k_combine_norm<T, TPR, EPT, V>, dim3(B), dim3(TPR), 0, st, a, kc, pair_of, pairbuf,      \
-           (const T *)h, (T *)ho, (T *)xo)
-#define BASE_CND(T, V)                          \
-  do {                                          \
-    if (d <= 2048) BASE_CN(T, 256, 8, V);       \
-    else if (d <= 4096) BASE_CN(T, 512, 8, V);  \
-    else if (d <= 8192) BASE_CN(T, 1024, 8, V); \
-    else BASE_CN(T, 1024, 16, V);               \
+#define BASE_CN(TPR, EPT, RPW)                                                                  \
+  do {                                                                                          \
+    if (bf16)                                                                                   \
+      launch_k(k_combine_norm<uint16_t, TPR, EPT, 8>, dim3(B), dim3(TPR), 0, st, a, kc, pair_of, \
+               pairbuf, (const uint16_t *)h, (uint16_t *)ho, (uint16_t *)xo);                   \
+    else                                                                                        \
+      launch_k(k_combine_norm<float, TPR, EPT, 4>, dim3(B), dim3(TPR), 0, st, a, kc, pair_of,   \
+               pairbuf, (const float *)h, (float *)ho, (float *)xo);                            \
   } while (0)
-  if (bf16) BASE_CND(uint16_t, 8);
-  else BASE_CND(float, 4);
-#undef BASE_CND
+  BASE_NORM_SHAPES(d, BASE_CN);
 #undef BASE_CN
   return hipGetLastError();
 }

@@ -219,7 +219,10 @@ def block_norms(bd, d, dtype, B, per_token, seed=0):
 @pytest.mark.parametrize("bf16,kind,d,B", [(True, "mx", 256, 1), (True, "mx", 512, 7), (True, "packed", 256, 40),
                                            (True, "mx", 256, 100), (False, "rowmajor", 256, 9),
                                            (True, "packed", 4096, 3), (True, "mx", 8192, 5),
-                                           (True, "packed", 16384, 2), (False, "rowmajor", 16384, 2)])
+                                           (True, "packed", 16384, 2), (False, "rowmajor", 16384, 2),
+                                           (False, "rowmajor", 512, 64), (False, "rowmajor", 1024, 64),
+                                           (False, "rowmajor", 2048, 64), (False, "rowmajor", 4096, 64),
+                                           (False, "rowmajor", 8192, 64)])
 def test_block_is_its_parts(gu, bd, bf16, kind, d, B):
     """base_decode_block against base_decode_layer and base_norm_residual, bit for
     bit, with shared experts, dropped routes (rows of nothing) and in place."""
