@@ -285,7 +285,7 @@ base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, i
   stage(6, st);
   if (mx_layer(L))
     HIP_TRY(launch_mx_gateup(x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13, L->w13_shared,
-                             rec, sptok, H, st));
+                             rec, sptok, H, n_cu, st));
   else
     HIP_TRY(launch_gateup(bf16, packed, x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13,
                           L->w13_shared, sel_ids, n_sel, offsets, at<int32_t>(ws, o.pair_tok), hdr,

@@ -6,11 +6,12 @@
 //
 // The launch works on records {expert, first pair, pairs}: a slot (B <= 64) or
 // a part of at most MX_NT 16-pair tiles of one, with their token lists, one copy
-// per die.  A workgroup takes (record, row group); its wavefronts own MX_T
-// 16-row tiles each over the whole contraction, so a sum has one writer and one
-// order.  Weights come to registers (16 bytes a lane: four operands and one
-// scale, see mx.hpp), MX_DW steps of 128 ahead; the record's token rows are
-// staged through an LDS ring that the wavefronts share.
+// per die.  A workgroup takes (record, row group): RW wavefronts side by side on
+// T 16-row tiles each, and KW such rows of wavefronts on consecutive shares
+// of the contraction, joined through LDS in ascending order -- a sum has
+// one writer and one order.  Weights come to registers (16 bytes a lane: four
+// operands and one scale, see mx.hpp) DT + 1 steps of 128 ahead, the token rows
+// of up to NT tiles to an LDS ring of DT + 1 steps that the RW wavefronts share.
 #include "common.hpp"
 #include "ffn.hpp"
 #include "internal.hpp"
@@ -18,263 +19,394 @@
 
 namespace basek {
 
-constexpr int MX_WAVES = 4;
-constexpr int MX_THREADS = MX_WAVES * WAVE;
-constexpr int MX_T = 2;    // tiles per wavefront (gate/up: a gate tile and its up tile)
-constexpr int MX_DW = 4;   // steps of weights in flight (a chunk: the stage index is static)
-constexpr int MX_DT = MX_DW - 1;   // steps of tokens in flight
-constexpr int MX_RING = MX_DT + 1;
-static_assert(MX_DW == MX_CHUNK, "one chunk of stages");
-
-// The record and row group of this workgroup.  Workgroup b runs on die b %
-// N_XCD; the row groups of slot `ord` are numbered on from the previous slot's
-// and number v lies on die v % N_XCD, so that all parts of a slot read a row
-// group's weights through one L2 and every die has its share of every slot.
-struct MxWork {
-  int u, p0, n, rg;
+template <int NT_, int T_, int RW_, int KW_, int DT_>
+struct MxShape {
+  static constexpr int NT = NT_, T = T_, RW = RW_, KW = KW_, DT = DT_;
+  static constexpr int WAVES = RW * KW, THREADS = WAVES * WAVE, RING = DT + 1;
+  static constexpr int SLOT = NT * 4096;               // a step's token rows
+  static constexpr int TL = NT * 4 / RW;               // token loads per wavefront and step
+  static constexpr int SL = KW == 1 ? T : 2 * T;       // scale loads per four steps
+  static constexpr int LDS = KW * RING * SLOT;
+  static constexpr int GROUP = RW * T;                 // tiles per workgroup
+  static constexpr int WPE = NT * T >= 16 ? 2 : DT == 1 ? 4 : 3;   // wavefronts per SIMD
+  static_assert(DT < MX_CHUNK, "weights, one step further ahead, have a chunk of stages");
+  static_assert(LDS >= (KW > 1 ? WAVES * T * NT * 1024 : 0), "partial sums in the ring");
 };
-__device__ __forceinline__ MxWork mx_work(int budget, int ns, int nrec, bool parts, int RG,
-                                          const SpRec *__restrict__ rec) {
+
+// The record, row group and first token tile of this workgroup.  Workgroup b runs
+// on die b % N_XCD; the row groups of slot `ord` are numbered on from the previous
+// slot's and number v lies on die v % N_XCD, so that all parts of a slot read a
+// row group's weights through one L2 and every die has its share of every slot.
+// `cuts` workgroups share a record's token tiles.
+struct MxPlan {
+  int budget, ns, nrec, parts, cuts;
+  const SpRec *rec;
+};
+struct MxWork {
+  int u, p0, n, rg, c0;
+};
+__device__ __forceinline__ MxWork mx_work(const MxPlan &pl, int RG, int NT) {
   const int die = blockIdx.x % N_XCD, q = blockIdx.x / N_XCD;
-  const int per = (RG + N_XCD - 1) / N_XCD;
-  const int y = q / per, k = q - y * per;
+  const int per = ((RG + N_XCD - 1) / N_XCD) * pl.cuts;
+  const int y = q / per, z = q - y * per, k = z / pl.cuts;
   // slots: the shared experts first, they run for every token
-  const int i = parts ? y : (y < ns ? budget + y : y - ns);
-  const SpRec r = rec[die * nrec + i];
-  const int ord = parts ? __builtin_amdgcn_readfirstlane(r.pad) : y;
+  const int i = pl.parts ? y : (y < pl.ns ? pl.budget + y : y - pl.ns);
+  const SpRec r = pl.rec[die * pl.nrec + i];
+  const int ord = pl.parts ? __builtin_amdgcn_readfirstlane(r.pad) : y;
   const int rg = ((die - ord * RG) & (N_XCD - 1)) + N_XCD * k;
   return {__builtin_amdgcn_readfirstlane(r.u), __builtin_amdgcn_readfirstlane(r.p0),
-          rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg};
+          rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg, (z - k * pl.cuts) * 16 * NT};
 }
 
-// acc[t][j] = sum over the K elements of tile t of the weights (resource rw[t])
-// times token tile j.  Token rows:
-// resource rx, this lane's row of tile j at byte tv[j] (FFN_TOK_PAD or more: a
-// zero row); it stages one 16-byte piece of the 256 a step has of the row.
-//  * LDS: row n of a tile at 256 n, its piece p at position p ^ n, so that
-//    neither the 16 rows' reads of one piece nor a row's write meet a bank twice.
-//  * Order of the loads: in iteration s the tokens of step s + MX_DT, then the
-//    weights of step s + MX_DW (with a chunk's first step, that chunk's scales).
-//    So when the tokens of step s have arrived, so have its weights, and the
-//    weights of the three steps after it may still be in flight.
-template <int NT>
-__device__ __forceinline__ void mx_stream(uint8_t *ring, const rsrc_t (&rw)[MX_T], int K,
-                                          rsrc_t rx, const uint32_t (&tv)[NT],
-                                          f32x4 (&acc)[MX_T][NT]) {
-  const int w = wave_id_u(), lane = lane_id();
-  const int S = mx_steps(K);
-  const int row = 4 * w + (lane >> 4);                       // of a tile, staged by this lane
-  const uint32_t pc = 16u * (uint32_t)((lane & 15) ^ row);   // its piece, in bytes of the step
+__device__ __forceinline__ int mx_block_pos(int g) { return (0x9C >> (2 * g)) & 3; }   // 0, 3, 1, 2
+__device__ __forceinline__ int mx_block_at(int pos) { return (0x78 >> (2 * pos)) & 3; }  // its inverse
+
+// The wait of a wavefront's step 4 i + p: until its tokens and, older, its weights
+// are there.  Behind the tokens of step s are the tokens of s + 1 .. s + DT - 1
+// (TL loads each) and the weights of s + 1 .. s + DT (T each, and SL scale loads
+// with every fourth); at first, with the prologue's weights in front of all
+// tokens, only the weights requested since.
+template <typename M>
+__device__ __forceinline__ void mx_wait(bool first, int p) {
+#define BASE_MXW(P)                                                                             \
+  case P:                                                                                       \
+    if (P < M::DT && first)                                                                     \
+      wait_vm<(M::DT - 1) * M::TL + P * M::T + (M::DT + P) / MX_CHUNK * M::SL>();               \
+    else                                                                                        \
+      wait_vm<(M::DT - 1) * M::TL + M::DT * M::T + (M::DT + P) / MX_CHUNK * M::SL>();           \
+    break;
+  switch (p) { BASE_MXW(0) BASE_MXW(1) BASE_MXW(2) BASE_MXW(3) }
+#undef BASE_MXW
+}
+
+// This wavefront's tiles of a matrix of `tiles` tiles of K elements: [t0, t0 + T), all
+// of them there or none (`tiles` is a multiple of T).
+template <int T>
+struct MxTiles {
+  int t0;
+  bool active;
+  rsrc_t rw[T];
+};
+template <typename M>
+__device__ __forceinline__ MxTiles<M::T> mx_tiles(const uint8_t *w, int rg, int tiles, int K) {
+  MxTiles<M::T> m;
+  m.t0 = (rg * M::RW + wave_id_u() % M::RW) * M::T;
+  m.active = m.t0 < tiles;
+  const size_t tb = mx_tile_bytes(K);
+#pragma unroll
+  for (int t = 0; t < M::T; ++t)
+    m.rw[t] = make_rsrc(w + (size_t)(m.active ? m.t0 + t : 0) * tb, m.active ? (uint32_t)tb : 0u);
+  return m;
+}
+// row groups of such a matrix
+__host__ __device__ inline int mx_groups(int tiles, int group) { return (tiles + group - 1) / group; }
+
+// acc[t][j] = sum over this wavefront's share of the K elements of tile t of the
+// weights times token tile j (N of them).  Token rows: resource rx; rows(i) says at
+// which byte row i starts (FFN_TOK_PAD: a row of zeros).
+//  * LDS: row n of a tile at 256 n, operand f of its block g in the 16 bytes at
+//    (4 mx_block_pos(g) + f) ^ n.  A 16-byte read takes 16 lanes at a time, the rows
+//    0..3 and 12..15 of an even block with the rows 4..11 of the odd one after it
+//    (or the other way round), so the two blocks' places have to differ by 12: with
+//    4 g + f half of the cycles were conflicts (Qwen3-shaped gate/up, B = 1024, 128
+//    experts 106 -> 95 us).
+//  * Order of the loads: in step s the tokens of step s + DT and the weights of step
+//    s + DT + 1, so that the wait for a step's tokens covers its weights and leaves
+//    those of the DT steps after it in flight.
+template <typename M, int N, typename Rows>
+__device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, int K, rsrc_t rx,
+                                          Rows rows, f32x4 (&acc)[M::T][N]) {
+  constexpr int T = M::T, DT = M::DT, L = 4 / M::RW;   // L loads of four rows per tile
+  constexpr int TL = N * L;
+  const int w = wave_id_u(), lane = lane_id(), kq = w / M::RW, rw = w % M::RW;
+  uint8_t *ring = lds + kq * (M::RING * M::SLOT);
+  const int S = mx_steps(K), s0 = kq * S / M::KW, s1 = (kq + 1) * S / M::KW;
+  const int most = (S + M::KW - 1) / M::KW;   // steps of the longest share
   const uint32_t Kb = (uint32_t)K * 2u;
-  const int n = lane & 15, g = lane >> 4;
-  auto tokens = [&](int s) {
-    uint8_t *slot = ring + (s % MX_RING) * (NT * 4096) + w * 1024;
-    const uint32_t at = (uint32_t)s * 256u + pc;
+  // the rows this lane stages: row r of every tile for r = 4 (rw L + q) + lane / 16,
+  // its 16 bytes in place lane % 16 of the row
+  uint32_t tv[N][L], pc[L];
+  // the ring's slots in turn, as running offsets: step i's to read and step i + DT's
+  // to fill (a remainder in the addresses costs an add per LDS read)
+  int fill = 0, read = 0;
+  auto next = [](int &slot) { slot = slot == (M::RING - 1) * M::SLOT ? 0 : slot + M::SLOT; };
+  auto tokens = [&](int i) {
+    uint8_t *slot = ring + fill + rw * (L * 1024);
+    next(fill);
+    const uint32_t at = (uint32_t)(s0 + i) * 256u;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) load_lds(rx, slot + j * 4096, at < Kb ? tv[j] + at : FFN_TOK_PAD, 0);
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int q = 0; q < L; ++q)
+        load_lds(rx, slot + j * 4096 + q * 1024,
+                 s0 + i < s1 && at + pc[q] < Kb ? tv[j][q] + at + pc[q] : FFN_TOK_PAD, 0);
   };
-  u32x4 wt[MX_DW][MX_T];
-  uint32_t sc[MX_T], sn[MX_T];
-  auto weights = [&](int p, int s) {
-    // past the tile: beyond its resource, zero
-    const uint32_t c0 = s < S ? (uint32_t)(s / MX_CHUNK) * MX_CHUNK_BYTES : FFN_TOK_PAD;
+  u32x4 wt[MX_CHUNK][T];
+  uint32_t sc[T], sn[T], sh[T];
+  auto weights = [&](int p, int i) {
+    const int s = s0 + i;
+    // past the share: beyond the tile's resource, zero
+    const uint32_t c0 = s < s1 ? (uint32_t)(s / MX_CHUNK) * MX_CHUNK_BYTES : FFN_TOK_PAD;
+    const uint32_t at = c0 + 256u + (uint32_t)(s % MX_CHUNK) * 1024u;
 #pragma unroll
-    for (int t = 0; t < MX_T; ++t) {
-      if (p == 0) sn[t] = __builtin_amdgcn_raw_buffer_load_b32(rw[t], (int)(c0 + lane * 4), 0, 0);
-      wt[p][t] = __builtin_bit_cast(u32x4, bload(rw[t], c0 + 256u + (uint32_t)p * 1024u + lane * 16, 0));
+    for (int t = 0; t < T; ++t) {
+      if (p == 0) {
+        sn[t] = __builtin_amdgcn_raw_buffer_load_b32(m.rw[t], (int)(c0 + lane * 4), 0, 0);
+        if (M::KW > 1)   // a share may begin inside a chunk
+          sh[t] = __builtin_amdgcn_raw_buffer_load_b32(m.rw[t], (int)(c0 + MX_CHUNK_BYTES + lane * 4), 0, 0);
+      }
+      wt[p][t] = __builtin_bit_cast(u32x4, bload(m.rw[t], at + lane * 16, 0));
     }
   };
 #pragma unroll
-  for (int t = 0; t < MX_T; ++t)
+  for (int t = 0; t < T; ++t) {
+    sc[t] = 0;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[t][j] = f32x4{0, 0, 0, 0};
-  // the groups of iterations -DW .. -1
-  weights(0, 0);
+    for (int j = 0; j < N; ++j) acc[t][j] = f32x4{0, 0, 0, 0};
+  }
+  // the weights first: the token list is still on its way
 #pragma unroll
-  for (int p = 0; p < MX_DT; ++p) {
-    tokens(p);
-    weights(p + 1, p + 1);
+  for (int p = 0; p <= DT; ++p) weights(p, p);
+#pragma unroll
+  for (int q = 0; q < L; ++q) {
+    const int r = 4 * (rw * L + q) + (lane >> 4), at16 = (lane & 15) ^ r;
+    pc[q] = 64u * (uint32_t)mx_block_at(at16 >> 2) + 16u * (uint32_t)(at16 & 3);
+#pragma unroll
+    for (int j = 0; j < N; ++j) tv[j][q] = rows(16 * j + r);
   }
 #pragma unroll
-  for (int t = 0; t < MX_T; ++t) sc[t] = 0;
-  for (int s0 = 0; s0 < S; s0 += MX_DW) {
+  for (int p = 0; p < DT; ++p) tokens(p);
+  const uint8_t *op[4];   // operand f of this lane's token and block, in slot 0
 #pragma unroll
-    for (int p = 0; p < MX_DW; ++p) {
-      const int s = s0 + p;
-      // in flight: the tokens of s + 1, s + 2 and the weights of s + 1 .. s + 3, one
-      // of which starts a chunk unless this step does
-      if (p == 0) wait_vm<2 * NT + 3 * MX_T>();
-      else wait_vm<2 * NT + 4 * MX_T>();
-      wg_barrier();
+  for (int f = 0; f < 4; ++f)
+    op[f] = ring + (lane & 15) * 256 + 16 * ((4 * mx_block_pos(lane >> 4) + f) ^ (lane & 15));
+  for (int i0 = 0; i0 < most; i0 += MX_CHUNK) {
+#pragma unroll
+    for (int p = 0; p < MX_CHUNK; ++p) {
+      const int i = i0 + p;
+      mx_wait<MxShape<N, T, M::RW, M::KW, DT>>(i0 == 0, p);
+      if (M::RW > 1) wg_barrier();   // the others' rows are there, the next slot is read
       __builtin_amdgcn_sched_barrier(0);
-      tokens(s + MX_DT);
+      tokens(i + DT);
+      if constexpr (DT + 1 < MX_CHUNK) weights((p + DT + 1) % MX_CHUNK, i + DT + 1);
       __builtin_amdgcn_sched_barrier(0);
       if (p == 0) {
 #pragma unroll
-        for (int t = 0; t < MX_T; ++t) sc[t] = sn[t];
+        for (int t = 0; t < T; ++t)
+          sc[t] = M::KW > 1 ? __builtin_amdgcn_alignbyte(sh[t], sn[t], (uint32_t)s0 & 3u) : sn[t];
       }
-      if (s < S) {
-        const uint8_t *sb = ring + (s % MX_RING) * (NT * 4096) + n * 256;
-        float scale[MX_T];
+      if (m.active && s0 + i < s1) {
+        float scale[T];
 #pragma unroll
-        for (int t = 0; t < MX_T; ++t) scale[t] = mx_scale((sc[t] >> (8 * p)) & 0xFFu);
+        for (int t = 0; t < T; ++t) scale[t] = mx_scale((sc[t] >> (8 * p)) & 0xFFu);
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-          bf16x8 x[NT];
+          bf16x8 x[N];
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
-            x[j] = *reinterpret_cast<const bf16x8 *>(sb + j * 4096 + 16 * ((4 * g + f) ^ n));
+          for (int j = 0; j < N; ++j)
+            x[j] = *reinterpret_cast<const bf16x8 *>(op[f] + read + j * 4096);
 #pragma unroll
-          for (int t = 0; t < MX_T; ++t) {
+          for (int t = 0; t < T; ++t) {
             const bf16x8 a = mx_decode8(wt[p][t][f], scale[t]);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[t][j] = mfma16(a, x[j], acc[t][j]);
+            for (int j = 0; j < N; ++j) acc[t][j] = mfma16(a, x[j], acc[t][j]);
           }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      weights(p, s + MX_DW);
+      next(read);
+      // ... of this step's own stage only once it has been read
+      if constexpr (DT + 1 == MX_CHUNK) weights(p, i + DT + 1);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
   wait_vm<0>();
+  if constexpr (M::KW > 1) {   // the shares' sums into the ring
+    wg_barrier();
+    f32x4 *red = reinterpret_cast<f32x4 *>(lds) + w * (T * N * WAVE) + lane;
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int j = 0; j < N; ++j) red[(t * N + j) * WAVE] = acc[t][j];
+    __syncthreads();
+  }
 }
 
-// this lane's staged row of token tile j: pair 16 j + row
-__device__ __forceinline__ int mx_stage_row(int j) { return 16 * j + 4 * wave_id() + (lane_id() >> 4); }
-
-template <int NT>
-__device__ __forceinline__ void mx_gateup_part(uint8_t *ring, const MxWork &k, int d, int I,
-                                               const uint8_t *__restrict__ w13, const int32_t *tok,
-                                               int n, rsrc_t rx, uint16_t *__restrict__ h0) {
-  const int w = wave_id_u(), lane = lane_id();
-  const int r = k.rg * MX_WAVES + w;   // row-pair tile: I / 16 is a multiple of MX_WAVES
-  const size_t tb = mx_tile_bytes(d);
-  rsrc_t rw[MX_T];
+// out(t, j, sum) for the C tiles from t on at a time (gate/up: a gate tile and its up
+// tile), each by one of the KW wavefronts that hold shares of them.
+template <typename M, int N, int C, typename Out>
+__device__ __forceinline__ void mx_emit(const uint8_t *lds, const f32x4 (&acc)[M::T][N], Out out) {
+  if constexpr (M::KW == 1) {
 #pragma unroll
-  for (int t = 0; t < MX_T; ++t) rw[t] = make_rsrc(w13 + (size_t)(2 * r + t) * tb, (uint32_t)tb);
-  uint32_t tv[NT];
+    for (int t = 0; t < M::T; t += C)
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int i = mx_stage_row(j);
-    tv[j] = i < n ? (uint32_t)tok[i] * (uint32_t)d * 2u : FFN_TOK_PAD;
-  }
-  f32x4 acc[MX_T][NT];
-  mx_stream<NT>(ring, rw, d, rx, tv, acc);
+      for (int j = 0; j < N; ++j) {
+        f32x4 v[C];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int p = 16 * j + (lane & 15);
-    if (p < n) {
-      uint16_t h[4];
+        for (int c = 0; c < C; ++c) v[c] = acc[t + c][j];
+        out(t, j, v);
+      }
+  } else {
+    const int w = wave_id_u(), kq = w / M::RW, rw = w % M::RW;
+    const f32x4 *red = reinterpret_cast<const f32x4 *>(lds) + rw * (M::T * N * WAVE) + lane_id();
+    for (int it = kq; it < M::T / C * N; it += M::KW) {
+      const int t = it / N * C, j = it % N;
+      f32x4 v[C];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) h[q] = f32_to_bf16(silu_bf16(acc[0][j][q]) * acc[1][j][q]);
-      const u32x2 pk = {(uint32_t)h[0] | ((uint32_t)h[1] << 16),
-                        (uint32_t)h[2] | ((uint32_t)h[3] << 16)};
-      *reinterpret_cast<u32x2 *>(h0 + (size_t)p * I + 16 * r + 4 * (lane >> 4)) = pk;
+      for (int c = 0; c < C; ++c) {
+        v[c] = red[((t + c) * N + j) * WAVE];
+#pragma unroll
+        for (int k = 1; k < M::KW; ++k) {
+          const f32x4 o = red[(k * M::RW * M::T * N + (t + c) * N + j) * WAVE];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[c][q] = v[c][q] + o[q];
+        }
+      }
+      out(t, j, v);
     }
   }
 }
 
-template <int NT>
-__global__ __launch_bounds__(MX_THREADS)
-void k_mx_gateup(int d, int I, int E, int budget, int ns, int nrec, int parts, int np,
-                 const uint8_t *__restrict__ w13r, const uint8_t *__restrict__ w13s,
-                 const SpRec *__restrict__ rec, const int32_t *__restrict__ sptok,
+template <typename M>
+__global__ __launch_bounds__(M::THREADS, M::WPE)
+void k_mx_gateup(int d, int I, int E, MxPlan pl, int np, const uint8_t *__restrict__ w13r,
+                 const uint8_t *__restrict__ w13s, const int32_t *__restrict__ sptok,
                  const uint16_t *__restrict__ x, int B, uint16_t *__restrict__ H) {
-  __shared__ __attribute__((aligned(16))) uint8_t ring[MX_RING * NT * 4096];
-  const MxWork k = mx_work(budget, ns, nrec, parts != 0, I / 16 / MX_WAVES, rec);
-  if (k.n <= 0) return;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
+  const MxWork k = mx_work(pl, mx_groups(I / 8, M::GROUP), M::NT);
   const size_t eb = (size_t)(I / 8) * mx_tile_bytes(d);
   const uint8_t *w13 = k.u < E ? w13r + (size_t)k.u * eb : w13s + (size_t)(k.u - E) * eb;
-  const int32_t *tok = sptok + (size_t)(blockIdx.x % N_XCD) * np + k.p0;
   const rsrc_t rx = make_rsrc(x, (uint32_t)B * (uint32_t)d * 2u);
-  for (int c = 0; c < k.n; c += 16 * NT) {
-    const int n = min(k.n - c, 16 * NT);
-    if (c > 0) wg_barrier();   // every wavefront is done with the ring
-    sp_tiles<NT>((n + 15) / 16, [&](auto N) {
-      mx_gateup_part<decltype(N)::value>(ring, k, d, I, w13, tok + c, n, rx,
-                                         H + (size_t)(k.p0 + c) * I);
+  const int lane = lane_id();
+  for (int c = k.c0; c < k.n; c += 16 * M::NT * pl.cuts) {
+    const int n = min(k.n - c, 16 * M::NT);
+    const int32_t *tok = sptok + (size_t)(blockIdx.x % N_XCD) * np + k.p0 + c;
+    uint16_t *h0 = H + (size_t)(k.p0 + c) * I;
+    if (c > k.c0) wg_barrier();   // every wavefront is done with the ring
+    sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
+      constexpr int N = decltype(NC)::value;
+      const MxTiles<M::T> m = mx_tiles<M>(w13, k.rg, I / 8, d);
+      f32x4 acc[M::T][N];
+      mx_stream<M, N>(lds, m, d, rx, [&](int i) {
+        return i < n ? (uint32_t)tok[i] * (uint32_t)d * 2u : FFN_TOK_PAD;
+      }, acc);
+      if (!m.active) return;
+      mx_emit<M, N, 2>(lds, acc, [&](int t, int j, const f32x4 (&v)[2]) {
+        const int p = 16 * j + (lane & 15);
+        if (p >= n) return;
+        uint16_t h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = f32_to_bf16(silu_bf16(v[0][q]) * v[1][q]);
+        const u32x2 pk = {(uint32_t)h[0] | ((uint32_t)h[1] << 16),
+                          (uint32_t)h[2] | ((uint32_t)h[3] << 16)};
+        *reinterpret_cast<u32x2 *>(h0 + (size_t)p * I + 8 * (m.t0 + t) + 4 * (lane >> 4)) = pk;
+      });
     });
   }
 }
 
-template <int NT>
-__device__ __forceinline__ void mx_down_part(uint8_t *ring, const MxWork &k, int d, int I,
-                                             const uint8_t *__restrict__ w2,
-                                             const uint16_t *__restrict__ h0, int n,
-                                             const float *__restrict__ gate0,
-                                             float *__restrict__ out0) {
-  const int w = wave_id_u(), lane = lane_id();
-  const int r = (k.rg * MX_WAVES + w) * MX_T;   // d / 16 is a multiple of MX_WAVES MX_T
-  const size_t tb = mx_tile_bytes(I);
-  rsrc_t rw[MX_T];
-#pragma unroll
-  for (int t = 0; t < MX_T; ++t) rw[t] = make_rsrc(w2 + (size_t)(r + t) * tb, (uint32_t)tb);
-  const rsrc_t rx = make_rsrc(h0, (uint32_t)n * (uint32_t)I * 2u);
-  float gt[NT];
-  uint32_t tv[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int i = mx_stage_row(j);
-    tv[j] = i < n ? (uint32_t)i * (uint32_t)I * 2u : FFN_TOK_PAD;
-    gt[j] = gate0[min(16 * j + (lane & 15), n - 1)];
-  }
-  f32x4 acc[MX_T][NT];
-  mx_stream<NT>(ring, rw, I, rx, tv, acc);
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int p = 16 * j + (lane & 15);
-    if (p < n) {
-#pragma unroll
-      for (int t = 0; t < MX_T; ++t) {
-        const f32x4 o = acc[t][j];
-        *reinterpret_cast<float4 *>(out0 + (size_t)p * d + 16 * (r + t) + 4 * (lane >> 4)) =
-            float4{gt[j] * o[0], gt[j] * o[1], gt[j] * o[2], gt[j] * o[3]};
-      }
-    }
-  }
-}
-
-template <int NT>
-__global__ __launch_bounds__(MX_THREADS)
-void k_mx_down(int d, int I, int E, int budget, int ns, int nrec, int parts,
-               const uint8_t *__restrict__ w2r, const uint8_t *__restrict__ w2s,
-               const SpRec *__restrict__ rec, const float *__restrict__ pair_gate,
+template <typename M>
+__global__ __launch_bounds__(M::THREADS, M::WPE)
+void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
+               const uint8_t *__restrict__ w2s, const float *__restrict__ pair_gate,
                const uint16_t *__restrict__ H, float *__restrict__ pairbuf) {
-  __shared__ __attribute__((aligned(16))) uint8_t ring[MX_RING * NT * 4096];
-  const MxWork k = mx_work(budget, ns, nrec, parts != 0, d / 16 / (MX_WAVES * MX_T), rec);
-  if (k.n <= 0) return;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
+  const MxWork k = mx_work(pl, mx_groups(d / 16, M::GROUP), M::NT);
   const size_t eb = (size_t)(d / 16) * mx_tile_bytes(I);
   const uint8_t *w2 = k.u < E ? w2r + (size_t)k.u * eb : w2s + (size_t)(k.u - E) * eb;
-  for (int c = 0; c < k.n; c += 16 * NT) {
-    const int n = min(k.n - c, 16 * NT), p0 = k.p0 + c;
-    if (c > 0) wg_barrier();
-    sp_tiles<NT>((n + 15) / 16, [&](auto N) {
-      mx_down_part<decltype(N)::value>(ring, k, d, I, w2, H + (size_t)p0 * I, n, pair_gate + p0,
-                                       pairbuf + (size_t)p0 * d);
+  const int lane = lane_id();
+  for (int c = k.c0; c < k.n; c += 16 * M::NT * pl.cuts) {
+    const int n = min(k.n - c, 16 * M::NT), p0 = k.p0 + c;
+    const rsrc_t rx = make_rsrc(H + (size_t)p0 * I, (uint32_t)n * (uint32_t)I * 2u);
+    float *out0 = pairbuf + (size_t)p0 * d;
+    if (c > k.c0) wg_barrier();
+    sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
+      constexpr int N = decltype(NC)::value;
+      const MxTiles<M::T> m = mx_tiles<M>(w2, k.rg, d / 16, I);
+      float gt[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) gt[j] = pair_gate[p0 + min(16 * j + (lane & 15), n - 1)];
+      f32x4 acc[M::T][N];
+      mx_stream<M, N>(lds, m, I, rx, [&](int i) {
+        return i < n ? (uint32_t)i * (uint32_t)I * 2u : FFN_TOK_PAD;
+      }, acc);
+      if (!m.active) return;
+      mx_emit<M, N, 1>(lds, acc, [&](int t, int j, const f32x4 (&v)[1]) {
+        const int p = 16 * j + (lane & 15);
+        if (p >= n) return;
+        float g = gt[0];
+#pragma unroll
+        for (int q = 1; q < N; ++q) g = j == q ? gt[q] : g;
+        *reinterpret_cast<float4 *>(out0 + (size_t)p * d + 16 * (m.t0 + t) + 4 * (lane >> 4)) =
+            float4{g * v[0][0], g * v[0][1], g * v[0][2], g * v[0][3]};
+      });
     });
   }
 }
 
 // ----------------------------------------------------------------- launch --
 namespace {
-// workgroups of `recs` records with RG row groups each, the same on every die
-dim3 mx_grid(int recs, int RG) { return dim3((unsigned)(N_XCD * recs * ((RG + N_XCD - 1) / N_XCD))); }
+// The shapes by batch.  Up to 16 tokens a slot has one token tile and the launch is a
+// weight stream whose latency counts: four wavefronts side by side, or, where
+// that leaves gate/up with fewer workgroups than compute units, two and two on
+// halves of the contraction (us, Qwen3-shaped gate/up, 8 slots at B = 1 and 10 at
+// B = 16, 96 and 120 workgroups: 8.3 and 9.6 against 6.9 and 7.7; OLMoE-shaped,
+// 24 slots at B = 5, 384 workgroups: 12.0 against 12.5; down, whose contraction is
+// short: 5.2, 5.2 and 7.8 against 5.0, 6.0 and 8.4).  Past 32 tokens the matrix
+// pipe is busy for most of the time and a tile's operands in LDS are read once per
+// wavefront, so more workgroups per CU pay more than deeper rings (DT = 1, 2, 3
+// at B = 256, 32 experts, gate/up 24.3, 24.9 and 30.1, down 17.6, 18.4 and 21.3), and
+// with enough workgroups four tiles a wavefront halve the LDS reads (B = 1024,
+// 128 experts: gate/up 85 -> 78; 672 wide ones of Mixtral's shape 89 -> 82; but 258 at B
+// = 256 24.3 -> 28.4, and 220 of Qwen1.5-MoE's shape at B = 61 17.0 -> 23.1; down
+// equal at best).  The line counts the workgroups of slots and full parts, which
+// the host knows.
+using MxFew = MxShape<1, 2, 4, 1, 2>;
+using MxFewSplit = MxShape<1, 2, 2, 2, 2>;
+using MxMid = MxShape<2, 2, 4, 1, 2>;
+using MxMany = MxShape<MX_NT, 2, 4, 1, 1>;
+using MxManyWide = MxShape<MX_NT, 4, 4, 1, 1>;
+
+int mx_workgroups(int B, int K, int slots, int ns, int groups) {
+  const int full = B * (K + ns) / (16 * MX_NT);
+  return (slots + ns > full ? slots + ns : full) * groups;
+}
+
+// workgroups: records times row groups (the same number on every die) times cuts
+dim3 mx_grid(int recs, int RG, int cuts) {
+  return dim3((unsigned)(N_XCD * recs * ((RG + N_XCD - 1) / N_XCD) * cuts));
+}
+// workgroups that share a record's tiles: what a record can hold over what one takes
+int mx_cuts(int B, int NT) {
+  const int tiles = mx_parts(B) ? MX_NT : (B + 15) / 16;
+  return (tiles + NT - 1) / NT;
+}
 }  // namespace
 
 hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, int budget, int slots,
                             int ns, const void *w13, const void *w13s, const SpRec *rec,
-                            const int32_t *sptok, void *H, hipStream_t st) {
+                            const int32_t *sptok, void *H, int n_cu, hipStream_t st) {
   const bool parts = mx_parts(B);
   const int nrec = mx_records(B, K, budget, ns);
-#define BASE_MXG(N)                                                                               \
-  launch_k(k_mx_gateup<N>, mx_grid(parts ? nrec : slots + ns, I / 16 / MX_WAVES), dim3(MX_THREADS), \
-           0, st, d, I, E, budget, ns, nrec, (int)parts, B * (K + ns), (const uint8_t *)w13,      \
-           (const uint8_t *)w13s, rec, sptok, (const uint16_t *)x, B, (uint16_t *)H)
-  if (B <= 16) BASE_MXG(1);
-  else if (B <= 32) BASE_MXG(2);
-  else BASE_MXG(MX_NT);
-#undef BASE_MXG
+  auto go = [&](auto shape) {
+    using M = decltype(shape);
+    const int cuts = mx_cuts(B, M::NT);
+    launch_k(k_mx_gateup<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(I / 8, M::GROUP), cuts),
+             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, rec},
+             B * (K + ns), (const uint8_t *)w13, (const uint8_t *)w13s, sptok, (const uint16_t *)x,
+             B, (uint16_t *)H);
+  };
+  auto wgs = [&](int group) { return mx_workgroups(B, K, slots, ns, mx_groups(I / 8, group)); };
+  if (B <= 16) {
+    if (wgs(MxFew::GROUP) >= n_cu) go(MxFew{});
+    else go(MxFewSplit{});
+  } else if (B <= 32) {
+    go(MxMid{});
+  } else if (2 * wgs(MxManyWide::GROUP) >= 3 * n_cu) {
+    go(MxManyWide{});
+  } else {
+    go(MxMany{});
+  }
   return hipGetLastError();
 }
 
@@ -283,14 +415,16 @@ hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slo
                           const void *H, float *pairbuf, hipStream_t st) {
   const bool parts = mx_parts(B);
   const int nrec = mx_records(B, K, budget, ns);
-#define BASE_MXD(N)                                                                                \
-  launch_k(k_mx_down<N>, mx_grid(parts ? nrec : slots + ns, d / 16 / (MX_WAVES * MX_T)),           \
-           dim3(MX_THREADS), 0, st, d, I, E, budget, ns, nrec, (int)parts, (const uint8_t *)w2,    \
-           (const uint8_t *)w2s, rec, pair_gate, (const uint16_t *)H, pairbuf)
-  if (B <= 16) BASE_MXD(1);
-  else if (B <= 32) BASE_MXD(2);
-  else BASE_MXD(MX_NT);
-#undef BASE_MXD
+  auto go = [&](auto shape) {
+    using M = decltype(shape);
+    const int cuts = mx_cuts(B, M::NT);
+    launch_k(k_mx_down<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(d / 16, M::GROUP), cuts),
+             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, rec},
+             (const uint8_t *)w2, (const uint8_t *)w2s, pair_gate, (const uint16_t *)H, pairbuf);
+  };
+  if (B <= 16) go(MxFew{});
+  else if (B <= 32) go(MxMid{});
+  else go(MxMany{});
   return hipGetLastError();
 }
 

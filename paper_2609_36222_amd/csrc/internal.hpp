@@ -325,7 +325,7 @@ hipError_t launch_down(bool bf16, bool packed, int B, int d, int I, int E, int K
 // the same on 4-bit weights; rec / sptok: see mx_records
 hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, int budget, int slots,
                             int ns, const void *w13, const void *w13s, const SpRec *rec,
-                            const int32_t *sptok, void *H, hipStream_t st);
+                            const int32_t *sptok, void *H, int n_cu, hipStream_t st);
 hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                           const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
                           const void *H, float *pairbuf, hipStream_t st);
