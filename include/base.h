@@ -299,8 +299,7 @@ typedef struct base_norms {
  *   h      the residual stream
  *   h_out  h', or NULL;  x_out  x', or NULL (not both)
  * Each is rows x d with its own row stride (>= d elements); elements between the
- * rows are not touched.  Element alignment suffices; 16-byte accesses are used
- * where d, every stride and every pointer allow them.  h_out may be h or y, and
+ * rows are not touched, and element alignment suffices.  h_out may be h or y, and
  * x_out may be y or h, with the same stride; otherwise they must not overlap.
  * BASE_ERR_SHAPE: d, rows, a stride, eps or res_scale outside the above;
  * BASE_ERR_FLAGS: h_out without y, h_out the same as x_out, or another stride in
@@ -310,8 +309,8 @@ base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y,
                                void *x_out, int64_t x_out_ld, void *stream);
 
 /* A decode block's tail in the layer's last launch: base_decode_layer without
- * a residual, then base_norm_residual on its output y and the residual stream h
- * (16-byte aligned rows), bit for bit, without y in memory.  h, h_out, x_out: [B][d], rows d elements
+ * a residual, then base_norm_residual on its output y and the residual stream h,
+ * bit for bit, without y in memory.  h, h_out, x_out: [B][d], rows d elements
  * apart, 16-B aligned, as are the gains and the gate (gate_ld a multiple of 4);
  * h_out may be h, and x_out may be x (the layer's input, read before).  N->d and
  * N->dtype are the layer's. */

@@ -190,7 +190,8 @@ def _ptr(t):
 def _stream(stream):
     import torch
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the current stream's handle without a Stream object around it (3 us a call)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -339,37 +340,37 @@ def packed_layer(layer: "Layer", K: int, stream=None) -> "Layer":
                  layer.norm_topk, W_PACKED, layer.score_rule, shared)
 
 
-def _on_device(t, what):
-    """The launches go to the current GPU, so the tensors have to lie there."""
+def _device():
+    """The current GPU, where the launches go and the tensors have to lie."""
     import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what}: on the current GPU, not {t.device}")
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+
+
+def _rows(t, what, dev):
+    """(dtype, rows, cols, row stride) of a 2-D tensor with adjacent columns."""
+    import torch
+    dt = t.dtype
+    if t.dim() != 2 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        raise ValueError(f"{what}: a 2-D fp32 or bf16 tensor")
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if t.get_device() != dev or (cols > 1 and one != 1):
+        raise ValueError(f"{what}: adjacent columns, on the current GPU")
+    return BASE_BF16 if dt is torch.bfloat16 else BASE_F32, rows, cols, ld if rows > 1 else cols
 
 
 # Microscaled 4-bit floating point (E2M1 codes, an E8M0 scale per 32 elements)
-def _rows(t, what):
-    """(dtype, rows, cols, row stride) of a 2-D tensor with adjacent columns."""
-    import torch
-    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"{what}: a 2-D fp32 or bf16 tensor")
-    _on_device(t, what)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{what}: adjacent columns")
-    return (BASE_BF16 if t.dtype == torch.bfloat16 else BASE_F32, rows, cols,
-            t.stride(0) if rows > 1 else cols)
-
-
 def mx_quantize(src, codes=None, scales=None, stream=None):
     """codes [rows, cols / 2] and scales [rows, cols / 32] (uint8) of src
     [rows, cols]; the rows may lie inside wider ones."""
     import torch
-    dt, rows, cols, ld = _rows(src, "src")
+    dev = _device()
+    dt, rows, cols, ld = _rows(src, "src", dev)
     if codes is None:
-        codes = torch.empty(rows, cols // 2, dtype=torch.uint8, device=src.device)
+        codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=src.device)
     if scales is None:
-        scales = torch.empty(rows, cols // 32, dtype=torch.uint8, device=src.device)
-    _mx_shapes(codes, scales, rows, cols)
+        scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=src.device)
+    _mx_shapes(codes, scales, (rows,), cols, dev)
     _check(load().base_mx_quantize(dt, _ptr(src), rows, cols, ld, _ptr(codes), _ptr(scales),
                                    _stream(stream)))
     return codes, scales
@@ -379,10 +380,11 @@ def mx_dequantize(codes, scales, dtype=None, out=None, stream=None):
     """The values [rows, cols] as `dtype` (bf16), or into `out`."""
     import torch
     rows, cols = codes.shape[0], 2 * codes.shape[1]
-    _mx_shapes(codes, scales, rows, cols)
+    dev = _device()
+    _mx_shapes(codes, scales, (rows,), cols, dev)
     if out is None:
-        out = torch.empty(rows, cols, dtype=dtype or torch.bfloat16, device=codes.device)
-    dt, r, c, ld = _rows(out, "out")
+        out = torch.empty((rows, cols), dtype=dtype or torch.bfloat16, device=codes.device)
+    dt, r, c, ld = _rows(out, "out", dev)
     if (r, c) != (rows, cols):
         raise ValueError("out: the codes' rows and columns")
     _check(load().base_mx_dequantize(_ptr(codes), _ptr(scales), rows, cols, dt, _ptr(out), ld,
@@ -390,13 +392,12 @@ def mx_dequantize(codes, scales, dtype=None, out=None, stream=None):
     return out
 
 
-def _mx_shapes(codes, scales, rows, cols):
+def _mx_shapes(codes, scales, lead, cols, dev):
     import torch
     for t, n, what in ((codes, cols // 2, "codes"), (scales, cols // 32, "scales")):
-        want = (*(rows if isinstance(rows, tuple) else (rows,)), n)
-        if t.dtype != torch.uint8 or tuple(t.shape) != want or not t.is_contiguous():
-            raise ValueError(f"{what}: contiguous uint8 {list(want)}")
-        _on_device(t, what)
+        if (t.dtype is not torch.uint8 or t.shape != (*lead, n) or not t.is_contiguous()
+                or t.get_device() != dev):
+            raise ValueError(f"{what}: contiguous uint8 {[*lead, n]} on the current GPU")
 
 
 def _mx_desc(E, d, I, dtype=BASE_BF16, w13=None, w2=None):
@@ -419,9 +420,10 @@ def mx_quantize_experts(w13, w2, stream=None):
     tensors of a W_MXFP4 layer."""
     import torch
     E, d, I = w2.shape
-    if tuple(w13.shape) != (E, 2 * I, d) or w13.dtype != w2.dtype or not (
-            w13.is_contiguous() and w2.is_contiguous()):
-        raise ValueError("w13 [E, 2I, d] and w2 [E, d, I], contiguous, of one dtype")
+    if (w13.shape != (E, 2 * I, d) or w13.dtype != w2.dtype
+            or w13.dtype not in (torch.bfloat16, torch.float32)
+            or any(not t.is_contiguous() or t.get_device() != _device() for t in (w13, w2))):
+        raise ValueError("w13 [E, 2I, d] and w2 [E, d, I], contiguous fp32 or bf16 on the current GPU")
     desc = _mx_desc(E, d, I, BASE_BF16 if w13.dtype == torch.bfloat16 else BASE_F32, w13, w2)
     out = _mx_out(desc, w13.device)
     _check(load().base_mx_quantize_experts(ctypes.byref(desc), _ptr(out[0]), _ptr(out[1]),
@@ -434,8 +436,8 @@ def mx_pack_experts(w13, w2, stream=None):
     w2 [E, d, I / 2] and [E, d, I / 32]."""
     E, d = w2[0].shape[:2]
     I = 2 * w2[0].shape[2]
-    _mx_shapes(*w13, (E, 2 * I), d)
-    _mx_shapes(*w2, (E, d), I)
+    _mx_shapes(*w13, (E, 2 * I), d, _device())
+    _mx_shapes(*w2, (E, d), I, _device())
     desc = _mx_desc(E, d, I)
     out = _mx_out(desc, w13[0].device)
     _check(load().base_mx_pack_experts(ctypes.byref(desc), *(_ptr(t) for t in (*w13, *w2, *out)),
@@ -474,42 +476,49 @@ class Norms:
 
     def __init__(self, d, dtype, post_gain=None, gate=None, pre_gain=None, res_scale=1.0, eps=1e-6):
         import torch
-        if dtype not in (torch.float32, torch.bfloat16):
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise ValueError("dtype: fp32 or bf16")
-        for t, what in ((post_gain, "post_gain"), (pre_gain, "pre_gain"), (gate, "gate")):
+        self.tensors = (post_gain, gate, pre_gain)
+        self.d, self.torch_dtype, self.gate_rows, ld = d, dtype, None, 0
+        dev = _device()
+        for t, what in zip(self.tensors, ("post_gain", "gate", "pre_gain")):
             if t is None:
                 continue
-            if (t.dtype != torch.float32 or t.shape[-1] != d or t.dim() > (2 if what == "gate" else 1)
-                    or (d > 1 and t.stride(-1) != 1)):
-                raise ValueError(f"{what}: fp32, {d} adjacent elements a row")
-            _on_device(t, what)
-        self.tensors = (post_gain, gate, pre_gain)
-        self.d, self.torch_dtype = d, dtype
-        self.gate_rows = gate.shape[0] if gate is not None and gate.dim() == 2 else None
-        ld = 0 if self.gate_rows is None else (gate.stride(0) if self.gate_rows > 1 else d)
-        self.desc = base_norms(d, BASE_BF16 if dtype == torch.bfloat16 else BASE_F32, eps, res_scale,
+            s = t.stride()
+            two = what == "gate" and len(s) == 2
+            if (t.dtype is not torch.float32 or not (two or len(s) == 1) or t.shape[-1] != d
+                    or (d > 1 and s[-1] != 1) or t.get_device() != dev):
+                raise ValueError(f"{what}: fp32, {d} adjacent elements a row, on the current GPU")
+            if two:
+                self.gate_rows = t.shape[0]
+                ld = s[0] if self.gate_rows > 1 else d
+        self.desc = base_norms(d, BASE_BF16 if dtype is torch.bfloat16 else BASE_F32, eps, res_scale,
                                _ptr(post_gain), _ptr(gate), ld, _ptr(pre_gain))
 
-    def _check_rows(self, rows, *tensors):
-        if self.gate_rows not in (None, rows):
+    def _pointers(self, rows, *tensors):
+        """The row count checked, and (pointer, row stride) of each named tensor."""
+        if self.gate_rows is not None and self.gate_rows != rows:
             raise ValueError(f"gate: one row, or {rows}")
+        out, dev, d = [], _device(), self.d
         for t, what in tensors:
             if t is None:
+                out += (None, 0)
                 continue
-            if t.dtype != self.torch_dtype or tuple(t.shape) != (rows, self.d):
-                raise ValueError(f"{what}: {self.torch_dtype} [{rows}, {self.d}]")
-            _rows(t, what)
+            s = t.stride()
+            if (t.dtype is not self.torch_dtype or t.shape != (rows, d) or (d > 1 and s[1] != 1)
+                    or t.get_device() != dev):
+                raise ValueError(f"{what}: {self.torch_dtype} [{rows}, {d}], adjacent columns, "
+                                 "on the current GPU")
+            out += (t.data_ptr(), s[0] if rows > 1 else d)
+        return out
 
 
 def base_norm_residual(norms: Norms, y, h, h_out=None, x_out=None, stream=None):
     """h_out = res_scale h + gate (post_gain n(y)), x_out = pre_gain n(h_out); [rows, d]
     tensors whose rows may lie inside wider ones; y None: x_out = pre_gain n(h)."""
     rows = h.shape[0]
-    norms._check_rows(rows, (y, "y"), (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
-    a = []
-    for t in (y, h, h_out, x_out):
-        a += [_ptr(t), 0 if t is None else _rows(t, "rows")[3]]
-    _check(load().base_norm_residual(ctypes.byref(norms.desc), rows, *a, _stream(stream)))
+    a = norms._pointers(rows, (y, "y"), (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
+    _check(load().base_norm_residual(norms.desc, rows, *a, _stream(stream)))
 
 
 def norm_residual(h, y=None, post_gain=None, gate=None, pre_gain=None, res_scale=1.0, eps=1e-6,
@@ -519,7 +528,7 @@ def norm_residual(h, y=None, post_gain=None, gate=None, pre_gain=None, res_scale
     import torch
     n = Norms(h.shape[1], h.dtype, post_gain, gate, pre_gain, res_scale, eps)
     if h_out is None and y is not None:
-        h_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        h_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)   # rows d apart
     if x_out is None and pre_gain is not None:
         x_out = torch.empty(h.shape, dtype=h.dtype, device=h.device)
     base_norm_residual(n, y, h, h_out, x_out, stream)
@@ -531,7 +540,7 @@ def base_decode_block(desc, norms: Norms, x, B, budget, flags, h, ws, h_out=None
     """base_decode_layer, then base_norm_residual on its output, in the layer's
     launches; returns the filled base_plan (device pointers into ws)."""
     plan = base_plan() if plan is None else plan
-    norms._check_rows(B, (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
+    norms._pointers(B, (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
     for t, what in ((h, "h"), (h_out, "h_out"), (x_out, "x_out")):
         if t is not None and not t.is_contiguous():
             raise ValueError(f"{what}: contiguous rows")

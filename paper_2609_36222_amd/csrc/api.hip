@@ -21,6 +21,7 @@ constexpr int FILL_DROP_BIT = BASE_FILL_DROP;
 static_assert(FLAG_UNIT_GATES != BASE_GATE_RENORM && FLAG_UNIT_GATES != BASE_FILL_DROP,
               "internal flag bit");
 
+static_assert(MAX_NORM_D == BASE_NORM_MAX_D, "norm limits");
 static_assert(SCORE_BASE == BASE_SCORE_BASE && SCORE_TOP1 == BASE_SCORE_TOP1 &&
                   SCORE_WEIGHT == BASE_SCORE_WEIGHT && SCORE_WEIGHT_SQ == BASE_SCORE_WEIGHT_SQ &&
                   SCORE_STATIC == BASE_SCORE_STATIC,
@@ -608,7 +609,7 @@ base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y,
     return BASE_ERR_FLAGS;
   HIP_TRY(launch_norm(N->dtype == BASE_BF16, N->d, N->eps, N->res_scale, N->post_gain, N->gate,
                       N->gate_ld, N->pre_gain, rows, y, y_ld, h, h_ld, h_out, h_out_ld, x_out,
-                      x_out_ld, (hipStream_t)stream));
+                      x_out_ld, device_cus(), (hipStream_t)stream));
   return BASE_OK;
 }
 

@@ -11,6 +11,7 @@ namespace basek {
 constexpr int MAX_K = 16;     // experts per token
 constexpr int MAX_E = 256;    // experts per layer
 constexpr int MAX_B = 1024;   // tokens per batch
+constexpr int MAX_NORM_D = 16384;   // a norm's row
 
 // Events attached to the next kernel launch (per host thread): when set,
 // launch_k hands them to the dispatch itself, which records `start` as the
@@ -352,9 +353,8 @@ hipError_t launch_combine(bool bf16, int B, int d, int kc,
 hipError_t launch_norm(bool bf16, int d, float eps, float scale, const float *post, const float *gate,
                        long long gate_ld, const float *pre, long long rows, const void *y,
                        long long y_ld, const void *h, long long h_ld, void *ho, long long ho_ld,
-                       void *xo, long long xo_ld, hipStream_t st);
-// the combine (no residual) and the same on its output, d a multiple of 256; every
-// pointer 16-byte aligned, gate_ld a multiple of four
+                       void *xo, long long xo_ld, int n_cu, hipStream_t st);
+// the combine (no residual) and the same on its output; rows of h, ho, xo d apart
 hipError_t launch_combine_norm(bool bf16, int B, int d, int kc, const int32_t *pair_of,
                                const float *pairbuf, float eps, float scale, const float *post,
                                const float *gate, long long gate_ld, const float *pre, const void *h,
