@@ -270,11 +270,17 @@ int part_records(const base_layer *L, int32_t B, const Layout &o) {
   return mx_layer(L) && mx_parts(B) ? o.nrec : 0;
 }
 
+// 4-bit experts and few tokens: down's launch also combines
+bool few_tokens(const base_layer *L, int32_t B, int32_t bc) {
+  return mx_layer(L) && mx_few(B, L->K, bc, L->n_shared);
+}
+
 // gate/up and down of the plan in the workspace (stages 6 and 7), on at most
-// `slots` kept slots
+// `slots` kept slots; y (few_tokens, else null): y = residual + the sum instead
+// of pair rows
 base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, int32_t slots,
                     const int32_t *sel_ids, const int32_t *n_sel, void *ws, const Layout &o,
-                    hipStream_t st) {
+                    hipStream_t st, const void *residual = nullptr, void *y = nullptr) {
   const bool bf16 = L->dtype == BASE_BF16, packed = L->w_layout == BASE_W_PACKED;
   const int ns = L->n_shared, n_cu = device_cus();
   const int32_t *offsets = at<int32_t>(ws, o.offsets);
@@ -294,7 +300,10 @@ base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, i
                           H, st));
   stage_end(st);
   stage(7, st);
-  if (mx_layer(L))
+  if (y)
+    HIP_TRY(launch_mx_down_combine(B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2, L->w2_shared, rec,
+                                   at<int32_t>(ws, o.pair_of), pair_gate, H, residual, y, st));
+  else if (mx_layer(L))
     HIP_TRY(launch_mx_down(B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2, L->w2_shared, rec,
                            pair_gate, H, at<float>(ws, o.pairbuf), st));
   else
@@ -355,7 +364,20 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
   stage_end(st);
   // the fused layer's kept set is part of its own batch's union; a caller of
   // base_moe_forward may bring any
-  BASE_TRY(run_ffn(L, x, B, bc, backfilled ? std::min(bc, B * L->K) : bc, sel_ids, n_sel, ws, o, st));
+  const int slots = backfilled ? std::min(bc, B * L->K) : bc;
+  if (few_tokens(L, B, bc)) {
+    // (a block's y lies in the pair rows' place, unused here)
+    void *y = tail.norms ? at<void>(ws, o.pairbuf) : tail.y;
+    BASE_TRY(run_ffn(L, x, B, bc, slots, sel_ids, n_sel, ws, o, st, tail.residual, y));
+    stage(8, st);
+    if (const base_norms *N = tail.norms)
+      HIP_TRY(launch_norm(true, L->d, N->eps, N->res_scale, N->post_gain, N->gate, N->gate_ld,
+                          N->pre_gain, B, y, L->d, tail.h, L->d, tail.h_out, L->d, tail.x_out, L->d,
+                          n_cu, st));
+    stage_end(st);
+    return BASE_OK;
+  }
+  BASE_TRY(run_ffn(L, x, B, bc, slots, sel_ids, n_sel, ws, o, st));
   stage(8, st);
   if (const base_norms *N = tail.norms)
     HIP_TRY(launch_combine_norm(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf), N->eps,
@@ -844,6 +866,7 @@ base_status base_layer_stages(const base_layer *L, int32_t B, int32_t budget,
   if (one_plan(L, B, layout(L, B, budget < L->E ? budget : L->E)))
     m &= ~(1 << 4);   // so is a small batch's compaction
   m &= ~(1 << 5);   // gate/up gathers its own tokens
+  if (few_tokens(L, B, budget < L->E ? budget : L->E)) m &= ~(1 << 8);   // down combines
   *stages = m;
   return BASE_OK;
 }

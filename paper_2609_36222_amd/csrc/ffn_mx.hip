@@ -344,6 +344,169 @@ void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
   }
 }
 
+// Down and the combine of few tokens (mx_few) in one launch: a workgroup
+// owns 16 columns of y, goes over every slot and joins the pairs of each token in
+// rank order, so that no pair rows go to memory and back.  A unit is (slot, share
+// of the contraction), one wavefront's at a time; a wavefront goes over the chunks
+// (four steps) of its units without a break, each step's registers and LDS rows
+// refilled from the next chunk as soon as they have been read.  Token rows are
+// staged four at a time, 256 contiguous bytes of each, and only as many as the
+// batch has (RL loads of four rows): gathered in the operand's own order, 64
+// scattered pieces a load, they took three times as long as the weights (24 slots,
+// B = 5, 16.4 us).  The sums go to LDS by pair, and
+// y_t = residual_t + sum_j gate_j o_j from there.  `shares` > 1 only where few
+// slots would leave wavefronts without work.  The pairs' gates and places, which
+// another die wrote, come straight into LDS behind the first chunk's loads.
+constexpr int MXF_WAVES = 16;
+constexpr int MXF_LDS = 148 << 10, MXF_SUMS = 24 << 10;   // dynamic LDS, the sums' part of it
+constexpr int MXF_PAIRS = 512;   // pairs' places and gates in LDS, a multiple of 256
+static_assert(MX_FEW_B * (MAX_K + MAX_SHARED) <= MXF_PAIRS, "the pairs of a batch");
+static_assert(MX_FEW_B * (MAX_K + MAX_SHARED) * 16 * 4 <= MXF_SUMS, "one share's sums");
+struct MxFewTail {
+  int B, kc, shares;
+  const int32_t *pair_of;
+  const float *pair_gate;
+  const void *residual;
+  void *y;
+};
+struct MxItem {   // a chunk of a unit's pairs from c on, 4 RL at a time
+  int k, u, p0, n, c, ch, ch1;
+};
+template <int RL>
+__global__ __launch_bounds__(MXF_WAVES * WAVE)
+void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
+                       const uint8_t *__restrict__ w2r, const uint8_t *__restrict__ w2s,
+                       const uint16_t *__restrict__ H) {
+  // the sums [share][pair][16], then every wavefront's token rows, four steps of RL KiB
+  extern __shared__ __attribute__((aligned(16))) float sums[];
+  __shared__ __attribute__((aligned(16))) int pair_s[MXF_PAIRS];
+  __shared__ __attribute__((aligned(16))) float gate_s[MXF_PAIRS];
+  __shared__ __attribute__((aligned(16))) SpRec rec_s[MAX_SLOTS];
+  const int w = wave_id_u(), lane = lane_id(), nw = (int)blockDim.x / WAVE;
+  const int np = tl.B * tl.kc, tile = blockIdx.x, nu = (slots + pl.ns) * tl.shares;
+  const SpRec *rec = pl.rec + (size_t)(blockIdx.x % N_XCD) * pl.nrec;
+  for (int y = threadIdx.x; y < slots + pl.ns; y += blockDim.x)
+    rec_s[y] = rec[y < pl.ns ? pl.budget + y : y - pl.ns];
+  __syncthreads();
+  const size_t tb = mx_tile_bytes(I), eb = (size_t)(d / 16) * tb;
+  const int S = mx_steps(I), C = mx_chunks(I);
+  const uint32_t Ib = (uint32_t)I * 2u;
+  // the item after `it`: its next chunk, the unit's next pairs, the next unit
+  // (k >= nu: none); shares in whole chunks, a chunk's scales with its steps
+  auto unit = [&](MxItem &it) {
+    for (; it.k < nu; it.k += nw) {
+      const int y = it.k / tl.shares, q = it.k - y * tl.shares;
+      const SpRec r = rec_s[y];
+      it.n = __builtin_amdgcn_readfirstlane(r.n);
+      it.ch = q * C / tl.shares;
+      it.ch1 = (q + 1) * C / tl.shares;
+      if (it.n <= 0) continue;
+      it.u = __builtin_amdgcn_readfirstlane(r.u);
+      it.p0 = __builtin_amdgcn_readfirstlane(r.p0);
+      it.c = 0;
+      return;
+    }
+  };
+  auto next = [&](MxItem it) {
+    if (++it.ch < it.ch1) return it;
+    const int q = it.k % tl.shares;
+    it.ch = q * C / tl.shares;
+    if ((it.c += 4 * RL) < it.n) return it;
+    it.k += nw;
+    unit(it);
+    return it;
+  };
+  uint8_t *ring = reinterpret_cast<uint8_t *>(sums + tl.shares * np * 16) + w * (MX_CHUNK * RL * 1024);
+  const int tok = lane & 15, g = lane >> 4;
+  // (a row past the staged ones repeats one of them, in a column nobody reads)
+  const uint8_t *op[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+    op[f] = ring + (tok % (4 * RL)) * 256 + 16 * ((4 * mx_block_pos(g) + f) ^ (tok % (4 * RL)));
+  uint32_t pc[RL], rb[RL];   // this lane's piece and row of each load
+#pragma unroll
+  for (int q = 0; q < RL; ++q) {
+    const int r = 4 * q + (lane >> 4), at16 = (lane & 15) ^ r;
+    pc[q] = 64u * (uint32_t)mx_block_at(at16 >> 2) + 16u * (uint32_t)(at16 & 3);
+    rb[q] = (uint32_t)r * Ib;   // rows past the slot's pairs are past rx: zeros
+  }
+  u32x4 a[MX_CHUNK];
+  uint32_t sn = 0;
+  rsrc_t rw = make_rsrc(w2r, 0), rx = make_rsrc(H, 0);
+  auto request = [&](const MxItem &it, int p) {
+    const bool have = it.k < nu;
+    if (p == 0 && have) {
+      const uint8_t *m = it.u < E ? w2r + (size_t)it.u * eb : w2s + (size_t)(it.u - E) * eb;
+      rw = make_rsrc(m + tile * tb, (uint32_t)tb);
+      const int n = min(it.n - it.c, 4 * RL);
+      rx = make_rsrc(H + (size_t)(it.p0 + it.c) * I, (uint32_t)n * Ib);
+    }
+    const int s = it.ch * MX_CHUNK + p;
+    const uint32_t c0 = have && s < S ? (uint32_t)it.ch * MX_CHUNK_BYTES : FFN_TOK_PAD;
+    if (p == 0) sn = __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(c0 + lane * 4), 0, 0);
+    a[p] = __builtin_bit_cast(u32x4, bload(rw, c0 + 256u + (uint32_t)p * 1024u + lane * 16, 0));
+    const uint32_t at = (uint32_t)s * 256u;
+#pragma unroll
+    for (int q = 0; q < RL; ++q)
+      load_lds(rx, ring + (p * RL + q) * 1024, have && at + pc[q] < Ib ? rb[q] + at + pc[q] : FFN_TOK_PAD, 0);
+  };
+  MxItem it{w, 0, 0, 0, 0, 0, 0};
+  unit(it);
+#pragma unroll
+  for (int p = 0; p < MX_CHUNK; ++p) request(it, p);
+  if (w == 0) {
+    const rsrc_t rp = make_rsrc(tl.pair_of, (uint32_t)np * 4u), rg = make_rsrc(tl.pair_gate, (uint32_t)np * 4u);
+#pragma unroll
+    for (int i = 0; i < MXF_PAIRS / 256; ++i) {
+      load_lds(rp, pair_s + 256 * i, 1024u * i + lane * 16, 0);
+      load_lds(rg, gate_s + 256 * i, 1024u * i + lane * 16, 0);
+    }
+  }
+  f32x4 acc = {0, 0, 0, 0};
+  while (it.k < nu) {
+    const MxItem nx = next(it);
+    const uint32_t sc = sn;
+#pragma unroll
+    for (int p = 0; p < MX_CHUNK; ++p) {
+      // behind this step are three others, one of them with its chunk's scales
+      // unless this step came with its own
+      if (p == 0) wait_vm<3 * (1 + RL)>();
+      else wait_vm<3 * (1 + RL) + 1>();
+      __builtin_amdgcn_sched_barrier(0);
+      const float scale = mx_scale((sc >> (8 * p)) & 0xFFu);
+      bf16x8 x[4];
+#pragma unroll
+      for (int f = 0; f < 4; ++f) x[f] = *reinterpret_cast<const bf16x8 *>(op[f] + p * (RL * 1024));
+#pragma unroll
+      for (int f = 0; f < 4; ++f) acc = mfma16(mx_decode8(a[p][f], scale), x[f], acc);
+      __builtin_amdgcn_sched_barrier(0);
+      request(nx, p);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (it.ch + 1 == it.ch1) {
+      if (tok < min(it.n - it.c, 4 * RL))
+        *reinterpret_cast<f32x4 *>(sums + ((it.k % tl.shares) * np + it.p0 + it.c + tok) * 16 + 4 * g) = acc;
+      acc = f32x4{0, 0, 0, 0};
+    }
+    it = nx;
+  }
+  wait_vm<0>();   // the pairs' places
+  __syncthreads();
+  for (int i = threadIdx.x; i < tl.B * 16; i += blockDim.x) {
+    const int t = i >> 4, r = i & 15;
+    const size_t o = (size_t)t * d + 16 * tile + r;
+    float v = tl.residual ? bf16_to_f32(static_cast<const uint16_t *>(tl.residual)[o]) : 0.0f;
+    for (int j = 0; j < tl.kc; ++j) {
+      const int p = pair_s[t * tl.kc + j];
+      if (p < 0) continue;   // a routed rank the token does not execute
+      float e = sums[p * 16 + r];
+      for (int q = 1; q < tl.shares; ++q) e = e + sums[(q * np + p) * 16 + r];
+      v = v + gate_s[p] * e;
+    }
+    static_cast<uint16_t *>(tl.y)[o] = f32_to_bf16(v);
+  }
+}
+
 // ----------------------------------------------------------------- launch --
 namespace {
 // The shapes by batch.  Up to 16 tokens a slot has one token tile and the launch is a
@@ -367,9 +530,9 @@ using MxMid = MxShape<2, 2, 4, 1, 2>;
 using MxMany = MxShape<MX_NT, 2, 4, 1, 1>;
 using MxManyWide = MxShape<MX_NT, 4, 4, 1, 1>;
 
-int mx_workgroups(int B, int K, int slots, int ns, int groups) {
-  const int full = B * (K + ns) / (16 * MX_NT);
-  return (slots + ns > full ? slots + ns : full) * groups;
+int mx_workgroups(int B, int K, int budget, int ns, int groups) {
+  const int kept = mx_kept(B, K, budget), full = B * (K + ns) / (16 * MX_NT);
+  return (kept + ns > full ? kept + ns : full) * groups;
 }
 
 // workgroups: records times row groups (the same number on every die) times cuts
@@ -396,7 +559,7 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
              B * (K + ns), (const uint8_t *)w13, (const uint8_t *)w13s, sptok, (const uint16_t *)x,
              B, (uint16_t *)H);
   };
-  auto wgs = [&](int group) { return mx_workgroups(B, K, slots, ns, mx_groups(I / 8, group)); };
+  auto wgs = [&](int group) { return mx_workgroups(B, K, budget, ns, mx_groups(I / 8, group)); };
   if (B <= 16) {
     if (wgs(MxFew::GROUP) >= n_cu) go(MxFew{});
     else go(MxFewSplit{});
@@ -425,6 +588,30 @@ hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slo
   if (B <= 16) go(MxFew{});
   else if (B <= 32) go(MxMid{});
   else go(MxMany{});
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget, int slots, int ns,
+                                  const void *w2, const void *w2s, const SpRec *rec,
+                                  const int32_t *pair_of, const float *pair_gate, const void *H,
+                                  const void *residual, void *y, hipStream_t st) {
+  const int units = mx_kept(B, K, budget) + ns, C = mx_chunks(I);
+  const int bytes = B * (K + ns) * 16 * (int)sizeof(float);   // a share's sums
+  const int rl = mx_row_loads(B);                             // loads of four rows a step
+  const int ring = MX_CHUNK * rl * 1024;                      // a wavefront's token rows
+  const int fit = (MXF_LDS - MXF_SUMS) / ring, waves = fit < MXF_WAVES ? fit : MXF_WAVES;
+  int shares = waves / units;
+  for (const int most : {C, MXF_SUMS / bytes})
+    if (shares > most) shares = most;
+  if (shares < 1) shares = 1;
+  const int work = (slots + ns) * shares, nw = work < waves ? work : waves;
+  const auto kern = rl == 1   ? k_mx_down_combine<1>
+                    : rl == 2 ? k_mx_down_combine<2>
+                              : k_mx_down_combine<4>;
+  launch_k(kern, dim3(d / 16), dim3(WAVE * nw), (uint32_t)(shares * bytes + nw * ring), st, d, I, E,
+           slots, MxPlan{budget, ns, budget + ns, 0, 1, rec},
+           MxFewTail{B, K + ns, shares, pair_of, pair_gate, residual, y}, (const uint8_t *)w2,
+           (const uint8_t *)w2s, (const uint16_t *)H);
   return hipGetLastError();
 }
 

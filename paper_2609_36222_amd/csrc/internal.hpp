@@ -165,6 +165,21 @@ struct alignas(16) SpRec {
 constexpr int MX_NT = 4;
 static_assert(FFN_SPLIT_B <= 16 * MX_NT, "a slot of a small batch is one part");
 inline bool mx_parts(int B) { return B > FFN_SPLIT_B; }
+// Few tokens: down and the combine in one launch (k_mx_down_combine), whose
+// workgroups go over every slot.  With one to four tokens (one load of four rows
+// a step) it always wins, with more only while the slots are few; the line is
+// slots (loads - 1) <= 12.  Layer, us, two launches against one: d = 2048, E = 128,
+// I = 768 B = 1, 8 slots 28.4 and 26.6, B = 4, 32 slots 34.8 and 34.5, B = 8, 12
+// slots 31.4 and 30.1, 24 slots 34.8 and 35.7, B = 16, 4 slots 29.4 and 27.3, 12 slots 32.0
+// and 33.4; d = 4096, I = 4096 B = 1, 2 slots 38.8 and 30.9, B = 8, 16 slots 92.7 and 93.0.
+// (kept: the slots the batch can fill, whatever base_moe_forward is given, so that
+// it takes the same sums as the fused layer)
+constexpr int MX_FEW_B = 16;
+inline int mx_kept(int B, int K, int budget) { return budget < B * K ? budget : B * K; }
+inline int mx_row_loads(int B) { return B <= 4 ? 1 : B <= 8 ? 2 : 4; }
+inline bool mx_few(int B, int K, int budget, int ns) {
+  return B <= MX_FEW_B && (mx_kept(B, K, budget) + ns) * (mx_row_loads(B) - 1) <= 12;
+}
 // slots' records, or an upper bound of the parts: the sum over slots of
 // ceil(tiles / MX_NT) is at most (tiles + (MX_NT - 1) slots) / MX_NT
 inline int mx_records(int B, int K, int budget, int ns) {
@@ -330,6 +345,11 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
 hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                           const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
                           const void *H, float *pairbuf, hipStream_t st);
+// (mx_few) down and the combine: y = residual (or null) + the experts' sum
+hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget, int slots, int ns,
+                                  const void *w2, const void *w2s, const SpRec *rec,
+                                  const int32_t *pair_of, const float *pair_gate, const void *H,
+                                  const void *residual, void *y, hipStream_t st);
 // rows [rows][cols] (row stride ld) to codes [rows][cols / 2] and scales [rows]
 // [cols / 32] and back; experts into the packed 4-bit layout (mx.hpp) from codes
 // and scales or from 16- or 32-bit weights

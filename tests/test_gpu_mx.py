@@ -258,12 +258,38 @@ def test_rules(gu, bd, rule):
     MxCase(gu, bd, 256, 16, 4, 64, 9, rule=rule, seed=3).check(gu, bd, 5)
 
 
+def test_staged_and_fused_take_the_same_sums(gu, bd):
+    """A budget far above the slots a few tokens can fill: the fused layer knows that
+    the slots are few, the staged call does not, and the bits agree all the same."""
+    c = MxCase(gu, bd, 512, 64, 1, 2048, 4, seed=31)
+    gl = c.gl
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    for _ in range(40):
+        x = torch.randn(4, 512, generator=g, device="cuda").bfloat16()
+        ws, y, z = gl.workspace(4, 64), gl.y_like(4), gl.y_like(4)
+        bd.base_decode_layer(gl.desc, x, 4, 64, 0, None, y, ws)
+        logits, ids, w = gl.route(x, 4)
+        _, _, sel, nsel, slot = gl.select(4, ids, gl.predict(x, 4, ids, w), 64)
+        bd.base_moe_forward(gl.desc, x, 4, logits, ids, sel, nsel, slot, 64, 0, None, z, ws)
+        assert torch.equal(y.view(torch.int16), z.view(torch.int16))
+
+
+@pytest.mark.parametrize("E,K,I,B,budget,ns", [(1, 1, 512, 1, 1, 0), (2, 2, 1088, 2, 2, 0), (4, 2, 2112, 3, 1, 2),
+                                               (16, 16, 576, 16, 1, 0), (256, 16, 64, 16, 256, 8),
+                                               (64, 16, 192, 16, 64, 0)])
+def test_few_tokens(gu, bd, E, K, I, B, budget, ns):
+    """Down's launch that combines: one slot shared by many wavefronts, more slots than
+    wavefronts, a chunk of one step and shares that end inside the contraction."""
+    MxCase(gu, bd, 256, E, K, I, B, ns, ns == 2, seed=E + I).check(gu, bd, budget, 0, True)
+
+
 def test_long_contraction(gu, bd):
     """Many chunks in both products."""
     MxCase(gu, bd, 4096, 3, 2, 4160, 7, seed=2).check(gu, bd, 2)
 
 
-@pytest.mark.parametrize("B", [40, 100])
+@pytest.mark.parametrize("B", [4, 40, 100])
 def test_an_expert_twice_among_a_tokens_routes(gu, bd, B):
     """Routes the router never makes: a slot then has more pairs than tokens."""
     c = MxCase(gu, bd, 256, 4, 4, 64, B, seed=8)
