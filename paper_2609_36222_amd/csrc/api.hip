@@ -397,6 +397,10 @@ bool one_plan(const base_layer *L, int32_t B, const Layout &o) {
   return L->dtype == BASE_BF16 ? o.split : ffn_small(B, L->I);
 }
 
+// ... which for 4-bit experts and few tokens also makes the routes and costs (16-bit
+// layers keep their launches, and with them their stages)
+bool few_plan(const base_layer *L, int32_t B) { return mx_layer(L) && B <= FEW_PLAN_B; }
+
 void fill_plan(base_plan *P, void *ws, const Layout &o, bool full) {
   if (!P) return;
   P->logits = full ? at<float>(ws, o.logits) : nullptr;
@@ -548,27 +552,42 @@ static base_status decode_layer(const base_layer *L, const void *x, int32_t B, i
   // a small batch's launch also makes the predictor's dot products: q lies in
   // the pair rows' buffer and ||x||^2 in the activations', free until the FFN
   const bool dense = scores_small(B, L->E) && L->score_rule == BASE_SCORE_BASE;
-  float *qd = dense ? at<float>(ws, o.pairbuf) : nullptr, *ss = dense ? at<float>(ws, o.H) : nullptr;
+  const bool few = few_plan(L, B);
+  // (few tokens: in the place of the rank order, which their plan does without; it
+  // writes the token lists into the pair rows' buffer while it reads these)
+  float *qd = !dense ? nullptr : at<float>(ws, few ? o.ex : o.pairbuf);
+  float *ss = !dense ? nullptr : at<float>(ws, few ? o.den : o.H);
+  int32_t *sptok = at<int32_t>(ws, o.pairbuf);
   HIP_TRY(launch_scores(bf16, x, B, L->d, L->w_router, L->b_router, L->E, shared_gate(L),
                         logits, at<float>(ws, o.gdot), st, dense ? L->pred_a : nullptr, qd, ss));
   stage_end(st);
   uint8_t *order = at<uint8_t>(ws, o.order);
   float *ex = at<float>(ws, o.ex), *den = at<float>(ws, o.den);
   stage(1, st);   // top-K, weights, (the method's rule) the routed pairs' predictor,
-              // and each token's experts in rank order for the backfill
-  HIP_TRY(launch_tail(bf16, B, L->E, L->K, L->d, L->norm_topk, logits, x, L->pred_a,
+              // and each token's experts in rank order for the backfill (few tokens:
+              // made by their plan)
+  if (!few)
+    HIP_TRY(launch_tail(bf16, B, L->E, L->K, L->d, L->norm_topk, logits, x, L->pred_a,
                       L->pred_b, ids, w, cost, 3, L->score_rule, st, order, ex, den, qd, ss));
   stage_end(st);
   stage(2, st);   // selection and backfill in one launch
   const bool joined = one_plan(L, B, o);   // ... and, for a small batch, the compaction
-  if (joined)
+  const float *gdot = shared_gate(L) ? at<float>(ws, o.gdot) : nullptr;
+  if (few)
+    HIP_TRY(launch_plan_few(
+        B, L->K, L->E, bc, L->n_shared, L->norm_topk, L->score_rule, flags, logits, qd, ss, L->pred_b,
+        gdot, ids, w, cost, at<float>(ws, o.scores), at<int32_t>(ws, o.counts), sel, nsel, slot,
+        at<int32_t>(ws, o.exec_ids), at<float>(ws, o.exec_gates), at<int32_t>(ws, o.offsets),
+        at<int32_t>(ws, o.pair_tok), at<float>(ws, o.pair_gate), at<int32_t>(ws, o.pair_of),
+        at<SpRec>(ws, o.sprec), sptok, st));
+  else if (joined)
     HIP_TRY(launch_plan_split(
         B, L->K, L->E, bc, L->n_shared, L->score_rule == BASE_SCORE_TOP1, flags, ids, cost, order,
-        ex, den, shared_gate(L) ? at<float>(ws, o.gdot) : nullptr, at<float>(ws, o.scores),
+        ex, den, gdot, at<float>(ws, o.scores),
         at<int32_t>(ws, o.counts), sel, nsel, slot, at<int32_t>(ws, o.exec_ids),
         at<float>(ws, o.exec_gates), at<int32_t>(ws, o.offsets), at<int32_t>(ws, o.pair_tok),
         at<float>(ws, o.pair_gate), at<int32_t>(ws, o.pair_of),
-        o.split ? at<SpRec>(ws, o.sprec) : nullptr, at<int32_t>(ws, o.pairbuf), st));
+        o.split ? at<SpRec>(ws, o.sprec) : nullptr, sptok, st));
   else
     HIP_TRY(launch_select_backfill(B, L->K, L->E, ids, cost, bc,
                                    L->score_rule == BASE_SCORE_TOP1, flags, order, ex, den,
@@ -866,6 +885,7 @@ base_status base_layer_stages(const base_layer *L, int32_t B, int32_t budget,
   if (one_plan(L, B, layout(L, B, budget < L->E ? budget : L->E)))
     m &= ~(1 << 4);   // so is a small batch's compaction
   m &= ~(1 << 5);   // gate/up gathers its own tokens
+  if (few_plan(L, B)) m &= ~(1 << 1);   // routes and costs: with the selection
   if (few_tokens(L, B, budget < L->E ? budget : L->E)) m &= ~(1 << 8);   // down combines
   *stages = m;
   return BASE_OK;

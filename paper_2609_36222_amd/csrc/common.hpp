@@ -196,6 +196,19 @@ __device__ __forceinline__ float base_exp(float x) {
   return __builtin_ldexpf(p, (int)n);
 }
 
+// w^2 exp(q / ||x|| + b), ss = ||x||^2, in the fixed order.
+__device__ __forceinline__ float pair_cost(float q, float ss, float b, float w) {
+  float inv = 0.0f;
+  if (ss > 0.0f) {
+    const float rt = sqrtf(ss);
+    inv = 1.0f / rt;
+  }
+  float s = q * inv;
+  s = s + b;
+  const float w2 = w * w;
+  return w2 * base_exp(s);
+}
+
 // SwiGLU activation of the expert FFN (not part of the bit-exact path).
 // silu(a) = a / (1 + exp(-a)) for fp32 results
 __device__ __forceinline__ float silu(float a) {

@@ -299,6 +299,16 @@ hipError_t launch_plan_split(int B, int K, int E, int budget, int ns, bool binar
                              int32_t *slot_of, int32_t *exec_ids, float *exec_gates,
                              int32_t *offsets, int32_t *pair_tok, float *pair_gate,
                              int32_t *pair_of, SpRec *rec, int32_t *sptok, hipStream_t st);
+// 4-bit layers of at most FEW_PLAN_B tokens: k_tail's work too, from launch_scores'
+// dot products (q, ss: of every expert, for SCORE_BASE)
+constexpr int FEW_PLAN_B = 16;
+hipError_t launch_plan_few(int B, int K, int E, int budget, int ns, int norm_topk, int rule, int flags,
+                           const float *logits, const float *q, const float *ss, const float *pb,
+                           const float *gdot, int32_t *ids, float *w, float *cost, float *scores,
+                           int32_t *counts, int32_t *sel_ids, int32_t *n_sel, int32_t *slot_of,
+                           int32_t *exec_ids, float *exec_gates, int32_t *offsets,
+                           int32_t *pair_tok, float *pair_gate, int32_t *pair_of, SpRec *rec,
+                           int32_t *sptok, hipStream_t st);
 hipError_t launch_backfill(int B, int E, int K, int norm_topk, int flags,
                            const float *logits, const int32_t *ids,
                            const int32_t *slot_of, const int32_t *n_sel,

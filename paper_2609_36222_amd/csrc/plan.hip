@@ -1370,6 +1370,366 @@ void k_plan_split(int B, int K, int E, int budget, int ns, int binary, int flags
   }
 }
 
+// Top-K, weights, costs, selection, backfill and compaction of few tokens (B <= 16,
+// one wavefront each) in one launch, from k_scores_small's dot products: k_tail
+// and k_plan_split with the same values and orders.  A token's experts are never
+// ranked as a whole: its routes are K successive wavefront maxima of the (logit,
+// index) keys, lane r mod 64 holding expert r, and its executed experts K more over
+// the kept ones -- a counting rank of E keys a token, as in k_tail, would take 16
+// wavefronts of one CU several times as long.  One workgroup per die, each
+// making the whole plan and writing its die's records; workgroup 0 writes the plan.
+struct FewScores {   // the dense scoring's outputs and the predictor's intercepts
+  const float *logits, *q, *ss, *pb, *gdot;
+  int norm_topk, rule;
+};
+struct FewPlan {
+  int32_t *ids;
+  float *w, *cost, *scores;
+  int32_t *counts, *sel_ids, *n_sel, *slot_of, *exec_ids;
+  float *exec_gates;
+  int32_t *offsets, *pair_tok;
+  float *pair_gate;
+  int32_t *pair_of;
+  SpRec *rec;
+  int32_t *sptok;
+};
+constexpr int PF_WAVES = 16;
+static_assert(MX_FEW_B <= PF_WAVES && FEW_PLAN_B == PF_WAVES, "a wavefront per token");
+
+// A logit's place in the unsigned order (rank_key's upper word), never 0
+__device__ __forceinline__ uint32_t order_key(float v) {
+  const uint32_t o = (uint32_t)(rank_key(v, 0) >> 32);
+  return o > 1u ? o : 1u;
+}
+__device__ __forceinline__ float order_value(uint32_t o) {
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp32(uint32_t k) {
+  return max(k, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)k, CTRL, 0xF, 0xF, false));
+}
+// The largest key of a wavefront, lane l holding experts l, l + 64, ..; its owner of
+// the lowest index goes to `e`, and its key to 0.  (A maximum of 64-bit keys,
+// with the index inside, takes four times the instructions: 16 of them 2 us of a
+// plan of 8.)
+template <int NCH>
+__device__ __forceinline__ uint32_t take_best(uint32_t (&k)[NCH], int &e) {
+  uint32_t m = k[0];
+#pragma unroll
+  for (int c = 1; c < NCH; ++c) m = max(m, k[c]);
+  m = max_dpp32<0xB1>(m);    // quad_perm [1, 0, 3, 2]
+  m = max_dpp32<0x4E>(m);    // quad_perm [2, 3, 0, 1]
+  m = max_dpp32<0x141>(m);   // row_half_mirror
+  m = max_dpp32<0x140>(m);   // row_mirror: the row of 16 lanes
+  const uint32_t a = (uint32_t)__builtin_amdgcn_readlane((int)m, 0), b = (uint32_t)__builtin_amdgcn_readlane((int)m, 16);
+  const uint32_t c2 = (uint32_t)__builtin_amdgcn_readlane((int)m, 32), d2 = (uint32_t)__builtin_amdgcn_readlane((int)m, 48);
+  const uint32_t ab = a > b ? a : b, cd = c2 > d2 ? c2 : d2, best = ab > cd ? ab : cd;
+  e = 0;
+#pragma unroll
+  for (int c = NCH - 1; c >= 0; --c) {
+    const uint64_t who = __ballot(k[c] == best);
+    if (who) e = WAVE * c + __builtin_ctzll(who);
+  }
+#pragma unroll
+  for (int c = 0; c < NCH; ++c)
+    if (e == (int)lane_id() + WAVE * c) k[c] = 0u;
+  return best;
+}
+
+template <int NCH>
+__global__ __launch_bounds__(PF_WAVES * WAVE)
+void k_plan_few(int B, int K, int E, int budget, int ns, int flags, FewScores sc, FewPlan pl) {
+  constexpr int TH = PF_WAVES * WAVE, PAD = PF_WAVES + 4;   // four lanes a row, distinct banks
+  __shared__ __attribute__((aligned(16))) float V[MAX_E * PAD];
+  __shared__ int cnt[MAX_E];
+  __shared__ __attribute__((aligned(16))) uint64_t key[MAX_E];
+  __shared__ int slot_s[MAX_E], sel_s[MAX_E];
+  __shared__ uint32_t mask[MAX_E];   // slot s: the tokens that execute it
+  __shared__ int off[MAX_E + 1];
+  __shared__ int n_union;
+  const int tid = threadIdx.x, lane = lane_id(), wv = wave_id_u();
+  const bool out = blockIdx.x == 0, token = wv < B;
+  const int kc = K + ns, t = min(wv, B - 1);
+  const bool base = sc.rule == SCORE_BASE, fit = base || sc.rule == SCORE_STATIC;
+  // every global load first
+  float lv[NCH], qv[NCH], bv[NCH];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    const int e = min(lane + WAVE * c, E - 1);
+    lv[c] = sc.logits[(size_t)t * E + e];
+    qv[c] = base ? sc.q[(size_t)t * E + e] : 0.0f;
+    bv[c] = fit ? sc.pb[e] : 0.0f;
+  }
+  const float ssv = base ? sc.ss[t] : 0.0f;
+  const float gd = sc.gdot ? sc.gdot[min(tid, B - 1)] : 0.0f;
+  for (int i = tid; i < E * PAD / 4; i += TH)
+    reinterpret_cast<float4 *>(V)[i] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (tid < E) {
+    cnt[tid] = 0;
+    mask[tid] = 0u;
+  }
+  if (tid == 0) n_union = 0;
+  __syncthreads();
+  // the routes: lane k < K has the token's k-th expert, its logit and weight
+  uint32_t keys[NCH];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) keys[c] = lane + WAVE * c < E ? order_key(lv[c]) : 0u;
+  int my_id = 0;
+  float my_l = 0.0f, lmax = 0.0f, S = 0.0f, my_w = 0.0f;
+  if (token) {
+    uint32_t left[NCH];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) left[c] = keys[c];
+    for (int k = 0; k < K; ++k) {
+      int e;
+      const float l = order_value(take_best(left, e));
+      if (lane == k) {
+        my_id = e;
+        my_l = l;
+      }
+      if (k == 0) lmax = l;
+    }
+    const float eps = base_exp(my_l - lmax);
+    if (sc.norm_topk) {
+      for (int k = 0; k < K; ++k)
+        S = S + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_int(eps), k));
+    } else {
+      float pt = 0.0f;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+        if (lane + WAVE * c < E) pt = pt + base_exp(lv[c] - lmax);
+      S = wave_tree_sum(pt);
+    }
+    my_w = eps / S;
+    // the routed pairs' scores under the rule
+    float qu = 0.0f, bu = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const float a = __shfl(qv[c], my_id & (WAVE - 1), WAVE), b = __shfl(bv[c], my_id & (WAVE - 1), WAVE);
+      if (my_id / WAVE == c) { qu = a; bu = b; }
+    }
+    float cost;
+    if (base) cost = pair_cost(qu, ssv, bu, my_w);
+    else if (sc.rule == SCORE_TOP1) cost = lane == 0 ? 1.0f : 0.0f;
+    else if (sc.rule == SCORE_WEIGHT) cost = my_w;
+    else if (sc.rule == SCORE_WEIGHT_SQ) cost = my_w * my_w;
+    else cost = pair_cost(0.0f, 0.0f, bu, my_w);
+    if (lane < K) {
+      V[my_id * PAD + t] = cost;
+      atomicAdd(&cnt[my_id], 1);
+      if (out) {
+        pl.ids[(size_t)t * K + lane] = my_id;
+        pl.w[(size_t)t * K + lane] = my_w;
+        pl.cost[(size_t)t * K + lane] = cost;
+      }
+    }
+  }
+  __syncthreads();
+  {   // the chunk tree over token positions, of which those past 16 are +0
+    const int u = tid >> 2, p = tid & 3;
+    const bool have = u < E;
+    float v[PF_WAVES / 4];
+#pragma unroll
+    for (int i = 0; i < PF_WAVES / 4; ++i) v[i] = have ? V[u * PAD + p + 4 * i] : 0.0f;
+#pragma unroll
+    for (int h = PF_WAVES / 8; h >= 1; h >>= 1)
+#pragma unroll
+      for (int i = 0; i < h; ++i) v[i] = v[i] + v[i + h];
+    float D = v[0];
+    D = D + xor_lane<2>(D);
+    D = D + xor_lane<1>(D);
+    const int n = have ? cnt[u] : 0;
+    const bool in = n > 0;
+    if (have && p == 0) {
+      const float kv = sc.rule == SCORE_TOP1 ? (D > 0.0f ? 1.0f : 0.0f) : D;
+      key[u] = in ? rank_key(kv, u) : 0;
+      if (out) {
+        pl.scores[u] = D;
+        pl.counts[u] = n;
+      }
+    } else if (!have && p == 0 && u < MAX_E) {
+      key[u] = 0;   // ranks after every expert
+    }
+    const uint64_t m = __ballot(in && p == 0);
+    if (lane == 0 && m) atomicAdd(&n_union, (int)__popcll(m));
+  }
+  __syncthreads();
+  const int n_sel = min(budget, n_union);
+  {   // ranks, tpe threads per expert over interleaved key pairs, as in select_rank
+    int E2 = WAVE;
+    while (E2 < E) E2 <<= 1;
+    const int tpe = TH / E2, npair = E2 / (2 * tpe);
+    const int u = tid / tpe, part = tid % tpe;
+    const uint64_t ku = key[u];
+    int r = 0;
+    for (int i0 = 0; i0 < npair; i0 += 8) {
+      u32x4 o[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (i0 + q < npair)
+          o[q] = *reinterpret_cast<const u32x4 *>(&key[2 * (part + tpe * (i0 + q))]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (i0 + q < npair) {
+          r += (((uint64_t)o[q].y << 32 | o[q].x) > ku);
+          r += (((uint64_t)o[q].w << 32 | o[q].z) > ku);
+        }
+    }
+    for (int h = 1; h < tpe; h <<= 1) r += __shfl_xor(r, h, WAVE);
+    if (u < E && part == 0) {
+      const int slot = ku != 0 && r < n_sel ? r : -1;
+      slot_s[u] = slot;
+      if (slot >= 0) sel_s[slot] = u;
+      if (out) {
+        pl.slot_of[u] = slot;
+        if (slot >= 0) pl.sel_ids[slot] = u;
+      }
+    }
+    if (out) {
+      for (int r2 = n_sel + tid; r2 < budget; r2 += TH) pl.sel_ids[r2] = -1;
+      if (tid == 0) *pl.n_sel = n_sel;
+    }
+  }
+  __syncthreads();
+  // backfill: lane j < nx has the expert executed at rank j, its slot and gate
+  const int kp = min(K, n_sel);
+  int nx = 0, ex_id = -1, ex_slot = -1;
+  float gate = 0.0f;
+  if (token) {
+    float num = 0.0f;
+    if (flags & 2) {   // drop: the kept routes, in routing order
+      const int sl = lane < K ? slot_s[my_id] : -1;
+      const uint64_t m = __ballot(sl >= 0);
+      nx = __popcll(m);
+      // route k goes to rank popcount(m below k): lane j takes its j-th set bit
+      int src = 0;
+      uint64_t mm = m;
+      for (int j = 0; j < nx; ++j) {
+        const int b = __builtin_ctzll(mm);
+        if (lane == j) src = b;
+        mm &= mm - 1;
+      }
+      const int id = __shfl(my_id, src, WAVE), s2 = __shfl(sl, src, WAVE);
+      const float l = __shfl(my_l, src, WAVE);
+      if (lane < nx) {
+        ex_id = id;
+        ex_slot = s2;
+        num = base_exp(l - lmax);
+      }
+    } else {
+      uint32_t left[NCH];
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+        left[c] = lane + WAVE * c < E && slot_s[lane + WAVE * c] >= 0 ? keys[c] : 0u;
+      float l = 0.0f;
+      nx = kp;
+      for (int j = 0; j < kp; ++j) {
+        int e;
+        const float v = order_value(take_best(left, e));
+        if (lane == j) {
+          ex_id = e;
+          l = v;
+        }
+      }
+      if (lane < nx) {
+        ex_slot = slot_s[ex_id];
+        num = base_exp(l - lmax);
+      }
+    }
+    float den = S;
+    if (flags & 1) {   // renormalised over the executed experts, in their order
+      den = 0.0f;
+      for (int j = 0; j < nx; ++j)
+        den = den + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_int(num), j));
+    }
+    if (lane < nx) {
+      gate = num / den;
+      atomicOr(&mask[ex_slot], 1u << t);
+    }
+    if (out && lane < K) {
+      pl.exec_ids[(size_t)t * K + lane] = ex_id;
+      pl.exec_gates[(size_t)t * K + lane] = gate;
+      if (lane >= nx) pl.pair_of[(size_t)t * kc + lane] = -1;
+    }
+  }
+  __syncthreads();
+  if (wv == 0) {   // exclusive prefixes of the slots' pair counts
+    constexpr int Q = MAX_E / WAVE;
+    int l[Q], s0 = 0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const int s = Q * lane + i;
+      l[i] = s < n_sel ? __popc(mask[s]) : 0;
+      s0 += l[i];
+    }
+    int inc = s0;
+#pragma unroll
+    for (int h = 1; h < WAVE; h <<= 1) {
+      const int o = __shfl_up(inc, h, WAVE);
+      if (lane >= h) inc += o;
+    }
+    int r = inc - s0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      off[Q * lane + i] = r;
+      r += l[i];
+    }
+    if (lane == WAVE - 1) off[MAX_E] = r;
+  }
+  __syncthreads();
+  const int routed = off[MAX_E];   // off[s] = routed for s >= n_sel
+  int32_t *tx = pl.sptok + (size_t)blockIdx.x * B * kc;
+  if (token && lane < nx) {
+    const int p = off[ex_slot] + __popc(mask[ex_slot] & ((1u << t) - 1u));
+    tx[p] = t;
+    if (out) {
+      pl.pair_tok[p] = t;
+      pl.pair_gate[p] = gate;
+      pl.pair_of[(size_t)t * kc + lane] = p;
+    }
+  }
+  SpRec *rx = pl.rec + (size_t)blockIdx.x * (budget + ns);
+  for (int s = tid; s < budget + ns; s += TH) {
+    const int i = s - budget;
+    rx[s] = i >= 0 ? SpRec{E + i, routed + i * B, B, 0}
+                   : (s < n_sel ? SpRec{sel_s[s], off[s], (int)__popc(mask[s]), 0} : SpRec{0, 0, 0, 0});
+  }
+  if (tid < B)
+    for (int i = 0; i < ns; ++i) tx[routed + i * B + tid] = tid;
+  if (!out) return;
+  for (int s = tid; s <= budget + ns; s += TH)
+    pl.offsets[s] = s <= budget ? off[min(s, MAX_E)] : routed + (s - budget) * B;
+  if (tid < B) {
+    float gs = 1.0f;
+    if (sc.gdot) {
+      const float e = base_exp(-gd);
+      const float dn = 1.0f + e;
+      gs = 1.0f / dn;
+    }
+    for (int i = 0; i < ns; ++i) {
+      const int p = routed + i * B + tid;
+      pl.pair_tok[p] = tid;
+      pl.pair_gate[p] = gs;
+      pl.pair_of[(size_t)tid * kc + K + i] = p;
+    }
+  }
+}
+
+hipError_t launch_plan_few(int B, int K, int E, int budget, int ns, int norm_topk, int rule, int flags,
+                           const float *logits, const float *q, const float *ss, const float *pb,
+                           const float *gdot, int32_t *ids, float *w, float *cost, float *scores,
+                           int32_t *counts, int32_t *sel_ids, int32_t *n_sel, int32_t *slot_of,
+                           int32_t *exec_ids, float *exec_gates, int32_t *offsets,
+                           int32_t *pair_tok, float *pair_gate, int32_t *pair_of, SpRec *rec,
+                           int32_t *sptok, hipStream_t st) {
+  const FewScores sc{logits, q, ss, pb, gdot, norm_topk, rule};
+  const FewPlan pl{ids, w, cost, scores, counts, sel_ids, n_sel, slot_of, exec_ids, exec_gates,
+                   offsets, pair_tok, pair_gate, pair_of, rec, sptok};
+  const auto kern = E <= WAVE ? k_plan_few<1> : E <= 2 * WAVE ? k_plan_few<2> : k_plan_few<4>;
+  launch_k(kern, dim3(N_XCD), dim3(PF_WAVES * WAVE), 0, st, B, K, E, budget, ns, flags, sc, pl);
+  return hipGetLastError();
+}
+
 hipError_t launch_plan_split(int B, int K, int E, int budget, int ns, bool binary, int flags,
                              const int32_t *ids, const float *cost, const uint8_t *order,
                              const float *ex, const float *den, const float *gdot,

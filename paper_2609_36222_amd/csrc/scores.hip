@@ -389,19 +389,6 @@ __host__ __device__ inline int tail_waves(int K, bool pred) {
   return wp > TL_RANK / WAVE ? wp : TL_RANK / WAVE;
 }
 
-// w^2 exp(q / ||x|| + b), ss = ||x||^2, in the fixed order.
-__device__ __forceinline__ float pair_cost(float q, float ss, float b, float w) {
-  float inv = 0.0f;
-  if (ss > 0.0f) {
-    const float rt = sqrtf(ss);
-    inv = 1.0f / rt;
-  }
-  float s = q * inv;
-  s = s + b;
-  const float w2 = w * w;
-  return w2 * base_exp(s);
-}
-
 // mode bit 0: route (top-K and weights from the logits into ids / w)
 // mode bit 1: per-pair scores of the routed pairs (ids / w, read back when
 //             bit 0 is off) under `rule`: SCORE_BASE w^2 exp(q / ||x|| + b_u)
