@@ -468,8 +468,9 @@ base_status base_calib_accumulate(const base_layer *L, const void *z, int32_t B,
  * kernel: FFN gate/up gathers its own token rows), 6 FFN gate/up, 7 FFN
  * down, 8 combine.  base_route runs stages 0 and 1,
  * base_select stage 2, base_moe_forward 3 to 8 (base_predict_cost runs the
- * tail kernel in its cost mode, untimed); a 4-bit layer of few tokens combines in
- * stage 7; base_decode_layer runs all of
+ * tail kernel in its cost mode, untimed); for a 4-bit layer base_moe_forward makes a
+ * small batch's compaction in stage 3, and few tokens are combined in stage 7 and, in
+ * base_decode_layer, routed in stage 2; base_decode_layer runs all of
  * them except that one
  * kernel makes the selection and the backfill (and, for small batches, the
  * compaction; base_layer_stages): stage 2 times it and stage 3 (and 4)

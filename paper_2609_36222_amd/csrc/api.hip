@@ -340,24 +340,30 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
   int32_t *pair_tok = at<int32_t>(ws, o.pair_tok);
   float *pair_gate = at<float>(ws, o.pair_gate);
   int32_t *pair_of = at<int32_t>(ws, o.pair_of);
-  stage(3, st);
-  if (!backfilled)
-    HIP_TRY(launch_backfill(B, L->E, L->K, L->norm_topk, flags, logits, ids,
-                            slot_of, n_sel, exec_ids, exec_gates, st));
-  stage_end(st);
-  stage(4, st);
   const int ns = L->n_shared;
   const int n_cu = device_cus();
+  SpRec *rec = o.split ? at<SpRec>(ws, o.sprec) : nullptr;
+  int32_t *sptok = at<int32_t>(ws, o.pairbuf);
+  const float *gdot = shared_gate(L) ? at<float>(ws, o.gdot) : nullptr;
+  stage(3, st);
+  if (!backfilled && mx_layer(L) && !mx_parts(B) && !(flags & FILL_DROP_BIT)) {
+    HIP_TRY(launch_plan_given(B, L->K, L->E, bc, ns, L->norm_topk, flags & BASE_GATE_RENORM, logits, ids,
+                              sel_ids, n_sel, slot_of, gdot, exec_ids, exec_gates, offsets, pair_tok,
+                              pair_gate, pair_of, rec, sptok, st));
+    planned = true;
+  } else if (!backfilled) {
+    HIP_TRY(launch_backfill(B, L->E, L->K, L->norm_topk, flags, logits, ids,
+                            slot_of, n_sel, exec_ids, exec_gates, st));
+  }
+  stage_end(st);
+  stage(4, st);
   FfnHdr *hdr = at<FfnHdr>(ws, o.hdr);
   FfnUnit *units_gu = at<FfnUnit>(ws, o.units_gu), *units_dn = at<FfnUnit>(ws, o.units_dn);
   uint32_t *tokoff = at<uint32_t>(ws, o.tokoff);
-  SpRec *rec = o.split ? at<SpRec>(ws, o.sprec) : nullptr;
-  int32_t *sptok = at<int32_t>(ws, o.pairbuf);
   // the same launch lists the FFN's parts and gate/up's token rows (bf16)
   if (!planned)
     HIP_TRY(launch_compact(B, L->K, L->E, bc, ns, exec_ids, exec_gates, slot_of, n_sel,
-                           shared_gate(L) ? at<float>(ws, o.gdot) : nullptr, offsets,
-                           pair_tok, pair_gate, pair_of, sel_ids, bf16 && !o.split, L->d, L->I, tokoff, hdr,
+                           gdot, offsets, pair_tok, pair_gate, pair_of, sel_ids, bf16 && !o.split, L->d, L->I, tokoff, hdr,
                            units_gu, units_dn, rec, sptok, part_records(L, B, o), n_cu, st));
   stage_end(st);
   stage(5, st);   // no launch of its own: gate/up gathers its tokens itself

@@ -309,6 +309,14 @@ hipError_t launch_plan_few(int B, int K, int E, int budget, int ns, int norm_top
                            int32_t *exec_ids, float *exec_gates, int32_t *offsets,
                            int32_t *pair_tok, float *pair_gate, int32_t *pair_of, SpRec *rec,
                            int32_t *sptok, hipStream_t st);
+// 4-bit layers, B <= FFN_SPLIT_B, backfill rule: launch_backfill and launch_compact
+// (slots' records) in one launch
+hipError_t launch_plan_given(int B, int K, int E, int budget, int ns, int norm_topk, bool renorm,
+                             const float *logits, const int32_t *ids, const int32_t *sel_ids,
+                             const int32_t *n_sel, const int32_t *slot_of, const float *gdot,
+                             int32_t *exec_ids, float *exec_gates, int32_t *offsets,
+                             int32_t *pair_tok, float *pair_gate, int32_t *pair_of, SpRec *rec,
+                             int32_t *sptok, hipStream_t st);
 hipError_t launch_backfill(int B, int E, int K, int norm_topk, int flags,
                            const float *logits, const int32_t *ids,
                            const int32_t *slot_of, const int32_t *n_sel,

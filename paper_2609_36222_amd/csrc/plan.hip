@@ -1715,6 +1715,208 @@ void k_plan_few(int B, int K, int E, int budget, int ns, int flags, FewScores sc
   }
 }
 
+// Backfill and compaction of a small batch (B <= FFN_SPLIT_B) on a selection from
+// the caller, in one launch: k_backfill's and k_compact's results for 4-bit layers.
+// A wavefront takes TPW tokens; the executed experts are K maxima over the kept
+// ones, as in k_plan_few, and a pair's place its slot's offset plus the tokens
+// before it, which needs a token's experts to be distinct -- they are, except among
+// the dropped routes of a caller's own making, so that the drop rule keeps the two
+// launches.  (Two launches 4.4 and 4.3 us at B = 16, 4.6 and 5.0 at B = 61.)
+template <int NCH, int TPW>
+__global__ __launch_bounds__(PF_WAVES * WAVE)
+void k_plan_given(int B, int K, int E, int budget, int ns, int norm_topk, int renorm,
+                  const float *__restrict__ logits, const int32_t *__restrict__ ids,
+                  const int32_t *__restrict__ sel_ids, const int32_t *__restrict__ n_sel_p,
+                  const int32_t *__restrict__ slot_of, const float *__restrict__ gdot, FewPlan pl) {
+  constexpr int TH = PF_WAVES * WAVE;
+  __shared__ int slot_s[MAX_E], sel_s[MAX_E];
+  __shared__ uint64_t mask[MAX_E];   // slot s: the tokens that execute it
+  __shared__ int off[MAX_E + 1];
+  const int tid = threadIdx.x, lane = lane_id(), wv = wave_id_u();
+  const bool out = blockIdx.x == 0;
+  const int kc = K + ns;
+  // every global load first
+  float lv[TPW][NCH];
+  int rv[TPW];
+#pragma unroll
+  for (int q = 0; q < TPW; ++q) {
+    const int t = min(wv + q * PF_WAVES, B - 1);
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) lv[q][c] = logits[(size_t)t * E + min(lane + WAVE * c, E - 1)];
+    rv[q] = route_of(ids, t, K);
+  }
+  const int slot_v = slot_of[min(tid, E - 1)], sel_v = sel_ids[min(tid, budget - 1)];
+  const int n_sel = min(max(*n_sel_p, 0), budget);
+  const float gd = gdot ? gdot[min(tid, B - 1)] : 0.0f;
+  if (tid < E) slot_s[tid] = slot_v;
+  if (tid < budget) sel_s[tid] = sel_v;
+  if (tid < MAX_E) mask[tid] = 0ull;
+  __syncthreads();
+  int kept_n = 0;
+  bool kept[NCH];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    kept[c] = lane + WAVE * c < E && slot_s[lane + WAVE * c] >= 0;
+    kept_n += __popcll(__ballot(kept[c]));
+  }
+  const int nx = min(min(K, n_sel), kept_n);
+  int ex_id[TPW], ex_slot[TPW];
+  float gate[TPW];
+#pragma unroll
+  for (int q = 0; q < TPW; ++q) {
+    const int t = wv + q * PF_WAVES;
+    ex_id[q] = ex_slot[q] = -1;
+    gate[q] = 0.0f;
+    if (t >= B) continue;
+    const int r_k = lane < K && rv[q] >= 0 && rv[q] < E ? rv[q] : 0;   // as k_backfill
+    float rl = 0.0f;   // the logit of route `lane`
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const float a = __shfl(lv[q][c], r_k & (WAVE - 1), WAVE);
+      if (r_k / WAVE == c) rl = a;
+    }
+    const float lmax = __shfl(rl, 0, WAVE);
+    uint32_t left[NCH];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) left[c] = kept[c] ? order_key(lv[q][c]) : 0u;
+    float l = 0.0f;
+    for (int j = 0; j < nx; ++j) {
+      int e;
+      const float v = order_value(take_best(left, e));
+      if (lane == j) {
+        ex_id[q] = e;
+        l = v;
+      }
+    }
+    const float num = lane < nx ? base_exp(l - lmax) : 0.0f;
+    float den = 0.0f;
+    if (renorm) {
+      for (int j = 0; j < nx; ++j)
+        den = den + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_int(num), j));
+    } else if (norm_topk) {
+      const float eps = base_exp(rl - lmax);
+      for (int k = 0; k < K; ++k)
+        den = den + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_int(eps), k));
+    } else {
+      float pt = 0.0f;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+        if (lane + WAVE * c < E) pt = pt + base_exp(lv[q][c] - lmax);
+      den = wave_tree_sum(pt);
+    }
+    if (lane < nx) {
+      gate[q] = num / den;
+      ex_slot[q] = slot_s[ex_id[q]] < n_sel ? slot_s[ex_id[q]] : -1;   // -1: a plan not made by base_select
+      if (ex_slot[q] >= 0) atomicOr((unsigned long long *)&mask[ex_slot[q]], 1ull << t);
+    }
+    if (out && lane < K) {
+      pl.exec_ids[(size_t)t * K + lane] = ex_id[q];
+      pl.exec_gates[(size_t)t * K + lane] = gate[q];
+    }
+  }
+  __syncthreads();
+  if (wv == 0) {   // exclusive prefixes of the slots' pair counts
+    constexpr int Q = MAX_E / WAVE;
+    int l[Q], s0 = 0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const int s = Q * lane + i;
+      l[i] = s < n_sel ? __popcll(mask[s]) : 0;
+      s0 += l[i];
+    }
+    int inc = s0;
+#pragma unroll
+    for (int h = 1; h < WAVE; h <<= 1) {
+      const int o = __shfl_up(inc, h, WAVE);
+      if (lane >= h) inc += o;
+    }
+    int r = inc - s0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      off[Q * lane + i] = r;
+      r += l[i];
+    }
+    if (lane == WAVE - 1) off[MAX_E] = r;
+  }
+  __syncthreads();
+  const int routed = off[MAX_E];   // off[s] = routed for s >= n_sel
+  int32_t *tx = pl.sptok + (size_t)blockIdx.x * B * kc;
+#pragma unroll
+  for (int q = 0; q < TPW; ++q) {
+    const int t = wv + q * PF_WAVES, s = ex_slot[q];
+    if (t >= B || lane >= K) continue;
+    const int p = s >= 0 ? off[s] + __popcll(mask[s] & ((1ull << t) - 1ull)) : -1;
+    if (p >= 0) tx[p] = t;
+    if (!out) continue;
+    pl.pair_of[(size_t)t * kc + lane] = p;
+    if (p >= 0) {
+      pl.pair_tok[p] = t;
+      pl.pair_gate[p] = gate[q];
+    }
+  }
+  SpRec *rx = pl.rec + (size_t)blockIdx.x * (budget + ns);
+  for (int s = tid; s < budget + ns; s += TH) {
+    const int i = s - budget;
+    SpRec r{0, 0, 0, 0};
+    if (i >= 0) r = SpRec{E + i, routed + i * B, B, 0};
+    // an expert out of range: only for a plan not made by base_select
+    else if (s < n_sel && sel_s[s] >= 0 && sel_s[s] < E + ns)
+      r = SpRec{sel_s[s], off[s], (int)__popcll(mask[s]), 0};
+    rx[s] = r;
+  }
+  if (tid < B)
+    for (int i = 0; i < ns; ++i) tx[routed + i * B + tid] = tid;
+  if (!out) return;
+  for (int s = tid; s <= budget + ns; s += TH)
+    pl.offsets[s] = s <= budget ? off[min(s, MAX_E)] : routed + (s - budget) * B;
+  if (tid < B) {
+    float gs = 1.0f;
+    if (gdot) {
+      const float e = base_exp(-gd);
+      const float dn = 1.0f + e;
+      gs = 1.0f / dn;
+    }
+    for (int i = 0; i < ns; ++i) {
+      const int p = routed + i * B + tid;
+      pl.pair_tok[p] = tid;
+      pl.pair_gate[p] = gs;
+      pl.pair_of[(size_t)tid * kc + K + i] = p;
+    }
+  }
+}
+
+hipError_t launch_plan_given(int B, int K, int E, int budget, int ns, int norm_topk, bool renorm,
+                             const float *logits, const int32_t *ids, const int32_t *sel_ids,
+                             const int32_t *n_sel, const int32_t *slot_of, const float *gdot,
+                             int32_t *exec_ids, float *exec_gates, int32_t *offsets,
+                             int32_t *pair_tok, float *pair_gate, int32_t *pair_of, SpRec *rec,
+                             int32_t *sptok, hipStream_t st) {
+  FewPlan pl{};
+  pl.exec_ids = exec_ids;
+  pl.exec_gates = exec_gates;
+  pl.offsets = offsets;
+  pl.pair_tok = pair_tok;
+  pl.pair_gate = pair_gate;
+  pl.pair_of = pair_of;
+  pl.rec = rec;
+  pl.sptok = sptok;
+#define BASE_PG(C, T)                                                                            \
+  launch_k(k_plan_given<C, T>, dim3(N_XCD), dim3(PF_WAVES * WAVE), 0, st, B, K, E, budget, ns,   \
+           norm_topk, (int)renorm, logits, ids, sel_ids, n_sel, slot_of, gdot, pl)
+  constexpr int TPW = FFN_SPLIT_B / PF_WAVES;
+  if (B <= PF_WAVES) {
+    if (E <= WAVE) BASE_PG(1, 1);
+    else if (E <= 2 * WAVE) BASE_PG(2, 1);
+    else BASE_PG(4, 1);
+  } else {
+    if (E <= WAVE) BASE_PG(1, TPW);
+    else if (E <= 2 * WAVE) BASE_PG(2, TPW);
+    else BASE_PG(4, TPW);
+  }
+#undef BASE_PG
+  return hipGetLastError();
+}
+
 hipError_t launch_plan_few(int B, int K, int E, int budget, int ns, int norm_topk, int rule, int flags,
                            const float *logits, const float *q, const float *ss, const float *pb,
                            const float *gdot, int32_t *ids, float *w, float *cost, float *scores,
