@@ -191,8 +191,8 @@ def _stream(stream):
     import torch
     if stream is None:
         # the current stream's handle without a Stream object around it (3 us a call)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
-    return ctypes.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 class Layer:
@@ -362,15 +362,16 @@ def _rows(t, what, dev):
 # Microscaled 4-bit floating point (E2M1 codes, an E8M0 scale per 32 elements)
 def mx_quantize(src, codes=None, scales=None, stream=None):
     """codes [rows, cols / 2] and scales [rows, cols / 32] (uint8) of src
-    [rows, cols]; the rows may lie inside wider ones."""
+    [rows, cols], into the two tensors given or into new ones; src's rows may
+    lie inside wider ones."""
     import torch
     dev = _device()
     dt, rows, cols, ld = _rows(src, "src", dev)
-    if codes is None:
+    if codes is None and scales is None:
         codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=src.device)
-    if scales is None:
         scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=src.device)
-    _mx_shapes(codes, scales, (rows,), cols, dev)
+    else:
+        _mx_shapes(codes, scales, (rows,), cols, dev)
     _check(load().base_mx_quantize(dt, _ptr(src), rows, cols, ld, _ptr(codes), _ptr(scales),
                                    _stream(stream)))
     return codes, scales
@@ -383,10 +384,15 @@ def mx_dequantize(codes, scales, dtype=None, out=None, stream=None):
     dev = _device()
     _mx_shapes(codes, scales, (rows,), cols, dev)
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype or torch.bfloat16, device=codes.device)
-    dt, r, c, ld = _rows(out, "out", dev)
-    if (r, c) != (rows, cols):
-        raise ValueError("out: the codes' rows and columns")
+        dtype = dtype or torch.bfloat16
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("dtype: fp32 or bf16")
+        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+        dt, ld = BASE_BF16 if dtype is torch.bfloat16 else BASE_F32, cols
+    else:
+        dt, r, c, ld = _rows(out, "out", dev)
+        if (r, c) != (rows, cols):
+            raise ValueError("out: the codes' rows and columns")
     _check(load().base_mx_dequantize(_ptr(codes), _ptr(scales), rows, cols, dt, _ptr(out), ld,
                                      _stream(stream)))
     return out
@@ -395,7 +401,7 @@ def mx_dequantize(codes, scales, dtype=None, out=None, stream=None):
 def _mx_shapes(codes, scales, lead, cols, dev):
     import torch
     for t, n, what in ((codes, cols // 2, "codes"), (scales, cols // 32, "scales")):
-        if (t.dtype is not torch.uint8 or t.shape != (*lead, n) or not t.is_contiguous()
+        if (t is None or t.dtype is not torch.uint8 or t.shape != (*lead, n) or not t.is_contiguous()
                 or t.get_device() != dev):
             raise ValueError(f"{what}: contiguous uint8 {[*lead, n]} on the current GPU")
 

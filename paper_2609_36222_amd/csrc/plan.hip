@@ -1436,6 +1436,63 @@ __device__ __forceinline__ uint32_t take_best(uint32_t (&k)[NCH], int &e) {
   return best;
 }
 
+// The first nx of a token's kept experts (lane + 64 c where kept[c], n_kept of them in
+// all) by (logit desc, index asc): lane j < nx gets the j-th, its expert and logit.
+// With few kept ones every lane counts the keys before its own, broadcast from the
+// wavefront's LDS, instead of nx maxima (16 tokens of K = 8 on ten kept experts 6.2
+// -> 4.8 us, four a wavefront of K = 4 on 16 10.0 -> 8.0); with many that takes longer.
+struct PickLds {
+  __attribute__((aligned(16))) uint64_t key[MAX_E];
+  uint64_t got[MAX_K];
+};
+constexpr int PICK_COUNT = 48;   // kept experts at most
+template <int NCH>
+__device__ __forceinline__ void pick_kept(PickLds &S, const bool (&kept)[NCH], int n_kept, int nx,
+                                          const float (&lv)[NCH], int &id, float &l) {
+  const int lane = lane_id();
+  if (n_kept > PICK_COUNT) {
+    uint32_t left[NCH];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) left[c] = kept[c] ? order_key(lv[c]) : 0u;
+    for (int j = 0; j < nx; ++j) {
+      int e;
+      const float v = order_value(take_best(left, e));
+      if (lane == j) {
+        id = e;
+        l = v;
+      }
+    }
+    return;
+  }
+  int pos = 0;
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    const uint64_t m = __ballot(kept[c]);
+    if (kept[c]) S.key[pos + __popcll(m & ((1ull << lane) - 1ull))] = rank_key(lv[c], lane + WAVE * c);
+    pos += __popcll(m);
+  }
+  const int n8 = (n_kept + 7) & ~7;
+  if (n_kept + lane < n8) S.key[n_kept + lane] = 0;   // ranks after every expert
+  const uint64_t mine = lane < n_kept ? S.key[lane] : 0;
+  int r = 0;
+  for (int f = 0; f < n8; f += 8) {
+    u32x4 o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] = *reinterpret_cast<const u32x4 *>(&S.key[f + 2 * q]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      r += (((uint64_t)o[q].y << 32 | o[q].x) > mine);
+      r += (((uint64_t)o[q].w << 32 | o[q].z) > mine);
+    }
+  }
+  if (lane < n_kept && r < nx) S.got[r] = mine;
+  const uint64_t k = S.got[min(lane, MAX_K - 1)];
+  if (lane < nx) {
+    id = (int)(0xFFFFFFFFu - (uint32_t)k);
+    l = order_value((uint32_t)(k >> 32));
+  }
+}
+
 template <int NCH>
 __global__ __launch_bounds__(PF_WAVES * WAVE)
 void k_plan_few(int B, int K, int E, int budget, int ns, int flags, FewScores sc, FewPlan pl) {
@@ -1447,6 +1504,7 @@ void k_plan_few(int B, int K, int E, int budget, int ns, int flags, FewScores sc
   __shared__ uint32_t mask[MAX_E];   // slot s: the tokens that execute it
   __shared__ int off[MAX_E + 1];
   __shared__ int n_union;
+  __shared__ PickLds pick[PF_WAVES];
   const int tid = threadIdx.x, lane = lane_id(), wv = wave_id_u();
   const bool out = blockIdx.x == 0, token = wv < B;
   const int kc = K + ns, t = min(wv, B - 1);
@@ -1617,20 +1675,12 @@ void k_plan_few(int B, int K, int E, int budget, int ns, int flags, FewScores sc
         num = base_exp(l - lmax);
       }
     } else {
-      uint32_t left[NCH];
+      bool kept[NCH];
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
-        left[c] = lane + WAVE * c < E && slot_s[lane + WAVE * c] >= 0 ? keys[c] : 0u;
+      for (int c = 0; c < NCH; ++c) kept[c] = lane + WAVE * c < E && slot_s[lane + WAVE * c] >= 0;
       float l = 0.0f;
       nx = kp;
-      for (int j = 0; j < kp; ++j) {
-        int e;
-        const float v = order_value(take_best(left, e));
-        if (lane == j) {
-          ex_id = e;
-          l = v;
-        }
-      }
+      pick_kept(pick[wv], kept, n_sel, nx, lv, ex_id, l);
       if (lane < nx) {
         ex_slot = slot_s[ex_id];
         num = base_exp(l - lmax);
@@ -1732,6 +1782,7 @@ void k_plan_given(int B, int K, int E, int budget, int ns, int norm_topk, int re
   __shared__ int slot_s[MAX_E], sel_s[MAX_E];
   __shared__ uint64_t mask[MAX_E];   // slot s: the tokens that execute it
   __shared__ int off[MAX_E + 1];
+  __shared__ PickLds pick[PF_WAVES];
   const int tid = threadIdx.x, lane = lane_id(), wv = wave_id_u();
   const bool out = blockIdx.x == 0;
   const int kc = K + ns;
@@ -1776,18 +1827,8 @@ void k_plan_given(int B, int K, int E, int budget, int ns, int norm_topk, int re
       if (r_k / WAVE == c) rl = a;
     }
     const float lmax = __shfl(rl, 0, WAVE);
-    uint32_t left[NCH];
-#pragma unroll
-    for (int c = 0; c < NCH; ++c) left[c] = kept[c] ? order_key(lv[q][c]) : 0u;
     float l = 0.0f;
-    for (int j = 0; j < nx; ++j) {
-      int e;
-      const float v = order_value(take_best(left, e));
-      if (lane == j) {
-        ex_id[q] = e;
-        l = v;
-      }
-    }
+    pick_kept(pick[wv], kept, kept_n, nx, lv[q], ex_id[q], l);
     const float num = lane < nx ? base_exp(l - lmax) : 0.0f;
     float den = 0.0f;
     if (renorm) {
