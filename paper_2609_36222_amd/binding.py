@@ -343,7 +343,7 @@ def packed_layer(layer: "Layer", K: int, stream=None) -> "Layer":
 def _device():
     """The current GPU, where the launches go and the tensors have to lie."""
     import torch
-    return torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
 
 
 def _rows(t, what, dev):
@@ -485,37 +485,42 @@ class Norms:
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise ValueError("dtype: fp32 or bf16")
         self.tensors = (post_gain, gate, pre_gain)
-        self.d, self.torch_dtype, self.gate_rows, ld = d, dtype, None, 0
-        dev = _device()
-        for t, what in zip(self.tensors, ("post_gain", "gate", "pre_gain")):
+        self.d, self.torch_dtype, self.gate_rows = d, dtype, None
+        dev, f32 = _device(), torch.float32
+        ptr, ld = [None, None, None], 0
+        for i, t in enumerate(self.tensors):
             if t is None:
                 continue
-            s = t.stride()
-            two = what == "gate" and len(s) == 2
-            if (t.dtype is not torch.float32 or not (two or len(s) == 1) or t.shape[-1] != d
-                    or (d > 1 and s[-1] != 1) or t.get_device() != dev):
-                raise ValueError(f"{what}: fp32, {d} adjacent elements a row, on the current GPU")
+            n, s = t.shape, t.stride()
+            two = i == 1 and len(n) == 2
+            if (t.dtype is not f32 or not (two or len(n) == 1) or n[-1] != d
+                    or (s[-1] != 1 and d > 1) or t.get_device() != dev):
+                raise ValueError(f"{('post_gain', 'gate', 'pre_gain')[i]}: fp32, {d} adjacent elements "
+                                 "a row, on the current GPU")
             if two:
-                self.gate_rows = t.shape[0]
-                ld = s[0] if self.gate_rows > 1 else d
+                self.gate_rows = n[0]
+                ld = s[0] if n[0] > 1 else d
+            ptr[i] = t.data_ptr()
         self.desc = base_norms(d, BASE_BF16 if dtype is torch.bfloat16 else BASE_F32, eps, res_scale,
-                               _ptr(post_gain), _ptr(gate), ld, _ptr(pre_gain))
+                               ptr[0], ptr[1], ld, ptr[2])
 
-    def _pointers(self, rows, *tensors):
-        """The row count checked, and (pointer, row stride) of each named tensor."""
+    def _pointers(self, rows, dev, tensors):
+        """The row count checked, and (pointer, row stride) of each tensor (of y, h,
+        h_out, x_out, in this order)."""
         if self.gate_rows is not None and self.gate_rows != rows:
             raise ValueError(f"gate: one row, or {rows}")
-        out, dev, d = [], _device(), self.d
-        for t, what in tensors:
+        out, d, dt = [], self.d, self.torch_dtype
+        shape = (rows, d)
+        for i, t in enumerate(tensors):
             if t is None:
                 out += (None, 0)
                 continue
-            s = t.stride()
-            if (t.dtype is not self.torch_dtype or t.shape != (rows, d) or (d > 1 and s[1] != 1)
-                    or t.get_device() != dev):
-                raise ValueError(f"{what}: {self.torch_dtype} [{rows}, {d}], adjacent columns, "
-                                 "on the current GPU")
-            out += (t.data_ptr(), s[0] if rows > 1 else d)
+            if t.dtype is not dt or t.shape != shape or t.get_device() != dev:
+                raise ValueError(f"{('y', 'h', 'h_out', 'x_out')[i]}: {dt} {list(shape)} on the current GPU")
+            ld, one = t.stride()
+            if one != 1 and d > 1:
+                raise ValueError(f"{('y', 'h', 'h_out', 'x_out')[i]}: adjacent columns")
+            out += (t.data_ptr(), ld if rows > 1 else d)
         return out
 
 
@@ -523,7 +528,7 @@ def base_norm_residual(norms: Norms, y, h, h_out=None, x_out=None, stream=None):
     """h_out = res_scale h + gate (post_gain n(y)), x_out = pre_gain n(h_out); [rows, d]
     tensors whose rows may lie inside wider ones; y None: x_out = pre_gain n(h)."""
     rows = h.shape[0]
-    a = norms._pointers(rows, (y, "y"), (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
+    a = norms._pointers(rows, _device(), (y, h, h_out, x_out))
     _check(load().base_norm_residual(norms.desc, rows, *a, _stream(stream)))
 
 
@@ -546,7 +551,7 @@ def base_decode_block(desc, norms: Norms, x, B, budget, flags, h, ws, h_out=None
     """base_decode_layer, then base_norm_residual on its output, in the layer's
     launches; returns the filled base_plan (device pointers into ws)."""
     plan = base_plan() if plan is None else plan
-    norms._pointers(B, (h, "h"), (h_out, "h_out"), (x_out, "x_out"))
+    norms._pointers(B, _device(), (None, h, h_out, x_out))
     for t, what in ((h, "h"), (h_out, "h_out"), (x_out, "x_out")):
         if t is not None and not t.is_contiguous():
             raise ValueError(f"{what}: contiguous rows")
