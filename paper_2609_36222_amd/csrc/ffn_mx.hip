@@ -24,7 +24,7 @@ struct MxShape {
   static constexpr int NT = NT_, T = T_, RW = RW_, KW = KW_, DT = DT_;
   static constexpr int WAVES = RW * KW, THREADS = WAVES * WAVE, RING = DT + 1;
   static constexpr int SLOT = NT * 4096;               // a step's token rows
-  static constexpr int TL = NT * 4 / RW;               // token loads per wavefront and step
+  static constexpr int TL = (NT * 4 + RW - 1) / RW;    // token loads per wavefront and step
   static constexpr int SL = KW == 1 ? T : 2 * T;       // scale loads per four steps
   static constexpr int LDS = KW * RING * SLOT;
   static constexpr int GROUP = RW * T;                 // tiles per workgroup
@@ -116,30 +116,29 @@ __host__ __device__ inline int mx_groups(int tiles, int group) { return (tiles +
 template <typename M, int N, typename Rows>
 __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, int K, rsrc_t rx,
                                           Rows rows, f32x4 (&acc)[M::T][N]) {
-  constexpr int T = M::T, DT = M::DT, L = 4 / M::RW;   // L loads of four rows per tile
-  constexpr int TL = N * L;
+  constexpr int T = M::T, DT = M::DT, L = (4 * N + M::RW - 1) / M::RW;   // loads of four rows
+  static_assert(L * M::RW <= 4 * M::NT, "token loads stay in their slot");
   const int w = wave_id_u(), lane = lane_id(), kq = w / M::RW, rw = w % M::RW;
   uint8_t *ring = lds + kq * (M::RING * M::SLOT);
   const int S = mx_steps(K), s0 = kq * S / M::KW, s1 = (kq + 1) * S / M::KW;
   const int most = (S + M::KW - 1) / M::KW;   // steps of the longest share
   const uint32_t Kb = (uint32_t)K * 2u;
-  // the rows this lane stages: row r of every tile for r = 4 (rw L + q) + lane / 16,
-  // its 16 bytes in place lane % 16 of the row
-  uint32_t tv[N][L], pc[L];
+  // the rows this lane stages: of the step's 4 N quarter tiles (four rows each) the
+  // RW wavefronts take one after another in turn; lane l row l / 16 of the quarter,
+  // the 16 bytes in place l % 16 of the row
+  uint32_t tv[L], pc[L];
   // the ring's slots in turn, as running offsets: step i's to read and step i + DT's
   // to fill (a remainder in the addresses costs an add per LDS read)
   int fill = 0, read = 0;
   auto next = [](int &slot) { slot = slot == (M::RING - 1) * M::SLOT ? 0 : slot + M::SLOT; };
   auto tokens = [&](int i) {
-    uint8_t *slot = ring + fill + rw * (L * 1024);
+    uint8_t *slot = ring + fill + rw * 1024;
     next(fill);
     const uint32_t at = (uint32_t)(s0 + i) * 256u;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int q = 0; q < L; ++q)
-        load_lds(rx, slot + j * 4096 + q * 1024,
-                 s0 + i < s1 && at + pc[q] < Kb ? tv[j][q] + at + pc[q] : FFN_TOK_PAD, 0);
+    for (int q = 0; q < L; ++q)
+      load_lds(rx, slot + q * (M::RW * 1024),
+               s0 + i < s1 && at + pc[q] < Kb ? tv[q] + at + pc[q] : FFN_TOK_PAD, 0);
   };
   u32x4 wt[MX_CHUNK][T];
   uint32_t sc[T], sn[T], sh[T];
@@ -169,10 +168,9 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
   for (int p = 0; p <= DT; ++p) weights(p, p);
 #pragma unroll
   for (int q = 0; q < L; ++q) {
-    const int r = 4 * (rw * L + q) + (lane >> 4), at16 = (lane & 15) ^ r;
+    const int k = rw + M::RW * q, r = 4 * (k & 3) + (lane >> 4), at16 = (lane & 15) ^ r;
     pc[q] = 64u * (uint32_t)mx_block_at(at16 >> 2) + 16u * (uint32_t)(at16 & 3);
-#pragma unroll
-    for (int j = 0; j < N; ++j) tv[j][q] = rows(16 * j + r);
+    tv[q] = rows(16 * (k >> 2) + r);
   }
 #pragma unroll
   for (int p = 0; p < DT; ++p) tokens(p);
@@ -516,19 +514,19 @@ namespace {
 // B = 16, 96 and 120 workgroups: 8.3 and 9.6 against 6.9 and 7.7; OLMoE-shaped,
 // 24 slots at B = 5, 384 workgroups: 12.0 against 12.5; down, whose contraction is
 // short: 5.2, 5.2 and 7.8 against 5.0, 6.0 and 8.4).  Past 32 tokens the matrix
-// pipe is busy for most of the time and a tile's operands in LDS are read once per
-// wavefront, so more workgroups per CU pay more than deeper rings (DT = 1, 2, 3
-// at B = 256, 32 experts, gate/up 24.3, 24.9 and 30.1, down 17.6, 18.4 and 21.3), and
-// with enough workgroups four tiles a wavefront halve the LDS reads (B = 1024,
-// 128 experts: gate/up 85 -> 78; 672 wide ones of Mixtral's shape 89 -> 82; but 258 at B
-// = 256 24.3 -> 28.4, and 220 of Qwen1.5-MoE's shape at B = 61 17.0 -> 23.1; down
-// equal at best).  The line counts the workgroups of slots and full parts, which
-// the host knows.
+// pipe is busy for most of the time, and more workgroups per CU pay more than
+// deeper rings (DT = 1, 2, 3 at B = 256, 32 experts, gate/up 24.3, 24.9 and 30.1,
+// down 17.6, 18.4 and 21.3).  With enough workgroups eight wavefronts share the
+// token rows instead of four, which halves their traffic (gate/up, B = 1024, 128
+// experts: 85 -> 77; 448 workgroups of Mixtral's shape 89 -> 81; but 192 at B = 256
+// 24.7 -> 27.5, and 220 of Qwen1.5-MoE's shape at B = 61 17.8 -> 21.4; down, of short
+// contractions, 52.8 and 52.9 at B = 1024, and 17.7 -> 19.2 at B = 256).  The line counts
+// the workgroups of slots and full parts, which the host knows.
 using MxFew = MxShape<1, 2, 4, 1, 2>;
 using MxFewSplit = MxShape<1, 2, 2, 2, 2>;
 using MxMid = MxShape<2, 2, 4, 1, 2>;
 using MxMany = MxShape<MX_NT, 2, 4, 1, 1>;
-using MxManyWide = MxShape<MX_NT, 4, 4, 1, 1>;
+using MxManyWide = MxShape<MX_NT, 2, 8, 1, 1>;
 
 int mx_workgroups(int B, int K, int budget, int ns, int groups) {
   const int kept = mx_kept(B, K, budget), full = B * (K + ns) / (16 * MX_NT);
