@@ -104,7 +104,7 @@ struct Layout {
   int nrec;
   size_t logits, gdot, topk_ids, topk_w, cost, scores, counts, sel_ids, n_sel,
       slot_of, exec_ids, exec_gates, offsets, pair_tok, pair_gate, pair_of, order, ex,
-      den, hdr, units_gu, units_dn, tokoff, sprec, H, pairbuf, total;
+      den, hdr, units_gu, units_dn, tokoff, sprec, H, Hlo, pairbuf, total;
 };
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -161,6 +161,7 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc, bool split) {
   } else {
     o.H = take(BK * L->I * 4);
   }
+  o.Hlo = take(mx_layer(L) && B <= MX_TWO_B ? P * (size_t)L->I : 0);   // the activations' 8-bit part
   // (small batches: gate/up's token lists, one per die, lie here until down
   // writes its rows)
   o.pairbuf = take(P * L->d * 4);
@@ -288,11 +289,11 @@ base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, i
   const FfnHdr *hdr = at<FfnHdr>(ws, o.hdr);
   const SpRec *rec = o.split ? at<SpRec>(ws, o.sprec) : nullptr;
   const float *pair_gate = at<float>(ws, o.pair_gate);
-  void *H = at<void>(ws, o.H);
+  void *H = at<void>(ws, o.H), *Hlo = at<void>(ws, o.Hlo);
   stage(6, st);
   if (mx_layer(L))
     HIP_TRY(launch_mx_gateup(x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13, L->w13_shared,
-                             rec, sptok, H, n_cu, st));
+                             rec, sptok, H, Hlo, n_cu, st));
   else
     HIP_TRY(launch_gateup(bf16, packed, x, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w13,
                           L->w13_shared, sel_ids, n_sel, offsets, at<int32_t>(ws, o.pair_tok), hdr,
@@ -302,10 +303,10 @@ base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, i
   stage(7, st);
   if (y)
     HIP_TRY(launch_mx_down_combine(B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2, L->w2_shared, rec,
-                                   at<int32_t>(ws, o.pair_of), pair_gate, H, residual, y, st));
+                                   at<int32_t>(ws, o.pair_of), pair_gate, H, Hlo, residual, y, st));
   else if (mx_layer(L))
     HIP_TRY(launch_mx_down(B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2, L->w2_shared, rec,
-                           pair_gate, H, at<float>(ws, o.pairbuf), st));
+                           pair_gate, H, Hlo, at<float>(ws, o.pairbuf), st));
   else
     HIP_TRY(launch_down(bf16, packed, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2,
                         L->w2_shared, sel_ids, n_sel, offsets, hdr, at<FfnUnit>(ws, o.units_dn),

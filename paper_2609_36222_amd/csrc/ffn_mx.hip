@@ -1,8 +1,17 @@
 // Grouped SwiGLU expert FFN on 4-bit weights (BASE_W_MXFP4): the same products as
 // ffn.hip's, H[p] = bf16(silu(x . W_g) * (x . W_u)), pairbuf[p] = gate_p *
 // (H[p] . W_d), with the weights' values e2m1 * 2^(s - 127) -- exact in bf16 --
-// on MFMA 16x16x32 bf16, fp32 sums in ascending k.  The activation H is rounded to
-// bf16 for the second product, as in the 16-bit layers.
+// on MFMA 16x16x32 bf16, fp32 sums in ascending k.
+//
+// The activation's rounding.  Up to MX_TWO_B tokens h goes to the second product as a
+// bf16 and an E5M2 part, h = hi + 2^-9 lo with lo = 2^9 (h - hi) rounded, so that its
+// error is an eighth of a bf16 rounding's (as much as that where lo leaves E5M2's
+// range, |h| < 2^-14 or > 57344): the launch is a weight stream, the scaled 16x16x128
+// product takes the weights' codes and scales as they lie in memory, and the layer
+// takes 2 to 4% longer.  Beyond, the matrix pipe is busy and the second part costs 7 to
+// 20% of the layer (B = 256 57 -> 64 us, B = 1024 154 -> 181), so h is rounded to bf16, as in
+// the 16-bit layers.  The output's error is then 1.4 times its own rounding's on average
+// and, where few activations make it, up to 1.6; with both parts 1.0.
 //
 // The launch works on records {expert, first pair, pairs}: a slot (B <= 64) or
 // a part of at most MX_NT 16-pair tiles of one, with their token lists, one copy
@@ -19,12 +28,16 @@
 
 namespace basek {
 
-template <int NT_, int T_, int RW_, int KW_, int DT_>
+// LO: the token rows have a second, 8-bit part (down)
+template <int NT_, int T_, int RW_, int KW_, int DT_, bool LO_ = false>
 struct MxShape {
   static constexpr int NT = NT_, T = T_, RW = RW_, KW = KW_, DT = DT_;
+  static constexpr bool LO = LO_;
   static constexpr int WAVES = RW * KW, THREADS = WAVES * WAVE, RING = DT + 1;
-  static constexpr int SLOT = NT * 4096;               // a step's token rows
-  static constexpr int TL = (NT * 4 + RW - 1) / RW;    // token loads per wavefront and step
+  static constexpr int HL = (NT * 4 + RW - 1) / RW;    // loads per wavefront and step: bf16 rows
+  static constexpr int LL = LO ? (NT * 2 + RW - 1) / RW : 0;   // ... the 8-bit parts
+  static constexpr int TL = HL + LL;
+  static constexpr int SLOT = NT * 4096 + LL * RW * 1024;      // a step's token rows
   static constexpr int SL = KW == 1 ? T : 2 * T;       // scale loads per four steps
   static constexpr int LDS = KW * RING * SLOT;
   static constexpr int GROUP = RW * T;                 // tiles per workgroup
@@ -56,6 +69,22 @@ __device__ __forceinline__ MxWork mx_work(const MxPlan &pl, int RG, int NT) {
   const int rg = ((die - ord * RG) & (N_XCD - 1)) + N_XCD * k;
   return {__builtin_amdgcn_readfirstlane(r.u), __builtin_amdgcn_readfirstlane(r.p0),
           rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg, (z - k * pl.cuts) * 16 * NT};
+}
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+// acc + the rows' codes and scale byte times 2^-9 times 128 E5M2 elements: lane (n, g)
+// has the elements 16 g .. +15 and 64 + 16 g .. +15 of column n
+__device__ __forceinline__ f32x4 mfma_lo(u32x4 codes, uint32_t byte, u32x4 lo0, u32x4 lo1, f32x4 acc) {
+  const i32x8 a = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
+  const i32x8 b = {(int)lo0[0], (int)lo0[1], (int)lo0[2], (int)lo0[3],
+                   (int)lo1[0], (int)lo1[1], (int)lo1[2], (int)lo1[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 1, 0, (int)byte, 0, 127 - 9);
+}
+// the E5M2 part of h beside its bf16 rounding, as fp32 for the conversion: within its
+// range, 0 for NaN and infinities
+__device__ __forceinline__ float mx_lo(float h, uint16_t hi) {
+  const float v = 512.0f * (h - bf16_to_f32(hi));
+  return v == v ? fminf(fmaxf(v, -57344.0f), 57344.0f) : 0.0f;
 }
 
 __device__ __forceinline__ int mx_block_pos(int g) { return (0x9C >> (2 * g)) & 3; }   // 0, 3, 1, 2
@@ -109,13 +138,14 @@ __host__ __device__ inline int mx_groups(int tiles, int group) { return (tiles +
 //    0..3 and 12..15 of an even block with the rows 4..11 of the odd one after it
 //    (or the other way round), so the two blocks' places have to differ by 12: with
 //    4 g + f half of the cycles were conflicts (Qwen3-shaped gate/up, B = 1024, 128
-//    experts 106 -> 95 us).
+//    experts 106 -> 95 us).  Behind them, row n of an 8-bit part at 128 n, its 16-byte
+//    piece p at p ^ (n / 2).
 //  * Order of the loads: in step s the tokens of step s + DT and the weights of step
 //    s + DT + 1, so that the wait for a step's tokens covers its weights and leaves
 //    those of the DT steps after it in flight.
 template <typename M, int N, typename Rows>
 __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, int K, rsrc_t rx,
-                                          Rows rows, f32x4 (&acc)[M::T][N]) {
+                                          rsrc_t rlo, Rows rows, f32x4 (&acc)[M::T][N]) {
   constexpr int T = M::T, DT = M::DT, L = (4 * N + M::RW - 1) / M::RW;   // loads of four rows
   static_assert(L * M::RW <= 4 * M::NT, "token loads stay in their slot");
   const int w = wave_id_u(), lane = lane_id(), kq = w / M::RW, rw = w % M::RW;
@@ -127,6 +157,9 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
   // RW wavefronts take one after another in turn; lane l row l / 16 of the quarter,
   // the 16 bytes in place l % 16 of the row
   uint32_t tv[L], pc[L];
+  constexpr int LL = M::LO ? (2 * N + M::RW - 1) / M::RW : 0;   // half tiles (eight rows) of the 8-bit part
+  static_assert(LL <= M::LL, "... in the slot");
+  uint32_t lv[LL + 1], lc[LL + 1];
   // the ring's slots in turn, as running offsets: step i's to read and step i + DT's
   // to fill (a remainder in the addresses costs an add per LDS read)
   int fill = 0, read = 0;
@@ -134,11 +167,16 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
   auto tokens = [&](int i) {
     uint8_t *slot = ring + fill + rw * 1024;
     next(fill);
+    const uint32_t al = (uint32_t)(s0 + i) * 128u;
     const uint32_t at = (uint32_t)(s0 + i) * 256u;
 #pragma unroll
     for (int q = 0; q < L; ++q)
       load_lds(rx, slot + q * (M::RW * 1024),
                s0 + i < s1 && at + pc[q] < Kb ? tv[q] + at + pc[q] : FFN_TOK_PAD, 0);
+#pragma unroll
+    for (int q = 0; q < LL; ++q)
+      load_lds(rlo, slot + M::NT * 4096 + q * (M::RW * 1024),
+               s0 + i < s1 && al + lc[q] < (uint32_t)K ? lv[q] + al + lc[q] : FFN_TOK_PAD, 0);
   };
   u32x4 wt[MX_CHUNK][T];
   uint32_t sc[T], sn[T], sh[T];
@@ -173,16 +211,27 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
     tv[q] = rows(16 * (k >> 2) + r);
   }
 #pragma unroll
+  for (int q = 0; q < LL; ++q) {
+    const int k = rw + M::RW * q, r = 8 * (k & 1) + (lane >> 3);
+    lc[q] = 16u * (uint32_t)((lane & 7) ^ (r >> 1));
+    const uint32_t v = rows(16 * (k >> 1) + r);
+    lv[q] = v == FFN_TOK_PAD ? v : v / 2;   // half the bytes of the bf16 row
+  }
+#pragma unroll
   for (int p = 0; p < DT; ++p) tokens(p);
   const uint8_t *op[4];   // operand f of this lane's token and block, in slot 0
 #pragma unroll
   for (int f = 0; f < 4; ++f)
     op[f] = ring + (lane & 15) * 256 + 16 * ((4 * mx_block_pos(lane >> 4) + f) ^ (lane & 15));
+  const uint8_t *ol[2];   // the 8-bit part's halves
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+    ol[f] = ring + M::NT * 4096 + (lane & 15) * 128 + 16 * ((4 * f + (lane >> 4)) ^ ((lane & 15) >> 1));
   for (int i0 = 0; i0 < most; i0 += MX_CHUNK) {
 #pragma unroll
     for (int p = 0; p < MX_CHUNK; ++p) {
       const int i = i0 + p;
-      mx_wait<MxShape<N, T, M::RW, M::KW, DT>>(i0 == 0, p);
+      mx_wait<MxShape<N, T, M::RW, M::KW, DT, M::LO>>(i0 == 0, p);
       if (M::RW > 1) wg_barrier();   // the others' rows are there, the next slot is read
       __builtin_amdgcn_sched_barrier(0);
       tokens(i + DT);
@@ -208,6 +257,16 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
             const bf16x8 a = mx_decode8(wt[p][t][f], scale[t]);
 #pragma unroll
             for (int j = 0; j < N; ++j) acc[t][j] = mfma16(a, x[j], acc[t][j]);
+          }
+        }
+        if constexpr (M::LO) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const u32x4 l0 = *reinterpret_cast<const u32x4 *>(ol[0] + read + j * 2048);
+            const u32x4 l1 = *reinterpret_cast<const u32x4 *>(ol[1] + read + j * 2048);
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+              acc[t][j] = mfma_lo(wt[p][t], (sc[t] >> (8 * p)) & 0xFFu, l0, l1, acc[t][j]);
           }
         }
       }
@@ -269,7 +328,8 @@ template <typename M>
 __global__ __launch_bounds__(M::THREADS, M::WPE)
 void k_mx_gateup(int d, int I, int E, MxPlan pl, int np, const uint8_t *__restrict__ w13r,
                  const uint8_t *__restrict__ w13s, const int32_t *__restrict__ sptok,
-                 const uint16_t *__restrict__ x, int B, uint16_t *__restrict__ H) {
+                 const uint16_t *__restrict__ x, int B, uint16_t *__restrict__ H,
+                 uint8_t *__restrict__ Hlo) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
   const MxWork k = mx_work(pl, mx_groups(I / 8, M::GROUP), M::NT);
   const size_t eb = (size_t)(I / 8) * mx_tile_bytes(d);
@@ -280,12 +340,13 @@ void k_mx_gateup(int d, int I, int E, MxPlan pl, int np, const uint8_t *__restri
     const int n = min(k.n - c, 16 * M::NT);
     const int32_t *tok = sptok + (size_t)(blockIdx.x % N_XCD) * np + k.p0 + c;
     uint16_t *h0 = H + (size_t)(k.p0 + c) * I;
+    uint8_t *l0 = Hlo + (size_t)(k.p0 + c) * I;
     if (c > k.c0) wg_barrier();   // every wavefront is done with the ring
     sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
       constexpr int N = decltype(NC)::value;
       const MxTiles<M::T> m = mx_tiles<M>(w13, k.rg, I / 8, d);
       f32x4 acc[M::T][N];
-      mx_stream<M, N>(lds, m, d, rx, [&](int i) {
+      mx_stream<M, N>(lds, m, d, rx, rx, [&](int i) {
         return i < n ? (uint32_t)tok[i] * (uint32_t)d * 2u : FFN_TOK_PAD;
       }, acc);
       if (!m.active) return;
@@ -293,11 +354,21 @@ void k_mx_gateup(int d, int I, int E, MxPlan pl, int np, const uint8_t *__restri
         const int p = 16 * j + (lane & 15);
         if (p >= n) return;
         uint16_t h[4];
+        float s[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) h[q] = f32_to_bf16(silu_bf16(v[0][q]) * v[1][q]);
+        for (int q = 0; q < 4; ++q) {
+          s[q] = silu_bf16(v[0][q]) * v[1][q];   // (silu within 2^-22)
+          h[q] = f32_to_bf16(s[q]);
+        }
         const u32x2 pk = {(uint32_t)h[0] | ((uint32_t)h[1] << 16),
                           (uint32_t)h[2] | ((uint32_t)h[3] << 16)};
-        *reinterpret_cast<u32x2 *>(h0 + (size_t)p * I + 8 * (m.t0 + t) + 4 * (lane >> 4)) = pk;
+        const size_t at = (size_t)p * I + 8 * (m.t0 + t) + 4 * (lane >> 4);
+        *reinterpret_cast<u32x2 *>(h0 + at) = pk;
+        if constexpr (M::NT < MX_NT) {   // up to MX_TWO_B tokens
+          int lp = __builtin_amdgcn_cvt_pk_bf8_f32(mx_lo(s[0], h[0]), mx_lo(s[1], h[1]), 0, false);
+          lp = __builtin_amdgcn_cvt_pk_bf8_f32(mx_lo(s[2], h[2]), mx_lo(s[3], h[3]), lp, true);
+          *reinterpret_cast<int *>(l0 + at) = lp;
+        }
       });
     });
   }
@@ -307,7 +378,8 @@ template <typename M>
 __global__ __launch_bounds__(M::THREADS, M::WPE)
 void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
                const uint8_t *__restrict__ w2s, const float *__restrict__ pair_gate,
-               const uint16_t *__restrict__ H, float *__restrict__ pairbuf) {
+               const uint16_t *__restrict__ H, const uint8_t *__restrict__ Hlo,
+               float *__restrict__ pairbuf) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
   const MxWork k = mx_work(pl, mx_groups(d / 16, M::GROUP), M::NT);
   const size_t eb = (size_t)(d / 16) * mx_tile_bytes(I);
@@ -316,6 +388,7 @@ void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
   for (int c = k.c0; c < k.n; c += 16 * M::NT * pl.cuts) {
     const int n = min(k.n - c, 16 * M::NT), p0 = k.p0 + c;
     const rsrc_t rx = make_rsrc(H + (size_t)p0 * I, (uint32_t)n * (uint32_t)I * 2u);
+    const rsrc_t rlo = M::LO ? make_rsrc(Hlo + (size_t)p0 * I, (uint32_t)n * (uint32_t)I) : rx;
     float *out0 = pairbuf + (size_t)p0 * d;
     if (c > k.c0) wg_barrier();
     sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
@@ -325,7 +398,7 @@ void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
 #pragma unroll
       for (int j = 0; j < N; ++j) gt[j] = pair_gate[p0 + min(16 * j + (lane & 15), n - 1)];
       f32x4 acc[M::T][N];
-      mx_stream<M, N>(lds, m, I, rx, [&](int i) {
+      mx_stream<M, N>(lds, m, I, rx, rlo, [&](int i) {
         return i < n ? (uint32_t)i * (uint32_t)I * 2u : FFN_TOK_PAD;
       }, acc);
       if (!m.active) return;
@@ -374,8 +447,9 @@ template <int RL>
 __global__ __launch_bounds__(MXF_WAVES * WAVE)
 void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
                        const uint8_t *__restrict__ w2r, const uint8_t *__restrict__ w2s,
-                       const uint16_t *__restrict__ H) {
-  // the sums [share][pair][16], then every wavefront's token rows, four steps of RL KiB
+                       const uint16_t *__restrict__ H, const uint8_t *__restrict__ Hlo) {
+  constexpr int LL = (RL + 1) / 2, STEP = (RL + LL) * 1024;   // loads of the 8-bit part; a step's rows
+  // the sums [share][pair][16], then every wavefront's token rows of four steps
   extern __shared__ __attribute__((aligned(16))) float sums[];
   __shared__ __attribute__((aligned(16))) int pair_s[MXF_PAIRS];
   __shared__ __attribute__((aligned(16))) float gate_s[MXF_PAIRS];
@@ -414,7 +488,7 @@ void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
     unit(it);
     return it;
   };
-  uint8_t *ring = reinterpret_cast<uint8_t *>(sums + tl.shares * np * 16) + w * (MX_CHUNK * RL * 1024);
+  uint8_t *ring = reinterpret_cast<uint8_t *>(sums + tl.shares * np * 16) + w * (MX_CHUNK * STEP);
   const int tok = lane & 15, g = lane >> 4;
   // (a row past the staged ones repeats one of them, in a column nobody reads)
   const uint8_t *op[4];
@@ -428,9 +502,20 @@ void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
     pc[q] = 64u * (uint32_t)mx_block_at(at16 >> 2) + 16u * (uint32_t)(at16 & 3);
     rb[q] = (uint32_t)r * Ib;   // rows past the slot's pairs are past rx: zeros
   }
+  uint32_t lc[LL], lb[LL];
+#pragma unroll
+  for (int q = 0; q < LL; ++q) {
+    const int r = 8 * q + (lane >> 3);
+    lc[q] = 16u * (uint32_t)((lane & 7) ^ (r >> 1));
+    lb[q] = (uint32_t)r * (uint32_t)I;
+  }
+  const uint8_t *ol[2];
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+    ol[f] = ring + RL * 1024 + (tok % (8 * LL)) * 128 + 16 * ((4 * f + g) ^ ((tok % (8 * LL)) >> 1));
   u32x4 a[MX_CHUNK];
   uint32_t sn = 0;
-  rsrc_t rw = make_rsrc(w2r, 0), rx = make_rsrc(H, 0);
+  rsrc_t rw = make_rsrc(w2r, 0), rx = make_rsrc(H, 0), rlo = rx;
   auto request = [&](const MxItem &it, int p) {
     const bool have = it.k < nu;
     if (p == 0 && have) {
@@ -438,6 +523,7 @@ void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
       rw = make_rsrc(m + tile * tb, (uint32_t)tb);
       const int n = min(it.n - it.c, 4 * RL);
       rx = make_rsrc(H + (size_t)(it.p0 + it.c) * I, (uint32_t)n * Ib);
+      rlo = make_rsrc(Hlo + (size_t)(it.p0 + it.c) * I, (uint32_t)(n * I));
     }
     const int s = it.ch * MX_CHUNK + p;
     const uint32_t c0 = have && s < S ? (uint32_t)it.ch * MX_CHUNK_BYTES : FFN_TOK_PAD;
@@ -446,7 +532,12 @@ void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
     const uint32_t at = (uint32_t)s * 256u;
 #pragma unroll
     for (int q = 0; q < RL; ++q)
-      load_lds(rx, ring + (p * RL + q) * 1024, have && at + pc[q] < Ib ? rb[q] + at + pc[q] : FFN_TOK_PAD, 0);
+      load_lds(rx, ring + p * STEP + q * 1024, have && at + pc[q] < Ib ? rb[q] + at + pc[q] : FFN_TOK_PAD, 0);
+    const uint32_t al = (uint32_t)s * 128u;
+#pragma unroll
+    for (int q = 0; q < LL; ++q)
+      load_lds(rlo, ring + p * STEP + (RL + q) * 1024,
+               have && al + lc[q] < (uint32_t)I ? lb[q] + al + lc[q] : FFN_TOK_PAD, 0);
   };
   MxItem it{w, 0, 0, 0, 0, 0, 0};
   unit(it);
@@ -468,15 +559,18 @@ void k_mx_down_combine(int d, int I, int E, int slots, MxPlan pl, MxFewTail tl,
     for (int p = 0; p < MX_CHUNK; ++p) {
       // behind this step are three others, one of them with its chunk's scales
       // unless this step came with its own
-      if (p == 0) wait_vm<3 * (1 + RL)>();
-      else wait_vm<3 * (1 + RL) + 1>();
+      if (p == 0) wait_vm<3 * (1 + RL + LL)>();
+      else wait_vm<3 * (1 + RL + LL) + 1>();
       __builtin_amdgcn_sched_barrier(0);
       const float scale = mx_scale((sc >> (8 * p)) & 0xFFu);
       bf16x8 x[4];
 #pragma unroll
-      for (int f = 0; f < 4; ++f) x[f] = *reinterpret_cast<const bf16x8 *>(op[f] + p * (RL * 1024));
+      for (int f = 0; f < 4; ++f) x[f] = *reinterpret_cast<const bf16x8 *>(op[f] + p * STEP);
+      const u32x4 l0 = *reinterpret_cast<const u32x4 *>(ol[0] + p * STEP);
+      const u32x4 l1 = *reinterpret_cast<const u32x4 *>(ol[1] + p * STEP);
 #pragma unroll
       for (int f = 0; f < 4; ++f) acc = mfma16(mx_decode8(a[p][f], scale), x[f], acc);
+      acc = mfma_lo(a[p], (sc >> (8 * p)) & 0xFFu, l0, l1, acc);
       __builtin_amdgcn_sched_barrier(0);
       request(nx, p);
       __builtin_amdgcn_sched_barrier(0);
@@ -522,11 +616,14 @@ namespace {
 // 24.7 -> 27.5, and 220 of Qwen1.5-MoE's shape at B = 61 17.8 -> 21.4; down, of short
 // contractions, 52.8 and 52.9 at B = 1024, and 17.7 -> 19.2 at B = 256).  The line counts
 // the workgroups of slots and full parts, which the host knows.
+static_assert(MX_TWO_B == 32, "MxMid's token tiles");
 using MxFew = MxShape<1, 2, 4, 1, 2>;
 using MxFewSplit = MxShape<1, 2, 2, 2, 2>;
 using MxMid = MxShape<2, 2, 4, 1, 2>;
 using MxMany = MxShape<MX_NT, 2, 4, 1, 1>;
 using MxManyWide = MxShape<MX_NT, 2, 8, 1, 1>;
+using MxFewDown = MxShape<1, 2, 4, 1, 2, true>;
+using MxMidDown = MxShape<2, 2, 4, 1, 2, true>;
 
 int mx_workgroups(int B, int K, int budget, int ns, int groups) {
   const int kept = mx_kept(B, K, budget), full = B * (K + ns) / (16 * MX_NT);
@@ -546,7 +643,7 @@ int mx_cuts(int B, int NT) {
 
 hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, int budget, int slots,
                             int ns, const void *w13, const void *w13s, const SpRec *rec,
-                            const int32_t *sptok, void *H, int n_cu, hipStream_t st) {
+                            const int32_t *sptok, void *H, void *Hlo, int n_cu, hipStream_t st) {
   const bool parts = mx_parts(B);
   const int nrec = mx_records(B, K, budget, ns);
   auto go = [&](auto shape) {
@@ -555,13 +652,13 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
     launch_k(k_mx_gateup<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(I / 8, M::GROUP), cuts),
              dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, rec},
              B * (K + ns), (const uint8_t *)w13, (const uint8_t *)w13s, sptok, (const uint16_t *)x,
-             B, (uint16_t *)H);
+             B, (uint16_t *)H, (uint8_t *)Hlo);
   };
   auto wgs = [&](int group) { return mx_workgroups(B, K, budget, ns, mx_groups(I / 8, group)); };
   if (B <= 16) {
     if (wgs(MxFew::GROUP) >= n_cu) go(MxFew{});
     else go(MxFewSplit{});
-  } else if (B <= 32) {
+  } else if (B <= MX_TWO_B) {
     go(MxMid{});
   } else if (2 * wgs(MxManyWide::GROUP) >= 3 * n_cu) {
     go(MxManyWide{});
@@ -573,7 +670,7 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
 
 hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                           const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
-                          const void *H, float *pairbuf, hipStream_t st) {
+                          const void *H, const void *Hlo, float *pairbuf, hipStream_t st) {
   const bool parts = mx_parts(B);
   const int nrec = mx_records(B, K, budget, ns);
   auto go = [&](auto shape) {
@@ -581,10 +678,11 @@ hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slo
     const int cuts = mx_cuts(B, M::NT);
     launch_k(k_mx_down<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(d / 16, M::GROUP), cuts),
              dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, rec},
-             (const uint8_t *)w2, (const uint8_t *)w2s, pair_gate, (const uint16_t *)H, pairbuf);
+             (const uint8_t *)w2, (const uint8_t *)w2s, pair_gate, (const uint16_t *)H,
+             (const uint8_t *)Hlo, pairbuf);
   };
-  if (B <= 16) go(MxFew{});
-  else if (B <= 32) go(MxMid{});
+  if (B <= 16) go(MxFewDown{});
+  else if (B <= MX_TWO_B) go(MxMidDown{});
   else go(MxMany{});
   return hipGetLastError();
 }
@@ -592,11 +690,11 @@ hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slo
 hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                                   const void *w2, const void *w2s, const SpRec *rec,
                                   const int32_t *pair_of, const float *pair_gate, const void *H,
-                                  const void *residual, void *y, hipStream_t st) {
+                                  const void *Hlo, const void *residual, void *y, hipStream_t st) {
   const int units = mx_kept(B, K, budget) + ns, C = mx_chunks(I);
   const int bytes = B * (K + ns) * 16 * (int)sizeof(float);   // a share's sums
   const int rl = mx_row_loads(B);                             // loads of four rows a step
-  const int ring = MX_CHUNK * rl * 1024;                      // a wavefront's token rows
+  const int ring = MX_CHUNK * (rl + (rl + 1) / 2) * 1024;     // a wavefront's token rows
   const int fit = (MXF_LDS - MXF_SUMS) / ring, waves = fit < MXF_WAVES ? fit : MXF_WAVES;
   int shares = waves / units;
   for (const int most : {C, MXF_SUMS / bytes})
@@ -609,7 +707,7 @@ hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget,
   launch_k(kern, dim3(d / 16), dim3(WAVE * nw), (uint32_t)(shares * bytes + nw * ring), st, d, I, E,
            slots, MxPlan{budget, ns, budget + ns, 0, 1, rec},
            MxFewTail{B, K + ns, shares, pair_of, pair_gate, residual, y}, (const uint8_t *)w2,
-           (const uint8_t *)w2s, (const uint16_t *)H);
+           (const uint8_t *)w2s, (const uint16_t *)H, (const uint8_t *)Hlo);
   return hipGetLastError();
 }
 

@@ -165,6 +165,8 @@ struct alignas(16) SpRec {
 constexpr int MX_NT = 4;
 static_assert(FFN_SPLIT_B <= 16 * MX_NT, "a slot of a small batch is one part");
 inline bool mx_parts(int B) { return B > FFN_SPLIT_B; }
+// up to this many tokens the activations have a second, 8-bit part (ffn_mx.hip)
+constexpr int MX_TWO_B = 32;
 // Few tokens: down and the combine in one launch (k_mx_down_combine), whose
 // workgroups go over every slot.  With one to four tokens (one load of four rows
 // a step) it always wins, with more only while the slots are few; the line is
@@ -356,18 +358,19 @@ hipError_t launch_down(bool bf16, bool packed, int B, int d, int I, int E, int K
                        const int32_t *n_sel, const int32_t *offsets,
                        const FfnHdr *hdr, const FfnUnit *units, const SpRec *rec, int n_cu,
                        const float *pair_gate, const void *H, float *pairbuf, hipStream_t st);
-// the same on 4-bit weights; rec / sptok: see mx_records
+// the same on 4-bit weights; rec / sptok: see mx_records; H and Hlo (up to
+// MX_TWO_B tokens): the activations' bf16 and E5M2 parts, rows of I
 hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, int budget, int slots,
                             int ns, const void *w13, const void *w13s, const SpRec *rec,
-                            const int32_t *sptok, void *H, int n_cu, hipStream_t st);
+                            const int32_t *sptok, void *H, void *Hlo, int n_cu, hipStream_t st);
 hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                           const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
-                          const void *H, float *pairbuf, hipStream_t st);
+                          const void *H, const void *Hlo, float *pairbuf, hipStream_t st);
 // (mx_few) down and the combine: y = residual (or null) + the experts' sum
 hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                                   const void *w2, const void *w2s, const SpRec *rec,
                                   const int32_t *pair_of, const float *pair_gate, const void *H,
-                                  const void *residual, void *y, hipStream_t st);
+                                  const void *Hlo, const void *residual, void *y, hipStream_t st);
 // rows [rows][cols] (row stride ld) to codes [rows][cols / 2] and scales [rows]
 // [cols / 32] and back; experts into the packed 4-bit layout (mx.hpp) from codes
 // and scales or from 16- or 32-bit weights

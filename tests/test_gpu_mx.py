@@ -7,7 +7,10 @@ output are each rounded to bf16 (at most 2^-8 of the value), the fp32 sums of n
 products are off by at most n 2^-24 of the sum of magnitudes; so with A = sum over
 the executed pairs of |gate| |W_d| |h| and P the same with |W_g| |x|, |W_u| |x| for
 h's own sums, |y - y64| <= 2^-8 |y| + 2^-8 A + (d + I + 64) 2^-23 (A + A').  A' bounds
-what the sums' error in g and u does to the output through |silu'| <= 1.1."""
+what the sums' error in g and u does to the output through |silu'| <= 1.1.  Up to 32
+tokens the activation has a second part of E5M2, whose rounding is off by at most
+2^-3 of it, so 2^-3 2^-8 of h where it is in range and nothing more below (2^-16 / 2 /
+2^9 = 2^-26): there 2^-11 A + 2^-26 A0 in the place of 2^-8 A, A0 = sum |gate| |W_d|."""
 import numpy as np
 import pytest
 
@@ -166,7 +169,7 @@ class MxCase:
         x = inp["x"].astype(np.float64)
         B, d, I = x.shape[0], sh.d, sh.I
         y = np.zeros_like(x) if residual is None else residual.astype(np.float64).copy()
-        A, A2 = np.zeros_like(x), np.zeros_like(x)
+        A, A2, A0 = np.zeros_like(x), np.zeros_like(x), np.zeros_like(x)
 
         def add(t, g, b13, b2):
             w13 = W.bf16_bits_to_f32(b13).astype(np.float64)
@@ -177,6 +180,7 @@ class MxCase:
             ag, au = np.abs(x[t]) @ np.abs(w13[:I]).T, np.abs(x[t]) @ np.abs(w13[I:]).T
             y[t] += g[:, None] * (h @ w2.T)
             A[t] += np.abs(g)[:, None] * (np.abs(h) @ np.abs(w2).T)
+            A0[t] += np.abs(g)[:, None] * np.abs(w2).sum(1)[None]
             A2[t] += np.abs(g)[:, None] * ((1.1 * ag * np.abs(uu) + np.abs(s) * au) @ np.abs(w2).T)
 
         for u in range(sh.E):
@@ -190,7 +194,8 @@ class MxCase:
                 g = method.shared_gate64(inp["x"], inp["shared_gate"])
             for i in range(self.ns):
                 add(np.arange(B), np.asarray(g, np.float64).reshape(B), inp["w13_shared"][i], inp["w2_shared"][i])
-        bound = 2.0 ** -8 * np.abs(y) + 2.0 ** -8 * A + (d + I + 64) * 2.0 ** -23 * (A + A2) + 1e-30
+        h_err = 2.0 ** -11 * A + 2.0 ** -26 * A0 if B <= 32 else 2.0 ** -8 * A
+        bound = 2.0 ** -8 * np.abs(y) + h_err + (d + I + 64) * 2.0 ** -23 * (A + A2) + 1e-30
         return y, bound
 
     def check(self, gu, bd, budget, flags=0, with_residual=False, seed=1):
@@ -217,8 +222,10 @@ class MxCase:
         yv = gu.to_np_f32(y[:B]).astype(np.float64)
         over = np.abs(yv - want) - bound
         assert (over <= 0).all(), (float(over.max()), int((over > 0).sum()))
-        # far below the worst case: independent roundings of h and y
-        assert np.linalg.norm(yv - want) <= 2.0 ** -8 * np.linalg.norm(want) + 1e-20
+        # far below the worst case: independent roundings of h (past 32 tokens) and y, each
+        # 2^-8 / sqrt 3 of the value at most in the mean
+        most = 2.0 ** -8 * np.sqrt((1 if B <= 32 else 2) / 3) * 1.1
+        assert np.linalg.norm(yv - want) <= most * np.linalg.norm(want) + 1e-20
         # staged calls: the same bits
         logits, ids, w = gl.route(x, B)
         cost = gl.predict(x, B, ids, w)
