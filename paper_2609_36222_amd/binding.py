@@ -452,8 +452,9 @@ def mx_pack_experts(w13, w2, stream=None):
 
 
 def mx_layer(layer: "Layer", stream=None) -> "Layer":
-    """A W_MXFP4 Layer with a row-major layer's experts quantised, sharing its
-    router and predictor tensors (one-time, on the device)."""
+    """A W_MXFP4 Layer (bf16 activations) with a row-major layer's experts, fp32 or
+    bf16, quantised, sharing its router and predictor tensors (one-time, on the
+    device)."""
     w_router, b_router, pred_a, pred_b, w13, w2 = layer.tensors
     if layer.w_layout != W_ROWMAJOR:
         raise ValueError("row-major experts")

@@ -161,7 +161,9 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc, bool split) {
   } else {
     o.H = take(BK * L->I * 4);
   }
-  o.Hlo = take(mx_layer(L) && B <= MX_TWO_B ? P * (size_t)L->I : 0);   // the activations' 8-bit part
+  // the activations' 8-bit part (of MX_TWO_B tokens for larger batches, which have
+  // none, so that a workspace for a batch holds every smaller one)
+  o.Hlo = take(mx_layer(L) ? (size_t)std::min(B, MX_TWO_B) * (L->K + ns) * L->I : 0);
   // (small batches: gate/up's token lists, one per die, lie here until down
   // writes its rows)
   o.pairbuf = take(P * L->d * 4);

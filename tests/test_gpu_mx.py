@@ -323,6 +323,66 @@ def test_noalloc_is_the_same(gu, bd, B, budget):
     assert torch.equal(y.view(torch.int16), z.view(torch.int16))
 
 
+@pytest.mark.parametrize("B", [3, 30, 90])
+def test_rows_beyond_a_slots_are_not_read(gu, bd, B):
+    """Garbage, NaN among it, in every place of the workspace and of y before the call,
+    and twice in a row on one workspace with a smaller batch between."""
+    c = MxCase(gu, bd, 512, 12, 3, 320, B, 1, True, seed=40)
+    gl, x = c.gl, c.gl.x(c.inp["x"])
+    out = []
+    for fill in (0x00, 0xFF, 0x7F):
+        ws, y = gl.workspace(B, 7), gl.y_like(B)
+        ws.fill_(fill)
+        bd.base_decode_layer(gl.desc, x, B, 7, 0, None, y, ws)
+        small = gl.y_like(2)
+        bd.base_decode_layer(gl.desc, x[:2].contiguous(), 2, 3, 2, None, small, ws)
+        again = gl.y_like(B)
+        bd.base_decode_layer(gl.desc, x, B, 7, 0, None, again, ws)
+        assert torch.equal(y.view(torch.int16), again.view(torch.int16))
+        out.append(y)
+    assert all(torch.equal(out[0].view(torch.int16), o.view(torch.int16)) for o in out[1:])
+
+
+def test_fp32_master_weights(gu, bd):
+    """An fp32 layer's experts quantised: its activations are bf16 from then on."""
+    inp = W.custom_layer(256, 4, 2, 128, 6, bf16=False, seed=3)
+    src = gu.GpuLayer(inp)
+    lay = bd.mx_layer(src.layer)
+    assert lay.torch_dtype == torch.bfloat16
+    c = MxCase.__new__(MxCase)
+    q = lambda a: W.f32_to_bf16_bits(mx.dequantize(*mx.quantize(a.reshape(-1, a.shape[-1]).astype(np.float64)))  # noqa: E731
+                                     .astype(np.float32)).reshape(a.shape)
+    x = rounded(inp["x"], "bf16")
+    c.inp = dict(inp, x=x, w13=q(inp["w13"]), w2=q(inp["w2"]))
+    c.sh, c.ns = inp["shape"], 0
+    desc = lay.desc(2)
+    ws = torch.empty(bd.base_workspace_bytes(desc, 6, 4), dtype=torch.uint8, device="cuda")
+    y = torch.empty(6, 256, dtype=torch.bfloat16, device="cuda")
+    plan = bd.base_decode_layer(desc, to_dev(x, "bf16"), 6, 4, 0, None, y, ws)
+    want, bound = c.outputs64(gu.plan_arrays(plan, ws, 6, 2, 4, 4, True), None)
+    assert (np.abs(gu.to_np_f32(y).astype(np.float64) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("scale", [1e-6, 1e4, 1e18])
+@pytest.mark.parametrize("B", [5, 40])
+def test_small_and_large_activations(gu, bd, B, scale):
+    """Activations below and above the second part's range, to 1e36: nothing is lost
+    but precision, nothing overflows that the values do not."""
+    c = MxCase(gu, bd, 256, 4, 2, 192, B, seed=50)
+    c.inp["x"] = rounded(c.inp["x"] * scale, "bf16")
+    gl, x = c.gl, c.gl.x(c.inp["x"])
+    logits = torch.randn(B, 4, device="cuda")
+    ids = torch.sort(logits, dim=1, descending=True, stable=True).indices[:, :2].int().contiguous()
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    ws, y = gl.workspace(B, 4), gl.y_like(B)
+    plan = bd.base_moe_forward(gl.desc, x, B, logits, ids, i32([0, 1, 2, 3]), i32([4]), i32([0, 1, 2, 3]), 4, 0,
+                               None, y, ws)
+    with np.errstate(over="ignore"):
+        want, bound = c.outputs64(gu.plan_arrays(plan, ws, B, 2, 4, 4, False), None)
+    got = gu.to_np_f32(y).astype(np.float64)
+    assert np.isfinite(got).all() and (np.abs(got - want) <= bound).all()
+
+
 @pytest.mark.parametrize("B,budget", [(1, 4), (48, 12), (200, 10)])
 def test_captured_and_replayed(gu, bd, B, budget):
     """A graph replayed between eager calls with other inputs, on a stream of its own."""

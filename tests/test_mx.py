@@ -79,6 +79,30 @@ def test_workspace_covers_smaller_budgets(lib, B):
     assert n == sorted(n) and n[-1] == n[-2] and n[0] > 0
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(d=256, E=4, K=2, I=64), dict(E=8, K=1, I=14336, n_shared=2,
+                                                                          w13_shared=FAKE, w2_shared=FAKE)])
+def test_workspace_covers_smaller_batches(lib, kw):
+    """A serving program sizes its workspace for its largest batch."""
+    L = layer(**kw, **MXL)
+    for budget in (1, 4, 200):
+        n = [lib.base_workspace_bytes(ctypes.byref(L), B, budget)
+             for B in (1, 2, 4, 5, 8, 9, 16, 17, 31, 32, 33, 48, 63, 64, 65, 66, 100, 128, 500, 1024)]
+        assert n == sorted(n) and n[0] > 0
+
+
+def test_stages(lib):
+    """The launches of a 4-bit layer: the plan of few tokens makes their routes, down's
+    launch their combine (while their slots are few)."""
+    def launched(B, budget, **kw):
+        return bd.layer_stages(layer(**kw, **MXL), B, budget)
+    assert launched(1, 10) == ("scores", "select", "ffn_gateup", "ffn_down")
+    assert launched(4, 128) == ("scores", "select", "ffn_gateup", "ffn_down")
+    assert launched(16, 10) == ("scores", "select", "ffn_gateup", "ffn_down", "combine")
+    assert launched(16, 4) == ("scores", "select", "ffn_gateup", "ffn_down")
+    assert launched(17, 4) == ("scores", "tail", "select", "ffn_gateup", "ffn_down", "combine")
+    assert launched(65, 4) == ("scores", "tail", "select", "compact", "ffn_gateup", "ffn_down", "combine")
+
+
 def test_quantize_refusals(lib):
     def q(dtype=1, src=FAKE, rows=4, cols=64, ld=64, codes=FAKE, scales=FAKE):
         return lib.base_mx_quantize(dtype, src, rows, cols, ld, codes, scales, None)
