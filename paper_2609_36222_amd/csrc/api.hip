@@ -166,7 +166,8 @@ Layout layout(const base_layer *L, int32_t B, int32_t bc, bool split) {
   o.Hlo = take(mx_layer(L) ? (size_t)std::min(B, MX_TWO_B) * (L->K + ns) * L->I : 0);
   // (small batches: gate/up's token lists, one per die, lie here until down
   // writes its rows)
-  o.pairbuf = take(P * L->d * 4);
+  // (and, for 4-bit experts, those of a contraction in shares)
+  o.pairbuf = take((P + (mx_layer(L) ? mx_split_rows(B, L->K, ns, L->d, L->I) : 0)) * L->d * 4);
   // (q [B][E] of the dense scores fits: E <= 256 <= d; ||x||^2 [B] in the
   // activations: B K / 16 tiles of 16 I 2 bytes with I >= 64, or B K I 4 bytes)
   static_assert(MAX_E <= 256, "q in the pair rows' buffer");
@@ -279,11 +280,12 @@ bool few_tokens(const base_layer *L, int32_t B, int32_t bc) {
 }
 
 // gate/up and down of the plan in the workspace (stages 6 and 7), on at most
-// `slots` kept slots; y (few_tokens, else null): y = residual + the sum instead
-// of pair rows
+// `slots` kept slots, `shares` rows a pair; y (few_tokens, else null): y = residual
+// + the sum instead of pair rows
 base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, int32_t slots,
                     const int32_t *sel_ids, const int32_t *n_sel, void *ws, const Layout &o,
-                    hipStream_t st, const void *residual = nullptr, void *y = nullptr) {
+                    hipStream_t st, int shares = 1, const void *residual = nullptr,
+                    void *y = nullptr) {
   const bool bf16 = L->dtype == BASE_BF16, packed = L->w_layout == BASE_W_PACKED;
   const int ns = L->n_shared, n_cu = device_cus();
   const int32_t *offsets = at<int32_t>(ws, o.offsets);
@@ -308,7 +310,7 @@ base_status run_ffn(const base_layer *L, const void *x, int32_t B, int32_t bc, i
                                    at<int32_t>(ws, o.pair_of), pair_gate, H, Hlo, residual, y, st));
   else if (mx_layer(L))
     HIP_TRY(launch_mx_down(B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2, L->w2_shared, rec,
-                           pair_gate, H, Hlo, at<float>(ws, o.pairbuf), st));
+                           pair_gate, H, Hlo, at<float>(ws, o.pairbuf), shares, st));
   else
     HIP_TRY(launch_down(bf16, packed, B, L->d, L->I, L->E, L->K, bc, slots, ns, L->w2,
                         L->w2_shared, sel_ids, n_sel, offsets, hdr, at<FfnUnit>(ws, o.units_dn),
@@ -377,7 +379,7 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
   if (few_tokens(L, B, bc)) {
     // (a block's y lies in the pair rows' place, unused here)
     void *y = tail.norms ? at<void>(ws, o.pairbuf) : tail.y;
-    BASE_TRY(run_ffn(L, x, B, bc, slots, sel_ids, n_sel, ws, o, st, tail.residual, y));
+    BASE_TRY(run_ffn(L, x, B, bc, slots, sel_ids, n_sel, ws, o, st, 1, tail.residual, y));
     stage(8, st);
     if (const base_norms *N = tail.norms)
       HIP_TRY(launch_norm(true, L->d, N->eps, N->res_scale, N->post_gain, N->gate, N->gate_ld,
@@ -386,15 +388,17 @@ base_status run_forward(const base_layer *L, const void *x, int32_t B,
     stage_end(st);
     return BASE_OK;
   }
-  BASE_TRY(run_ffn(L, x, B, bc, slots, sel_ids, n_sel, ws, o, st));
+  const int shares = mx_layer(L) ? mx_down_shares(B, L->K, bc, ns, L->d, L->I) : 1;
+  const size_t stride = (size_t)B * (L->K + ns) * L->d;
+  BASE_TRY(run_ffn(L, x, B, bc, slots, sel_ids, n_sel, ws, o, st, shares));
   stage(8, st);
   if (const base_norms *N = tail.norms)
-    HIP_TRY(launch_combine_norm(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf), N->eps,
-                                N->res_scale, N->post_gain, N->gate, N->gate_ld, N->pre_gain, tail.h,
-                                tail.h_out, tail.x_out, st));
+    HIP_TRY(launch_combine_norm(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf), shares,
+                                stride, N->eps, N->res_scale, N->post_gain, N->gate, N->gate_ld,
+                                N->pre_gain, tail.h, tail.h_out, tail.x_out, st));
   else
-    HIP_TRY(launch_combine(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf),
-                           tail.residual, tail.y, st));
+    HIP_TRY(launch_combine(bf16, B, L->d, L->K + ns, pair_of, at<float>(ws, o.pairbuf), shares,
+                           stride, tail.residual, tail.y, st));
   stage_end(st);
   return BASE_OK;
 }

@@ -872,8 +872,8 @@ constexpr int CB_GROUP = 4;   // ranks whose rows are in flight together
 template <bool BF16>
 __global__ __launch_bounds__(CB_THREADS)
 void k_combine(int B, int d, int kc, const int32_t *__restrict__ pair_of,
-               const float *__restrict__ pairbuf, const void *__restrict__ res,
-               void *__restrict__ y) {
+               const float *__restrict__ pairbuf, int shares, size_t stride,
+               const void *__restrict__ res, void *__restrict__ y) {
   const int t = blockIdx.x;
   const int c = (blockIdx.y * CB_THREADS + threadIdx.x) * 4;
   if (t >= B || c >= d) return;
@@ -896,6 +896,11 @@ void k_combine(int B, int d, int kc, const int32_t *__restrict__ pair_of,
 #pragma unroll
     for (int i = 0; i < CB_GROUP; ++i) {
       if (p[i] < 0) continue;   // a routed rank the token does not execute
+      for (int s = 1; s < shares; ++s) {   // a contraction in shares: their rows in order
+        const float4 o = *reinterpret_cast<const float4 *>(pairbuf + s * stride + (size_t)p[i] * d + c);
+        v[i].x = v[i].x + o.x; v[i].y = v[i].y + o.y;
+        v[i].z = v[i].z + o.z; v[i].w = v[i].w + o.w;
+      }
       acc[0] = acc[0] + v[i].x; acc[1] = acc[1] + v[i].y;
       acc[2] = acc[2] + v[i].z; acc[3] = acc[3] + v[i].w;
     }
@@ -983,15 +988,15 @@ hipError_t launch_down(bool bf16, bool packed, int B, int d, int I, int E, int K
 }
 
 hipError_t launch_combine(bool bf16, int B, int d, int kc,
-                          const int32_t *pair_of, const float *pairbuf,
+                          const int32_t *pair_of, const float *pairbuf, int shares, size_t stride,
                           const void *residual, void *y, hipStream_t st) {
   dim3 grid(B, (d + CB_THREADS * 4 - 1) / (CB_THREADS * 4));
   if (bf16)
     launch_k(k_combine<true>, grid, dim3(CB_THREADS), 0, st, B, d, kc,
-                       pair_of, pairbuf, residual, y);
+                       pair_of, pairbuf, shares, stride, residual, y);
   else
     launch_k(k_combine<false>, grid, dim3(CB_THREADS), 0, st, B, d, kc,
-                       pair_of, pairbuf, residual, y);
+                       pair_of, pairbuf, shares, stride, residual, y);
   return hipGetLastError();
 }
 

@@ -50,25 +50,27 @@ struct MxShape {
 // on die b % N_XCD; the row groups of slot `ord` are numbered on from the previous
 // slot's and number v lies on die v % N_XCD, so that all parts of a slot read a
 // row group's weights through one L2 and every die has its share of every slot.
-// `cuts` workgroups share a record's token tiles.
+// `cuts` workgroups share a record's token tiles, `shares` its contraction.
 struct MxPlan {
-  int budget, ns, nrec, parts, cuts;
+  int budget, ns, nrec, parts, cuts, shares;
   const SpRec *rec;
 };
 struct MxWork {
-  int u, p0, n, rg, c0;
+  int u, p0, n, rg, c0, share;
 };
+template <bool SPLIT = false>
 __device__ __forceinline__ MxWork mx_work(const MxPlan &pl, int RG, int NT) {
   const int die = blockIdx.x % N_XCD, q = blockIdx.x / N_XCD;
-  const int per = ((RG + N_XCD - 1) / N_XCD) * pl.cuts;
-  const int y = q / per, z = q - y * per, k = z / pl.cuts;
+  const int shares = SPLIT ? pl.shares : 1, per = ((RG + N_XCD - 1) / N_XCD) * pl.cuts * shares;
+  const int y = q / per, zs = q - y * per, z = zs / shares, k = z / pl.cuts;
   // slots: the shared experts first, they run for every token
   const int i = pl.parts ? y : (y < pl.ns ? pl.budget + y : y - pl.ns);
   const SpRec r = pl.rec[die * pl.nrec + i];
   const int ord = pl.parts ? __builtin_amdgcn_readfirstlane(r.pad) : y;
   const int rg = ((die - ord * RG) & (N_XCD - 1)) + N_XCD * k;
   return {__builtin_amdgcn_readfirstlane(r.u), __builtin_amdgcn_readfirstlane(r.p0),
-          rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg, (z - k * pl.cuts) * 16 * NT};
+          rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg, (z - k * pl.cuts) * 16 * NT,
+          zs - z * shares};
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -143,15 +145,21 @@ __host__ __device__ inline int mx_groups(int tiles, int group) { return (tiles +
 //  * Order of the loads: in step s the tokens of step s + DT and the weights of step
 //    s + DT + 1, so that the wait for a step's tokens covers its weights and leaves
 //    those of the DT steps after it in flight.
-template <typename M, int N, typename Rows>
+template <typename M, int N, bool SPLIT = false, typename Rows>
 __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, int K, rsrc_t rx,
-                                          rsrc_t rlo, Rows rows, f32x4 (&acc)[M::T][N]) {
+                                          rsrc_t rlo, Rows rows, f32x4 (&acc)[M::T][N],
+                                          int share = 0, int shares = 1) {
   constexpr int T = M::T, DT = M::DT, L = (4 * N + M::RW - 1) / M::RW;   // loads of four rows
   static_assert(L * M::RW <= 4 * M::NT, "token loads stay in their slot");
   const int w = wave_id_u(), lane = lane_id(), kq = w / M::RW, rw = w % M::RW;
   uint8_t *ring = lds + kq * (M::RING * M::SLOT);
-  const int S = mx_steps(K), s0 = kq * S / M::KW, s1 = (kq + 1) * S / M::KW;
-  const int most = (S + M::KW - 1) / M::KW;   // steps of the longest share
+  // this wavefront's steps [s0, s1) and those of the longest share: the KW rows', or
+  // (SPLIT) the workgroup's among `shares` of them, in whole chunks
+  static_assert(!SPLIT || M::KW == 1, "one way to share a contraction");
+  const int S = mx_steps(K), C = mx_chunks(K);
+  const int s0 = SPLIT ? share * C / shares * MX_CHUNK : kq * S / M::KW;
+  const int s1 = SPLIT ? min((share + 1) * C / shares * MX_CHUNK, S) : (kq + 1) * S / M::KW;
+  const int most = SPLIT ? s1 - s0 : (S + M::KW - 1) / M::KW;
   const uint32_t Kb = (uint32_t)K * 2u;
   // the rows this lane stages: of the step's 4 N quarter tiles (four rows each) the
   // RW wavefronts take one after another in turn; lane l row l / 16 of the quarter,
@@ -374,14 +382,14 @@ void k_mx_gateup(int d, int I, int E, MxPlan pl, int np, const uint8_t *__restri
   }
 }
 
-template <typename M>
+template <typename M, bool SPLIT>
 __global__ __launch_bounds__(M::THREADS, M::WPE)
 void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
                const uint8_t *__restrict__ w2s, const float *__restrict__ pair_gate,
                const uint16_t *__restrict__ H, const uint8_t *__restrict__ Hlo,
-               float *__restrict__ pairbuf) {
+               float *__restrict__ pairbuf, size_t stride) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
-  const MxWork k = mx_work(pl, mx_groups(d / 16, M::GROUP), M::NT);
+  const MxWork k = mx_work<SPLIT>(pl, mx_groups(d / 16, M::GROUP), M::NT);
   const size_t eb = (size_t)(d / 16) * mx_tile_bytes(I);
   const uint8_t *w2 = k.u < E ? w2r + (size_t)k.u * eb : w2s + (size_t)(k.u - E) * eb;
   const int lane = lane_id();
@@ -389,7 +397,7 @@ void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
     const int n = min(k.n - c, 16 * M::NT), p0 = k.p0 + c;
     const rsrc_t rx = make_rsrc(H + (size_t)p0 * I, (uint32_t)n * (uint32_t)I * 2u);
     const rsrc_t rlo = M::LO ? make_rsrc(Hlo + (size_t)p0 * I, (uint32_t)n * (uint32_t)I) : rx;
-    float *out0 = pairbuf + (size_t)p0 * d;
+    float *out0 = pairbuf + (SPLIT ? k.share * stride : 0) + (size_t)p0 * d;
     if (c > k.c0) wg_barrier();
     sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
       constexpr int N = decltype(NC)::value;
@@ -398,9 +406,9 @@ void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
 #pragma unroll
       for (int j = 0; j < N; ++j) gt[j] = pair_gate[p0 + min(16 * j + (lane & 15), n - 1)];
       f32x4 acc[M::T][N];
-      mx_stream<M, N>(lds, m, I, rx, rlo, [&](int i) {
+      mx_stream<M, N, SPLIT>(lds, m, I, rx, rlo, [&](int i) {
         return i < n ? (uint32_t)i * (uint32_t)I * 2u : FFN_TOK_PAD;
-      }, acc);
+      }, acc, k.share, pl.shares);
       if (!m.active) return;
       mx_emit<M, N, 1>(lds, acc, [&](int t, int j, const f32x4 (&v)[1]) {
         const int p = 16 * j + (lane & 15);
@@ -630,9 +638,10 @@ int mx_workgroups(int B, int K, int budget, int ns, int groups) {
   return (kept + ns > full ? kept + ns : full) * groups;
 }
 
-// workgroups: records times row groups (the same number on every die) times cuts
-dim3 mx_grid(int recs, int RG, int cuts) {
-  return dim3((unsigned)(N_XCD * recs * ((RG + N_XCD - 1) / N_XCD) * cuts));
+// workgroups: records times row groups (the same number on every die) times what
+// shares one
+dim3 mx_grid(int recs, int RG, int by) {
+  return dim3((unsigned)(N_XCD * recs * ((RG + N_XCD - 1) / N_XCD) * by));
 }
 // workgroups that share a record's tiles: what a record can hold over what one takes
 int mx_cuts(int B, int NT) {
@@ -650,7 +659,7 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
     using M = decltype(shape);
     const int cuts = mx_cuts(B, M::NT);
     launch_k(k_mx_gateup<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(I / 8, M::GROUP), cuts),
-             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, rec},
+             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, 1, rec},
              B * (K + ns), (const uint8_t *)w13, (const uint8_t *)w13s, sptok, (const uint16_t *)x,
              B, (uint16_t *)H, (uint8_t *)Hlo);
   };
@@ -670,16 +679,20 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
 
 hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                           const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
-                          const void *H, const void *Hlo, float *pairbuf, hipStream_t st) {
+                          const void *H, const void *Hlo, float *pairbuf, int shares,
+                          hipStream_t st) {
   const bool parts = mx_parts(B);
   const int nrec = mx_records(B, K, budget, ns);
   auto go = [&](auto shape) {
     using M = decltype(shape);
     const int cuts = mx_cuts(B, M::NT);
-    launch_k(k_mx_down<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(d / 16, M::GROUP), cuts),
-             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, rec},
-             (const uint8_t *)w2, (const uint8_t *)w2s, pair_gate, (const uint16_t *)H,
-             (const uint8_t *)Hlo, pairbuf);
+    static_assert(M::GROUP == MX_DOWN_GROUP && M::KW == 1, "mx_down_shares");
+    launch_k(shares > 1 ? k_mx_down<M, true> : k_mx_down<M, false>,
+             mx_grid(parts ? nrec : slots + ns, mx_groups(d / 16, M::GROUP), cuts * shares),
+             dim3(M::THREADS), 0, st, d, I, E,
+             MxPlan{budget, ns, nrec, (int)parts, cuts, shares, rec}, (const uint8_t *)w2,
+             (const uint8_t *)w2s, pair_gate, (const uint16_t *)H, (const uint8_t *)Hlo, pairbuf,
+             (size_t)B * (K + ns) * d);
   };
   if (B <= 16) go(MxFewDown{});
   else if (B <= MX_TWO_B) go(MxMidDown{});
@@ -705,7 +718,7 @@ hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget,
                     : rl == 2 ? k_mx_down_combine<2>
                               : k_mx_down_combine<4>;
   launch_k(kern, dim3(d / 16), dim3(WAVE * nw), (uint32_t)(shares * bytes + nw * ring), st, d, I, E,
-           slots, MxPlan{budget, ns, budget + ns, 0, 1, rec},
+           slots, MxPlan{budget, ns, budget + ns, 0, 1, 1, rec},
            MxFewTail{B, K + ns, shares, pair_of, pair_gate, residual, y}, (const uint8_t *)w2,
            (const uint8_t *)w2s, (const uint16_t *)H, (const uint8_t *)Hlo);
   return hipGetLastError();

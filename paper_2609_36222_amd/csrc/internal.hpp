@@ -189,6 +189,36 @@ inline int mx_records(int B, int K, int budget, int ns) {
   return (ffn_max_tiles(B, K, budget, ns) + (MX_NT - 1) * (budget + ns)) / MX_NT;
 }
 
+// Workgroups that share the contraction of one (record, row group) of down, each
+// writing pair rows of its own, which the combine adds in their order.  A share
+// saves a part of the steps of 128 (0.26 us each between one share and four) and
+// costs a write and a read of every pair row (1 us per 10^5 values), so: at least
+// MX_SPLIT_STEPS steps, at most MX_SPLIT_VALUES values in the pair rows per step,
+// and at most MX_SPLIT_UNITS (record, row group) pairs, half of the 256 compute
+// units, counted from the slots and full parts.  Whole layers, 8 experts top-2,
+// without shares -> with four: d = 4096, I = 14336, B = 64, 2 kept 117.7 -> 83.1 us,
+// 4 kept 129.1 -> 111.1; d = 2048, I = 4096, B = 24, 8 kept 51.9 -> 46.8; and beyond
+// the lines d = 6144, I = 8192, B = 128, 4 kept (192 pairs) 129.7 -> 134.0; d = I =
+// 4096, B = 128, 4 kept (too many values) 71.2 -> 73.7; d = I = 2048, B = 64, 8 kept
+// (few steps) 40.0 -> 41.1.  Six shares at d = I = 4096: 71 -> 81.
+constexpr int MX_DOWN_GROUP = 8, MX_SPLIT_UNITS = 128, MX_SPLIT_STEPS = 32, MX_SPLIT_MOST = 4;
+constexpr long long MX_SPLIT_VALUES = 24576;
+inline long long mx_split_values(int I) {   // 0: the contraction is not shared
+  const int steps = (I + 127) / 128;
+  return steps < MX_SPLIT_STEPS ? 0 : MX_SPLIT_VALUES * steps;
+}
+inline int mx_down_shares(int B, int K, int budget, int ns, int d, int I) {
+  const long long P = (long long)B * (K + ns), kept = mx_kept(B, K, budget) + ns;
+  const long long full = P / (16 * MX_NT);
+  const long long units = (kept > full ? kept : full) * (d / 16 / MX_DOWN_GROUP);
+  return units <= MX_SPLIT_UNITS && P * d <= mx_split_values(I) ? MX_SPLIT_MOST : 1;
+}
+// pair rows beyond the batch's own that a batch of this size or a smaller one may need
+inline size_t mx_split_rows(int B, int K, int ns, int d, int I) {
+  const size_t P = (size_t)B * (K + ns), most = (size_t)(mx_split_values(I) / d);
+  return (MX_SPLIT_MOST - 1) * (P < most ? P : most);
+}
+
 // A unit: expert u (u >= E: shared expert u - E), the part's first 16-pair
 // tile, its tile count, its first pair in the compacted order and its pair
 // count, and the unit's row group (gate/up: hdr.rp_gu row-pair tiles;
@@ -365,7 +395,8 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
                             const int32_t *sptok, void *H, void *Hlo, int n_cu, hipStream_t st);
 hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                           const void *w2, const void *w2s, const SpRec *rec, const float *pair_gate,
-                          const void *H, const void *Hlo, float *pairbuf, hipStream_t st);
+                          const void *H, const void *Hlo, float *pairbuf, int shares,
+                          hipStream_t st);   // shares: 1 or mx_down_shares
 // (mx_few) down and the combine: y = residual (or null) + the experts' sum
 hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget, int slots, int ns,
                                   const void *w2, const void *w2s, const SpRec *rec,
@@ -384,8 +415,9 @@ hipError_t launch_mx_pack(const uint8_t *w13c, const uint8_t *w13s, const uint8_
 hipError_t launch_mx_quantize_experts(bool bf16, const void *w13, const void *w2, int E, int d,
                                       int I, void *w13m, void *w2m, hipStream_t st);
 // kc: columns of pair_of (K routed + the shared experts)
+// (both combines: a pair's row is the sum of `shares` rows, `stride` floats apart)
 hipError_t launch_combine(bool bf16, int B, int d, int kc,
-                          const int32_t *pair_of, const float *pairbuf,
+                          const int32_t *pair_of, const float *pairbuf, int shares, size_t stride,
                           const void *residual, void *y, hipStream_t st);
 
 // h' = scale h + gate (post n(y)), x' = pre n(h') (norm.hip): rows of d elements
@@ -397,9 +429,10 @@ hipError_t launch_norm(bool bf16, int d, float eps, float scale, const float *po
                        void *xo, long long xo_ld, int n_cu, hipStream_t st);
 // the combine (no residual) and the same on its output; rows of h, ho, xo d apart
 hipError_t launch_combine_norm(bool bf16, int B, int d, int kc, const int32_t *pair_of,
-                               const float *pairbuf, float eps, float scale, const float *post,
-                               const float *gate, long long gate_ld, const float *pre, const void *h,
-                               void *ho, void *xo, hipStream_t st);
+                               const float *pairbuf, int shares, size_t stride, float eps,
+                               float scale, const float *post, const float *gate,
+                               long long gate_ld, const float *pre, const void *h, void *ho,
+                               void *xo, hipStream_t st);
 
 // Calibration statistics (per expert u): head[u] = (n, sum y, sum y^2, 0)
 // fp64, sz[u][d] and q[u][d] fp64, G[u][d][d] fp32; each array 256-byte

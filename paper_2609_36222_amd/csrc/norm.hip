@@ -208,7 +208,8 @@ void k_norm(NormArgs a, long long rows, const T *y, long long y_ld, const T *h, 
 template <typename T, int EPT, bool WG>
 __global__ __launch_bounds__(WG ? 1024 : WAVE)
 void k_combine_norm(NormArgs a, int kc, const int32_t *__restrict__ pair_of,
-                    const float *__restrict__ pairbuf, const T *h, T *ho, T *xo) {
+                    const float *__restrict__ pairbuf, int shares, size_t stride, const T *h, T *ho,
+                    T *xo) {
   __shared__ float red[WG ? 32 : 1];
   constexpr int GROUP = 4;   // ranks whose rows are in flight together
   NormRow<T, EPT, WG> n;
@@ -229,6 +230,12 @@ void k_combine_norm(NormArgs a, int kc, const int32_t *__restrict__ pair_of,
       if (p[g] < 0) continue;   // a routed rank the token does not execute
       float o[EPT];
       n.load(pairbuf + (size_t)p[g] * d, d, o);
+      for (int q = 1; q < shares; ++q) {   // a contraction in shares: their rows in order
+        float e[EPT];
+        n.load(pairbuf + q * stride + (size_t)p[g] * d, d, e);
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) o[i] = o[i] + e[i];
+      }
 #pragma unroll
       for (int i = 0; i < EPT; ++i) s[i] = s[i] + o[i];
     }
@@ -267,14 +274,15 @@ hipError_t launch_norm(bool bf16, int d, float eps, float scale, const float *po
 }
 
 hipError_t launch_combine_norm(bool bf16, int B, int d, int kc, const int32_t *pair_of,
-                               const float *pairbuf, float eps, float scale, const float *post,
-                               const float *gate, long long gate_ld, const float *pre, const void *h,
-                               void *ho, void *xo, hipStream_t st) {
+                               const float *pairbuf, int shares, size_t stride, float eps,
+                               float scale, const float *post, const float *gate,
+                               long long gate_ld, const float *pre, const void *h, void *ho,
+                               void *xo, hipStream_t st) {
   const NormArgs a{d, eps, scale, post, gate, pre, gate_ld};
   const int threads = norm_threads(d);
 #define BASE_CN(T, EPT, WG)                                                                      \
   launch_k(k_combine_norm<T, EPT, WG>, dim3(B), dim3(threads), 0, st, a, kc, pair_of, pairbuf,   \
-           (const T *)h, (T *)ho, (T *)xo)
+           shares, stride, (const T *)h, (T *)ho, (T *)xo)
 #define BASE_CN_T(T)                                                                             \
   do {                                                                                           \
     if (threads > WAVE) { if (norm_ept(d) == 8) BASE_CN(T, 8, true); else BASE_CN(T, 16, true); } \

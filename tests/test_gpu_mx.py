@@ -296,6 +296,24 @@ def test_long_contraction(gu, bd):
     MxCase(gu, bd, 4096, 3, 2, 4160, 7, seed=2).check(gu, bd, 2)
 
 
+@pytest.mark.parametrize("E,K,I,B,budget,ns", [(2, 1, 4096, 17, 2, 0), (3, 2, 4160, 40, 3, 0), (2, 2, 4416, 70, 2, 1),
+                                               (1, 1, 4096, 300, 1, 0), (16, 8, 3968, 12, 16, 0),
+                                               (16, 8, 4096, 12, 16, 0)])
+def test_contraction_in_shares(gu, bd, E, K, I, B, budget, ns):
+    """Few slots of long contractions: down's workgroups share one, with a last share
+    that ends inside a chunk; the shapes on both sides of the line."""
+    c = MxCase(gu, bd, 256, E, K, I, B, ns, seed=60 + B)
+    c.check(gu, bd, budget, 0, True)
+    gl, x = c.gl, c.gl.x(c.inp["x"])
+    n = bd.Norms(256, torch.bfloat16, torch.ones(256, device="cuda"), None, torch.ones(256, device="cuda"), 0.5)
+    ws, y, h = gl.workspace(B, budget), gl.y_like(B), torch.randn(B, 256, device="cuda").bfloat16()
+    bd.base_decode_layer(gl.desc, x, B, budget, 0, None, y, ws)
+    want, got = (torch.empty_like(h), torch.empty_like(h)), (torch.empty_like(h), torch.empty_like(h))
+    bd.base_norm_residual(n, y, h, *want)
+    bd.base_decode_block(gl.desc, n, x, B, budget, 0, h, ws, *got)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 @pytest.mark.parametrize("B", [4, 40, 100])
 def test_an_expert_twice_among_a_tokens_routes(gu, bd, B):
     """Routes the router never makes: a slot then has more pairs than tokens."""
