@@ -125,7 +125,9 @@ enum {
      * row), in the layout base_mx_pack_experts or base_mx_quantize_experts
      * writes: base_mx_w13_bytes and base_mx_w2_bytes bytes.  x, y and the
      * products' sums are those of a bf16 layer (dtype BASE_BF16) whose weights
-     * have these values. */
+     * have these values; the activation between the two products is bf16, up to
+     * 32 tokens with an 8-bit part beside it that makes its rounding 8 times
+     * smaller. */
     BASE_W_MXFP4 = 4
 };
 
@@ -294,7 +296,8 @@ typedef struct base_norms {
 #define BASE_NORM_MAX_D 16384
 #define BASE_NORM_MAX_ROWS 0x7FFFFFFFLL
 
-/*   y      the block's output, or NULL: h' = h (the norm before the first block;
+/*   rows   1 .. BASE_NORM_MAX_ROWS
+ *   y      the block's output, or NULL: h' = h (the norm before the first block;
  *          res_scale, gate and post_gain are not read, and h_out must be NULL)
  *   h      the residual stream
  *   h_out  h', or NULL;  x_out  x', or NULL (not both)
@@ -308,9 +311,10 @@ base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y,
                                const void *h, int64_t h_ld, void *h_out, int64_t h_out_ld,
                                void *x_out, int64_t x_out_ld, void *stream);
 
-/* A decode block's tail in the layer's last launch: base_decode_layer without
- * a residual, then base_norm_residual on its output y and the residual stream h,
- * bit for bit, without y in memory.  h, h_out, x_out: [B][d], rows d elements
+/* A decode block's tail: base_decode_layer without a residual, then
+ * base_norm_residual on its output y and the residual stream h, bit for bit, in
+ * the layer's last launch (where a 4-bit layer's few tokens are combined by down's
+ * launch: in one after it, with y in the workspace).  h, h_out, x_out: [B][d], rows d elements
  * apart, 16-B aligned, as are the gains and the gate (gate_ld a multiple of 4);
  * h_out may be h, and x_out may be x (the layer's input, read before).  N->d and
  * N->dtype are the layer's. */
