@@ -869,7 +869,10 @@ void k_down_f32(int d, int I, int E, const float *__restrict__ w2,
 constexpr int CB_THREADS = 256;
 constexpr int CB_GROUP = 4;   // ranks whose rows are in flight together
 
-template <bool BF16>
+// SPLIT: a pair's row is the sum of `shares` rows `stride` apart, added in their
+// order (4-bit layers' long contractions; in one instance for all, the loop over one
+// share cost 16 tokens' launch 3.4 -> 4.5 us)
+template <bool BF16, bool SPLIT = false>
 __global__ __launch_bounds__(CB_THREADS)
 void k_combine(int B, int d, int kc, const int32_t *__restrict__ pair_of,
                const float *__restrict__ pairbuf, int shares, size_t stride,
@@ -896,7 +899,7 @@ void k_combine(int B, int d, int kc, const int32_t *__restrict__ pair_of,
 #pragma unroll
     for (int i = 0; i < CB_GROUP; ++i) {
       if (p[i] < 0) continue;   // a routed rank the token does not execute
-      for (int s = 1; s < shares; ++s) {   // a contraction in shares: their rows in order
+      for (int s = 1; SPLIT && s < shares; ++s) {
         const float4 o = *reinterpret_cast<const float4 *>(pairbuf + s * stride + (size_t)p[i] * d + c);
         v[i].x = v[i].x + o.x; v[i].y = v[i].y + o.y;
         v[i].z = v[i].z + o.z; v[i].w = v[i].w + o.w;
@@ -992,7 +995,7 @@ hipError_t launch_combine(bool bf16, int B, int d, int kc,
                           const void *residual, void *y, hipStream_t st) {
   dim3 grid(B, (d + CB_THREADS * 4 - 1) / (CB_THREADS * 4));
   if (bf16)
-    launch_k(k_combine<true>, grid, dim3(CB_THREADS), 0, st, B, d, kc,
+    launch_k(shares > 1 ? k_combine<true, true> : k_combine<true>, grid, dim3(CB_THREADS), 0, st, B, d, kc,
                        pair_of, pairbuf, shares, stride, residual, y);
   else
     launch_k(k_combine<false>, grid, dim3(CB_THREADS), 0, st, B, d, kc,
