@@ -21,6 +21,15 @@
 // one writer and one order.  Weights come to registers (16 bytes a lane: four
 // operands and one scale, see mx.hpp) DT + 1 steps of 128 ahead, the token rows
 // of up to NT tiles to an LDS ring of DT + 1 steps that the RW wavefronts share.
+//
+// What bounds it.  Few tokens: latency.  B = 1, 8 Qwen3-shaped slots, 13 MB of gate and
+// up weights in 7.0 us, six steps of loads behind the launch, the records and the
+// token list.  Beyond 32 tokens: the matrix pipe, the conversions in front of it and the
+// token rows' way through LDS, in turn rather than at once.  B = 256, 32 slots:
+// gate/up 24.4 us (530 TFLOP/s, 2.2 TB/s of weights), without its products 13.9,
+// without either kind of loads 21; down 17.7, 4.5 of it the fp32 pair rows'
+// stores.  Mixtral-shaped, B = 128, 4 slots: gate/up 83 to 91 (660 to 720 TFLOP/s),
+// without products 21.6, without loads 64; down 52.
 #include "common.hpp"
 #include "ffn.hpp"
 #include "internal.hpp"

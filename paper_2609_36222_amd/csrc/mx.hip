@@ -13,7 +13,10 @@
 // The conversions are the gfx950 scale-converts (v_cvt_scalef32_*_fp4), whose
 // scale operand is the float with the byte as its exponent field (0: 2^-127,
 // 255: NaN); checked over every code and scale byte.  These kernels are streams:
-// 16 bytes in or out per lane and access.
+// 16 bytes in or out per lane and access.  A Qwen3-shaped layer's gate and up
+// weights (196,608 rows of 2048 bf16, 1.02 GB moved) take 214 us to quantise (4.8
+// TB/s) and 160 to read back (6.4 TB/s), one expert's 3.8 us either way, of which
+// its 8 MB are 1.6 and the rest is the launch and the first loads.
 #include "common.hpp"
 #include "internal.hpp"
 #include "mx.hpp"

@@ -1376,7 +1376,8 @@ void k_plan_split(int B, int K, int E, int budget, int ns, int binary, int flags
 // ranked as a whole: its routes are K successive wavefront maxima of the (logit,
 // index) keys, lane r mod 64 holding expert r, and its executed experts K more over
 // the kept ones -- a counting rank of E keys a token, as in k_tail, would take 16
-// wavefronts of one CU several times as long.  One workgroup per die, each
+// wavefronts of one CU several times as long (Qwen3-shaped, B = 1: 6.8 us for this
+// launch, 3.8 + 6.0 for the two it replaces).  One workgroup per die, each
 // making the whole plan and writing its die's records; workgroup 0 writes the plan.
 struct FewScores {   // the dense scoring's outputs and the predictor's intercepts
   const float *logits, *q, *ss, *pb, *gdot;
@@ -1771,7 +1772,8 @@ void k_plan_few(int B, int K, int E, int budget, int ns, int flags, FewScores sc
 // ones, as in k_plan_few, and a pair's place its slot's offset plus the tokens
 // before it, which needs a token's experts to be distinct -- they are, except among
 // the dropped routes of a caller's own making, so that the drop rule keeps the two
-// launches.  (Two launches 4.4 and 4.3 us at B = 16, 4.6 and 5.0 at B = 61.)
+// launches.  (5.1 us at B = 16 and 7.9 at B = 61; the two launches 4.4 + 4.3 and 4.6 +
+// 5.0.)
 template <int NCH, int TPW>
 __global__ __launch_bounds__(PF_WAVES * WAVE)
 void k_plan_given(int B, int K, int E, int budget, int ns, int norm_topk, int renorm,
