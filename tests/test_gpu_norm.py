@@ -143,6 +143,18 @@ def test_strides_and_alignment(bd, dtype, d, pad, off):
     run(bd, 7, d, dtype, pad=pad, off=off)
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+@pytest.mark.parametrize("d,rows", [(3, 40), (5, 7), (9, 33), (87, 515), (126, 3), (128, 21), (129, 301), (200, 3), (255, 1001),
+                                    (256, 9), (257, 65), (511, 6), (1023, 700), (1029, 801), (1501, 600), (5003, 300),
+                                    (8191, 5), (8193, 5)])
+@pytest.mark.parametrize("post", [True, False])
+def test_rows_that_share_wavefronts_or_overlap_their_pieces(bd, dtype, d, rows, post):
+    """Lengths on both sides of each line and off the pieces' size, apart and in place,
+    with row counts that leave a wavefront's last rows empty."""
+    for inplace in ("", "h", "y", "hy"):
+        run(bd, rows, d, dtype, post=post, gate="token", inplace=inplace)
+
+
 @pytest.mark.parametrize("inplace", ["h", "y", "hy"])
 @pytest.mark.parametrize("d,pad", [(512, 0), (2048, 16), (4099, 0)])
 def test_in_place(bd, inplace, d, pad):
