@@ -46,6 +46,12 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
   u += 0x7FFFu + ((u >> 16) & 1u);
   return (uint16_t)(u >> 16);
 }
+// the same of any value: NaN stays NaN (the sum above carries out of one whose bits
+// are all ones, which is what memory filled with 0xFF holds, and makes it a zero).
+// The gfx950 conversion; it and f32_to_bf16 agree on all floats that are not NaN.
+__device__ __forceinline__ uint16_t f32_to_bf16_any(float f) {
+  return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
 
 // Four consecutive activations as fp32 (exact widening for bf16).
 __device__ __forceinline__ void load4(const float *p, float v[4]) {

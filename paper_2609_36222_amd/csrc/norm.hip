@@ -112,12 +112,12 @@ __device__ __forceinline__ void norm_store(uint16_t *p, int left, const float *v
     u32x4 q;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      q[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
+      q[i] = (uint32_t)f32_to_bf16_any(v[2 * i]) | ((uint32_t)f32_to_bf16_any(v[2 * i + 1]) << 16);
     reinterpret_cast<Any16H *>(p)->v = q;
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (e < left) p[e] = f32_to_bf16(v[e]);
+      if (e < left) p[e] = f32_to_bf16_any(v[e]);
   }
 }
 

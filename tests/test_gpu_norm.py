@@ -181,6 +181,31 @@ def test_nan_and_infinity_stay_in_their_rows(bd, d):
     assert torch.isnan(xo[1]).all() and torch.isnan(ho[2]).all() and torch.isfinite(xo[[0, 3, 4, 5]]).all()
 
 
+@pytest.mark.parametrize("bits", [0xFFFFFFFF, 0x7FFFFFFF, 0x7F800001], ids=hex)
+@pytest.mark.parametrize("d", [87, 128, 513, 2048, 5001])
+def test_every_nan_of_a_gate_or_gain_reaches_bf16_rows(bd, d, bits):
+    """NaNs whose bits are all ones (memory filled with 0xFF), where an integer
+    rounding carries into a zero: h' and x' are NaN where the formula is."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    h, y = r(5, d).bfloat16(), r(5, d).bfloat16()
+    bad = torch.tensor([bits], dtype=torch.int64).to(torch.int32).view(torch.float32).cuda()
+    def call(which, at):
+        w = dict(post_gain=1 + 0.1 * r(d), gate=r(5, d), pre_gain=1 + 0.1 * r(d))
+        w[which].view(-1, d)[-1, at] = bad[0]
+        assert torch.isnan(w[which]).any()
+        return bd.norm_residual(h, y, **w)
+    for at in (0, d - 1):
+        ho, xo = call("gate", at)            # the last row's gate
+        assert torch.isnan(ho[4, at]) and int(torch.isnan(ho).sum()) == 1
+        assert torch.isnan(xo[4]).all() and int(torch.isnan(xo).sum()) == d
+        ho, xo = call("post_gain", at)
+        assert torch.isnan(ho[:, at]).all() and int(torch.isnan(ho).sum()) == 5 and torch.isnan(xo).all()
+        ho, xo = call("pre_gain", at)
+        assert torch.isfinite(ho).all() and torch.isnan(xo[:, at]).all() and int(torch.isnan(xo).sum()) == 5
+
+
 def test_small_and_large_values(bd):
     """Squares near both ends of fp32."""
     for f in (1e-15, 1e15):
