@@ -224,14 +224,22 @@ class Layer:
     def mxfp4(cls, w_router, b_router, pred_a, pred_b, w13, w2, I: int, norm_topk: int = 1,
               score_rule: int = 0, shared=None):
         """A layer of 4-bit experts: w13, w2 (and the shared ones) are the byte
-        tensors base_mx_pack_experts / base_mx_quantize_experts wrote; shared:
+        tensors base_mx_pack_experts / base_mx_quantize_experts wrote, whose
+        lengths have to be those of the router's experts and I; shared:
         (w13_shared, w2_shared, gate or None, how many)."""
         import torch
+        E, d = w_router.shape
+        _mx_bytes("w13, w2", w13, w2, E, d, I, w_router)
+        if shared is not None and shared[3] != 0:
+            _mx_bytes("shared w13, w2", *shared[:2], shared[3], d, I, w_router)
+            gate = shared[2]
+            if gate is not None and (gate.dtype is not torch.float32 or gate.shape != (d,)
+                                     or not gate.is_contiguous()):
+                raise ValueError(f"shared gate: fp32, {d} adjacent elements")
         self = cls.__new__(cls)
         self.tensors = (w_router, b_router, pred_a, pred_b, w13, w2)
         self.dtype, self.torch_dtype = BASE_BF16, torch.bfloat16
-        self.E, self.d = w_router.shape
-        self.I, self.K = I, None
+        self.E, self.d, self.I, self.K = E, d, I, None
         self.norm_topk, self.w_layout, self.score_rule = norm_topk, W_MXFP4, score_rule
         self.shared = shared
         self._desc = None
@@ -411,12 +419,34 @@ def _mx_desc(E, d, I, dtype=BASE_BF16, w13=None, w2=None):
                       _ptr(w2), 0, None, None, None)
 
 
-def _mx_out(desc, device):
-    import torch
+def _mx_sizes(desc):
     n13, n2 = (int(f(ctypes.byref(desc))) for f in (load().base_mx_w13_bytes,
                                                     load().base_mx_w2_bytes))
     if n13 == 0:
         raise BaseError(-2, status_string(-2))
+    return n13, n2
+
+
+def _mx_bytes(what, w13, w2, n, d, I, near):
+    """Packed experts have the bytes of n experts of this shape, where `near` lies: the
+    kernels take their sizes from the shape."""
+    import torch
+    for t, size in zip((w13, w2), _mx_sizes(_mx_desc(n, d, I))):
+        if (t.dtype is not torch.uint8 or t.numel() != size or not t.is_contiguous()
+                or t.device != near.device):
+            raise ValueError(f"{what}: the packed bytes of {n} experts with d = {d}, I = {I} "
+                             f"({size}, not {t.numel()}), on the router's device")
+
+
+def _mx_same_shape(what, w13, w2, n, d, I):
+    """w13 [n, 2I, d] and w2 [n, d, I] by their shapes."""
+    if w13 != (n, 2 * I, d) or w2 != (n, d, I):
+        raise ValueError(f"{what}: [{n}, {2 * I}, {d}] and [{n}, {d}, {I}], not {list(w13)} and {list(w2)}")
+
+
+def _mx_out(desc, device):
+    import torch
+    n13, n2 = _mx_sizes(desc)
     return (torch.empty(n13, dtype=torch.uint8, device=device),
             torch.empty(n2, dtype=torch.uint8, device=device))
 
@@ -458,9 +488,12 @@ def mx_layer(layer: "Layer", stream=None) -> "Layer":
     w_router, b_router, pred_a, pred_b, w13, w2 = layer.tensors
     if layer.w_layout != W_ROWMAJOR:
         raise ValueError("row-major experts")
+    _mx_same_shape("w13, w2", tuple(w13.shape), tuple(w2.shape), layer.E, layer.d, layer.I)
     shared = None
     if layer.shared is not None:
         w13s, w2s, gate = layer.shared
+        _mx_same_shape("shared w13, w2", tuple(w13s.shape), tuple(w2s.shape), int(w13s.shape[0]),
+                       layer.d, layer.I)
         shared = (*mx_quantize_experts(w13s, w2s, stream), gate, int(w13s.shape[0]))
     return Layer.mxfp4(w_router, b_router, pred_a, pred_b, *mx_quantize_experts(w13, w2, stream),
                        layer.I, layer.norm_topk, layer.score_rule, shared)
@@ -470,11 +503,16 @@ def mx_layer_from_codes(w_router, b_router, pred_a, pred_b, w13, w2, norm_topk: 
                         score_rule: int = 0, shared=None, stream=None) -> "Layer":
     """A W_MXFP4 Layer from experts held as (codes, scales) pairs (mx_pack_experts);
     shared: None or (w13 pair, w2 pair, gate or None)."""
+    E, d = w_router.shape
+    I = 2 * w2[0].shape[2]
+    values = lambda q: (*q[0].shape[:-1], 2 * q[0].shape[-1])  # noqa: E731
+    _mx_same_shape("w13, w2", values(w13), values(w2), E, d, I)
     if shared is not None:
         w13s, w2s, gate = shared
+        _mx_same_shape("shared w13, w2", values(w13s), values(w2s), int(w13s[0].shape[0]), d, I)
         shared = (*mx_pack_experts(w13s, w2s, stream), gate, int(w13s[0].shape[0]))
     return Layer.mxfp4(w_router, b_router, pred_a, pred_b, *mx_pack_experts(w13, w2, stream),
-                       2 * w2[0].shape[2], norm_topk, score_rule, shared)
+                       I, norm_topk, score_rule, shared)
 
 
 class Norms:

@@ -163,3 +163,58 @@ def test_binding_refuses_host_tensors():
         bd.mx_quantize(torch.zeros(2, 64, dtype=torch.float16))
     with pytest.raises(ValueError):
         bd.mx_dequantize(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 3, dtype=torch.uint8))
+
+
+def packed(n, d, I):
+    torch = pytest.importorskip("torch")
+    L = layer(E=n, K=1, d=d, I=I)
+    return [torch.zeros(f(ctypes.byref(L)), dtype=torch.uint8)
+            for f in (bd.load().base_mx_w13_bytes, bd.load().base_mx_w2_bytes)]
+
+
+def test_binding_compares_packed_experts_with_the_router():
+    """The packed bytes carry no shape, and the kernels read as far as the layer's."""
+    torch = pytest.importorskip("torch")
+    def make(E=4, d=512, w=(4, 512, 192), I=192, shared=None, **kw):
+        return bd.Layer.mxfp4(torch.zeros(E, d), None, None, None, *packed(*w), I, shared=shared, **kw)
+    lay = make(shared=(*packed(2, 512, 192), torch.zeros(512), 2))
+    assert (lay.E, lay.d, lay.I, lay.desc(2).n_shared) == (4, 512, 192, 2)
+    assert make(shared=(None, None, None, 0)).desc(2).n_shared == 0
+    for kw in (dict(E=5), dict(E=3), dict(d=768), dict(I=256), dict(I=128),
+               dict(shared=(*packed(1, 512, 192), None, 2)),              # fewer than said
+               dict(shared=(*packed(1, 512, 768), None, 1)),              # a wider one in one piece
+               dict(shared=(*packed(1, 256, 192), None, 1)),
+               dict(shared=(*packed(1, 512, 192), torch.zeros(256), 1)),
+               dict(shared=(*packed(1, 512, 192), torch.zeros(512).bfloat16(), 1))):
+        with pytest.raises(ValueError):
+            make(**kw)
+    for bad in (lambda t: t[:-1], lambda t: t.view(torch.int8), lambda t: torch.cat((t, t))[::2]):
+        a, b = packed(4, 512, 192)
+        for pair in ((bad(a), b), (a, bad(b))):
+            with pytest.raises(ValueError):
+                bd.Layer.mxfp4(torch.zeros(4, 512), None, None, None, *pair, 192)
+    with pytest.raises(bd.BaseError):
+        make(I=100)
+
+
+def test_binding_compares_experts_with_the_router():
+    """... of as many bytes, too: half the experts of twice the width."""
+    torch = pytest.importorskip("torch")
+    z = torch.zeros
+    def rowmajor(E, d, n, dw, I, Is=None, ds=None):
+        shared = None if Is is None else (z(1, 2 * Is, ds), z(1, ds, Is), None)
+        return bd.Layer(z(E, d), None, None, None, z(n, 2 * I, dw), z(n, dw, I), shared=shared)
+    for a in ((4, 256, 2, 512, 64), (4, 512, 3, 512, 64), (4, 256, 4, 512, 64), (4, 256, 4, 256, 64, 128, 256),
+              (4, 256, 4, 256, 64, 64, 512)):
+        with pytest.raises(ValueError, match="w13, w2: "):
+            bd.mx_layer(rowmajor(*a))
+    u8 = dict(dtype=torch.uint8)
+    def pair(n, rows, cols):
+        return z(n, rows, cols // 2, **u8), z(n, rows, cols // 32, **u8)
+    def codes(E, d, n, dw, I, Is=None, ds=None):
+        shared = None if Is is None else (pair(1, 2 * Is, ds), pair(1, ds, Is), None)
+        return bd.mx_layer_from_codes(z(E, d), None, None, None, pair(n, 2 * I, dw), pair(n, dw, I), shared=shared)
+    for a in ((4, 256, 2, 512, 64), (4, 512, 3, 512, 64), (4, 256, 4, 512, 64), (4, 256, 4, 256, 64, 128, 256),
+              (4, 256, 4, 256, 64, 64, 512)):
+        with pytest.raises(ValueError, match="w13, w2: "):
+            codes(*a)
