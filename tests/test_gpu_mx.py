@@ -496,3 +496,35 @@ def test_nan_and_infinity_in_one_token_stay_in_its_row(gu, bd):
     keep = [t for t in range(20) if t not in (7, 11)]
     assert torch.equal(ys[0][keep].view(torch.int16), ys[1][keep].view(torch.int16))
     assert not torch.isfinite(ys[1][[7, 11]]).any()
+
+
+def pool_of(t):
+    """The stream in whose memory a tensor lies."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not the allocator's")
+
+
+def test_new_tensors_lie_in_the_memory_of_the_stream_that_writes_them(gu, bd):
+    """A block freed on the current stream may still be in use there, so a kernel on
+    another stream must not get it."""
+    cur, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    src, gain = torch.randn(8, 256, device="cuda").bfloat16(), torch.ones(256, device="cuda")
+    inp = W.custom_layer(256, 4, 2, 64, 5, seed=3, n_shared=1, shared_gate=True)
+    gl = gu.GpuLayer(inp)
+    torch.cuda.synchronize()
+    for stream, where in ((side, side.cuda_stream), (None, cur.cuda_stream)):
+        codes, scales = bd.mx_quantize(src, stream=stream)
+        new = [codes, scales, bd.mx_dequantize(codes, scales, stream=stream)]
+        new += bd.norm_residual(src, src, pre_gain=gain, stream=stream)
+        for lay in (bd.mx_layer(gl.layer, stream), bd.packed_layer(gl.layer, 2, stream)):
+            new += [*lay.tensors[4:6], *lay.shared[:2]]
+        torch.cuda.synchronize()
+        assert all(pool_of(t) == where for t in new)
+    want = bd.mx_quantize(src)
+    torch.cuda.synchronize()
+    for stream in (side, None):
+        got = bd.mx_quantize(src, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
