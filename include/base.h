@@ -478,7 +478,10 @@ base_status base_calib_accumulate(const base_layer *L, const void *z, int32_t B,
  * them except that one
  * kernel makes the selection and the backfill (and, for small batches, the
  * compaction; base_layer_stages): stage 2 times it and stage 3 (and 4)
- * records its pair back to back.  The setting belongs
+ * records its pair back to back.  base_decode_layer_noalloc and
+ * base_decode_block run base_decode_layer's stages, the norm in stage 8; no
+ * other call touches the events, base_calib_accumulate's own run of the experts
+ * among them.  The setting belongs
  * to the calling host thread; the caller keeps the events alive while it
  * is set.  Calls on a stream that is being captured ignore it (no event is
  * recorded into the graph).

@@ -223,6 +223,16 @@ void stage_end(hipStream_t st) {
   }
 }
 
+// No stage events while one of these lives: a call that base_set_stage_events does
+// not list leaves the events of the thread's decode layers as they are.
+struct UntimedStages {
+  void *const *kept = g_stage_events;
+  UntimedStages() { g_stage_events = nullptr; }
+  ~UntimedStages() { g_stage_events = kept; }
+  UntimedStages(const UntimedStages &) = delete;
+  UntimedStages &operator=(const UntimedStages &) = delete;
+};
+
 // Compute units of the current device (queried once per device): the FFN
 // launches are sized from it.
 int device_cus() {
@@ -777,6 +787,7 @@ base_status base_calib_accumulate(const base_layer *L, const void *z, int32_t B,
                          at<float>(ws, o.pair_gate), at<int32_t>(ws, o.pair_of), sel,
                          bf16 && !o.split, C.d, C.I, at<uint32_t>(ws, o.tokoff), hdr, units_gu, units_dn,
                          rec, sptok, part_records(&C, B, o), n_cu, st));
+  const UntimedStages untimed;
   BASE_TRY(run_ffn(&C, z, B, bc, std::min(bc, B * C.K), sel, nsel, ws, o, st));
   double *inv = at<double>(ws, o.total);
   double *y = at<double>(ws, o.total + up256((size_t)B * 8));

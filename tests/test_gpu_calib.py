@@ -237,3 +237,54 @@ def test_gram_of_scaled_rows(gu, d, E, K, B, scale):
         ref = 2.0 * zb[t].T @ zb[t]
         assert np.max(np.abs(G[u] - ref)) <= (len(t) + 3) * 2.0 ** -23, u
         assert np.array_equal(G[u], G[u].T), u
+
+
+@pytest.mark.parametrize("kind", ["rowmajor", "packed", "mx"])
+def test_calibration_leaves_the_stage_events(gu, kind):
+    """A thread that times its decode layers and accumulates statistics between them
+    keeps the layer's times: every event is the one the layer recorded."""
+    import ctypes
+    import re
+    from paper_2609_36222_amd import binding as bd
+    maps = open("/proc/self/maps").read()
+    hip = ctypes.CDLL(sorted(set(re.findall(r"(/\S*libamdhip64\.so[.\d]*)", maps)))[0])
+    hip.hipEventCreate.argtypes = [ctypes.POINTER(ctypes.c_void_p)]
+    hip.hipEventElapsedTime.argtypes = [ctypes.POINTER(ctypes.c_float), ctypes.c_void_p, ctypes.c_void_p]
+    hip.hipEventDestroy.argtypes = [ctypes.c_void_p]
+    evs = []
+    for _ in range(2 * bd.N_STAGES):
+        e = ctypes.c_void_p()
+        assert hip.hipEventCreate(ctypes.byref(e)) == 0
+        evs.append(e.value)
+    inp = W.custom_layer(256, 8, 2, 64, 40, seed=7)
+    gl = gu.GpuLayer(inp, packed=kind == "packed")
+    if kind == "mx":
+        gl.layer = bd.mx_layer(gl.layer)
+        gl.desc = gl.layer.desc(gl.K)
+    x, stats = gl.x(inp["x"]), bd.calib_stats(gl.desc)
+    cws = bd.calib_accumulate(gl.desc, x, 40, stats)
+    ws, y = gl.workspace(40, 4), gl.y_like(40)
+    ms = ctypes.c_float()
+
+    def times():
+        torch.cuda.synchronize()
+        out = []
+        for e in evs[1:]:
+            assert hip.hipEventElapsedTime(ctypes.byref(ms), evs[0], e) == 0
+            out.append(ms.value)
+        return out
+
+    keep = bd.base_set_stage_events(evs)
+    try:
+        bd.base_decode_layer(gl.desc, x, 40, 4, 0, None, y, ws)
+        before = times()
+        bd.calib_accumulate(gl.desc, x, 40, stats, cws)
+        assert times() == before
+        bd.base_decode_layer(gl.desc, x, 40, 4, 0, None, y, ws)     # still set, and taken again
+        after = times()
+        assert after != before and after[12] > 0.0
+    finally:
+        bd.base_set_stage_events(None)
+    del keep
+    for e in evs:
+        hip.hipEventDestroy(e)
