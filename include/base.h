@@ -295,15 +295,18 @@ typedef struct base_norms {
 } base_norms;
 #define BASE_NORM_MAX_D 16384
 #define BASE_NORM_MAX_ROWS 0x7FFFFFFFLL
+#define BASE_NORM_MAX_LD (1LL << 40)
 
 /*   rows   1 .. BASE_NORM_MAX_ROWS
  *   y      the block's output, or NULL: h' = h (the norm before the first block;
- *          res_scale, gate and post_gain are not read, and h_out must be NULL)
+ *          res_scale, gate, gate_ld and post_gain are not read, whatever they
+ *          hold, and h_out must be NULL)
  *   h      the residual stream
  *   h_out  h', or NULL;  x_out  x', or NULL (not both)
- * Each is rows x d with its own row stride (>= d elements); elements between the
- * rows are not touched, and element alignment suffices.  h_out may be h or y, and
- * x_out may be y or h, with the same stride; otherwise they must not overlap.
+ * Each is rows x d with its own row stride (d to BASE_NORM_MAX_LD elements, as the
+ * gate's where it is not 0); elements between the rows are not touched, and
+ * element alignment suffices.  h_out may be h or y, and x_out may be y or h, with
+ * the same stride; otherwise they must not overlap.
  * BASE_ERR_SHAPE: d, rows, a stride, eps or res_scale outside the above;
  * BASE_ERR_FLAGS: h_out without y, h_out the same as x_out, or another stride in
  * place. */

@@ -551,10 +551,11 @@ class Norms:
         self.desc = base_norms(d, BASE_BF16 if dtype is torch.bfloat16 else BASE_F32, eps, res_scale,
                                ptr[0], ptr[1], ld, ptr[2])
 
-    def _pointers(self, rows, dev, tensors):
-        """The row count checked, and (pointer, row stride) of each tensor (of y, h,
-        h_out, x_out, in this order)."""
-        if self.gate_rows is not None and self.gate_rows != rows:
+    def _pointers(self, rows, dev, tensors, block):
+        """The row count checked (the gate's where there is a block, else it is not
+        read), and (pointer, row stride) of each tensor (of y, h, h_out, x_out, in this
+        order)."""
+        if block and self.gate_rows is not None and self.gate_rows != rows:
             raise ValueError(f"gate: one row, or {rows}")
         out, d, dt = [], self.d, self.torch_dtype
         shape = (rows, d)
@@ -575,7 +576,7 @@ def base_norm_residual(norms: Norms, y, h, h_out=None, x_out=None, stream=None):
     """h_out = res_scale h + gate (post_gain n(y)), x_out = pre_gain n(h_out); [rows, d]
     tensors whose rows may lie inside wider ones; y None: x_out = pre_gain n(h)."""
     rows = h.shape[0]
-    a = norms._pointers(rows, _device(), (y, h, h_out, x_out))
+    a = norms._pointers(rows, _device(), (y, h, h_out, x_out), y is not None)
     _check(load().base_norm_residual(norms.desc, rows, *a, _stream(stream)))
 
 
@@ -597,7 +598,7 @@ def base_decode_block(desc, norms: Norms, x, B, budget, flags, h, ws, h_out=None
     """base_decode_layer, then base_norm_residual on its output, in the layer's
     launches; returns the filled base_plan (device pointers into ws)."""
     plan = base_plan() if plan is None else plan
-    norms._pointers(B, _device(), (None, h, h_out, x_out))
+    norms._pointers(B, _device(), (None, h, h_out, x_out), True)
     for t, what in ((h, "h"), (h_out, "h_out"), (x_out, "x_out")):
         if t is not None and not t.is_contiguous():
             raise ValueError(f"{what}: contiguous rows")

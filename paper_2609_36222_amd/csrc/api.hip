@@ -645,16 +645,16 @@ static base_status check_norms(const base_norms *N, int64_t rows, bool has_y, co
   if (N->dtype != BASE_F32 && N->dtype != BASE_BF16) return BASE_ERR_DTYPE;
   if (N->d < 1 || N->d > BASE_NORM_MAX_D || rows < 1 || rows > BASE_NORM_MAX_ROWS)
     return BASE_ERR_SHAPE;
-  if (!(N->eps >= 0.0f) || !std::isfinite(N->eps) || !std::isfinite(N->res_scale))
-    return BASE_ERR_SHAPE;
-  if (N->gate && N->gate_ld != 0 && (N->gate_ld < N->d || N->gate_ld > BASE_MX_MAX_LD))
+  if (!(N->eps >= 0.0f) || !std::isfinite(N->eps)) return BASE_ERR_SHAPE;
+  // without y the block's own parameters are not read, whatever they are
+  if (has_y && (!std::isfinite(N->res_scale) ||
+                (N->gate && N->gate_ld != 0 && (N->gate_ld < N->d || N->gate_ld > BASE_NORM_MAX_LD))))
     return BASE_ERR_SHAPE;
   if (x_out && !N->pre_gain) return BASE_ERR_NULL;
   if (!has_y && h_out) return BASE_ERR_FLAGS;   // nothing to add: h' is h
   if (h_out && h_out == x_out) return BASE_ERR_FLAGS;
-  for (const float *p : {N->post_gain, N->gate, N->pre_gain})
-    if (p && !aligned(p, 4)) return BASE_ERR_ALIGN;
-  return BASE_OK;
+  if (has_y && (!aligned(N->post_gain, 4) || !aligned(N->gate, 4))) return BASE_ERR_ALIGN;
+  return aligned(N->pre_gain, 4) ? BASE_OK : BASE_ERR_ALIGN;
 }
 
 base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y, int64_t y_ld,
@@ -664,7 +664,7 @@ base_status base_norm_residual(const base_norms *N, int64_t rows, const void *y,
   const struct { const void *p; int64_t ld; } rs[] = {{y, y_ld}, {h, h_ld}, {h_out, h_out_ld}, {x_out, x_out_ld}};
   for (const auto &r : rs) {
     if (!r.p) continue;
-    if (r.ld < N->d || r.ld > BASE_MX_MAX_LD) return BASE_ERR_SHAPE;
+    if (r.ld < N->d || r.ld > BASE_NORM_MAX_LD) return BASE_ERR_SHAPE;
     if (!aligned(r.p, elem_bytes(N->dtype))) return BASE_ERR_ALIGN;
   }
   // in place only row by row

@@ -319,7 +319,8 @@ hipError_t launch_norm(bool bf16, int d, float eps, float scale, const float *po
                        long long gate_ld, const float *pre, long long rows, const void *y,
                        long long y_ld, const void *h, long long h_ld, void *ho, long long ho_ld,
                        void *xo, long long xo_ld, int n_cu, hipStream_t st) {
-  const NormArgs a{d, eps, scale, post, gate, pre, gate_ld};
+  // (a norm without y reads no parameter of the block's, pointers among them)
+  const NormArgs a{d, eps, scale, y ? post : nullptr, y ? gate : nullptr, pre, gate_ld};
   const int V = bf16 ? 8 : 4, lpr = d <= 128 ? 16 : d < 256 ? 32 : d <= 16 * WAVE ? WAVE : 0;
   // rows that V does not divide, in workgroups of more threads: with 16 elements a
   // thread the registers spill (past 8192 elements there are not as many threads)

@@ -136,6 +136,28 @@ def test_norm_before_the_first_block(bd, dtype, d):
     run(bd, 5, d, dtype, block=False, post=False)
 
 
+def test_without_a_block_its_parameters_are_not_read(bd):
+    """One Norms for a step: its norm before the first block, where the residual scale,
+    the gate and the post gain have no part, whatever they hold."""
+    import ctypes
+    h, pre = torch.randn(5, 96, device="cuda").bfloat16(), torch.randn(96, device="cuda")
+    want, x = torch.empty_like(h), torch.empty_like(h)
+    bd.base_norm_residual(bd.Norms(96, h.dtype, pre_gain=pre), None, h, None, want)
+    n = bd.Norms(96, h.dtype, torch.ones(96, device="cuda"), torch.ones(7, 96, device="cuda"), pre)
+    bd.base_norm_residual(n, None, h, None, x)               # a gate for another batch
+    assert torch.equal(x, want)
+    for kw in (dict(res_scale=float("nan")), dict(res_scale=float("inf")), dict(gate_ld=-1), dict(gate_ld=1 << 50),
+               dict(post_gain=2), dict(gate=1)):
+        v = dict(d=96, dtype=1, eps=1e-6, res_scale=1.0, post_gain=0, gate=pre.data_ptr(), gate_ld=0,
+                 pre_gain=pre.data_ptr())
+        v.update(kw)
+        x.fill_(3.0)
+        N = bd.base_norms(*(v[f] for f, _ in bd.base_norms._fields_))
+        assert bd.load().base_norm_residual(ctypes.byref(N), 5, None, 0, h.data_ptr(), 96, None, 0, x.data_ptr(), 96,
+                                            bd._stream(None)) == 0, kw
+        assert torch.equal(x, want), kw
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
 @pytest.mark.parametrize("d,pad,off", [(512, 8, 0), (512, 4, 0), (512, 3, 0), (512, 0, 1), (2048, 64, 0),
                                        (2048, 1, 3), (5001, 7, 1)])
