@@ -286,7 +286,7 @@ int part_records(const base_layer *L, int32_t B, const Layout &o) {
 
 // 4-bit experts and few tokens: down's launch also combines
 bool few_tokens(const base_layer *L, int32_t B, int32_t bc) {
-  return mx_layer(L) && mx_few(B, L->K, bc, L->n_shared);
+  return mx_layer(L) && mx_few(B, L->K, bc, L->n_shared, L->d, L->I);
 }
 
 // gate/up and down of the plan in the workspace (stages 6 and 7), on at most

@@ -167,20 +167,39 @@ static_assert(FFN_SPLIT_B <= 16 * MX_NT, "a slot of a small batch is one part");
 inline bool mx_parts(int B) { return B > FFN_SPLIT_B; }
 // up to this many tokens the activations have a second, 8-bit part (ffn_mx.hip)
 constexpr int MX_TWO_B = 32;
-// Few tokens: down and the combine in one launch (k_mx_down_combine), whose
-// workgroups go over every slot.  With one to four tokens (one load of four rows
-// a step) it always wins, with more only while the slots are few; the line is
-// slots (loads - 1) <= 12.  Layer, us, two launches against one: d = 2048, E = 128,
-// I = 768 B = 1, 8 slots 28.4 and 26.6, B = 4, 32 slots 34.8 and 34.5, B = 8, 12
-// slots 31.4 and 30.1, 24 slots 34.8 and 35.7, B = 16, 4 slots 29.4 and 27.3, 12 slots 32.0
-// and 33.4; d = 4096, I = 4096 B = 1, 2 slots 38.8 and 30.9, B = 8, 16 slots 92.7 and 93.0.
-// (kept: the slots the batch can fill, whatever base_moe_forward is given, so that
+// Few tokens: down and the combine in one launch (k_mx_down_combine).  It saves the combine's
+// launch and the pair rows' way through memory, 2 to 4 us, but its d / 16 workgroups each go
+// over every slot's contraction, chunk by chunk of 512 elements, 15 chunks at a time with one
+// load of four rows a step (one to four tokens), 10 with two, 5 with four.  So the line is on
+// the slots and on the chunks, slots ceil(I / 512), and by d: with few workgroups the chunks
+// take long (the other launch spreads them over the compute units), and with more of them
+// than compute units (d > 4096) they come in rounds.  Whole layers, us, two launches against
+// one (slots, chunks):
+//   one to four tokens, d = 256 (8, 16) 21.9 and 20.5, (16, 32) 22.5 and 23.5, (6, 84) 33.5
+//   and 31.6, (8, 112) 36.5 and 40.8, (32, 448) 48 and 69, (32, 896) 70 and 135; d = 1024 (8,
+//   32) 29.7 and 27.0, (32, 128) 38 and 45, (16, 224) 62 and 84; d = 2048 (8, 16) 27.9 and
+//   25.6, (8, 64) 46.6 and 44.0, (8, 96) 58.5 and 59.0, (8, 160) 75.8 and 84.0, (16, 32) 30.4
+//   and 29.8, (32, 64) 34.8 and 37.9 at I = 768 and 36.7 and 37.6 at I = 1024; d = 2560 to
+//   4096 up to 15 slots (12, 108) 68.7 and 67.7, (8, 224) 135.6 and 132.6, (6, 168) 125.5 and
+//   106.3, more of them (32, 64) 57.1 and 54.0, (16, 80) 66.5 and 67.9, (16, 192) 120.6 and
+//   130.6; d = 4608 (2, 6) 34.9 and 31.0, (4, 12) 35.5 and 36.5, (32, 96) 78.6 and 87.6, (8,
+//   224) 145.7 and 155.3, (4, 112) 120.2 and 114.4
+//   five to eight, d = 2048 (10, 40) 35.6 and 34.6, (12, 48) 37.9 and 40.7, (4, 48) 38.5 and
+//   36.7, (6, 72) 48.4 and 54.5, (8, 224) 79.8 and 102.9
+//   nine to sixteen, d = 2048 (4, 16) 33.3 and 31.2, (2, 24) 33.4 and 34.7, (3, 36) 37.4 and
+//   46.0, (2, 56) 46.1 and 54.9
+// (slots: those the batch can fill, whatever base_moe_forward is given, so that
 // it takes the same sums as the fused layer)
 constexpr int MX_FEW_B = 16;
 inline int mx_kept(int B, int K, int budget) { return budget < B * K ? budget : B * K; }
 inline int mx_row_loads(int B) { return B <= 4 ? 1 : B <= 8 ? 2 : 4; }
-inline bool mx_few(int B, int K, int budget, int ns) {
-  return B <= MX_FEW_B && (mx_kept(B, K, budget) + ns) * (mx_row_loads(B) - 1) <= 12;
+inline bool mx_few(int B, int K, int budget, int ns, int d, int I) {
+  if (B > MX_FEW_B) return false;
+  const int loads = mx_row_loads(B), slots = mx_kept(B, K, budget) + ns, chunks = slots * ((I + 511) / 512);
+  if (d > 4096 && chunks > 8) return false;
+  if (loads == 2) return slots <= 10 && chunks <= 40;
+  if (loads == 4) return slots <= 4 && chunks <= 16;
+  return slots <= 15 ? d > 2048 || chunks <= 64 : d >= 2048 && chunks <= 64;
 }
 // slots' records, or an upper bound of the parts: the sum over slots of
 // ceil(tiles / MX_NT) is at most (tiles + (MX_NT - 1) slots) / MX_NT

@@ -291,6 +291,16 @@ def test_few_tokens(gu, bd, E, K, I, B, budget, ns):
     MxCase(gu, bd, 256, E, K, I, B, ns, ns == 2, seed=E + I).check(gu, bd, budget, 0, True)
 
 
+@pytest.mark.parametrize("d,E,K,I,B,budget,ns", [(2048, 32, 8, 64, 4, 32, 0), (2048, 16, 8, 64, 3, 16, 2),
+                                                 (2304, 4, 2, 4288, 4, 4, 0), (4608, 4, 2, 320, 2, 4, 1),
+                                                 (256, 8, 8, 4608, 2, 8, 0), (256, 32, 8, 768, 4, 32, 0),
+                                                 (4608, 8, 2, 320, 3, 6, 3), (512, 16, 8, 2048, 8, 11, 0)])
+def test_few_tokens_on_both_sides_of_the_line(gu, bd, d, E, K, I, B, budget, ns):
+    """More slots than a workgroup's wavefronts, many chunks a wavefront, and the shapes
+    next to these that take down and the combine in two launches."""
+    MxCase(gu, bd, d, E, K, I, B, ns, bool(ns), seed=d + B).check(gu, bd, budget, 0, True)
+
+
 def test_long_contraction(gu, bd):
     """Many chunks in both products."""
     MxCase(gu, bd, 4096, 3, 2, 4160, 7, seed=2).check(gu, bd, 2)

@@ -103,6 +103,24 @@ def test_stages(lib):
     assert launched(65, 4) == ("scores", "tail", "select", "compact", "ffn_gateup", "ffn_down", "combine")
 
 
+@pytest.mark.parametrize("d,E,K,I,B,budget,joined", [
+    # one to four tokens: few workgroups, long ones
+    (256, 64, 8, 768, 1, 8, True), (256, 32, 8, 768, 4, 32, False), (256, 32, 8, 7168, 1, 8, False),
+    (256, 32, 8, 14336, 4, 32, False), (512, 64, 8, 4096, 4, 8, True), (512, 64, 8, 4608, 4, 8, False),
+    (1024, 64, 8, 512, 2, 16, False), (1024, 16, 2, 14336, 2, 2, True), (1024, 64, 8, 7168, 4, 16, False),
+    (2048, 128, 8, 768, 4, 32, True), (2048, 64, 8, 4096, 1, 8, True), (2048, 32, 8, 6144, 1, 8, False),
+    (2048, 8, 2, 14336, 4, 8, False), (3584, 32, 8, 6144, 4, 12, True), (3584, 32, 8, 6144, 4, 16, False),
+    (4096, 8, 2, 14336, 4, 8, True), (4096, 64, 8, 1024, 4, 32, True), (4608, 64, 8, 1408, 1, 2, True),
+    (4608, 64, 8, 1408, 1, 4, False), (16384, 16, 4, 4096, 4, 4, False),
+    # five to eight, nine to sixteen
+    (2048, 64, 8, 2048, 8, 10, True), (2048, 64, 8, 2048, 8, 12, False), (2048, 16, 4, 6144, 8, 6, False),
+    (2048, 64, 8, 2048, 16, 4, True), (2048, 64, 8, 2048, 16, 5, False), (2048, 16, 4, 6144, 16, 2, False)])
+def test_where_downs_launch_combines(lib, d, E, K, I, B, budget, joined):
+    """The side of its line that is faster, for both sides of each term."""
+    s = bd.layer_stages(layer(d=d, E=E, K=K, I=I, **MXL), B, budget)
+    assert ("combine" not in s) == joined, s
+
+
 def test_quantize_refusals(lib):
     def q(dtype=1, src=FAKE, rows=4, cols=64, ld=64, codes=FAKE, scales=FAKE):
         return lib.base_mx_quantize(dtype, src, rows, cols, ld, codes, scales, None)
