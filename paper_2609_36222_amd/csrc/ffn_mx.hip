@@ -642,11 +642,6 @@ using MxManyWide = MxShape<MX_NT, 2, 8, 1, 1>;
 using MxFewDown = MxShape<1, 2, 4, 1, 2, true>;
 using MxMidDown = MxShape<2, 2, 4, 1, 2, true>;
 
-int mx_workgroups(int B, int K, int budget, int ns, int groups) {
-  const int kept = mx_kept(B, K, budget), full = B * (K + ns) / (16 * MX_NT);
-  return (kept + ns > full ? kept + ns : full) * groups;
-}
-
 // workgroups: records times row groups (the same number on every die) times what
 // shares one
 dim3 mx_grid(int recs, int RG, int by) {
@@ -672,16 +667,15 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
              B * (K + ns), (const uint8_t *)w13, (const uint8_t *)w13s, sptok, (const uint16_t *)x,
              B, (uint16_t *)H, (uint8_t *)Hlo);
   };
-  auto wgs = [&](int group) { return mx_workgroups(B, K, budget, ns, mx_groups(I / 8, group)); };
-  if (B <= 16) {
-    if (wgs(MxFew::GROUP) >= n_cu) go(MxFew{});
-    else go(MxFewSplit{});
-  } else if (B <= MX_TWO_B) {
-    go(MxMid{});
-  } else if (2 * wgs(MxManyWide::GROUP) >= 3 * n_cu) {
-    go(MxManyWide{});
-  } else {
-    go(MxMany{});
+  static_assert(MxFew::GROUP == MX_GU_GROUP && MxFewSplit::GROUP <= MX_GU_GROUP &&
+                    MxManyWide::GROUP == MX_GU_WIDE,
+                "mx_gateup_shape's row groups");
+  switch (mx_gateup_shape(B, I, K, budget, ns, n_cu)) {
+    case MX_GU_FEW: go(MxFew{}); break;
+    case MX_GU_FEW_SPLIT: go(MxFewSplit{}); break;
+    case MX_GU_MID: go(MxMid{}); break;
+    case MX_GU_MANY: go(MxMany{}); break;
+    case MX_GU_MANY_WIDE: go(MxManyWide{}); break;
   }
   return hipGetLastError();
 }

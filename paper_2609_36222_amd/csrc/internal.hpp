@@ -208,6 +208,22 @@ inline int mx_records(int B, int K, int budget, int ns) {
   return (ffn_max_tiles(B, K, budget, ns) + (MX_NT - 1) * (budget + ns)) / MX_NT;
 }
 
+// Gate/up's shape of a batch (the shapes and the lines' figures: ffn_mx.hip), from the
+// workgroups of slots and full parts, which the host knows, on row groups of
+// MX_GU_GROUP or, side by side with twice the wavefronts, MX_GU_WIDE tiles.
+enum MxGateup { MX_GU_FEW, MX_GU_FEW_SPLIT, MX_GU_MID, MX_GU_MANY, MX_GU_MANY_WIDE };
+constexpr int MX_GU_GROUP = 8, MX_GU_WIDE = 16;
+inline int mx_gateup_workgroups(int B, int I, int K, int budget, int ns, int group) {
+  const int kept = mx_kept(B, K, budget), full = B * (K + ns) / (16 * MX_NT);
+  return (kept + ns > full ? kept + ns : full) * ((I / 8 + group - 1) / group);
+}
+inline MxGateup mx_gateup_shape(int B, int I, int K, int budget, int ns, int n_cu) {
+  if (B <= 16)
+    return mx_gateup_workgroups(B, I, K, budget, ns, MX_GU_GROUP) >= n_cu ? MX_GU_FEW : MX_GU_FEW_SPLIT;
+  if (B <= MX_TWO_B) return MX_GU_MID;
+  return 2 * mx_gateup_workgroups(B, I, K, budget, ns, MX_GU_WIDE) >= 3 * n_cu ? MX_GU_MANY_WIDE : MX_GU_MANY;
+}
+
 // Workgroups that share the contraction of one (record, row group) of down, each
 // writing pair rows of its own, which the combine adds in their order.  A share
 // saves a part of the steps of 128 (0.26 us each between one share and four) and

@@ -260,6 +260,41 @@ def test_layer(gu, bd, shape):
     MxCase(gu, bd, d, E, K, I, B, ns, gate, norm_topk, seed=B).check(gu, bd, budget, flags, res)
 
 
+# with SHAPES, every kernel instance of a 4-bit layer (test_mx_instances.py asks the
+# library's own rules which ones these are)
+INSTANCES = [
+    # the plans, by experts (64, 128, more), tokens a wavefront and kept experts (48, more)
+    (256, 128, 4, 64, 1, 3, 0, 0, False, 1, False),
+    (256, 128, 8, 64, 16, 60, 0, 0, False, 0, True),
+    (256, 128, 8, 64, 48, 20, 0, 1, True, 1, False),
+    (256, 128, 8, 64, 40, 100, 1, 0, False, 0, True),
+    (512, 200, 4, 64, 9, 30, 0, 0, False, 1, False),
+    (256, 256, 16, 64, 16, 200, 1, 0, False, 1, False),
+    (256, 200, 8, 64, 40, 150, 0, 0, False, 1, True),
+    (256, 200, 8, 64, 33, 12, 1, 0, False, 0, False),
+    (256, 64, 8, 64, 40, 60, 0, 0, False, 1, False),
+    (256, 64, 16, 64, 16, 64, 1, 0, False, 1, False),
+    # gate/up of eight wavefronts side by side, its last row group half there, slots of
+    # one to four token tiles
+    (256, 64, 4, 832, 72, 64, 0, 0, False, 1, False),
+    (256, 24, 4, 1856, 200, 24, 0, 2, True, 0, True),
+    (256, 24, 8, 2112, 120, 24, 2, 0, False, 1, False),
+    # down with the combine, two and four loads of four rows a step
+    (512, 16, 4, 576, 7, 4, 0, 1, True, 1, True),
+    (512, 16, 4, 576, 13, 3, 0, 0, False, 0, False),
+    # down in shares, one, two and four token tiles
+    (256, 4, 4, 4352, 12, 4, 0, 0, False, 1, True),
+    (256, 2, 1, 4096, 17, 2, 0, 0, False, 1, False),
+    (256, 3, 2, 4160, 40, 3, 0, 0, False, 0, True),
+]
+
+
+@pytest.mark.parametrize("shape", INSTANCES, ids=lambda s: "-".join(str(int(v)) for v in s))
+def test_layer_instances(gu, bd, shape):
+    d, E, K, I, B, budget, flags, ns, gate, norm_topk, res = shape
+    MxCase(gu, bd, d, E, K, I, B, ns, gate, norm_topk, seed=B + E).check(gu, bd, budget, flags, res)
+
+
 @pytest.mark.parametrize("rule", [1, 2, 3, 4])
 def test_rules(gu, bd, rule):
     MxCase(gu, bd, 256, 16, 4, 64, 9, rule=rule, seed=3).check(gu, bd, 5)
