@@ -51,35 +51,34 @@ struct MxShape {
   static constexpr int LDS = KW * RING * SLOT;
   static constexpr int GROUP = RW * T;                 // tiles per workgroup
   static constexpr int WPE = NT * T >= 16 ? 2 : DT == 1 ? 4 : 3;   // wavefronts per SIMD
-  static_assert(DT < MX_CHUNK, "weights, one step further ahead, have a chunk of stages");
+  static_assert(DT + 1 < MX_CHUNK, "weights, one step further ahead, have a stage to spare");
   static_assert(LDS >= (KW > 1 ? WAVES * T * NT * 1024 : 0), "partial sums in the ring");
 };
 
-// The record, row group and first token tile of this workgroup.  Workgroup b runs
+// The record and row group of this workgroup.  Workgroup b runs
 // on die b % N_XCD; the row groups of slot `ord` are numbered on from the previous
 // slot's and number v lies on die v % N_XCD, so that all parts of a slot read a
 // row group's weights through one L2 and every die has its share of every slot.
-// `cuts` workgroups share a record's token tiles, `shares` its contraction.
+// `shares` workgroups share a record's contraction.
 struct MxPlan {
-  int budget, ns, nrec, parts, cuts, shares;
+  int budget, ns, nrec, parts, shares;
   const SpRec *rec;
 };
 struct MxWork {
-  int u, p0, n, rg, c0, share;
+  int u, p0, n, rg, share;
 };
 template <bool SPLIT = false>
-__device__ __forceinline__ MxWork mx_work(const MxPlan &pl, int RG, int NT) {
+__device__ __forceinline__ MxWork mx_work(const MxPlan &pl, int RG) {
   const int die = blockIdx.x % N_XCD, q = blockIdx.x / N_XCD;
-  const int shares = SPLIT ? pl.shares : 1, per = ((RG + N_XCD - 1) / N_XCD) * pl.cuts * shares;
-  const int y = q / per, zs = q - y * per, z = zs / shares, k = z / pl.cuts;
+  const int shares = SPLIT ? pl.shares : 1, per = ((RG + N_XCD - 1) / N_XCD) * shares;
+  const int y = q / per, zs = q - y * per, k = zs / shares;
   // slots: the shared experts first, they run for every token
   const int i = pl.parts ? y : (y < pl.ns ? pl.budget + y : y - pl.ns);
   const SpRec r = pl.rec[die * pl.nrec + i];
   const int ord = pl.parts ? __builtin_amdgcn_readfirstlane(r.pad) : y;
   const int rg = ((die - ord * RG) & (N_XCD - 1)) + N_XCD * k;
   return {__builtin_amdgcn_readfirstlane(r.u), __builtin_amdgcn_readfirstlane(r.p0),
-          rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg, (z - k * pl.cuts) * 16 * NT,
-          zs - z * shares};
+          rg < RG ? __builtin_amdgcn_readfirstlane(r.n) : 0, rg, zs - k * shares};
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -252,7 +251,7 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
       if (M::RW > 1) wg_barrier();   // the others' rows are there, the next slot is read
       __builtin_amdgcn_sched_barrier(0);
       tokens(i + DT);
-      if constexpr (DT + 1 < MX_CHUNK) weights((p + DT + 1) % MX_CHUNK, i + DT + 1);
+      weights((p + DT + 1) % MX_CHUNK, i + DT + 1);
       __builtin_amdgcn_sched_barrier(0);
       if (p == 0) {
 #pragma unroll
@@ -289,9 +288,6 @@ __device__ __forceinline__ void mx_stream(uint8_t *lds, const MxTiles<M::T> &m, 
       }
       __builtin_amdgcn_sched_barrier(0);
       next(read);
-      // ... of this step's own stage only once it has been read
-      if constexpr (DT + 1 == MX_CHUNK) weights(p, i + DT + 1);
-      __builtin_amdgcn_sched_barrier(0);
     }
   }
   wait_vm<0>();
@@ -348,17 +344,19 @@ void k_mx_gateup(int d, int I, int E, MxPlan pl, int np, const uint8_t *__restri
                  const uint16_t *__restrict__ x, int B, uint16_t *__restrict__ H,
                  uint8_t *__restrict__ Hlo) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
-  const MxWork k = mx_work(pl, mx_groups(I / 8, M::GROUP), M::NT);
+  const MxWork k = mx_work(pl, mx_groups(I / 8, M::GROUP));
   const size_t eb = (size_t)(I / 8) * mx_tile_bytes(d);
   const uint8_t *w13 = k.u < E ? w13r + (size_t)k.u * eb : w13s + (size_t)(k.u - E) * eb;
   const rsrc_t rx = make_rsrc(x, (uint32_t)B * (uint32_t)d * 2u);
   const int lane = lane_id();
-  for (int c = k.c0; c < k.n; c += 16 * M::NT * pl.cuts) {
+  // (more than once only for routes that name an expert twice: a shape's token tiles
+  // hold a slot of its batches or a part)
+  for (int c = 0; c < k.n; c += 16 * M::NT) {
     const int n = min(k.n - c, 16 * M::NT);
     const int32_t *tok = sptok + (size_t)(blockIdx.x % N_XCD) * np + k.p0 + c;
     uint16_t *h0 = H + (size_t)(k.p0 + c) * I;
     uint8_t *l0 = Hlo + (size_t)(k.p0 + c) * I;
-    if (c > k.c0) wg_barrier();   // every wavefront is done with the ring
+    if (c > 0) wg_barrier();   // every wavefront is done with the ring
     sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
       constexpr int N = decltype(NC)::value;
       const MxTiles<M::T> m = mx_tiles<M>(w13, k.rg, I / 8, d);
@@ -398,16 +396,16 @@ void k_mx_down(int d, int I, int E, MxPlan pl, const uint8_t *__restrict__ w2r,
                const uint16_t *__restrict__ H, const uint8_t *__restrict__ Hlo,
                float *__restrict__ pairbuf, size_t stride) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[M::LDS];
-  const MxWork k = mx_work<SPLIT>(pl, mx_groups(d / 16, M::GROUP), M::NT);
+  const MxWork k = mx_work<SPLIT>(pl, mx_groups(d / 16, M::GROUP));
   const size_t eb = (size_t)(d / 16) * mx_tile_bytes(I);
   const uint8_t *w2 = k.u < E ? w2r + (size_t)k.u * eb : w2s + (size_t)(k.u - E) * eb;
   const int lane = lane_id();
-  for (int c = k.c0; c < k.n; c += 16 * M::NT * pl.cuts) {
+  for (int c = 0; c < k.n; c += 16 * M::NT) {
     const int n = min(k.n - c, 16 * M::NT), p0 = k.p0 + c;
     const rsrc_t rx = make_rsrc(H + (size_t)p0 * I, (uint32_t)n * (uint32_t)I * 2u);
     const rsrc_t rlo = M::LO ? make_rsrc(Hlo + (size_t)p0 * I, (uint32_t)n * (uint32_t)I) : rx;
     float *out0 = pairbuf + (SPLIT ? k.share * stride : 0) + (size_t)p0 * d;
-    if (c > k.c0) wg_barrier();
+    if (c > 0) wg_barrier();
     sp_tiles<M::NT>((n + 15) / 16, [&](auto NC) {
       constexpr int N = decltype(NC)::value;
       const MxTiles<M::T> m = mx_tiles<M>(w2, k.rg, d / 16, I);
@@ -633,6 +631,8 @@ namespace {
 // 24.7 -> 27.5, and 220 of Qwen1.5-MoE's shape at B = 61 17.8 -> 21.4; down, of short
 // contractions, 52.8 and 52.9 at B = 1024, and 17.7 -> 19.2 at B = 256).  The line counts
 // the workgroups of slots and full parts, which the host knows.
+// (a shape's token tiles hold every slot of its batches: B <= 16, MX_TWO_B, FFN_SPLIT_B,
+// or a part)
 static_assert(MX_TWO_B == 32, "MxMid's token tiles");
 using MxFew = MxShape<1, 2, 4, 1, 2>;
 using MxFewSplit = MxShape<1, 2, 2, 2, 2>;
@@ -642,15 +642,10 @@ using MxManyWide = MxShape<MX_NT, 2, 8, 1, 1>;
 using MxFewDown = MxShape<1, 2, 4, 1, 2, true>;
 using MxMidDown = MxShape<2, 2, 4, 1, 2, true>;
 
-// workgroups: records times row groups (the same number on every die) times what
-// shares one
-dim3 mx_grid(int recs, int RG, int by) {
-  return dim3((unsigned)(N_XCD * recs * ((RG + N_XCD - 1) / N_XCD) * by));
-}
-// workgroups that share a record's tiles: what a record can hold over what one takes
-int mx_cuts(int B, int NT) {
-  const int tiles = mx_parts(B) ? MX_NT : (B + 15) / 16;
-  return (tiles + NT - 1) / NT;
+// workgroups: records times row groups (the same number on every die) times the
+// shares of a contraction
+dim3 mx_grid(int recs, int RG, int shares) {
+  return dim3((unsigned)(N_XCD * recs * ((RG + N_XCD - 1) / N_XCD) * shares));
 }
 }  // namespace
 
@@ -661,9 +656,8 @@ hipError_t launch_mx_gateup(const void *x, int B, int d, int I, int E, int K, in
   const int nrec = mx_records(B, K, budget, ns);
   auto go = [&](auto shape) {
     using M = decltype(shape);
-    const int cuts = mx_cuts(B, M::NT);
-    launch_k(k_mx_gateup<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(I / 8, M::GROUP), cuts),
-             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, cuts, 1, rec},
+    launch_k(k_mx_gateup<M>, mx_grid(parts ? nrec : slots + ns, mx_groups(I / 8, M::GROUP), 1),
+             dim3(M::THREADS), 0, st, d, I, E, MxPlan{budget, ns, nrec, (int)parts, 1, rec},
              B * (K + ns), (const uint8_t *)w13, (const uint8_t *)w13s, sptok, (const uint16_t *)x,
              B, (uint16_t *)H, (uint8_t *)Hlo);
   };
@@ -688,12 +682,11 @@ hipError_t launch_mx_down(int B, int d, int I, int E, int K, int budget, int slo
   const int nrec = mx_records(B, K, budget, ns);
   auto go = [&](auto shape) {
     using M = decltype(shape);
-    const int cuts = mx_cuts(B, M::NT);
     static_assert(M::GROUP == MX_DOWN_GROUP && M::KW == 1, "mx_down_shares");
     launch_k(shares > 1 ? k_mx_down<M, true> : k_mx_down<M, false>,
-             mx_grid(parts ? nrec : slots + ns, mx_groups(d / 16, M::GROUP), cuts * shares),
+             mx_grid(parts ? nrec : slots + ns, mx_groups(d / 16, M::GROUP), shares),
              dim3(M::THREADS), 0, st, d, I, E,
-             MxPlan{budget, ns, nrec, (int)parts, cuts, shares, rec}, (const uint8_t *)w2,
+             MxPlan{budget, ns, nrec, (int)parts, shares, rec}, (const uint8_t *)w2,
              (const uint8_t *)w2s, pair_gate, (const uint16_t *)H, (const uint8_t *)Hlo, pairbuf,
              (size_t)B * (K + ns) * d);
   };
@@ -721,7 +714,7 @@ hipError_t launch_mx_down_combine(int B, int d, int I, int E, int K, int budget,
                     : rl == 2 ? k_mx_down_combine<2>
                               : k_mx_down_combine<4>;
   launch_k(kern, dim3(d / 16), dim3(WAVE * nw), (uint32_t)(shares * bytes + nw * ring), st, d, I, E,
-           slots, MxPlan{budget, ns, budget + ns, 0, 1, 1, rec},
+           slots, MxPlan{budget, ns, budget + ns, 0, 1, rec},
            MxFewTail{B, K + ns, shares, pair_of, pair_gate, residual, y}, (const uint8_t *)w2,
            (const uint8_t *)w2s, (const uint16_t *)H, (const uint8_t *)Hlo);
   return hipGetLastError();

@@ -32,11 +32,6 @@ struct NormArgs {
 struct __attribute__((packed, aligned(4))) Any16F { f32x4 v; };
 struct __attribute__((packed, aligned(2))) Any16H { u32x4 v; };
 
-__device__ __forceinline__ float norm_get(const float *p) { return *p; }
-__device__ __forceinline__ float norm_get(const uint16_t *p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void norm_put(float *p, float v) { *p = v; }
-__device__ __forceinline__ void norm_put(uint16_t *p, float v) { *p = f32_to_bf16(v); }
-
 // V (4 or 8) consecutive elements, `left` of them in the row (zeros past it)
 template <int V>
 __device__ __forceinline__ void norm_load(const float *p, int left, float *v) {
