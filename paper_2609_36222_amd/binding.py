@@ -195,15 +195,15 @@ def _stream(stream):
     return stream.cuda_stream
 
 
-def _empty(shape, dtype, device, stream):
-    """A new tensor for a kernel on `stream` to write, in that stream's memory (as
-    under torch.cuda.stream(stream)): memory of the current stream may still be read
-    or written by what was enqueued there before its last tensor was freed."""
+def _empty(near, shape, dtype, stream):
+    """A new tensor on near's device for a kernel on `stream` to write, in that stream's
+    memory (as under torch.cuda.stream(stream)): memory of the current stream may still
+    be read or written by what was enqueued there before its last tensor was freed."""
+    if stream is None:
+        return near.new_empty(shape, dtype=dtype)
     import torch
-    if isinstance(stream, torch.cuda.Stream):
-        with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=device)
-    return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+        return near.new_empty(shape, dtype=dtype)
 
 
 class Layer:
@@ -343,7 +343,7 @@ def packed_layer(layer: "Layer", K: int, stream=None) -> "Layer":
     """A Layer sharing router/predictor tensors, with expert weights packed
     into new tensors by base_pack_experts (one-time, on the device)."""
     w_router, b_router, pred_a, pred_b, w13, w2 = layer.tensors
-    w13p, w2p = (_empty(t.shape, t.dtype, t.device, stream) for t in (w13, w2))
+    w13p, w2p = (_empty(t, t.shape, t.dtype, stream) for t in (w13, w2))
     base_pack_experts(layer.desc(K), w13p, w2p, stream)
     shared = None
     if layer.shared is not None:
@@ -351,7 +351,7 @@ def packed_layer(layer: "Layer", K: int, stream=None) -> "Layer":
         d = base_layer(layer.d, int(w13s.shape[0]), 1, layer.I, layer.dtype, layer.norm_topk,
                        W_ROWMAJOR, 0, None, None, None, None, _ptr(w13s), _ptr(w2s),
                        0, None, None, None)
-        w13sp, w2sp = (_empty(t.shape, t.dtype, t.device, stream) for t in (w13s, w2s))
+        w13sp, w2sp = (_empty(t, t.shape, t.dtype, stream) for t in (w13s, w2s))
         base_pack_experts(d, w13sp, w2sp, stream)
         shared = (w13sp, w2sp, gate)
     return Layer(w_router, b_router, pred_a, pred_b, w13p, w2p,
@@ -386,8 +386,8 @@ def mx_quantize(src, codes=None, scales=None, stream=None):
     dev = _device()
     dt, rows, cols, ld = _rows(src, "src", dev)
     if codes is None and scales is None:
-        codes = _empty((rows, cols // 2), torch.uint8, src.device, stream)
-        scales = _empty((rows, cols // 32), torch.uint8, src.device, stream)
+        codes = _empty(src, (rows, cols // 2), torch.uint8, stream)
+        scales = _empty(src, (rows, cols // 32), torch.uint8, stream)
     else:
         _mx_shapes(codes, scales, (rows,), cols, dev)
     _check(load().base_mx_quantize(dt, _ptr(src), rows, cols, ld, _ptr(codes), _ptr(scales),
@@ -405,7 +405,7 @@ def mx_dequantize(codes, scales, dtype=None, out=None, stream=None):
         dtype = dtype or torch.bfloat16
         if dtype not in (torch.bfloat16, torch.float32):
             raise ValueError("dtype: fp32 or bf16")
-        out = _empty((rows, cols), dtype, codes.device, stream)
+        out = _empty(codes, (rows, cols), dtype, stream)
         dt, ld = BASE_BF16 if dtype is torch.bfloat16 else BASE_F32, cols
     else:
         dt, r, c, ld = _rows(out, "out", dev)
@@ -454,9 +454,9 @@ def _mx_same_shape(what, w13, w2, n, d, I):
         raise ValueError(f"{what}: [{n}, {2 * I}, {d}] and [{n}, {d}, {I}], not {list(w13)} and {list(w2)}")
 
 
-def _mx_out(desc, device, stream):
+def _mx_out(desc, near, stream):
     import torch
-    return tuple(_empty((n,), torch.uint8, device, stream) for n in _mx_sizes(desc))
+    return tuple(_empty(near, (n,), torch.uint8, stream) for n in _mx_sizes(desc))
 
 
 def mx_quantize_experts(w13, w2, stream=None):
@@ -469,7 +469,7 @@ def mx_quantize_experts(w13, w2, stream=None):
             or any(not t.is_contiguous() or t.get_device() != _device() for t in (w13, w2))):
         raise ValueError("w13 [E, 2I, d] and w2 [E, d, I], contiguous fp32 or bf16 on the current GPU")
     desc = _mx_desc(E, d, I, BASE_BF16 if w13.dtype == torch.bfloat16 else BASE_F32, w13, w2)
-    out = _mx_out(desc, w13.device, stream)
+    out = _mx_out(desc, w13, stream)
     _check(load().base_mx_quantize_experts(ctypes.byref(desc), _ptr(out[0]), _ptr(out[1]),
                                            _stream(stream)))
     return out
@@ -483,7 +483,7 @@ def mx_pack_experts(w13, w2, stream=None):
     _mx_shapes(*w13, (E, 2 * I), d, _device())
     _mx_shapes(*w2, (E, d), I, _device())
     desc = _mx_desc(E, d, I)
-    out = _mx_out(desc, w13[0].device, stream)
+    out = _mx_out(desc, w13[0], stream)
     _check(load().base_mx_pack_experts(ctypes.byref(desc), *(_ptr(t) for t in (*w13, *w2, *out)),
                                        _stream(stream)))
     return out
@@ -586,9 +586,9 @@ def norm_residual(h, y=None, post_gain=None, gate=None, pre_gain=None, res_scale
     tensors where they are not given (None where there is nothing to write)."""
     n = Norms(h.shape[1], h.dtype, post_gain, gate, pre_gain, res_scale, eps)
     if h_out is None and y is not None:
-        h_out = _empty(h.shape, h.dtype, h.device, stream)   # rows d apart
+        h_out = _empty(h, h.shape, h.dtype, stream)   # rows d apart
     if x_out is None and pre_gain is not None:
-        x_out = _empty(h.shape, h.dtype, h.device, stream)
+        x_out = _empty(h, h.shape, h.dtype, stream)
     base_norm_residual(n, y, h, h_out, x_out, stream)
     return h_out, x_out
 
@@ -646,7 +646,7 @@ def calib_accumulate(desc, z, B, stats, ws=None, stream=None):
     """Adds one batch of calibration hidden states z [B, d] to stats."""
     import torch
     if ws is None:
-        ws = _empty((int(load().base_calib_ws_bytes(ctypes.byref(desc), B)),), torch.uint8, "cuda", stream)
+        ws = _empty(stats, (int(load().base_calib_ws_bytes(ctypes.byref(desc), B)),), torch.uint8, stream)
     _check(load().base_calib_accumulate(ctypes.byref(desc), _ptr(z), B, _ptr(stats),
                                         _ptr(ws), ws.numel(), _stream(stream)))
     return ws
