@@ -201,6 +201,17 @@ inline bool mx_few(int B, int K, int budget, int ns, int d, int I) {
   if (loads == 4) return slots <= 4 && chunks <= 16;
   return slots <= 15 ? d > 2048 || chunks <= 64 : d >= 2048 && chunks <= 64;
 }
+// A token's nx executed experts out of n_kept, in the plans of small batches: a lane
+// counts the kept keys before its own, which grows with n_kept (a lane each, so 64
+// at most), or nx wavefront maxima are taken.  base_moe_forward, d = 256, I = 64, 61
+// tokens, us, maxima against counting (n_kept): E = 64 nx = 1 (4) 16.1 and 16.5, nx = 2
+// (8) 16.9 and 16.7, (12) 16.5 and 16.9, nx = 3 (16) 17.2 and 16.9, (20) 17.3 and 17.6,
+// nx = 4 (24) 18.1 and 17.7, (40) 19.0 and 19.9, nx = 6 (40) 21.2 and 20.7, (48) 21.2
+// and 21.3, nx = 8 (10) 24.2 and 20.7, (64) 22.8 and 22.9, nx = 16 (64) 31.4 and 25.9; E
+// = 256 later, nx = 4 (40) 22.1 and 22.0, (64) 22.2 and 23.8, nx = 8 (64) 27.7 and 25.1.
+__host__ __device__ inline bool mx_pick_counts(int n_kept, int nx) {
+  return n_kept <= (nx >= 8 ? 64 : 8 * (nx - 1));
+}
 // slots' records, or an upper bound of the parts: the sum over slots of
 // ceil(tiles / MX_NT) is at most (tiles + (MX_NT - 1) slots) / MX_NT
 inline int mx_records(int B, int K, int budget, int ns) {

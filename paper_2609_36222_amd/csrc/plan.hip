@@ -1439,19 +1439,17 @@ __device__ __forceinline__ uint32_t take_best(uint32_t (&k)[NCH], int &e) {
 
 // The first nx of a token's kept experts (lane + 64 c where kept[c], n_kept of them in
 // all) by (logit desc, index asc): lane j < nx gets the j-th, its expert and logit.
-// With few kept ones every lane counts the keys before its own, broadcast from the
-// wavefront's LDS, instead of nx maxima (16 tokens of K = 8 on ten kept experts 6.2
-// -> 4.8 us, four a wavefront of K = 4 on 16 10.0 -> 8.0); with many that takes longer.
+// With few kept ones for the nx (mx_pick_counts) every lane counts the keys before its
+// own, broadcast from the wavefront's LDS, instead of nx maxima.
 struct PickLds {
   __attribute__((aligned(16))) uint64_t key[MAX_E];
   uint64_t got[MAX_K];
 };
-constexpr int PICK_COUNT = 48;   // kept experts at most
 template <int NCH>
 __device__ __forceinline__ void pick_kept(PickLds &S, const bool (&kept)[NCH], int n_kept, int nx,
                                           const float (&lv)[NCH], int &id, float &l) {
   const int lane = lane_id();
-  if (n_kept > PICK_COUNT) {
+  if (!mx_pick_counts(n_kept, nx)) {
     uint32_t left[NCH];
 #pragma unroll
     for (int c = 0; c < NCH; ++c) left[c] = kept[c] ? order_key(lv[c]) : 0u;

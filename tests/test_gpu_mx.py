@@ -263,7 +263,8 @@ def test_layer(gu, bd, shape):
 # with SHAPES, every kernel instance of a 4-bit layer (test_mx_instances.py asks the
 # library's own rules which ones these are)
 INSTANCES = [
-    # the plans, by experts (64, 128, more), tokens a wavefront and kept experts (48, more)
+    # the plans, by experts (64, 128, more), tokens a wavefront and the way they rank the
+    # kept experts
     (256, 128, 4, 64, 1, 3, 0, 0, False, 1, False),
     (256, 128, 8, 64, 16, 60, 0, 0, False, 0, True),
     (256, 128, 8, 64, 48, 20, 0, 1, True, 1, False),
@@ -274,6 +275,11 @@ INSTANCES = [
     (256, 200, 8, 64, 33, 12, 1, 0, False, 0, False),
     (256, 64, 8, 64, 40, 60, 0, 0, False, 1, False),
     (256, 64, 16, 64, 16, 64, 1, 0, False, 1, False),
+    (256, 128, 2, 64, 16, 24, 0, 0, False, 1, True),
+    (256, 200, 8, 64, 10, 40, 0, 0, False, 0, False),
+    (256, 64, 1, 64, 12, 9, 0, 0, False, 1, False),
+    (256, 64, 2, 64, 40, 30, 1, 0, False, 1, False),
+    (256, 128, 3, 64, 33, 40, 0, 0, False, 0, True),
     # gate/up of eight wavefronts side by side, its last row group half there, slots of
     # one to four token tiles
     (256, 64, 4, 832, 72, 64, 0, 0, False, 1, False),

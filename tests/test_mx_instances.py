@@ -21,6 +21,7 @@ extern "C" int shares(int B, int K, int budget, int ns, int d, int I) {
   return mx_down_shares(B, K, budget, ns, d, I);
 }
 extern "C" int parts(int B) { return mx_parts(B); }
+extern "C" int counts(int n_kept, int nx) { return mx_pick_counts(n_kept, nx); }
 extern "C" int few_plan_b() { return FEW_PLAN_B; }
 extern "C" int two_b() { return MX_TWO_B; }
 """ % N_CU
@@ -62,13 +63,15 @@ def test_every_plan_instance_has_a_case(rules):
     experts a lane, tokens a wavefront and the way kept experts are ranked."""
     few, given, dropped = set(), set(), 0
     for d, E, K, I, B, budget, flags, ns, _, _, _ in shapes():
-        lane, many = 1 if E <= 64 else 2 if E <= 128 else 4, min(budget, E) > 48
-        if many:
-            assert B * K >= 48 + min(budget, E) // 4      # a union of that many
+        kept = min(budget, E, B * K)
+        lane, count = 1 if E <= 64 else 2 if E <= 128 else 4, bool(rules.counts(kept, min(K, kept)))
+        if not count and K >= 8:
+            # a union that is as large or, with fewer experts, still beyond the line
+            assert B * K >= 100 and not rules.counts(3 * kept // 4, K)
         if B <= rules.few_plan_b() and not flags & 2:
-            few.add((lane, many))
+            few.add((lane, count))
         if not rules.parts(B) and not flags & 2:
-            given.add((lane, B <= 16, many))
+            given.add((lane, B <= 16, count))
         dropped += bool(flags & 2)
     assert few == {(n, m) for n in (1, 2, 4) for m in (False, True)}
     assert given == {(n, s, m) for n in (1, 2, 4) for s in (False, True) for m in (False, True)}
