@@ -246,7 +246,12 @@ inline MxGateup mx_gateup_shape(int B, int I, int K, int budget, int ns, int n_c
 // 4 kept 129.1 -> 111.1; d = 2048, I = 4096, B = 24, 8 kept 51.9 -> 46.8; and beyond
 // the lines d = 6144, I = 8192, B = 128, 4 kept (192 pairs) 129.7 -> 134.0; d = I =
 // 4096, B = 128, 4 kept (too many values) 71.2 -> 73.7; d = I = 2048, B = 64, 8 kept
-// (few steps) 40.0 -> 41.1.  Six shares at d = I = 4096: 71 -> 81.
+// (few steps) 40.0 -> 41.1.  Six shares at d = I = 4096: 71 -> 81.  Between 128 and 256
+// pairs it depends on the steps: I = 14336, d = 4096, 160 pairs B = 20 to 128 4 to 9% less, 256
+// 0 to 5% less; d = 6144, 144 pairs 3 to 16% less, 240 3% more to none; I = 8192, 160 pairs
+// 8% less to 9% more, 192 6% less to 4% more, 256 up to 10% more; I = 4096 1 to 10% more.
+// (A constant and not the device's own number: a layer's sums keep their order on
+// any partition of it.)
 constexpr int MX_DOWN_GROUP = 8, MX_SPLIT_UNITS = 128, MX_SPLIT_STEPS = 32, MX_SPLIT_MOST = 4;
 constexpr long long MX_SPLIT_VALUES = 24576;
 inline long long mx_split_values(int I) {   // 0: the contraction is not shared

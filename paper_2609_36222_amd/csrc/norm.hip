@@ -117,7 +117,10 @@ __device__ __forceinline__ void norm_store(uint16_t *p, int left, const float *v
 }
 
 // Elements a thread and threads a row: the same for k_norm and k_combine_norm, so
-// that their sums have one order and the block call the bits of its parts.
+// that their sums have one order and the block call the bits of its parts.  (From 513
+// to 1024 a row is one wavefront's with 16; with 8 and two wavefronts, us: 255 rows 4.7
+// -> 3.9; bf16, 8191 rows of 640 13.9 -> 11.4, of 1024 14.4 -> 14.3, 40,000 of 640 52.6 ->
+// 43.9; fp32, 8191 of 640 16.4 -> 14.7, 40,000 of 640 81.1 -> 81.0, of 1000 126 -> 131.)
 __host__ __device__ inline int norm_ept(int d) { return d <= 512 || (d > 1024 && d <= 2048) ? 8 : 16; }
 __host__ __device__ inline int norm_threads(int d) {
   const int per = WAVE * norm_ept(d);
