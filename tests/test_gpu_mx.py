@@ -301,6 +301,44 @@ def test_layer_instances(gu, bd, shape):
     MxCase(gu, bd, d, E, K, I, B, ns, gate, norm_topk, seed=B + E).check(gu, bd, budget, flags, res)
 
 
+@pytest.mark.parametrize("E,K,B,budget,flags,rule,norm_topk", [
+    (16, 6, 1, 4, 2, 0, 1), (16, 6, 9, 5, 3, 0, 0), (100, 8, 16, 7, 2, 2, 1), (200, 5, 12, 9, 3, 0, 0), (40, 4, 16, 40, 0, 0, 1),
+    (128, 16, 16, 30, 1, 2, 0), (256, 16, 5, 64, 2, 1, 1), (24, 6, 33, 5, 0, 2, 1), (200, 8, 64, 90, 1, 0, 0),
+    (128, 8, 80, 20, 3, 3, 1)])
+def test_ties_and_dropped_routes(gu, bd, E, K, B, budget, flags, rule, norm_topk):
+    """Groups of experts with one logit each (+0 and -0 among them), identical tokens
+    and so tied batch scores, a token of zeros; the whole plan, the routes' weights and
+    the scores against the staged calls too."""
+    c = MxCase(gu, bd, 256, E, K, 64, B, rule=rule, norm_topk=norm_topk, seed=E + B)
+    inp, gl = c.inp, c.gl
+    wr, br = inp["w_router"].copy(), inp["b_router"].copy()
+    for experts, bias in ((range(3, 8), 1.5), (range(9, E, 4), -0.0), (range(10, E, 4), 0.0)):
+        for e in experts:
+            wr[e], br[e] = 0.0, bias
+    inp["w_router"], inp["b_router"] = wr, br
+    inp["pred_a"] = np.repeat(inp["pred_a"][::2], 2, 0)[:E].copy()
+    inp["pred_b"] = np.repeat(inp["pred_b"][::2], 2)[:E].copy()
+    inp["x"] = inp["x"].copy()
+    inp["x"][B // 2:] = inp["x"][B // 2]
+    if B > 1:
+        inp["x"][0] = 0.0
+    for t, a in zip(gl.layer.tensors[:4], (wr, br, inp["pred_a"], inp["pred_b"])):
+        t.copy_(torch.from_numpy(a))
+    c.check(gu, bd, budget, flags, True)
+    x = gl.x(inp["x"])
+    logits, ids, w = gl.route(x, B)
+    cost = gl.predict(x, B, ids, w)
+    scores, counts, sel, nsel, _ = gl.select(B, ids, cost, budget)
+    ws, y = gl.workspace(B, budget), gl.y_like(B)
+    got = gu.plan_arrays(bd.base_decode_layer(gl.desc, x, B, budget, flags, None, y, ws), ws, B, K, E, budget, True)
+    for name, t in dict(logits=logits, topk_ids=ids, topk_w=w, cost=cost, scores=scores, counts=counts,
+                        sel_ids=sel).items():
+        assert np.array_equal(got[name], t.cpu().numpy()), name
+    assert got["n_sel"] == int(nsel[0])
+    routes = logits.gather(1, ids.long())
+    assert B == 1 or bool((routes[:, 1:] == routes[:, :-1]).any())      # ties did decide
+
+
 @pytest.mark.parametrize("rule", [1, 2, 3, 4])
 def test_rules(gu, bd, rule):
     MxCase(gu, bd, 256, 16, 4, 64, 9, rule=rule, seed=3).check(gu, bd, 5)
