@@ -325,6 +325,120 @@ base_status base_decode_block(const base_layer *L, const base_norms *N, const vo
                               int32_t budget, int32_t flags, const void *h, void *h_out, void *x_out,
                               base_plan *plan_out, void *ws, size_t ws_bytes, void *stream);
 
+/* The heads of queries, keys and values: rotation by position, a paged cache and the
+ * attention over it.  Heads are given by a pointer and two strides: element e of head h
+ * of row r at p[r row + h head + e], so that they may be parts of wider rows (of one
+ * projection's output, say).  Element alignment suffices; elements between the heads are
+ * not touched. */
+typedef struct base_heads {
+    void *p;
+    int64_t row, head;      /* in elements, 0 to BASE_HEAD_MAX_LD; outputs' heads must not
+                               overlap */
+} base_heads;
+#define BASE_HEAD_MAX_D 256
+#define BASE_MAX_HEADS 1024
+#define BASE_HEAD_MAX_LD (1LL << 40)
+#define BASE_HEAD_MAX_ROWS 0x7FFFFFFFLL
+
+/* Which elements of a head turn together: i and i + rot / 2, or 2 i and 2 i + 1. */
+enum { BASE_ROPE_HALF = 0, BASE_ROPE_INTERLEAVED = 1 };
+
+/* Norm of a head and its rotation by a position p:
+ *   t = gain * x / sqrt(mean x^2 + eps)    (0 where mean x^2 + eps = 0; x without gain)
+ *   (a, b) -> rot_scale (a cos w - b sin w, a sin w + b cos w),  w = p inv_freq[i]
+ * for the pairs i < rot / 2 of t's first `rot` elements; the others are t's.  In fp32
+ * and rounded to `dtype` once; w in fp64 up to its fraction of a turn. */
+typedef struct base_rope {
+    int32_t D;              /* head size: a multiple of 8, 8 to BASE_HEAD_MAX_D */
+    int32_t rot;            /* rotated elements: even, 0 to D */
+    int32_t dtype;          /* base_dtype of the heads */
+    int32_t layout;         /* BASE_ROPE_* */
+    float eps;              /* >= 0 */
+    float rot_scale;        /* finite (1, or a scaled context's factor) */
+    const float *inv_freq;  /* [rot / 2] fp32; not needed if rot = 0 */
+    const float *q_gain;    /* [D] fp32, or NULL: not normalised */
+    const float *k_gain;
+} base_rope;
+
+/*   rows       1 to BASE_HEAD_MAX_ROWS
+ *   positions  [rows] int32 (any sign); not needed if rot = 0
+ *   q, q_out   Hq heads a row (0 to BASE_MAX_HEADS; 0: q and q_out are not looked at)
+ *   k, k_out   Hk heads a row, likewise
+ * An output may be its input, with the same strides; otherwise they must not overlap. */
+base_status base_head_rope(const base_rope *R, int64_t rows, const int32_t *positions, int32_t Hq,
+                           const base_heads *q, const base_heads *q_out, int32_t Hk,
+                           const base_heads *k, const base_heads *k_out, void *stream);
+
+/* A layer's paged cache of keys and values.  Element e of key head h of the token in
+ * slot i of page g lies at k[g k_page + i k_slot + h k_head + e] (v likewise). */
+typedef struct base_kv_cache {
+    int32_t Hk;             /* key heads: 1 to BASE_MAX_HEADS */
+    int32_t D;              /* head size, as base_rope's */
+    int32_t dtype;          /* base_dtype */
+    int32_t page_size;      /* tokens a page: a power of two, 16 to 65536 */
+    int32_t n_pages;        /* >= 1 */
+    void *k, *v;            /* 16-B aligned */
+    int64_t k_page, k_slot, k_head;   /* strides in elements, 0 to BASE_HEAD_MAX_LD, */
+    int64_t v_page, v_slot, v_head;   /* each a multiple of 16 bytes */
+} base_kv_cache;
+
+/* The sequences of a batch and their new tokens.  Row t of the batch belongs to the
+ * sequence s with q_start[s] <= t < q_start[s + 1]; the sequence has kv_len[s] tokens,
+ * its new ones the last of them: row t is token kv_len[s] - q_start[s + 1] + t.  Token i
+ * lies in page table[s table_ld + i / page_size].  These arrays are device data and are
+ * not validated; no access goes out of bounds whatever they hold: starts are taken
+ * within 0 .. rows, lengths within 0 .. max_pages page_size.  A page number outside the
+ * cache is left out by base_kv_append and read as page 0 by base_paged_attention, where
+ * the results are then unspecified; entries of the table past a sequence's last page, or
+ * before the first page that a window leaves, are not looked at. */
+typedef struct base_kv_batch {
+    int32_t n_seq;          /* 1 to BASE_MAX_SEQ */
+    int32_t max_pages;      /* entries of a table row, >= 1; max_pages page_size at most 2^30 */
+    int64_t table_ld;       /* >= max_pages */
+    int32_t max_q;          /* no sequence has more new tokens; rows past it get no attention */
+    const int32_t *table;   /* [n_seq] rows */
+    const int32_t *q_start; /* [n_seq + 1], ascending; a sequence may have no new token */
+    const int32_t *kv_len;  /* [n_seq] */
+} base_kv_batch;
+#define BASE_MAX_SEQ 65536
+
+/* The new tokens on their way into the cache: q (Hq heads) to q_out as base_head_rope,
+ * k (the cache's Hk heads) the same into the cache, v unchanged beside it.
+ *   rows       of q, q_out, k and v; those behind the last sequence are left out, as is a
+ *              token of negative number (more new tokens than kv_len) in the cache
+ *   positions  [rows] int32, or NULL: each token's number in its sequence
+ *   R          its D and dtype are the cache's
+ * Two rows of one slot (sequences that share a page which both write) leave either.
+ * q_out may be q, with the same strides. */
+base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const base_kv_batch *S,
+                           int64_t rows, const int32_t *positions, int32_t Hq, const base_heads *q,
+                           const base_heads *q_out, const base_heads *k, const base_heads *v,
+                           void *stream);
+
+/* Attention of the new tokens over the cache, their own keys in it: for query head h of
+ * token i (its number in the sequence) and key head h / (Hq / Hk), over the keys j of the
+ * sequence with j <= i and, if window > 0, j > i - window,
+ *   out = sum_j e^(scale q.k_j - m) v_j / sum_j e^(scale q.k_j - m),  m the maximum,
+ *   lse = m + log sum_j e^(scale q.k_j - m);
+ * a token that sees no key gets zeros and -infinity.  Products' sums, maxima and sums in
+ * fp32; with 16-bit heads the exponentials are rounded to bf16 for the product with v.
+ * Keys that no new token of its sequence sees may hold anything.  Rows behind the last
+ * sequence are left as they were.  Deterministic run to run.
+ *   rows   of q, out and lse: 1 to BASE_HEAD_MAX_ROWS
+ *   Hq     a multiple of C->Hk, at most BASE_MAX_HEADS
+ *   out    may be q, with the same strides
+ *   lse    [rows][Hq] fp32, or NULL
+ *   scale  finite;  window >= 0 (0: none)
+ *   ws     at least base_attention_workspace_bytes of the same cache, batch (its n_seq,
+ *          max_pages and max_q), rows and Hq; 256-B aligned.  Nothing in it needs a
+ *          value; calls that overlap need one each. */
+size_t base_attention_workspace_bytes(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
+                                      int32_t Hq);
+base_status base_paged_attention(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
+                                 int32_t Hq, const base_heads *q, const base_heads *out, float *lse,
+                                 float scale, int32_t window, void *ws, size_t ws_bytes,
+                                 void *stream);
+
 /* For callers that cannot allocate device memory (code under stream
  * capture, tight serving loops, harnesses that forbid allocation): the same
  * layer as base_decode_layer, with the workspace replaced by a fixed scratch

@@ -29,7 +29,9 @@ EXPORTS = ("base_workspace_bytes", "base_route", "base_predict_cost",
            "base_calib_accumulate",
            "base_mx_quantize", "base_mx_dequantize", "base_mx_w13_bytes", "base_mx_w2_bytes",
            "base_mx_pack_experts", "base_mx_quantize_experts",
-           "base_norm_residual", "base_decode_block")
+           "base_norm_residual", "base_decode_block",
+           "base_head_rope", "base_kv_append", "base_attention_workspace_bytes",
+           "base_paged_attention")
 CALIB_LIB_PATH = os.path.join(HERE, "_lib", "libbase_calib.so")
 N_STAGES = 9     # one kernel each; base_set_stage_events takes 2 events per stage
 STAGES = ("scores", "tail", "select", "backfill", "compact", "gather",
@@ -62,6 +64,27 @@ class base_norms(ctypes.Structure):
     _fields_ = [("d", _i32), ("dtype", _i32), ("eps", ctypes.c_float),
                 ("res_scale", ctypes.c_float), ("post_gain", _vp), ("gate", _vp),
                 ("gate_ld", _i64), ("pre_gain", _vp)]
+
+
+class base_heads(ctypes.Structure):
+    _fields_ = [("p", _vp), ("row", _i64), ("head", _i64)]
+
+
+class base_rope(ctypes.Structure):
+    _fields_ = [("D", _i32), ("rot", _i32), ("dtype", _i32), ("layout", _i32),
+                ("eps", ctypes.c_float), ("rot_scale", ctypes.c_float), ("inv_freq", _vp),
+                ("q_gain", _vp), ("k_gain", _vp)]
+
+
+class base_kv_cache(ctypes.Structure):
+    _fields_ = [("Hk", _i32), ("D", _i32), ("dtype", _i32), ("page_size", _i32),
+                ("n_pages", _i32), ("k", _vp), ("v", _vp), ("k_page", _i64), ("k_slot", _i64),
+                ("k_head", _i64), ("v_page", _i64), ("v_slot", _i64), ("v_head", _i64)]
+
+
+class base_kv_batch(ctypes.Structure):
+    _fields_ = [("n_seq", _i32), ("max_pages", _i32), ("table_ld", _i64), ("max_q", _i32),
+                ("table", _vp), ("q_start", _vp), ("kv_len", _vp)]
 
 
 class BaseError(RuntimeError):
@@ -147,6 +170,18 @@ def load(path: str = LIB_PATH):
     L.base_decode_block.argtypes = [ctypes.POINTER(base_layer), ctypes.POINTER(base_norms), _vp,
                                     _i32, _i32, _i32, _vp, _vp, _vp, ctypes.POINTER(base_plan),
                                     _vp, ctypes.c_size_t, _vp]
+    heads, cache, batch = (ctypes.POINTER(t) for t in (base_heads, base_kv_cache, base_kv_batch))
+    L.base_head_rope.restype = _i32
+    L.base_head_rope.argtypes = [ctypes.POINTER(base_rope), _i64, _vp, _i32, heads, heads, _i32,
+                                 heads, heads, _vp]
+    L.base_kv_append.restype = _i32
+    L.base_kv_append.argtypes = [ctypes.POINTER(base_rope), cache, batch, _i64, _vp, _i32, heads,
+                                 heads, heads, heads, _vp]
+    L.base_attention_workspace_bytes.restype = ctypes.c_size_t
+    L.base_attention_workspace_bytes.argtypes = [cache, batch, _i64, _i32]
+    L.base_paged_attention.restype = _i32
+    L.base_paged_attention.argtypes = [cache, batch, _i64, _i32, heads, heads, _vp,
+                                       ctypes.c_float, _i32, _vp, ctypes.c_size_t, _vp]
     _lib = L
     return L
 
@@ -607,6 +642,198 @@ def base_decode_block(desc, norms: Norms, x, B, budget, flags, h, ws, h_out=None
         _ptr(h_out), _ptr(x_out), ctypes.byref(plan), _ptr(ws), ws.numel() * ws.element_size(),
         _stream(stream)))
     return plan
+
+
+# Heads: rotation by position, a paged cache, attention over it
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+
+
+def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, fast=32.0, slow=1.0):
+    """(inv_freq [rot / 2] fp32 on the CPU, rot_scale) of the angles p base^(-2 i / rot),
+    for contexts `factor` times as long as the trained one.  trained None: every angle is
+    divided by the factor (rot_scale 1).  Else, with the trained length: pairs that turn
+    more than `fast` times over it keep their angle, pairs that turn less than `slow`
+    times have it divided, those between a mixture linear in the pair's number; rot_scale
+    = 0.1 ln(factor) + 1."""
+    import math
+
+    import torch
+    if rot < 0 or rot % 2 or not base > 0 or not factor >= 1:
+        raise ValueError("rot even, base > 0, factor >= 1")
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    inv = float(base) ** (-2.0 * i / max(rot, 1))
+    if factor == 1 or rot == 0:
+        return inv.float(), 1.0
+    if trained is None:
+        return (inv / factor).float(), 1.0
+    if not fast > slow > 0 or trained < 1 or not base > 1:
+        raise ValueError("fast > slow > 0, trained >= 1 and base > 1")
+    # the pair that turns n times over the trained length
+    pair = lambda n: rot * math.log(trained / (n * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
+    lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot // 2 - 1)
+    far = ((i - lo) / max(hi - lo, 0.001)).clamp(0, 1)
+    return (inv * (1 - far) + inv / factor * far).float(), 0.1 * math.log(factor) + 1.0
+
+
+def _heads(t, what, dtype, dev, rows=None, H=None, D=None):
+    """base_heads of a [rows, H, D] tensor with adjacent elements in a head."""
+    if (t.dim() != 3 or t.dtype is not dtype or t.get_device() != dev
+            or (rows is not None and t.shape[0] != rows) or (H is not None and t.shape[1] != H)
+            or (D is not None and t.shape[2] != D) or (t.stride(2) != 1 and t.shape[2] > 1)):
+        shape = ", ".join(str(v) if v is not None else n for n, v in (("rows", rows), ("heads", H), ("D", D)))
+        raise ValueError(f"{what}: {dtype} [{shape}], adjacent elements, on the current GPU")
+    # (one row or one head has no stride to speak of)
+    return base_heads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _ints(t, what, dev, shape=None):
+    import torch
+    if t.dtype is not torch.int32 or t.get_device() != dev or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what}: int32{'' if shape is None else ' ' + str(list(shape))} on the current GPU")
+    return t
+
+
+def _flat(t, what, dev, shape=None):
+    if not _ints(t, what, dev, shape).is_contiguous():
+        raise ValueError(f"{what}: adjacent elements")
+    return t
+
+
+class Rope:
+    """Norms of query and key heads with the rotation by position (base_rope): inv_freq
+    [rot / 2] fp32 (None: no rotation), fp32 gains [D] or None."""
+
+    def __init__(self, D, dtype, inv_freq=None, interleaved=False, rot_scale=1.0, q_gain=None,
+                 k_gain=None, eps=1e-6):
+        import torch
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            raise ValueError("dtype: fp32 or bf16")
+        dev = _device()
+        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        for t, n, what in ((inv_freq, rot // 2, "inv_freq"), (q_gain, D, "q_gain"), (k_gain, D, "k_gain")):
+            if t is not None and (t.dtype is not torch.float32 or t.shape != (n,) or not t.is_contiguous()
+                                  or t.get_device() != dev):
+                raise ValueError(f"{what}: fp32, {n} adjacent elements, on the current GPU")
+        self.tensors = (inv_freq, q_gain, k_gain)
+        self.D, self.rot, self.torch_dtype = D, rot, dtype
+        self.desc = base_rope(D, rot, BASE_BF16 if dtype is torch.bfloat16 else BASE_F32,
+                              ROPE_INTERLEAVED if interleaved else ROPE_HALF, eps, rot_scale,
+                              _ptr(inv_freq), _ptr(q_gain), _ptr(k_gain))
+
+
+class KVCache:
+    """A paged cache (base_kv_cache): k and v [pages, page size, Hk, D], fp32 or bf16,
+    views with any strides of 16 bytes' multiples (pages that hold their tokens head by
+    head are such a view) and adjacent elements in a head."""
+
+    def __init__(self, k, v):
+        import torch
+        dev = _device()
+        for t, what in ((k, "k"), (v, "v")):
+            if (t.dim() != 4 or t.shape != k.shape or t.dtype is not k.dtype or t.get_device() != dev
+                    or t.dtype not in (torch.bfloat16, torch.float32) or t.stride(3) != 1):
+                raise ValueError(f"{what}: fp32 or bf16 [pages, page size, heads, D], adjacent elements, k's "
+                                 "and v's alike, on the current GPU")
+        self.tensors = (k, v)
+        self.torch_dtype = k.dtype
+        self.n_pages, self.page_size, self.Hk, self.D = k.shape
+        ld = [t.stride(i) if t.shape[i] > 1 else 0 for t in (k, v) for i in (0, 1, 2)]
+        self.desc = base_kv_cache(self.Hk, self.D, BASE_BF16 if k.dtype is torch.bfloat16 else BASE_F32,
+                                  self.page_size, self.n_pages, _ptr(k), _ptr(v), *ld)
+
+
+class KVBatch:
+    """The sequences of a batch (base_kv_batch): int32 table [n_seq, pages], q_start
+    [n_seq + 1], kv_len [n_seq]; max_q: the most new tokens of a sequence.  The tensors'
+    contents may change between calls."""
+
+    def __init__(self, table, q_start, kv_len, max_q):
+        dev = _device()
+        n = kv_len.shape[0] if kv_len.dim() == 1 else -1
+        if table.dim() != 2 or table.shape[0] != n or (table.stride(1) != 1 and table.shape[1] > 1):
+            raise ValueError("table: int32 [n_seq, pages], adjacent entries")
+        _ints(table, "table", dev)
+        self.tensors = (table, _flat(q_start, "q_start", dev, (n + 1,)), _flat(kv_len, "kv_len", dev))
+        self.n_seq, self.max_q = n, max_q
+        self.desc = base_kv_batch(n, table.shape[1], table.stride(0) if n > 1 else table.shape[1], max_q,
+                                  *(_ptr(t) for t in self.tensors))
+
+
+def base_head_rope(rope: Rope, positions, q, k, q_out, k_out, stream=None):
+    """q_out and k_out [rows, heads, D] from q and k (either pair None) at int32 positions
+    [rows] (None where nothing rotates)."""
+    dev, args, n = _device(), [], None
+    for t, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if t is None or out is None:
+            if t is not None or out is not None:
+                raise ValueError(f"{what} and {what}_out: both or neither")
+            args += [0, None, None]
+            continue
+        n = t.shape[0] if n is None else n
+        args += [t.shape[1], _heads(t, what, rope.torch_dtype, dev, n, None, rope.D),
+                 _heads(out, what + "_out", rope.torch_dtype, dev, n, t.shape[1], rope.D)]
+    if n is None:
+        raise ValueError("q or k")
+    if positions is not None:
+        _flat(positions, "positions", dev, (n,))
+    _check(load().base_head_rope(rope.desc, n, _ptr(positions), *args, _stream(stream)))
+
+
+def head_rope(rope: Rope, positions, q, k=None, stream=None):
+    """base_head_rope into new tensors; returns (q_out, k_out or None)."""
+    out = [None if t is None else _empty(t, t.shape, t.dtype, stream) for t in (q, k)]
+    base_head_rope(rope, positions, q, k, *out, stream)
+    return tuple(out)
+
+
+def base_kv_append(rope: Rope, cache: KVCache, batch: KVBatch, q, k, v, q_out, positions=None, stream=None):
+    """The new tokens' k [rows, Hk, D], normalised and rotated, and v into the cache; q
+    [rows, Hq, D] the same to q_out.  positions: int32 [rows], or None: the tokens' numbers
+    in their sequences."""
+    dev, dt = _device(), rope.torch_dtype
+    n, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    if positions is not None:
+        _flat(positions, "positions", dev, (n,))
+    _check(load().base_kv_append(
+        rope.desc, cache.desc, batch.desc, n, _ptr(positions), Hq, _heads(q, "q", dt, dev, n, Hq, rope.D),
+        _heads(q_out, "q_out", dt, dev, n, Hq, rope.D), _heads(k, "k", dt, dev, n, cache.Hk, rope.D),
+        _heads(v, "v", dt, dev, n, cache.Hk, rope.D), _stream(stream)))
+
+
+def attention_workspace_bytes(cache: KVCache, batch: KVBatch, rows, Hq) -> int:
+    n = int(load().base_attention_workspace_bytes(cache.desc, batch.desc, rows, Hq))
+    if n == 0:
+        raise BaseError(-2, status_string(-2))
+    return n
+
+
+def base_paged_attention(cache: KVCache, batch: KVBatch, q, out, ws, scale=None, window=0, lse=None,
+                         stream=None):
+    """out [rows, Hq, D] (and lse [rows, Hq] fp32) of q over the cache; scale None: 1 /
+    sqrt(D); ws: a uint8 tensor of attention_workspace_bytes."""
+    import torch
+    dev, dt = _device(), cache.torch_dtype
+    n, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, Hq) or not lse.is_contiguous()
+                            or lse.get_device() != dev):
+        raise ValueError(f"lse: contiguous fp32 {[n, Hq]} on the current GPU")
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws: contiguous, on the current GPU")
+    _check(load().base_paged_attention(
+        cache.desc, batch.desc, n, Hq, _heads(q, "q", dt, dev, n, Hq, cache.D),
+        _heads(out, "out", dt, dev, n, Hq, cache.D), _ptr(lse), cache.D ** -0.5 if scale is None else scale,
+        window, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def paged_attention(q, cache: KVCache, batch: KVBatch, scale=None, window=0, return_lse=False, stream=None):
+    """base_paged_attention into a new tensor, with a workspace of its own; returns out, or
+    (out, lse)."""
+    import torch
+    out = _empty(q, q.shape, q.dtype, stream)
+    lse = _empty(q, q.shape[:2], torch.float32, stream) if return_lse else None
+    ws = _empty(q, (attention_workspace_bytes(cache, batch, q.shape[0], q.shape[1]),), torch.uint8, stream)
+    base_paged_attention(cache, batch, q, out, ws, scale, window, lse, stream)
+    return (out, lse) if return_lse else out
 
 
 def base_set_stage_events(events):

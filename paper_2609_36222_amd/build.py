@@ -23,7 +23,7 @@ LIB = os.path.join(OUT_DIR, "libbase.so")
 PROBE_LIB = os.path.join(OUT_DIR, "libbase_probe.so")   # bench's streaming-read probe
 CALIB_LIB = os.path.join(OUT_DIR, "libbase_calib.so")   # predictor fit (links rocSOLVER)
 SOURCES = ["api.hip", "scores.hip", "plan.hip", "ffn.hip", "ffn_mx.hip", "mx.hip",
-           "norm.hip", "pack.hip", "calib.hip"]
+           "norm.hip", "heads.hip", "attn.hip", "pack.hip", "calib.hip"]
 ARCH = os.environ.get("BASE_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -22,6 +22,7 @@ static_assert(FLAG_UNIT_GATES != BASE_GATE_RENORM && FLAG_UNIT_GATES != BASE_FIL
               "internal flag bit");
 
 static_assert(MAX_NORM_D == BASE_NORM_MAX_D, "norm limits");
+static_assert(MAX_HEAD_D == BASE_HEAD_MAX_D, "head sizes");
 static_assert(SCORE_BASE == BASE_SCORE_BASE && SCORE_TOP1 == BASE_SCORE_TOP1 &&
                   SCORE_WEIGHT == BASE_SCORE_WEIGHT && SCORE_WEIGHT_SQ == BASE_SCORE_WEIGHT_SQ &&
                   SCORE_STATIC == BASE_SCORE_STATIC,
@@ -693,6 +694,141 @@ base_status base_decode_block(const base_layer *L, const base_norms *N, const vo
   if (N->gate && N->gate_ld % 4) return BASE_ERR_ALIGN;
   return decode_layer(L, x, B, budget, flags, Tail{nullptr, nullptr, N, h, h_out, x_out}, plan_out, ws,
                       ws_bytes, stream);
+}
+
+// ------------------------------------------------------------- heads --
+static base_status check_heads(const base_heads *h, int32_t dtype) {
+  if (!h || !h->p) return BASE_ERR_NULL;
+  if (h->row < 0 || h->row > BASE_HEAD_MAX_LD || h->head < 0 || h->head > BASE_HEAD_MAX_LD)
+    return BASE_ERR_SHAPE;
+  return aligned(h->p, elem_bytes(dtype)) ? BASE_OK : BASE_ERR_ALIGN;
+}
+// in place only element by element
+static bool moved(const base_heads *a, const base_heads *b) {
+  return a->p == b->p && (a->row != b->row || a->head != b->head);
+}
+static HeadRows head_rows(const base_heads *h) { return {h->p, h->row, h->head}; }
+
+static base_status check_rope(const base_rope *R, int64_t rows) {
+  if (!R) return BASE_ERR_NULL;
+  if (R->dtype != BASE_F32 && R->dtype != BASE_BF16) return BASE_ERR_DTYPE;
+  if (R->D < 8 || R->D > BASE_HEAD_MAX_D || R->D % 8 || R->rot < 0 || R->rot > R->D || R->rot % 2)
+    return BASE_ERR_SHAPE;
+  if (rows < 1 || rows > BASE_HEAD_MAX_ROWS) return BASE_ERR_SHAPE;
+  if (!(R->eps >= 0.0f) || !std::isfinite(R->eps) || !std::isfinite(R->rot_scale)) return BASE_ERR_SHAPE;
+  if (R->layout != BASE_ROPE_HALF && R->layout != BASE_ROPE_INTERLEAVED) return BASE_ERR_FLAGS;
+  if (R->rot > 0 && !R->inv_freq) return BASE_ERR_NULL;
+  if (!aligned(R->inv_freq, 4) || !aligned(R->q_gain, 4) || !aligned(R->k_gain, 4)) return BASE_ERR_ALIGN;
+  return BASE_OK;
+}
+static RopeArgs rope_args(const base_rope *R) {
+  return {R->D, R->rot, R->layout == BASE_ROPE_INTERLEAVED, R->eps, R->rot_scale, R->inv_freq,
+          R->q_gain, R->k_gain};
+}
+
+static base_status check_cache(const base_kv_cache *C, const base_kv_batch *S, bool pointers) {
+  if (!C || !S) return BASE_ERR_NULL;
+  if (C->dtype != BASE_F32 && C->dtype != BASE_BF16) return BASE_ERR_DTYPE;
+  if (C->Hk < 1 || C->Hk > BASE_MAX_HEADS || C->D < 8 || C->D > BASE_HEAD_MAX_D || C->D % 8)
+    return BASE_ERR_SHAPE;
+  if (C->page_size < 16 || C->page_size > 65536 || (C->page_size & (C->page_size - 1))) return BASE_ERR_SHAPE;
+  if (C->n_pages < 1 || S->n_seq < 1 || S->n_seq > BASE_MAX_SEQ || S->max_pages < 1 ||
+      S->max_pages > (1 << 30) / C->page_size || S->max_q < 1)
+    return BASE_ERR_SHAPE;
+  if (!pointers) return BASE_OK;
+  const int64_t piece = 16 / elem_bytes(C->dtype);
+  for (int64_t ld : {C->k_page, C->k_slot, C->k_head, C->v_page, C->v_slot, C->v_head}) {
+    if (ld < 0 || ld > BASE_HEAD_MAX_LD) return BASE_ERR_SHAPE;
+    if (ld % piece) return BASE_ERR_ALIGN;
+  }
+  if (S->table_ld < S->max_pages || S->table_ld > BASE_HEAD_MAX_LD) return BASE_ERR_SHAPE;
+  BASE_TRY(check_ptr(C->k, 16));
+  BASE_TRY(check_ptr(C->v, 16));
+  BASE_TRY(check_ptr(S->table, 4));
+  BASE_TRY(check_ptr(S->q_start, 4));
+  return check_ptr(S->kv_len, 4);
+}
+static KvCache kv_cache(const base_kv_cache *C) {
+  return {C->k, C->v, C->k_page, C->k_slot, C->k_head, C->v_page, C->v_slot, C->v_head, C->n_pages,
+          __builtin_ctz(C->page_size), C->Hk};
+}
+static KvBatch kv_batch(const base_kv_batch *S) {
+  return {S->table, S->q_start, S->kv_len, S->table_ld, S->n_seq, S->max_pages, S->max_q};
+}
+
+base_status base_head_rope(const base_rope *R, int64_t rows, const int32_t *positions, int32_t Hq,
+                           const base_heads *q, const base_heads *q_out, int32_t Hk,
+                           const base_heads *k, const base_heads *k_out, void *stream) {
+  BASE_TRY(check_rope(R, rows));
+  if (Hq < 0 || Hq > BASE_MAX_HEADS || Hk < 0 || Hk > BASE_MAX_HEADS || Hq + Hk < 1) return BASE_ERR_SHAPE;
+  if (R->rot > 0) BASE_TRY(check_ptr(positions, 4));
+  HeadRows at[4] = {};
+  const base_heads *hs[4] = {Hq ? q : nullptr, Hq ? q_out : nullptr, Hk ? k : nullptr, Hk ? k_out : nullptr};
+  for (int i = 0; i < 4; ++i) {
+    if (!(i < 2 ? Hq : Hk)) continue;
+    BASE_TRY(check_heads(hs[i], R->dtype));
+    at[i] = head_rows(hs[i]);
+  }
+  for (int i = 0; i < 4; i += 2)
+    if (hs[i] && moved(hs[i], hs[i + 1])) return BASE_ERR_FLAGS;
+  HIP_TRY(launch_heads(R->dtype == BASE_BF16, rope_args(R), rows, R->rot > 0 ? positions : nullptr, Hq,
+                       at[0], at[1], Hk, at[2], at[3], HeadRows{}, nullptr, nullptr, (hipStream_t)stream));
+  return BASE_OK;
+}
+
+base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const base_kv_batch *S,
+                           int64_t rows, const int32_t *positions, int32_t Hq, const base_heads *q,
+                           const base_heads *q_out, const base_heads *k, const base_heads *v,
+                           void *stream) {
+  BASE_TRY(check_rope(R, rows));
+  BASE_TRY(check_cache(C, S, true));
+  if (R->D != C->D) return BASE_ERR_SHAPE;
+  if (R->dtype != C->dtype) return BASE_ERR_DTYPE;
+  if (Hq < 1 || Hq > BASE_MAX_HEADS) return BASE_ERR_SHAPE;
+  for (const base_heads *h : {q, q_out, k, v}) BASE_TRY(check_heads(h, R->dtype));
+  if (moved(q, q_out)) return BASE_ERR_FLAGS;
+  if (!aligned(positions, 4)) return BASE_ERR_ALIGN;
+  const KvCache c = kv_cache(C);
+  const KvBatch b = kv_batch(S);
+  HIP_TRY(launch_heads(R->dtype == BASE_BF16, rope_args(R), rows, positions, Hq, head_rows(q),
+                       head_rows(q_out), C->Hk, head_rows(k), HeadRows{}, head_rows(v), &c, &b,
+                       (hipStream_t)stream));
+  return BASE_OK;
+}
+
+static base_status check_attention(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
+                                   int32_t Hq, bool pointers) {
+  BASE_TRY(check_cache(C, S, pointers));
+  if (rows < 1 || rows > BASE_HEAD_MAX_ROWS || Hq < 1 || Hq > BASE_MAX_HEADS || Hq % C->Hk)
+    return BASE_ERR_SHAPE;
+  // a sequence's packed rows are counted in 32 bits
+  return S->max_q > 0x40000000 / (Hq / C->Hk) ? BASE_ERR_SHAPE : BASE_OK;
+}
+
+size_t base_attention_workspace_bytes(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
+                                      int32_t Hq) {
+  if (check_attention(C, S, rows, Hq, false) != BASE_OK) return 0;
+  return attn_ws_bytes(C->dtype == BASE_BF16, C->D, Hq, kv_cache(C), kv_batch(S), rows, device_cus());
+}
+
+base_status base_paged_attention(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
+                                 int32_t Hq, const base_heads *q, const base_heads *out, float *lse,
+                                 float scale, int32_t window, void *ws, size_t ws_bytes,
+                                 void *stream) {
+  BASE_TRY(check_attention(C, S, rows, Hq, true));
+  if (!std::isfinite(scale) || window < 0) return BASE_ERR_SHAPE;
+  BASE_TRY(check_heads(q, C->dtype));
+  BASE_TRY(check_heads(out, C->dtype));
+  if (moved(q, out)) return BASE_ERR_FLAGS;
+  if (!aligned(lse, 4)) return BASE_ERR_ALIGN;
+  BASE_TRY(check_ptr(ws, 256));
+  const KvCache c = kv_cache(C);
+  const KvBatch b = kv_batch(S);
+  const int n_cu = device_cus();
+  const AttnCall a{C->dtype == BASE_BF16, C->D, Hq, window, scale, rows, head_rows(q), head_rows(out), lse};
+  if (ws_bytes < attn_ws_bytes(a.bf16, a.D, Hq, c, b, rows, n_cu)) return BASE_ERR_WORKSPACE;
+  HIP_TRY(launch_attn(a, c, b, ws, n_cu, (hipStream_t)stream));
+  return BASE_OK;
 }
 
 base_status base_decode_layer_noalloc(const base_layer *L, const void *x, int32_t B,

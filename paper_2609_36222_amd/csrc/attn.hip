@@ -1,0 +1,471 @@
+// Attention of each sequence's new tokens over its paged cache:
+//   o = sum_j e^(c q.k_j - m) v_j / sum_j e^(c q.k_j - m)    over the keys j that the
+// token sees (its own position and those before it, of a window if there is one), in one
+// pass over the keys with the running maximum m and sum.
+//
+// The products are made transposed, S^T = K Q^T and O^T = V^T P^T: a lane's accumulators
+// then belong to one packed row (query head and token), so m and the sum are values of
+// the lane, and S^T's registers, rounded, are the operand P^T of the second product as
+// they lie: its keys are taken in the order in which the first product left them.
+//
+// k_attn_few: tiles of 32 packed rows, the wavefronts on blocks of keys of their own,
+// joined through LDS at the unit's end.  16-bit rows come asynchronously to a ring in
+// LDS (wavefront's own: no barrier in the loop), where 16-byte pieces are permuted so that
+// neither product's operand reads meet in a bank; V's operand is read transposed.
+#include "attn.hpp"
+#include "ffn.hpp"
+
+namespace basek {
+
+namespace {
+
+// 16 bytes of zeros: what a lane reads in the place of a key or element that is not there
+__device__ __attribute__((aligned(16))) uint32_t g_zero[4];
+
+typedef __attribute__((address_space(3))) void *lds_p;
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x4 *lds_b4;
+
+// 16 bytes per lane from global memory to LDS, lane l's at lds + 16 l (lds uniform).  The
+// compiler's builtin makes every transposed read wait for all such loads, those of the
+// steps ahead among them; here the reader waits for its own (wait_vm).  No register is
+// written; a wait of the compiler's for a load of its own is only the longer for these.
+// (m0 holds nothing that the compiler keeps: it sets it in front of each use.)
+__device__ __forceinline__ uint32_t lds_addr(const void *p) {
+  return (uint32_t)(uintptr_t)(lds_p)p;
+}
+__device__ __forceinline__ void glb_to_lds(const char *p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory");
+}
+// Four 16-bit elements a lane, transposed in groups of 16 lanes: lane 4 r + c gives the
+// address of elements 4 c .. + 3 of row r, and lane i gets element i of the rows 0 .. 3
+__device__ __forceinline__ bf16x4 read_tr(const char *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_b4)(lds_p)p);
+}
+
+struct __attribute__((packed, aligned(2))) Any16H { u32x4 v; };
+struct __attribute__((packed, aligned(4))) Any16F { f32x4 v; };
+struct __attribute__((packed, aligned(2))) Any8H { u32x2 v; };
+
+__device__ __forceinline__ void put4(uint16_t *p, f32x4 v) {
+  u32x2 q;
+  q[0] = (uint32_t)f32_to_bf16_any(v[0]) | ((uint32_t)f32_to_bf16_any(v[1]) << 16);
+  q[1] = (uint32_t)f32_to_bf16_any(v[2]) | ((uint32_t)f32_to_bf16_any(v[3]) << 16);
+  reinterpret_cast<Any8H *>(p)->v = q;
+}
+__device__ __forceinline__ void put4(float *p, f32x4 v) { reinterpret_cast<Any16F *>(p)->v = v; }
+
+// m's rise that is left to the products' exponents: P stays below 2^LAG, and the
+// accumulators are rescaled only when the maximum has risen by more
+constexpr float LAG = 8.0f;
+
+template <typename T, int DP_>
+struct FewShape {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int DP = DP_, NR = 2, R = 16 * NR;
+  static constexpr int TK = BF ? 32 : 16;                  // keys of a wavefront's step
+  static constexpr int WAVES = BF && DP == 256 ? 2 : 4, THREADS = WAVES * WAVE, BK = WAVES * TK;
+  static constexpr int CH = DP / 8;                        // 16-byte pieces of a 16-bit row
+  static constexpr int ROWB = DP * 2, STAGE = 2 * TK * ROWB, RING = 2, LOADS = CH;
+  static constexpr int JOIN = WAVES * R * (DP + 2) * 4;
+  static constexpr int LDS = BF && WAVES * RING * STAGE > JOIN ? WAVES * RING * STAGE : JOIN;
+};
+
+// pieces' places in a row of the ring: K's row r at piece ^ few_k(r), V's at piece ^ few_v(r)
+template <int CH> __device__ __forceinline__ int few_k(int r) { return CH == 8 ? (r >> 1) & 7 : r & 15; }
+template <int CH> __device__ __forceinline__ int few_v(int r) { return CH == 8 ? 2 * ((r >> 1) & 3) : 2 * (r & 7); }
+
+template <typename T, int DP>
+__global__ __launch_bounds__((FewShape<T, DP>::THREADS), 1)
+void k_attn_few(AttnArgs a) {
+  using M = FewShape<T, DP>;
+  constexpr bool BF = M::BF;
+  constexpr int R = M::R, NR = M::NR, TK = M::TK;
+  constexpr int DT = DP / 16;                     // accumulator tiles
+  constexpr int QS = BF ? DP / 32 : DP / 16;      // operand pieces of 16 bytes
+  __shared__ __attribute__((aligned(256))) char lds[M::LDS];
+  const int wave = wave_id_u(), lane = lane_id(), n = lane % 16, g = lane / 16;
+  const int w = blockIdx.x;
+  const char *zero = reinterpret_cast<const char *>(g_zero);
+  AttnPart begun{};
+  AttnWork<R, M::BK> work(a, w);
+  typename AttnWork<R, M::BK>::Segment sg;
+  while (work.next(sg, begun)) {
+    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = sg.n > 16 ? 2 : 1;
+    int pos[NR];
+    u32x4 qv[NR][QS];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const int r = 16 * c + n, pr = sg.r0 + min(r, sg.n - 1), tok = pr / a.G;
+      pos[c] = r < sg.n ? work.q.pos0 + tok : -1;
+      const T *p = (const T *)a.q.p + (long long)(work.q.first + tok) * a.q.row +
+                   (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
+#pragma unroll
+      for (int s = 0; s < QS; ++s) {
+        const int d = BF ? 32 * s + 8 * g : 16 * s + 4 * g;
+        const T *at = p + min(d, a.D - (BF ? 8 : 4));
+        u32x4 v;
+        if constexpr (BF) v = reinterpret_cast<const Any16H *>(at)->v;
+        else v = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
+        qv[c][s] = d < a.D ? v : u32x4{0, 0, 0, 0};
+      }
+    }
+    const int pmin = work.q.pos0 + sg.r0 / a.G, pmax = work.q.pos0 + (sg.r0 + sg.n - 1) / a.G;
+    f32x4 acc[NR][DT];
+    float m[NR], l[NR];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      m[c] = -INFINITY;
+      l[c] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) acc[c][t] = f32x4{0, 0, 0, 0};
+    }
+
+    // the wavefront's steps: keys key0(i) .. + TK - 1 with a key in [lo, hi)
+    auto key0 = [&](int i) { return i * M::BK + wave * TK; };
+    int i0 = sg.k0, i1 = sg.k1;
+    while (i0 < i1 && key0(i0) + TK <= lo) ++i0;
+    while (i1 > i0 && key0(i1 - 1) >= hi) --i1;
+
+    // p (rounded for the second product) from the products of a step, and m, l, acc's scale
+    auto soften = [&](int c, int k0, float (&x)[TK / 4]) {
+      const bool cut = k0 + TK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window) || c * 16 + 16 > sg.n;
+      float top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < TK / 4; ++e) x[e] = x[e] * a.scale;
+      if (cut) {
+#pragma unroll
+        for (int e = 0; e < TK / 4; ++e) {
+          const int key = k0 + 16 * (e / 4) + 4 * g + e % 4;
+          const bool seen = key <= pos[c] && (a.window == 0 || key > pos[c] - a.window);
+          x[e] = seen ? x[e] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < TK / 4; ++e) top = fmaxf(top, x[e]);
+      top = fmaxf(top, xor_lane<16>(top));
+      top = fmaxf(top, xor_lane<32>(top));
+      if (__any(top > m[c] + LAG)) {
+        const float to = fmaxf(m[c], top), f = m[c] == to ? 1.0f : __builtin_amdgcn_exp2f(m[c] - to);
+        m[c] = to;
+        l[c] *= f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[c][t][e] *= f;
+      }
+      const float mm = m[c] == -INFINITY ? 0.0f : m[c];
+#pragma unroll
+      for (int e = 0; e < TK / 4; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(x[e] - mm);
+        l[c] += x[e];
+      }
+    };
+
+    if constexpr (BF) {
+      char *ring = lds + wave * M::RING * M::STAGE;
+      const uint32_t ring_at = lds_addr(ring);
+      // the pages of 32 steps at a time, two a step (16 keys lie in one page): lane l has
+      // those of step from + l / 2
+      int from = i0, pages = 0;
+      auto fetch_pages = [&](int i) {
+        from = i;
+        const int key = key0(i + lane / 2) + 16 * (lane & 1);
+        pages = attn_page(a, work.s, min(key, hi - 1));
+      };
+      auto issue = [&](int i) {
+        if (i - from >= 32) fetch_pages(i);
+        const int k0 = key0(i);
+        const uint32_t st = ring_at + (i & 1) * M::STAGE;
+        const bool all = k0 >= lo && k0 + TK <= hi && a.D == DP;
+        const char *kb[2], *vb[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int key = k0 + 16 * h;
+          const long long page = __builtin_amdgcn_readlane(pages, 2 * (i - from) + h);
+          const long long slot = key & ((1 << a.c.shift) - 1);
+          kb[h] = (const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head);
+          vb[h] = (const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head);
+        }
+#pragma unroll
+        for (int j = 0; j < M::CH / 2; ++j) {
+          const int row = (lane + WAVE * j) / M::CH, at = (lane + WAVE * j) % M::CH;
+          const int ck = at ^ few_k<M::CH>(row), cv = at ^ few_v<M::CH>(row);
+          const int h = WAVE * j / M::CH / 16;
+          const char *pk = kb[h] + 2 * ((row & 15) * a.c.k_slot + 8 * ck);
+          const char *pv = vb[h] + 2 * ((row & 15) * a.c.v_slot + 8 * cv);
+          if (!all) {
+            const bool in = k0 + row >= lo && k0 + row < hi;
+            pk = in && 8 * ck < a.D ? pk : zero;
+            pv = in && 8 * cv < a.D ? pv : zero;
+          }
+          glb_to_lds(pk, st + j * 1024);
+          glb_to_lds(pv, st + TK * M::ROWB + j * 1024);
+        }
+      };
+      if (i0 < i1) {
+        fetch_pages(i0);
+        issue(i0);
+      }
+      if (i0 + 1 < i1) issue(i0 + 1);
+      for (int i = i0; i < i1; ++i) {
+        if (i + 1 < i1) wait_vm<M::LOADS>();
+        else wait_vm<0>();
+        const char *st = ring + (i & 1) * M::STAGE, *sv = st + TK * M::ROWB;
+        const int k0 = key0(i);
+        f32x4 s[NR][2];
+#pragma unroll
+        for (int c = 0; c < NR; ++c) s[c][0] = s[c][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int q = 0; q < QS; ++q) {
+            const int row = 16 * b + n;
+            const bf16x8 kv = *reinterpret_cast<const bf16x8 *>(
+                st + row * M::ROWB + (((4 * q + g) ^ few_k<M::CH>(row)) * 16));
+            s[0][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[0][q]), s[0][b]);
+            if (nr > 1) s[1][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[1][q]), s[1][b]);
+          }
+        bf16x8 p[NR];
+#pragma unroll
+        for (int c = 0; c < NR; ++c) {
+          if (c < nr) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[c][e / 4][e % 4];
+            soften(c, k0, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)x[e];
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          const int row = 4 * g + n / 4, piece = 2 * t + (n & 3) / 2;
+          const char *at = sv + row * M::ROWB + ((piece ^ few_v<M::CH>(row)) * 16) + (n & 1) * 8;
+          const bf16x4 v0 = read_tr(at), v1 = read_tr(at + 16 * M::ROWB);
+          const bf16x8 vv = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+          acc[0][t] = mfma16(vv, p[0], acc[0][t]);
+          if (nr > 1) acc[1][t] = mfma16(vv, p[1], acc[1][t]);
+        }
+        // this stage's reads are done before its next rows are requested
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + 2 < i1) issue(i + 2);
+      }
+    } else {
+      for (int i = i0; i < i1; ++i) {
+        const int k0 = key0(i);
+        const long long page = attn_page(a, work.s, k0), slot = k0 & ((1 << a.c.shift) - 1);
+        const float *kb = (const float *)a.c.k + page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head;
+        const float *vb = (const float *)a.c.v + page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head;
+        const float *zf = reinterpret_cast<const float *>(zero);
+        f32x4 kv[QS];
+        const bool kin = k0 + n >= lo && k0 + n < hi;
+#pragma unroll
+        for (int q = 0; q < QS; ++q) {
+          const int d = 16 * q + 4 * g;
+          kv[q] = *reinterpret_cast<const f32x4 *>(kin && d < a.D ? kb + n * a.c.k_slot + d : zf);
+        }
+        float vv[4][DT];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = k0 + 4 * g + e;
+          const bool vin = key >= lo && key < hi;
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+            vv[e][t] = *(vin && 16 * t + n < a.D ? vb + (4 * g + e) * a.c.v_slot + 16 * t + n : zf);
+        }
+#pragma unroll
+        for (int c = 0; c < NR; ++c) {
+          if (c >= nr) continue;
+          f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+          for (int q = 0; q < QS; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[q][e], __uint_as_float(qv[c][q][e]), s, 0, 0, 0);
+          float x[4] = {s[0], s[1], s[2], s[3]};
+          soften(c, k0, x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+              acc[c][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[e][t], x[e], acc[c][t], 0, 0, 0);
+        }
+      }
+    }
+
+    // the wavefronts' states, joined in their order
+    float *join = reinterpret_cast<float *>(lds), *ml = join + M::WAVES * R * DP;
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      if (c >= nr) continue;
+      float t = l[c];
+      t = t + xor_lane<16>(t);
+      t = t + xor_lane<32>(t);
+      const int row = wave * R + 16 * c + n;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)   // pieces of 16 bytes permuted: a row is 2 to 8 times all banks
+        *reinterpret_cast<f32x4 *>(join + row * DP + 4 * ((4 * d + g) ^ n)) = acc[c][d];
+      if (g == 0) {
+        ml[2 * row] = m[c];
+        ml[2 * row + 1] = t;
+      }
+    }
+    __syncthreads();
+    for (int u = threadIdx.x; u < sg.n * (DP / 4); u += M::THREADS) {
+      const int r = u / (DP / 4), piece = u % (DP / 4);
+      float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < M::WAVES; ++v) top = fmaxf(top, ml[2 * (v * R + r)]);
+      const float mm = top == -INFINITY ? 0.0f : top;
+      f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+      for (int v = 0; v < M::WAVES; ++v) {
+        const float f = __builtin_amdgcn_exp2f(ml[2 * (v * R + r)] - mm);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(join + (v * R + r) * DP + 4 * (piece ^ (r & 15)));
+        sum = __builtin_fmaf(f, ml[2 * (v * R + r) + 1], sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
+      }
+      if (sg.slot >= 0) {
+        float *part = a.part + sg.slot * attn_part_floats<R, DP>();
+        *reinterpret_cast<f32x4 *>(part + r * DP + 4 * piece) = o;
+        if (piece == 0) {
+          part[R * DP + r] = top;
+          part[R * DP + R + r] = sum;
+        }
+      } else {
+        const int pr = sg.r0 + r, tok = pr / a.G, head = sg.hk * a.G + pr - tok * a.G;
+        const long long row = work.q.first + tok;
+        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= inv;
+        if (4 * piece < a.D) put4((T *)a.o.p + row * a.o.row + head * a.o.head + 4 * piece, o);
+        if (a.lse && piece == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+      }
+    }
+    __syncthreads();
+  }
+  if (!a.whole && threadIdx.x == 0) a.rec[w] = begun;
+}
+
+// The parts of a unit, in order: a wavefront a row
+template <typename T, int R, int DP>
+__global__ __launch_bounds__(256)
+void k_attn_join(AttnArgs a) {
+  const AttnPart p = a.rec[blockIdx.x];
+  const int r = blockIdx.y * 4 + wave_id_u(), lane = lane_id();
+  if (p.count == 0 || r >= p.n) return;
+  constexpr size_t F = attn_part_floats<R, DP>();
+  constexpr int E = DP / WAVE;
+  auto part = [&](int k) { return a.part + (k == 0 ? p.slot : 2 * (p.w + k)) * F; };
+  float top = -INFINITY;
+  for (int k = lane; k < p.count; k += WAVE) top = fmaxf(top, part(k)[R * DP + r]);
+  top = fmaxf(top, xor_lane<32>(top));
+  top = fmaxf(top, xor_lane<16>(top));
+  top = fmaxf(top, xor_lane<8>(top));
+  top = fmaxf(top, xor_lane<4>(top));
+  top = fmaxf(top, xor_lane<2>(top));
+  top = fmaxf(top, xor_lane<1>(top));
+  const float mm = top == -INFINITY ? 0.0f : top;
+  float o[E], sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.0f;
+  for (int k0 = 0; k0 < p.count; k0 += WAVE) {
+    const int k = k0 + lane;
+    const float f = k < p.count ? __builtin_amdgcn_exp2f(part(min(k, p.count - 1))[R * DP + r] - mm) : 0.0f;
+    sum += wave_tree_sum(k < p.count ? f * part(k)[R * DP + R + r] : 0.0f);
+    const int left = min(WAVE, p.count - k0);
+#pragma unroll 8
+    for (int j = 0; j < left; ++j) {
+      const float fj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j));
+      const float *src = part(k0 + j) + r * DP + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(fj, src[e], o[e]);
+    }
+  }
+  const int pr = p.r0 + r, tok = pr / a.G, head = p.head + pr - tok * a.G;
+  const long long row = p.token + tok;
+  const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+  T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (lane * E + e >= a.D) continue;
+    if constexpr (sizeof(T) == 2) out[lane * E + e] = f32_to_bf16_any(o[e] * inv);
+    else out[lane * E + e] = o[e] * inv;
+  }
+  if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+}
+
+// The launch of a call: workgroups, whether units are cut, bytes of the workspace
+struct Plan {
+  int dp, R, BK, W;
+  bool whole;
+  size_t part_bytes, bytes;
+};
+Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows, int n_cu) {
+  Plan p;
+  p.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  p.R = 32;
+  p.BK = !bf16 ? 64 : p.dp == 256 ? 64 : 128;
+  const long long G = Hq / c.Hk, tiles = ((long long)b.max_q * G + p.R - 1) / p.R;
+  const long long blocks = (((long long)b.max_pages << c.shift) + p.BK - 1) / p.BK;
+  const long long units = (long long)b.n_seq * c.Hk * tiles;
+  p.whole = blocks <= 2;
+  long long most = p.whole ? units : (double)units * blocks < 1e9 ? units * blocks : n_cu;
+  if (!p.whole && most > n_cu) most = n_cu;
+  if (most > 65536) most = 65536;
+  p.W = (int)most;
+  p.part_bytes = p.whole ? 0 : 2 * (size_t)p.W * p.R * (p.dp + 2) * 4;
+  p.bytes = p.part_bytes + (p.whole ? 256 : (size_t)p.W * sizeof(AttnPart));
+  return p;
+}
+
+}  // namespace
+
+size_t attn_ws_bytes(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows,
+                     int n_cu) {
+  return (plan(bf16, D, Hq, c, b, rows, n_cu).bytes + 255) & ~(size_t)255;
+}
+
+hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b, void *ws, int n_cu,
+                       hipStream_t st) {
+  const Plan p = plan(call.bf16, call.D, call.Hq, c, b, call.rows, n_cu);
+  AttnArgs a{};
+  a.q = call.q;
+  a.o = call.o;
+  a.lse = call.lse;
+  a.c = c;
+  a.b = b;
+  a.rows = (int)call.rows;
+  a.Hq = call.Hq;
+  a.G = call.Hq / c.Hk;
+  a.D = call.D;
+  a.window = call.window;
+  a.scale = call.scale * LOG2E;
+  a.above = 0;
+  a.upto = 0x7FFFFFFF;
+  a.W = p.W;
+  a.whole = p.whole;
+  a.part = static_cast<float *>(ws);
+  a.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + p.part_bytes);
+  const long long most = (long long)b.max_q * a.G;
+  const dim3 join((unsigned)p.W, (unsigned)(((most < p.R ? most : p.R) + 3) / 4));
+#define BASE_FEW(T, DP)                                                                          \
+  do {                                                                                           \
+    launch_k(k_attn_few<T, DP>, dim3(p.W), dim3(FewShape<T, DP>::THREADS), 0, st, a);            \
+    if (!p.whole) launch_k(k_attn_join<T, 32, DP>, join, dim3(256), 0, st, a);                   \
+  } while (0)
+#define BASE_FEW_D(T)                                                                            \
+  do { if (p.dp == 64) BASE_FEW(T, 64); else if (p.dp == 128) BASE_FEW(T, 128); else BASE_FEW(T, 256); } while (0)
+  if (call.bf16) BASE_FEW_D(uint16_t);
+  else BASE_FEW_D(float);
+#undef BASE_FEW_D
+#undef BASE_FEW
+  return hipGetLastError();
+}
+
+}  // namespace basek

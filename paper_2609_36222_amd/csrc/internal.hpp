@@ -12,6 +12,7 @@ constexpr int MAX_K = 16;     // experts per token
 constexpr int MAX_E = 256;    // experts per layer
 constexpr int MAX_B = 1024;   // tokens per batch
 constexpr int MAX_NORM_D = 16384;   // a norm's row
+constexpr int MAX_HEAD_D = 256;     // a head of queries, keys or values
 
 // Events attached to the next kernel launch (per host thread): when set,
 // launch_k hands them to the dispatch itself, which records `start` as the
@@ -484,6 +485,50 @@ hipError_t launch_combine_norm(bool bf16, int B, int d, int kc, const int32_t *p
                                float scale, const float *post, const float *gate,
                                long long gate_ld, const float *pre, const void *h, void *ho,
                                void *xo, hipStream_t st);
+
+// The heads of a batch of rows: element e of head h of row r at p[r row + h head + e]
+struct HeadRows {
+  void *p;
+  long long row, head;
+};
+// A paged cache: element e of head h of the token in slot i of page g at k[g page + i
+// slot + h head + e], strides in elements, and the sequences whose new tokens a call
+// brings (see base_kv_batch)
+struct KvCache {
+  void *k, *v;
+  long long k_page, k_slot, k_head, v_page, v_slot, v_head;
+  int n_pages, shift, Hk;   // 2^shift tokens a page
+};
+struct KvBatch {
+  const int32_t *table, *q_start, *kv_len;
+  long long table_ld;
+  int n_seq, max_pages, max_q;
+};
+// (heads.hip) y = R(position) (gain n(x)) for Hq query and Hk key heads; with a cache
+// the key heads and, unchanged, the value heads go there, the position is the token's
+// (pos null) and rows of no sequence are left out
+struct RopeArgs {
+  int D, rot;
+  bool interleaved;
+  float eps, scale;
+  const float *inv, *q_gain, *k_gain;
+};
+hipError_t launch_heads(bool bf16, const RopeArgs &R, long long rows, const int32_t *pos, int Hq,
+                        HeadRows q, HeadRows q_out, int Hk, HeadRows k, HeadRows k_out,
+                        HeadRows v, const KvCache *cache, const KvBatch *batch, hipStream_t st);
+// (attn.hip) attention of the batch's new tokens over the cache; scale: of the products
+struct AttnCall {
+  bool bf16;
+  int D, Hq, window;   // window 0: none
+  float scale;
+  long long rows;
+  HeadRows q, o;
+  float *lse;          // [rows][Hq] or null
+};
+size_t attn_ws_bytes(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows,
+                     int n_cu);
+hipError_t launch_attn(const AttnCall &a, const KvCache &c, const KvBatch &b, void *ws, int n_cu,
+                       hipStream_t st);
 
 // Calibration statistics (per expert u): head[u] = (n, sum y, sum y^2, 0)
 // fp64, sz[u][d] and q[u][d] fp64, G[u][d][d] fp32; each array 256-byte

@@ -1,0 +1,262 @@
+"""Attention over a paged cache on the GPU against 64-bit arithmetic: every head size's
+kernel, head layouts, lengths, page sizes, windows, rows that see nothing, garbage around
+what is seen.  Tolerances: see attn_util.attend."""
+import numpy as np
+import pytest
+
+import attn_util as U
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+BF, F32 = U.BF, U.F32
+
+
+@pytest.fixture(scope="module")
+def bd(gpu):
+    return gpu
+
+
+def check(bd, b, Hq, scale=None, window=0, max_q=None, q=None, pad_rows=0):
+    q = b.queries(Hq) if q is None else q
+    cache, batch = b.device(bd, max_q)
+    rows = b.rows + pad_rows
+    qd = torch.full((rows, Hq, b.D), float("nan"), dtype=b.dtype, device="cuda")
+    qd[:b.rows] = q.cuda()
+    out = torch.full((rows, Hq, b.D), 7.0, dtype=b.dtype, device="cuda")
+    lse = torch.full((rows, Hq), 7.0, device="cuda")
+    n = bd.attention_workspace_bytes(cache, batch, rows, Hq)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    bd.base_paged_attention(cache, batch, qd, out, ws, scale, window, lse)
+    torch.cuda.synchronize()
+    want, bound, wl, lb = U.attend(b, q, b.D ** -0.5 if scale is None else scale, window)
+    U.near(out[:b.rows], want, bound, b.dtype, "out")
+    got = lse[:b.rows].double().cpu().numpy()
+    assert np.array_equal(np.isinf(got), np.isinf(wl))
+    fine = np.isfinite(wl)
+    assert (np.abs(got - wl)[fine] <= lb[fine]).all(), np.abs(got - wl)[fine].max()
+    assert (out[b.rows:] == 7).all() and (lse[b.rows:] == 7).all()
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [8, 40, 64, 72, 96, 128, 136, 200, 256])
+def test_head_sizes(bd, dtype, D):
+    b = U.Batch([(1, 300), (3, 33), (1, 1)], 2, D, 16, dtype, seed=D)
+    b.fill()
+    check(bd, b, 6)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hq,Hk", [(1, 1), (3, 3), (8, 1), (12, 4), (32, 1), (40, 2), (66, 2)])
+def test_head_layouts(bd, dtype, Hq, Hk):
+    b = U.Batch([(1, 700), (2, 70), (1, 129)], Hk, 64, 32, dtype, seed=Hq)
+    b.fill()
+    check(bd, b, Hq)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kv", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 4097])
+def test_lengths(bd, dtype, kv):
+    b = U.Batch([(1, kv)], 2, 128, 16, dtype, seed=kv)
+    b.fill()
+    check(bd, b, 8)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("ps,heads_first", [(16, True), (16, False), (64, False), (128, True), (1024, True)])
+def test_pages(bd, dtype, ps, heads_first):
+    b = U.Batch([(1, 1000), (5, 517), (2, 48)], 3, 128, ps, dtype, seed=ps, heads_first=heads_first)
+    b.fill()
+    check(bd, b, 6)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,kv", [(2, 2), (5, 5), (17, 100), (33, 33), (64, 64), (65, 300), (130, 130), (257, 700)])
+def test_chunks(bd, dtype, D, n, kv):
+    b = U.Batch([(n, kv)], 2, D, 16, dtype, seed=n)
+    b.fill()
+    check(bd, b, 8)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window", [1, 2, 16, 31, 64, 100, 1000])
+def test_windows(bd, dtype, window):
+    """The keys that a window leaves behind may hold anything, their pages may be gone."""
+    lens = [(1, 900), (7, 300), (130, 401), (3, 3)]
+    b = U.Batch(lens, 2, 64, 16, dtype, seed=window)
+    lowest = [max(0, kv - n + 1 - window) for n, kv in lens]
+    b.fill(lowest)
+    for s, lo in enumerate(lowest):
+        b.table[s, :lo // 16] = -1
+    check(bd, b, 8, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_mixed_and_empty(bd, dtype):
+    """Single tokens, chunks, places without a sequence, more new tokens than tokens, rows
+    behind the last sequence."""
+    lens = [(1, 77), (0, 0), (150, 150), (0, 40), (1, 1), (40, 1200), (9, 4), (2, 0), (1, 2000), (0, 0)]
+    b = U.Batch(lens, 2, 128, 16, dtype, seed=5)
+    b.fill()
+    check(bd, b, 8, pad_rows=5)
+    check(bd, b, 8, pad_rows=5, max_q=1000)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_sequences(bd, dtype):
+    g = np.random.default_rng(3)
+    lens = [(int(g.integers(0, 3)), int(g.integers(2, 90))) for _ in range(211)]
+    b = U.Batch(lens, 1, 64, 16, dtype, seed=6)
+    b.fill()
+    check(bd, b, 4)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale", [1.0, -0.3, 0.0, 30.0])
+def test_scales(bd, dtype, scale):
+    b = U.Batch([(1, 600), (40, 111)], 2, 64, 16, dtype, seed=9)
+    b.fill()
+    check(bd, b, 4, scale=scale)
+
+
+def test_every_key_counts(bd):
+    """With equal products lse is the log of the number of keys, and a mean of ones and
+    zeros counts them."""
+    for dtype in (BF, F32):
+        for n, kv, window in ((1, 5000, 0), (100, 1000, 0), (100, 1000, 37), (3, 120, 0)):
+            b = U.Batch([(n, kv)], 1, 64, 16, dtype, seed=kv)
+            b.fill()
+            q = torch.zeros(b.rows, 4, 64, dtype=dtype)
+            _, lse = check(bd, b, 4, window=window, q=q)
+            seen = np.minimum(kv - n + 1 + np.arange(n), window or kv)
+            assert (np.round(np.exp(lse.double().cpu().numpy())) == seen[:, None]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_strides_and_in_place(bd, dtype):
+    """q and out inside wider rows at odd offsets; out in q's place."""
+    b = U.Batch([(1, 333), (50, 222)], 2, 64, 16, dtype, seed=11)
+    b.fill()
+    Hq, D = 6, 64
+    q = b.queries(Hq)
+    cache, batch = b.device(bd)
+    want, bound, *_ = U.attend(b, q, D ** -0.5)
+    ws = torch.empty(bd.attention_workspace_bytes(cache, batch, b.rows, Hq), dtype=torch.uint8, device="cuda")
+
+    def wide(fill):
+        buf = torch.full((b.rows * (Hq * (D + 3) + 5) + 1,), fill, dtype=dtype, device="cuda")
+        return buf, buf[1:].view(b.rows, Hq * (D + 3) + 5)[:, 5:].unflatten(1, (Hq, D + 3))[..., 3:]
+    qb, qv = wide(3.0)
+    qv.copy_(q)
+    ob, ov = wide(9.0)
+    bd.base_paged_attention(cache, batch, qv, ov, ws)
+    U.near(ov, want, bound, dtype)
+    before = ob.clone()
+    ov.fill_(9.0)
+    assert (ob == 9).all() and (before != 9).any()
+    bd.base_paged_attention(cache, batch, qv, qv, ws)
+    U.near(qv, want, bound, dtype)
+    qv.fill_(3.0)
+    assert (qb == 3).all()
+
+
+def test_long_context_far_offsets(bd):
+    """Pages past 2^32 elements and bytes from the cache's start, and a long context."""
+    ps, Hk, D, kv = 256, 1, 128, 70001
+    b = U.Batch([(1, kv)], Hk, D, ps, BF, seed=12)
+    n = 280
+    stride = 1 << 24                       # elements from page to page: the last at 280 2^24 > 2^32
+    base = torch.zeros(1, dtype=BF, device="cuda")
+    need = (n - 1) * stride + ps * D
+    buf = torch.empty(need * 2, dtype=BF, device="cuda")     # 18.8 GB
+    k = buf[:need].as_strided((n, ps, Hk, D), (stride, D, D, 1))
+    v = buf[need:].as_strided((n, ps, Hk, D), (stride, D, D, 1))
+    order = np.random.default_rng(1).permutation(n)[:b.width]
+    b.table[0, :] = -1
+    b.table[0, :len(order)] = order[:b.width]
+    page, slot = b.slots(0, 0, kv)
+    k[page.cuda(), slot.cuda()], v[page.cuda(), slot.cuda()] = b.k[0].cuda(), b.v[0].cuda()
+    q = b.queries(8)
+    put = lambda t: torch.from_numpy(t).cuda()  # noqa: E731
+    batch = bd.KVBatch(put(b.table), put(b.starts), put(np.array([kv], np.int32)), 1)
+    out = bd.paged_attention(q.cuda(), bd.KVCache(k, v), batch)
+    want, bound, *_ = U.attend(b, q, D ** -0.5)
+    U.near(out, want, bound, BF)
+    del base
+
+
+def test_repeat_and_graph(bd):
+    """The same bits every time, with any workspace, eagerly and replayed from a graph whose
+    lengths and tables change between replays."""
+    lens = [(1, 3000), (1, 40), (1, 700), (1, 1)]
+    b = U.Batch(lens, 2, 128, 16, BF, seed=13)
+    b.fill()
+    q = b.queries(16).cuda()
+    cache, batch = b.device(bd)
+    n = bd.attention_workspace_bytes(cache, batch, b.rows, 16)
+    ws = torch.full((n,), 0x7F, dtype=torch.uint8, device="cuda")
+    first = torch.empty_like(q)
+    bd.base_paged_attention(cache, batch, q, first, ws)
+    for fill in (0, 0xFF):
+        ws.fill_(fill)
+        again = torch.empty_like(q)
+        bd.base_paged_attention(cache, batch, q, again, ws)
+        assert torch.equal(again, first)
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            bd.base_paged_attention(cache, batch, q, out, ws)
+    torch.cuda.synchronize()
+    full = batch.tensors[2].clone()
+    for cut in (0, 17, 700, 0, 2999):
+        batch.tensors[2].copy_((full - cut).clamp_min(0))
+        eager = torch.empty_like(q)
+        ws2 = torch.empty_like(ws)
+        bd.base_paged_attention(cache, batch, q, eager, ws2)
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        if cut == 0:
+            assert torch.equal(out, first)
+
+
+def test_other_stream(bd):
+    b = U.Batch([(1, 900), (64, 300)], 2, 64, 16, BF, seed=14)
+    b.fill()
+    q = b.queries(8).cuda()
+    cache, batch = b.device(bd)
+    want = bd.paged_attention(q, cache, batch)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got, lse = bd.paged_attention(q, cache, batch, return_lse=True, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want) and lse.isfinite().all()
+
+
+def test_bad_device_data_stays_in_bounds(bd):
+    """Page numbers outside the cache, starts and lengths beyond everything: no fault (the
+    kernels bound each access), and sequences with sound data keep their results."""
+    lens = [(1, 500), (2, 200), (1, 300)]
+    b = U.Batch(lens, 2, 64, 16, BF, seed=15, fill=0.0)
+    b.fill()
+    q = b.queries(4)
+    want, bound, *_ = U.attend(b, q, 0.125)
+    b.table[1, :] = [b.n_pages, -7, 1 << 30, -(1 << 31)] * (b.width // 4) + [5] * (b.width % 4)
+    cache, batch = b.device(bd)
+    out = bd.paged_attention(q.cuda(), cache, batch)
+    U.near(out[:1], want[:1], bound[:1], BF)
+    U.near(out[3:], want[3:], bound[3:], BF)
+    batch.tensors[2].copy_(torch.tensor([500, 2 ** 31 - 1, -5], dtype=torch.int32))
+    out = bd.paged_attention(q.cuda(), cache, batch)
+    U.near(out[:1], want[:1], bound[:1], BF)
+    assert (out[3:] == 0).all()             # a length below zero: no key
+    batch.tensors[1].copy_(torch.tensor([0, 1, -3, 2 ** 31 - 1], dtype=torch.int32))
+    bd.paged_attention(q.cuda(), cache, batch)
+    torch.cuda.synchronize()
