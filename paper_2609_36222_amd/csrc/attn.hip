@@ -109,7 +109,8 @@ void k_attn_few(AttnArgs a) {
         u32x4 v;
         if constexpr (BF) v = reinterpret_cast<const Any16H *>(at)->v;
         else v = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
-        qv[c][s] = d < a.D ? v : u32x4{0, 0, 0, 0};
+        const uint32_t keep = d < a.D ? ~0u : 0u;
+        qv[c][s] = v & keep;
       }
     }
     const int pmin = work.q.pos0 + sg.r0 / a.G, pmax = work.q.pos0 + (sg.r0 + sg.n - 1) / a.G;
@@ -352,6 +353,215 @@ void k_attn_few(AttnArgs a) {
   if (!a.whole && threadIdx.x == 0) a.rec[w] = begun;
 }
 
+// ------------------------------------------------------------- chunks --
+// k_attn_many: tiles of 32 packed rows a wavefront on 32x32x16 products, the workgroup's
+// wavefronts on the same block of BK keys, whose rows they bring to a ring of three in LDS
+// together; one barrier a block.
+template <int DP_>
+struct ManyShape {
+  static constexpr int DP = DP_, WAVES = DP == 256 ? 4 : 8, THREADS = WAVES * WAVE, R = 32 * WAVES;
+  static constexpr int BK = DP == 256 ? 32 : 64, CH = DP / 8, ROWB = DP * 2, RING = 3;
+  static constexpr int HALF = BK * ROWB, STAGE = 2 * HALF, LDS = RING * STAGE;
+  static constexpr int PI = HALF / 1024 / WAVES;   // loads of K, and of V, a wavefront and block
+  static constexpr int WPE = DP == 256 ? 1 : 2;
+  static_assert(PI * WAVES * 1024 == HALF && WAVE / CH <= 16, "a load's rows lie in one page");
+};
+template <int CH> __device__ __forceinline__ int many_k(int r) { return CH == 8 ? (r >> 1) & 7 : r & 15; }
+template <int CH> __device__ __forceinline__ int many_v(int r) { return CH == 8 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); }
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+template <int DP>
+__global__ __launch_bounds__((ManyShape<DP>::THREADS), (ManyShape<DP>::WPE))
+void k_attn_many(AttnArgs a) {
+  using M = ManyShape<DP>;
+  constexpr int R = M::R, BK = M::BK, CH = M::CH, QS = DP / 16, DT = DP / 32, KB = BK / 32;
+  __shared__ __attribute__((aligned(256))) char lds[M::LDS];
+  const uint32_t ring_at = lds_addr(lds);
+  const int wave = wave_id_u(), lane = lane_id(), n = lane % 32, h = lane / 32;
+  const int w = a.W % N_XCD ? blockIdx.x : blockIdx.x % N_XCD * (a.W / N_XCD) + blockIdx.x / N_XCD;
+  const char *zero = reinterpret_cast<const char *>(g_zero);
+  const float scale = a.scale != 0.0f ? fabsf(a.scale) : 1.0f;
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+  AttnPart begun{};
+  AttnWork<R, BK> work(a, w);
+  typename AttnWork<R, BK>::Segment sg;
+  while (work.next(sg, begun)) {
+    const int lo = sg.keys.lo, hi = sg.keys.hi;
+    const int r = 32 * wave + n, pr = sg.r0 + min(r, sg.n - 1), tok = pr / a.G;
+    const bool mine = 32 * wave < sg.n;
+    const int pos = r < sg.n ? work.q.pos0 + tok : -1;
+    // positions of the wavefront's first and last row
+    const int wlast = min(32 * wave + 31, sg.n - 1);
+    const int pmin = work.q.pos0 + (sg.r0 + 32 * wave) / a.G, pmax = work.q.pos0 + (sg.r0 + wlast) / a.G;
+    bf16x8 qv[QS];
+    {
+      const uint16_t *p = (const uint16_t *)a.q.p + (long long)(work.q.first + tok) * a.q.row +
+                          (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
+#pragma unroll
+      for (int s = 0; s < QS; ++s) {
+        const int d = 16 * s + 8 * h;
+        const u32x4 v = reinterpret_cast<const Any16H *>(p + min(d, a.D - 8))->v;
+        // a negative scale is taken over by the queries' signs, 0 by queries of 0: the
+        // scaled maximum is then the maximum scaled
+        const uint32_t keep = a.scale != 0.0f && d < a.D ? ~0u : 0u;
+        qv[s] = __builtin_bit_cast(bf16x8, (v ^ flip) & keep);
+      }
+    }
+    f32x16 acc[DT];
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[t][e] = 0.0f;
+
+    // the pages of 64 / PI blocks at a time: lane e has that of load e % PI of block
+    // from + e / PI
+    int from = sg.k0, pages = 0;
+    auto row0 = [&](int j) { return (wave + M::WAVES * j) * WAVE / CH; };   // of load j
+    auto fetch_pages = [&](int i) {
+      from = i;
+      const int key = (i + lane / M::PI) * BK + (wave + M::WAVES * (lane % M::PI)) * WAVE / CH;
+      pages = attn_page(a, work.s, min(key, hi - 1));
+    };
+    auto issue = [&](int i, int at) {
+      if (i - from >= WAVE / M::PI) fetch_pages(i);
+      const int k0 = i * BK;
+      const uint32_t st = ring_at + at * M::STAGE;
+      const bool all = k0 >= lo && k0 + BK <= hi && a.D == DP;
+#pragma unroll
+      for (int j = 0; j < M::PI; ++j) {
+        const long long page = __builtin_amdgcn_readlane(pages, M::PI * (i - from) + j);
+        const int row = row0(j) + lane / CH, piece = lane % CH;
+        const long long slot = (k0 + row0(j)) & ((1 << a.c.shift) - 1);
+        const char *kb = (const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head);
+        const char *vb = (const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head);
+        const int ck = piece ^ many_k<CH>(row), cv = piece ^ many_v<CH>(row);
+        const char *pk = kb + 2 * (lane / CH * a.c.k_slot + 8 * ck);
+        const char *pv = vb + 2 * (lane / CH * a.c.v_slot + 8 * cv);
+        if (!all) {
+          const bool in = k0 + row >= lo && k0 + row < hi;
+          pk = in && 8 * ck < a.D ? pk : zero;
+          pv = in && 8 * cv < a.D ? pv : zero;
+        }
+        glb_to_lds(pk, st + row0(j) * M::ROWB);
+        glb_to_lds(pv, st + M::HALF + row0(j) * M::ROWB);
+      }
+    };
+    const int k1 = hi > 0 ? sg.k1 : sg.k0;
+    if (sg.k0 < k1) {
+      fetch_pages(sg.k0);
+      issue(sg.k0, 0);
+    }
+    if (sg.k0 + 1 < k1) issue(sg.k0 + 1, 1);
+    int at = 0;
+    for (int i = sg.k0; i < k1; ++i) {
+      if (i + 1 < k1) wait_vm<2 * M::PI>();
+      else wait_vm<0>();
+      lds_barrier();
+      if (i + 2 < k1) issue(i + 2, at == 0 ? 2 : at - 1);
+      const int k0 = i * BK;
+      const char *sk = lds + at * M::STAGE, *sv = sk + M::HALF;
+      at = at == 2 ? 0 : at + 1;
+      if (!mine || k0 > pmax || (a.window > 0 && k0 + BK - 1 <= pmin - a.window)) continue;
+      f32x16 s[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+        const int row = 32 * b + n;
+#pragma unroll
+        for (int q = 0; q < QS; ++q) {
+          const bf16x8 kv = *reinterpret_cast<const bf16x8 *>(
+              sk + row * M::ROWB + (((2 * q + h) ^ many_k<CH>(row)) * 16));
+          s[b] = mfma32(kv, qv[q], s[b]);
+        }
+      }
+      if (k0 + BK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window)) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = k0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4;
+            const bool seen = key <= pos && (a.window == 0 || key > pos - a.window);
+            s[b][e] = seen ? s[b][e] : -INFINITY;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+      top = fmaxf(top, xor_lane<32>(top)) * scale;
+      if (__any(top > m + LAG)) {
+        const float to = fmaxf(m, top), f = m == to ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[t][e] *= f;
+      }
+      const float mm = m == -INFINITY ? 0.0f : m;
+      bf16x8 p[2 * KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale, -mm));
+          l += x;
+          p[2 * b + e / 8][e % 8] = (__bf16)x;
+        }
+#pragma unroll
+      for (int ks = 0; ks < 2 * KB; ++ks)
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          const int row = 16 * ks + 4 * h + (lane % 16) / 4;
+          const int piece = 4 * t + (lane / 16 & 1) * 2 + (lane & 3) / 2;
+          const char *p0 = sv + row * M::ROWB + ((piece ^ many_v<CH>(row)) * 16) + (lane & 1) * 8;
+          const char *p1 = sv + (row + 8) * M::ROWB + ((piece ^ many_v<CH>(row + 8)) * 16) + (lane & 1) * 8;
+          const bf16x4 v0 = read_tr(p0), v1 = read_tr(p1);
+          const bf16x8 vv = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+          acc[t] = mfma32(vv, p[ks], acc[t]);
+        }
+    }
+    l = l + xor_lane<32>(l);
+    if (r < sg.n) {
+      if (sg.slot >= 0) {
+        float *part = a.part + sg.slot * attn_part_floats<R, DP>();
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<f32x4 *>(part + r * DP + 32 * t + 2 * e + 4 * h) =
+                f32x4{acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]};
+        if (h == 0) {
+          part[R * DP + r] = m;
+          part[R * DP + R + r] = l;
+        }
+      } else {
+        const int head = sg.hk * a.G + pr - tok * a.G;
+        const long long row = work.q.first + tok;
+        const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+        uint16_t *out = (uint16_t *)a.o.p + row * a.o.row + head * a.o.head;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            if (32 * t + 2 * e + 4 * h < a.D)
+              put4(out + 32 * t + 2 * e + 4 * h,
+                   f32x4{acc[t][e] * inv, acc[t][e + 1] * inv, acc[t][e + 2] * inv, acc[t][e + 3] * inv});
+        if (a.lse && h == 0) a.lse[row * a.Hq + head] = l > 0.0f ? (m + __log2f(l)) * LN2 : -INFINITY;
+      }
+    }
+    __syncthreads();   // the ring is free for the next segment
+  }
+  if (threadIdx.x == 0) a.rec[w] = begun;
+}
+
 // The parts of a unit, in order: a wavefront a row
 template <typename T, int R, int DP>
 __global__ __launch_bounds__(256)
@@ -400,27 +610,41 @@ void k_attn_join(AttnArgs a) {
   if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
 }
 
-// The launch of a call: workgroups, whether units are cut, bytes of the workspace
-struct Plan {
-  int dp, R, BK, W;
+// The launches of a call.  Sequences of at most FEW_ROWS packed rows are k_attn_few's,
+// longer ones (16-bit) k_attn_many's; where there may be both, both run, on parts of the
+// workspace of their own.
+constexpr int FEW_ROWS = 32;
+struct Launch {
+  int R, BK, W;             // W 0: none
   bool whole;
-  size_t part_bytes, bytes;
+  size_t part, rec;         // in the workspace, bytes
+};
+struct Plan {
+  int dp;
+  Launch few, many;
+  size_t bytes;
 };
 Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows, int n_cu) {
-  Plan p;
+  Plan p{};
   p.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  p.R = 32;
-  p.BK = !bf16 ? 64 : p.dp == 256 ? 64 : 128;
-  const long long G = Hq / c.Hk, tiles = ((long long)b.max_q * G + p.R - 1) / p.R;
-  const long long blocks = (((long long)b.max_pages << c.shift) + p.BK - 1) / p.BK;
-  const long long units = (long long)b.n_seq * c.Hk * tiles;
-  p.whole = blocks <= 2;
-  long long most = p.whole ? units : (double)units * blocks < 1e9 ? units * blocks : n_cu;
-  if (!p.whole && most > n_cu) most = n_cu;
-  if (most > 65536) most = 65536;
-  p.W = (int)most;
-  p.part_bytes = p.whole ? 0 : 2 * (size_t)p.W * p.R * (p.dp + 2) * 4;
-  p.bytes = p.part_bytes + (p.whole ? 256 : (size_t)p.W * sizeof(AttnPart));
+  const long long G = Hq / c.Hk, most = b.max_q * G;
+  auto shape = [&](Launch &l, int R, int BK, bool may_be_whole) {
+    l.R = R;
+    l.BK = BK;
+    const long long blocks = (((long long)b.max_pages << c.shift) + BK - 1) / BK;
+    const double units = (double)b.n_seq * c.Hk * ((most + R - 1) / R);
+    l.whole = may_be_whole && blocks <= 2;
+    const double want = l.whole ? (units < 65536 ? units : 65536) : units * blocks;
+    l.W = l.whole || want < n_cu ? (int)want : n_cu;
+    l.part = p.bytes;
+    if (!l.whole) p.bytes += 2 * (size_t)l.W * R * (p.dp + 2) * 4;
+    l.rec = p.bytes = (p.bytes + 255) & ~(size_t)255;
+    if (!l.whole) p.bytes += ((size_t)l.W * sizeof(AttnPart) + 255) & ~(size_t)255;
+  };
+  if (!bf16 || most <= FEW_ROWS || b.n_seq > 1)
+    shape(p.few, 32, !bf16 || p.dp == 256 ? 64 : 128, true);
+  if (bf16 && most > FEW_ROWS) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, false);
+  if (p.bytes == 0) p.bytes = 256;
   return p;
 }
 
@@ -428,7 +652,7 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
 
 size_t attn_ws_bytes(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows,
                      int n_cu) {
-  return (plan(bf16, D, Hq, c, b, rows, n_cu).bytes + 255) & ~(size_t)255;
+  return plan(bf16, D, Hq, c, b, rows, n_cu).bytes;
 }
 
 hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b, void *ws, int n_cu,
@@ -446,25 +670,42 @@ hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b,
   a.D = call.D;
   a.window = call.window;
   a.scale = call.scale * LOG2E;
-  a.above = 0;
-  a.upto = 0x7FFFFFFF;
-  a.W = p.W;
-  a.whole = p.whole;
-  a.part = static_cast<float *>(ws);
-  a.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + p.part_bytes);
   const long long most = (long long)b.max_q * a.G;
-  const dim3 join((unsigned)p.W, (unsigned)(((most < p.R ? most : p.R) + 3) / 4));
+  auto use = [&](const Launch &l, int above, int upto) {
+    a.above = above;
+    a.upto = upto;
+    a.W = l.W;
+    a.whole = l.whole;
+    a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
+    a.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);
+    return dim3((unsigned)l.W, (unsigned)(((most < l.R ? most : l.R) + 3) / 4));
+  };
+#define BASE_MANY(DP)                                                                            \
+  do {                                                                                           \
+    launch_k(k_attn_many<DP>, dim3(p.many.W), dim3(ManyShape<DP>::THREADS), 0, st, a);           \
+    launch_k(k_attn_join<uint16_t, ManyShape<DP>::R, DP>, join, dim3(256), 0, st, a);            \
+  } while (0)
 #define BASE_FEW(T, DP)                                                                          \
   do {                                                                                           \
-    launch_k(k_attn_few<T, DP>, dim3(p.W), dim3(FewShape<T, DP>::THREADS), 0, st, a);            \
-    if (!p.whole) launch_k(k_attn_join<T, 32, DP>, join, dim3(256), 0, st, a);                   \
+    launch_k(k_attn_few<T, DP>, dim3(p.few.W), dim3(FewShape<T, DP>::THREADS), 0, st, a);        \
+    if (!p.few.whole) launch_k(k_attn_join<T, 32, DP>, join, dim3(256), 0, st, a);               \
   } while (0)
 #define BASE_FEW_D(T)                                                                            \
   do { if (p.dp == 64) BASE_FEW(T, 64); else if (p.dp == 128) BASE_FEW(T, 128); else BASE_FEW(T, 256); } while (0)
-  if (call.bf16) BASE_FEW_D(uint16_t);
-  else BASE_FEW_D(float);
+  if (p.many.W) {
+    const dim3 join = use(p.many, p.few.W ? FEW_ROWS : 0, 0x7FFFFFFF);
+    if (p.dp == 64) BASE_MANY(64);
+    else if (p.dp == 128) BASE_MANY(128);
+    else BASE_MANY(256);
+  }
+  if (p.few.W) {
+    const dim3 join = use(p.few, 0, p.many.W ? FEW_ROWS : 0x7FFFFFFF);
+    if (call.bf16) BASE_FEW_D(uint16_t);
+    else BASE_FEW_D(float);
+  }
 #undef BASE_FEW_D
 #undef BASE_FEW
+#undef BASE_MANY
   return hipGetLastError();
 }
 
