@@ -326,15 +326,12 @@ base_status base_decode_block(const base_layer *L, const base_norms *N, const vo
                               base_plan *plan_out, void *ws, size_t ws_bytes, void *stream);
 
 /* The heads of queries, keys and values: rotation by position, a paged cache and the
- * attention over it.  Heads are given by a pointer and two strides: element e of head h
- * of row r at p[r row + h head + e], so that they may be parts of wider rows (of one
- * projection's output, say).  Element alignment suffices; elements between the heads are
- * not touched. */
-typedef struct base_heads {
-    void *p;
-    int64_t row, head;      /* in elements, 0 to BASE_HEAD_MAX_LD; outputs' heads must not
-                               overlap */
-} base_heads;
+ * attention over it.  Heads x are given by a pointer and two strides: element e of head h
+ * of row r at x[r x_row + h x_head + e], so that they may be parts of wider rows (of one
+ * projection's output, say).  Strides are in elements, 0 to BASE_HEAD_MAX_LD; element
+ * alignment suffices, and elements between the heads are not touched.  An output's heads
+ * must not overlap each other, nor an input's; it may be its input, with the same
+ * strides, where that is said. */
 #define BASE_HEAD_MAX_D 256
 #define BASE_MAX_HEADS 1024
 #define BASE_HEAD_MAX_LD (1LL << 40)
@@ -364,10 +361,12 @@ typedef struct base_rope {
  *   positions  [rows] int32 (any sign); not needed if rot = 0
  *   q, q_out   Hq heads a row (0 to BASE_MAX_HEADS; 0: q and q_out are not looked at)
  *   k, k_out   Hk heads a row, likewise
- * An output may be its input, with the same strides; otherwise they must not overlap. */
+ * q_out may be q, and k_out k. */
 base_status base_head_rope(const base_rope *R, int64_t rows, const int32_t *positions, int32_t Hq,
-                           const base_heads *q, const base_heads *q_out, int32_t Hk,
-                           const base_heads *k, const base_heads *k_out, void *stream);
+                           const void *q, int64_t q_row, int64_t q_head, void *q_out,
+                           int64_t q_out_row, int64_t q_out_head, int32_t Hk, const void *k,
+                           int64_t k_row, int64_t k_head, void *k_out, int64_t k_out_row,
+                           int64_t k_out_head, void *stream);
 
 /* A layer's paged cache of keys and values.  Element e of key head h of the token in
  * slot i of page g lies at k[g k_page + i k_slot + h k_head + e] (v likewise). */
@@ -378,8 +377,8 @@ typedef struct base_kv_cache {
     int32_t page_size;      /* tokens a page: a power of two, 16 to 65536 */
     int32_t n_pages;        /* >= 1 */
     void *k, *v;            /* 16-B aligned */
-    int64_t k_page, k_slot, k_head;   /* strides in elements, 0 to BASE_HEAD_MAX_LD, */
-    int64_t v_page, v_slot, v_head;   /* each a multiple of 16 bytes */
+    int64_t k_page, k_slot, k_head;   /* strides in elements, 0 to BASE_HEAD_MAX_LD (slots: */
+    int64_t v_page, v_slot, v_head;   /* BASE_KV_MAX_SLOT), each a multiple of 16 bytes */
 } base_kv_cache;
 
 /* The sequences of a batch and their new tokens.  Row t of the batch belongs to the
@@ -401,6 +400,7 @@ typedef struct base_kv_batch {
     const int32_t *kv_len;  /* [n_seq] */
 } base_kv_batch;
 #define BASE_MAX_SEQ 65536
+#define BASE_KV_MAX_SLOT (1LL << 25)
 
 /* The new tokens on their way into the cache: q (Hq heads) to q_out as base_head_rope,
  * k (the cache's Hk heads) the same into the cache, v unchanged beside it.
@@ -409,11 +409,12 @@ typedef struct base_kv_batch {
  *   positions  [rows] int32, or NULL: each token's number in its sequence
  *   R          its D and dtype are the cache's
  * Two rows of one slot (sequences that share a page which both write) leave either.
- * q_out may be q, with the same strides. */
+ * q_out may be q. */
 base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const base_kv_batch *S,
-                           int64_t rows, const int32_t *positions, int32_t Hq, const base_heads *q,
-                           const base_heads *q_out, const base_heads *k, const base_heads *v,
-                           void *stream);
+                           int64_t rows, const int32_t *positions, int32_t Hq, const void *q,
+                           int64_t q_row, int64_t q_head, void *q_out, int64_t q_out_row,
+                           int64_t q_out_head, const void *k, int64_t k_row, int64_t k_head,
+                           const void *v, int64_t v_row, int64_t v_head, void *stream);
 
 /* Attention of the new tokens over the cache, their own keys in it: for query head h of
  * token i (its number in the sequence) and key head h / (Hq / Hk), over the keys j of the
@@ -426,7 +427,7 @@ base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const bas
  * sequence are left as they were.  Deterministic run to run.
  *   rows   of q, out and lse: 1 to BASE_HEAD_MAX_ROWS
  *   Hq     a multiple of C->Hk, at most BASE_MAX_HEADS
- *   out    may be q, with the same strides
+ *   out    may be q
  *   lse    [rows][Hq] fp32, or NULL
  *   scale  finite;  window >= 0 (0: none)
  *   ws     at least base_attention_workspace_bytes of the same cache, batch (its n_seq,
@@ -435,9 +436,9 @@ base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const bas
 size_t base_attention_workspace_bytes(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
                                       int32_t Hq);
 base_status base_paged_attention(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
-                                 int32_t Hq, const base_heads *q, const base_heads *out, float *lse,
-                                 float scale, int32_t window, void *ws, size_t ws_bytes,
-                                 void *stream);
+                                 int32_t Hq, const void *q, int64_t q_row, int64_t q_head, void *out,
+                                 int64_t out_row, int64_t out_head, float *lse, float scale,
+                                 int32_t window, void *ws, size_t ws_bytes, void *stream);
 
 /* For callers that cannot allocate device memory (code under stream
  * capture, tight serving loops, harnesses that forbid allocation): the same

@@ -66,10 +66,6 @@ class base_norms(ctypes.Structure):
                 ("gate_ld", _i64), ("pre_gain", _vp)]
 
 
-class base_heads(ctypes.Structure):
-    _fields_ = [("p", _vp), ("row", _i64), ("head", _i64)]
-
-
 class base_rope(ctypes.Structure):
     _fields_ = [("D", _i32), ("rot", _i32), ("dtype", _i32), ("layout", _i32),
                 ("eps", ctypes.c_float), ("rot_scale", ctypes.c_float), ("inv_freq", _vp),
@@ -170,18 +166,17 @@ def load(path: str = LIB_PATH):
     L.base_decode_block.argtypes = [ctypes.POINTER(base_layer), ctypes.POINTER(base_norms), _vp,
                                     _i32, _i32, _i32, _vp, _vp, _vp, ctypes.POINTER(base_plan),
                                     _vp, ctypes.c_size_t, _vp]
-    heads, cache, batch = (ctypes.POINTER(t) for t in (base_heads, base_kv_cache, base_kv_batch))
+    heads = [_vp, _i64, _i64]
+    cache, batch = ctypes.POINTER(base_kv_cache), ctypes.POINTER(base_kv_batch)
     L.base_head_rope.restype = _i32
-    L.base_head_rope.argtypes = [ctypes.POINTER(base_rope), _i64, _vp, _i32, heads, heads, _i32,
-                                 heads, heads, _vp]
+    L.base_head_rope.argtypes = [ctypes.POINTER(base_rope), _i64, _vp, *2 * [_i32, *2 * heads], _vp]
     L.base_kv_append.restype = _i32
-    L.base_kv_append.argtypes = [ctypes.POINTER(base_rope), cache, batch, _i64, _vp, _i32, heads,
-                                 heads, heads, heads, _vp]
+    L.base_kv_append.argtypes = [ctypes.POINTER(base_rope), cache, batch, _i64, _vp, _i32, *4 * heads, _vp]
     L.base_attention_workspace_bytes.restype = ctypes.c_size_t
     L.base_attention_workspace_bytes.argtypes = [cache, batch, _i64, _i32]
     L.base_paged_attention.restype = _i32
-    L.base_paged_attention.argtypes = [cache, batch, _i64, _i32, heads, heads, _vp,
-                                       ctypes.c_float, _i32, _vp, ctypes.c_size_t, _vp]
+    L.base_paged_attention.argtypes = [cache, batch, _i64, _i32, *2 * heads, _vp, ctypes.c_float, _i32,
+                                       _vp, ctypes.c_size_t, _vp]
     _lib = L
     return L
 
@@ -675,15 +670,23 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, fast=32.0, slo
     return (inv * (1 - far) + inv / factor * far).float(), 0.1 * math.log(factor) + 1.0
 
 
-def _heads(t, what, dtype, dev, rows=None, H=None, D=None):
-    """base_heads of a [rows, H, D] tensor with adjacent elements in a head."""
-    if (t.dim() != 3 or t.dtype is not dtype or t.get_device() != dev
-            or (rows is not None and t.shape[0] != rows) or (H is not None and t.shape[1] != H)
-            or (D is not None and t.shape[2] != D) or (t.stride(2) != 1 and t.shape[2] > 1)):
-        shape = ", ".join(str(v) if v is not None else n for n, v in (("rows", rows), ("heads", H), ("D", D)))
-        raise ValueError(f"{what}: {dtype} [{shape}], adjacent elements, on the current GPU")
-    # (one row or one head has no stride to speak of)
-    return base_heads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+def _heads(t, what, dtype, dev, shape):
+    """(pointer, row stride, head stride) of a tensor [rows, H, D] with adjacent elements in
+    a head."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what}: {dtype} {list(shape)} on the current GPU")
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{what}: adjacent elements in a head")
+    # (a single row or head has no stride to speak of)
+    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+
+
+def _head_shape(t, what, D):
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != D:
+        raise ValueError(f"{what}: [rows, heads, {D}]")
+    return shape
 
 
 def _ints(t, what, dev, shape=None):
@@ -759,24 +762,29 @@ class KVBatch:
                                   *(_ptr(t) for t in self.tensors))
 
 
+_NO_HEADS = (0, None, 0, 0, None, 0, 0)
+
+
 def base_head_rope(rope: Rope, positions, q, k, q_out, k_out, stream=None):
     """q_out and k_out [rows, heads, D] from q and k (either pair None) at int32 positions
     [rows] (None where nothing rotates)."""
-    dev, args, n = _device(), [], None
+    dev, dt, args, n = _device(), rope.torch_dtype, (), None
     for t, out, what in ((q, q_out, "q"), (k, k_out, "k")):
         if t is None or out is None:
             if t is not None or out is not None:
                 raise ValueError(f"{what} and {what}_out: both or neither")
-            args += [0, None, None]
+            args += _NO_HEADS
             continue
-        n = t.shape[0] if n is None else n
-        args += [t.shape[1], _heads(t, what, rope.torch_dtype, dev, n, None, rope.D),
-                 _heads(out, what + "_out", rope.torch_dtype, dev, n, t.shape[1], rope.D)]
+        shape = _head_shape(t, what, rope.D)
+        if n is not None and shape[0] != n:
+            raise ValueError(f"{what}: q's rows")
+        n = shape[0]
+        args += (shape[1], *_heads(t, what, dt, dev, shape), *_heads(out, what + "_out", dt, dev, shape))
     if n is None:
         raise ValueError("q or k")
     if positions is not None:
-        _flat(positions, "positions", dev, (n,))
-    _check(load().base_head_rope(rope.desc, n, _ptr(positions), *args, _stream(stream)))
+        positions = _flat(positions, "positions", dev, (n,)).data_ptr()
+    _check(load().base_head_rope(rope.desc, n, positions, *args, _stream(stream)))
 
 
 def head_rope(rope: Rope, positions, q, k=None, stream=None):
@@ -791,13 +799,15 @@ def base_kv_append(rope: Rope, cache: KVCache, batch: KVBatch, q, k, v, q_out, p
     [rows, Hq, D] the same to q_out.  positions: int32 [rows], or None: the tokens' numbers
     in their sequences."""
     dev, dt = _device(), rope.torch_dtype
-    n, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    shape = _head_shape(q, "q", rope.D)
+    n = shape[0]
     if positions is not None:
-        _flat(positions, "positions", dev, (n,))
+        positions = _flat(positions, "positions", dev, (n,)).data_ptr()
+    new = (n, cache.Hk, rope.D)
     _check(load().base_kv_append(
-        rope.desc, cache.desc, batch.desc, n, _ptr(positions), Hq, _heads(q, "q", dt, dev, n, Hq, rope.D),
-        _heads(q_out, "q_out", dt, dev, n, Hq, rope.D), _heads(k, "k", dt, dev, n, cache.Hk, rope.D),
-        _heads(v, "v", dt, dev, n, cache.Hk, rope.D), _stream(stream)))
+        rope.desc, cache.desc, batch.desc, n, positions, shape[1], *_heads(q, "q", dt, dev, shape),
+        *_heads(q_out, "q_out", dt, dev, shape), *_heads(k, "k", dt, dev, new), *_heads(v, "v", dt, dev, new),
+        _stream(stream)))
 
 
 def attention_workspace_bytes(cache: KVCache, batch: KVBatch, rows, Hq) -> int:
@@ -811,18 +821,20 @@ def base_paged_attention(cache: KVCache, batch: KVBatch, q, out, ws, scale=None,
                          stream=None):
     """out [rows, Hq, D] (and lse [rows, Hq] fp32) of q over the cache; scale None: 1 /
     sqrt(D); ws: a uint8 tensor of attention_workspace_bytes."""
-    import torch
     dev, dt = _device(), cache.torch_dtype
-    n, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, Hq) or not lse.is_contiguous()
-                            or lse.get_device() != dev):
-        raise ValueError(f"lse: contiguous fp32 {[n, Hq]} on the current GPU")
+    shape = _head_shape(q, "q", cache.D)
+    n, Hq, _ = shape
+    if lse is not None:
+        import torch
+        if (lse.dtype is not torch.float32 or lse.shape != (n, Hq) or not lse.is_contiguous()
+                or lse.get_device() != dev):
+            raise ValueError(f"lse: contiguous fp32 {[n, Hq]} on the current GPU")
+        lse = lse.data_ptr()
     if ws.get_device() != dev or not ws.is_contiguous():
         raise ValueError("ws: contiguous, on the current GPU")
     _check(load().base_paged_attention(
-        cache.desc, batch.desc, n, Hq, _heads(q, "q", dt, dev, n, Hq, cache.D),
-        _heads(out, "out", dt, dev, n, Hq, cache.D), _ptr(lse), cache.D ** -0.5 if scale is None else scale,
-        window, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        cache.desc, batch.desc, n, Hq, *_heads(q, "q", dt, dev, shape), *_heads(out, "out", dt, dev, shape),
+        lse, cache.D ** -0.5 if scale is None else scale, window, ws.data_ptr(), ws.nbytes, _stream(stream)))
 
 
 def paged_attention(q, cache: KVCache, batch: KVBatch, scale=None, window=0, return_lse=False, stream=None):

@@ -697,17 +697,19 @@ base_status base_decode_block(const base_layer *L, const base_norms *N, const vo
 }
 
 // ------------------------------------------------------------- heads --
-static base_status check_heads(const base_heads *h, int32_t dtype) {
-  if (!h || !h->p) return BASE_ERR_NULL;
-  if (h->row < 0 || h->row > BASE_HEAD_MAX_LD || h->head < 0 || h->head > BASE_HEAD_MAX_LD)
+static HeadRows head_rows(const void *p, int64_t row, int64_t head) {
+  return {const_cast<void *>(p), row, head};
+}
+static base_status check_heads(const HeadRows &h, int32_t dtype) {
+  if (!h.p) return BASE_ERR_NULL;
+  if (h.row < 0 || h.row > BASE_HEAD_MAX_LD || h.head < 0 || h.head > BASE_HEAD_MAX_LD)
     return BASE_ERR_SHAPE;
-  return aligned(h->p, elem_bytes(dtype)) ? BASE_OK : BASE_ERR_ALIGN;
+  return aligned(h.p, elem_bytes(dtype)) ? BASE_OK : BASE_ERR_ALIGN;
 }
 // in place only element by element
-static bool moved(const base_heads *a, const base_heads *b) {
-  return a->p == b->p && (a->row != b->row || a->head != b->head);
+static bool moved(const HeadRows &a, const HeadRows &b) {
+  return a.p == b.p && (a.row != b.row || a.head != b.head);
 }
-static HeadRows head_rows(const base_heads *h) { return {h->p, h->row, h->head}; }
 
 static base_status check_rope(const base_rope *R, int64_t rows) {
   if (!R) return BASE_ERR_NULL;
@@ -741,6 +743,7 @@ static base_status check_cache(const base_kv_cache *C, const base_kv_batch *S, b
     if (ld < 0 || ld > BASE_HEAD_MAX_LD) return BASE_ERR_SHAPE;
     if (ld % piece) return BASE_ERR_ALIGN;
   }
+  if (C->k_slot > BASE_KV_MAX_SLOT || C->v_slot > BASE_KV_MAX_SLOT) return BASE_ERR_SHAPE;
   if (S->table_ld < S->max_pages || S->table_ld > BASE_HEAD_MAX_LD) return BASE_ERR_SHAPE;
   BASE_TRY(check_ptr(C->k, 16));
   BASE_TRY(check_ptr(C->v, 16));
@@ -757,42 +760,42 @@ static KvBatch kv_batch(const base_kv_batch *S) {
 }
 
 base_status base_head_rope(const base_rope *R, int64_t rows, const int32_t *positions, int32_t Hq,
-                           const base_heads *q, const base_heads *q_out, int32_t Hk,
-                           const base_heads *k, const base_heads *k_out, void *stream) {
+                           const void *q, int64_t q_row, int64_t q_head, void *q_out,
+                           int64_t q_out_row, int64_t q_out_head, int32_t Hk, const void *k,
+                           int64_t k_row, int64_t k_head, void *k_out, int64_t k_out_row,
+                           int64_t k_out_head, void *stream) {
   BASE_TRY(check_rope(R, rows));
   if (Hq < 0 || Hq > BASE_MAX_HEADS || Hk < 0 || Hk > BASE_MAX_HEADS || Hq + Hk < 1) return BASE_ERR_SHAPE;
   if (R->rot > 0) BASE_TRY(check_ptr(positions, 4));
-  HeadRows at[4] = {};
-  const base_heads *hs[4] = {Hq ? q : nullptr, Hq ? q_out : nullptr, Hk ? k : nullptr, Hk ? k_out : nullptr};
-  for (int i = 0; i < 4; ++i) {
-    if (!(i < 2 ? Hq : Hk)) continue;
-    BASE_TRY(check_heads(hs[i], R->dtype));
-    at[i] = head_rows(hs[i]);
-  }
-  for (int i = 0; i < 4; i += 2)
-    if (hs[i] && moved(hs[i], hs[i + 1])) return BASE_ERR_FLAGS;
+  const HeadRows hs[4] = {head_rows(q, q_row, q_head), head_rows(q_out, q_out_row, q_out_head),
+                          head_rows(k, k_row, k_head), head_rows(k_out, k_out_row, k_out_head)};
+  for (int i = 0; i < 4; ++i)
+    if (i < 2 ? Hq : Hk) BASE_TRY(check_heads(hs[i], R->dtype));
+  if ((Hq && moved(hs[0], hs[1])) || (Hk && moved(hs[2], hs[3]))) return BASE_ERR_FLAGS;
   HIP_TRY(launch_heads(R->dtype == BASE_BF16, rope_args(R), rows, R->rot > 0 ? positions : nullptr, Hq,
-                       at[0], at[1], Hk, at[2], at[3], HeadRows{}, nullptr, nullptr, (hipStream_t)stream));
+                       hs[0], hs[1], Hk, hs[2], hs[3], HeadRows{}, nullptr, nullptr, (hipStream_t)stream));
   return BASE_OK;
 }
 
 base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const base_kv_batch *S,
-                           int64_t rows, const int32_t *positions, int32_t Hq, const base_heads *q,
-                           const base_heads *q_out, const base_heads *k, const base_heads *v,
-                           void *stream) {
+                           int64_t rows, const int32_t *positions, int32_t Hq, const void *q,
+                           int64_t q_row, int64_t q_head, void *q_out, int64_t q_out_row,
+                           int64_t q_out_head, const void *k, int64_t k_row, int64_t k_head,
+                           const void *v, int64_t v_row, int64_t v_head, void *stream) {
   BASE_TRY(check_rope(R, rows));
   BASE_TRY(check_cache(C, S, true));
   if (R->D != C->D) return BASE_ERR_SHAPE;
   if (R->dtype != C->dtype) return BASE_ERR_DTYPE;
   if (Hq < 1 || Hq > BASE_MAX_HEADS) return BASE_ERR_SHAPE;
-  for (const base_heads *h : {q, q_out, k, v}) BASE_TRY(check_heads(h, R->dtype));
-  if (moved(q, q_out)) return BASE_ERR_FLAGS;
+  const HeadRows hs[4] = {head_rows(q, q_row, q_head), head_rows(q_out, q_out_row, q_out_head),
+                          head_rows(k, k_row, k_head), head_rows(v, v_row, v_head)};
+  for (const HeadRows &h : hs) BASE_TRY(check_heads(h, R->dtype));
+  if (moved(hs[0], hs[1])) return BASE_ERR_FLAGS;
   if (!aligned(positions, 4)) return BASE_ERR_ALIGN;
   const KvCache c = kv_cache(C);
   const KvBatch b = kv_batch(S);
-  HIP_TRY(launch_heads(R->dtype == BASE_BF16, rope_args(R), rows, positions, Hq, head_rows(q),
-                       head_rows(q_out), C->Hk, head_rows(k), HeadRows{}, head_rows(v), &c, &b,
-                       (hipStream_t)stream));
+  HIP_TRY(launch_heads(R->dtype == BASE_BF16, rope_args(R), rows, positions, Hq, hs[0], hs[1], C->Hk,
+                       hs[2], HeadRows{}, hs[3], &c, &b, (hipStream_t)stream));
   return BASE_OK;
 }
 
@@ -812,20 +815,21 @@ size_t base_attention_workspace_bytes(const base_kv_cache *C, const base_kv_batc
 }
 
 base_status base_paged_attention(const base_kv_cache *C, const base_kv_batch *S, int64_t rows,
-                                 int32_t Hq, const base_heads *q, const base_heads *out, float *lse,
-                                 float scale, int32_t window, void *ws, size_t ws_bytes,
-                                 void *stream) {
+                                 int32_t Hq, const void *q, int64_t q_row, int64_t q_head, void *out,
+                                 int64_t out_row, int64_t out_head, float *lse, float scale,
+                                 int32_t window, void *ws, size_t ws_bytes, void *stream) {
   BASE_TRY(check_attention(C, S, rows, Hq, true));
   if (!std::isfinite(scale) || window < 0) return BASE_ERR_SHAPE;
-  BASE_TRY(check_heads(q, C->dtype));
-  BASE_TRY(check_heads(out, C->dtype));
-  if (moved(q, out)) return BASE_ERR_FLAGS;
+  const HeadRows hq = head_rows(q, q_row, q_head), ho = head_rows(out, out_row, out_head);
+  BASE_TRY(check_heads(hq, C->dtype));
+  BASE_TRY(check_heads(ho, C->dtype));
+  if (moved(hq, ho)) return BASE_ERR_FLAGS;
   if (!aligned(lse, 4)) return BASE_ERR_ALIGN;
   BASE_TRY(check_ptr(ws, 256));
   const KvCache c = kv_cache(C);
   const KvBatch b = kv_batch(S);
   const int n_cu = device_cus();
-  const AttnCall a{C->dtype == BASE_BF16, C->D, Hq, window, scale, rows, head_rows(q), head_rows(out), lse};
+  const AttnCall a{C->dtype == BASE_BF16, C->D, Hq, window, scale, rows, hq, ho, lse};
   if (ws_bytes < attn_ws_bytes(a.bf16, a.D, Hq, c, b, rows, n_cu)) return BASE_ERR_WORKSPACE;
   HIP_TRY(launch_attn(a, c, b, ws, n_cu, (hipStream_t)stream));
   return BASE_OK;

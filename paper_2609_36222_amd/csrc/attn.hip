@@ -39,6 +39,16 @@ __device__ __forceinline__ void glb_to_lds(const char *p, uint32_t lds) {
                "s"(__builtin_amdgcn_readfirstlane(lds))
                : "memory");
 }
+// the same from a uniform address and a lane's offset
+__device__ __forceinline__ void glb_to_lds(const char *base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory");
+}
+__device__ __forceinline__ const char *uni_at(const char *p) {
+  const uintptr_t v = (uintptr_t)p;
+  return (const char *)(((uintptr_t)(uint32_t)uni((int)(v >> 32)) << 32) | (uint32_t)uni((int)v));
+}
 // Four 16-bit elements a lane, transposed in groups of 16 lanes: lane 4 r + c gives the
 // address of elements 4 c .. + 3 of row r, and lane i gets element i of the rows 0 .. 3
 __device__ __forceinline__ bf16x4 read_tr(const char *p) {
@@ -61,26 +71,28 @@ __device__ __forceinline__ void put4(float *p, f32x4 v) { reinterpret_cast<Any16
 // accumulators are rescaled only when the maximum has risen by more
 constexpr float LAG = 8.0f;
 
-template <typename T, int DP_>
+template <typename T, int DP_, int NR_>
 struct FewShape {
   static constexpr bool BF = sizeof(T) == 2;
-  static constexpr int DP = DP_, NR = 2, R = 16 * NR;
+  static constexpr int DP = DP_, NR = NR_, R = 16 * NR;
   static constexpr int TK = BF ? 32 : 16;                  // keys of a wavefront's step
-  static constexpr int WAVES = BF && DP == 256 ? 2 : 4, THREADS = WAVES * WAVE, BK = WAVES * TK;
+  static constexpr int WAVES = BF ? 2 : 4, THREADS = WAVES * WAVE, BK = WAVES * TK;
   static constexpr int CH = DP / 8;                        // 16-byte pieces of a 16-bit row
   static constexpr int ROWB = DP * 2, STAGE = 2 * TK * ROWB, RING = 2, LOADS = CH;
   static constexpr int JOIN = WAVES * R * (DP + 2) * 4;
   static constexpr int LDS = BF && WAVES * RING * STAGE > JOIN ? WAVES * RING * STAGE : JOIN;
+  static constexpr int OCC = BF ? (DP == 64 ? 4 : DP == 128 ? 2 : 1) : DP == 64 ? 2 : 1;   // workgroups a CU
+  static constexpr int WPE = OCC * WAVES >= 4 ? OCC * WAVES / 4 : 1;
 };
 
 // pieces' places in a row of the ring: K's row r at piece ^ few_k(r), V's at piece ^ few_v(r)
 template <int CH> __device__ __forceinline__ int few_k(int r) { return CH == 8 ? (r >> 1) & 7 : r & 15; }
 template <int CH> __device__ __forceinline__ int few_v(int r) { return CH == 8 ? 2 * ((r >> 1) & 3) : 2 * (r & 7); }
 
-template <typename T, int DP>
-__global__ __launch_bounds__((FewShape<T, DP>::THREADS), 1)
+template <typename T, int DP, int NR_>
+__global__ __launch_bounds__((FewShape<T, DP, NR_>::THREADS), (FewShape<T, DP, NR_>::WPE))
 void k_attn_few(AttnArgs a) {
-  using M = FewShape<T, DP>;
+  using M = FewShape<T, DP, NR_>;
   constexpr bool BF = M::BF;
   constexpr int R = M::R, NR = M::NR, TK = M::TK;
   constexpr int DT = DP / 16;                     // accumulator tiles
@@ -89,16 +101,26 @@ void k_attn_few(AttnArgs a) {
   const int wave = wave_id_u(), lane = lane_id(), n = lane % 16, g = lane / 16;
   const int w = blockIdx.x;
   const char *zero = reinterpret_cast<const char *>(g_zero);
+  // the lane's places in the loads of a step (piece j of 64 16-byte pieces)
+  uint32_t ko[BF ? M::CH / 2 : 1], vo[BF ? M::CH / 2 : 1];
+  if constexpr (BF) {
+#pragma unroll
+    for (int j = 0; j < M::CH / 2; ++j) {
+      const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
+      ko[j] = 2 * ((row & 15) * (uint32_t)a.c.k_slot + 8 * (piece ^ few_k<M::CH>(row)));
+      vo[j] = 2 * ((row & 15) * (uint32_t)a.c.v_slot + 8 * (piece ^ few_v<M::CH>(row)));
+    }
+  }
   AttnPart begun{};
   AttnWork<R, M::BK> work(a, w);
   typename AttnWork<R, M::BK>::Segment sg;
   while (work.next(sg, begun)) {
-    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = sg.n > 16 ? 2 : 1;
+    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1;
     int pos[NR];
     u32x4 qv[NR][QS];
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
-      const int r = 16 * c + n, pr = sg.r0 + min(r, sg.n - 1), tok = pr / a.G;
+      const int r = 16 * c + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
       pos[c] = r < sg.n ? work.q.pos0 + tok : -1;
       const T *p = (const T *)a.q.p + (long long)(work.q.first + tok) * a.q.row +
                    (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
@@ -106,14 +128,21 @@ void k_attn_few(AttnArgs a) {
       for (int s = 0; s < QS; ++s) {
         const int d = BF ? 32 * s + 8 * g : 16 * s + 4 * g;
         const T *at = p + min(d, a.D - (BF ? 8 : 4));
-        u32x4 v;
-        if constexpr (BF) v = reinterpret_cast<const Any16H *>(at)->v;
-        else v = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
-        const uint32_t keep = d < a.D ? ~0u : 0u;
-        qv[c][s] = v & keep;
+        if constexpr (BF) qv[c][s] = reinterpret_cast<const Any16H *>(at)->v;
+        else qv[c][s] = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
       }
     }
-    const int pmin = work.q.pos0 + sg.r0 / a.G, pmax = work.q.pos0 + (sg.r0 + sg.n - 1) / a.G;
+    // (behind the pages' load, so that the two are waited for together)
+    auto mask_queries = [&] {
+#pragma unroll
+      for (int c = 0; c < NR; ++c)
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+          const uint32_t keep = (BF ? 32 * s + 8 * g : 16 * s + 4 * g) < a.D ? ~0u : 0u;
+          qv[c][s] = qv[c][s] & keep;
+        }
+    };
+    const int pmin = work.q.pos0 + over(sg.r0, a.by_G), pmax = work.q.pos0 + over(sg.r0 + sg.n - 1, a.by_G);
     f32x4 acc[NR][DT];
     float m[NR], l[NR];
 #pragma unroll
@@ -187,31 +216,38 @@ void k_attn_few(AttnArgs a) {
           const int key = k0 + 16 * h;
           const long long page = __builtin_amdgcn_readlane(pages, 2 * (i - from) + h);
           const long long slot = key & ((1 << a.c.shift) - 1);
-          kb[h] = (const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head);
-          vb[h] = (const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head);
+          kb[h] = uni_at((const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head));
+          vb[h] = uni_at((const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head));
         }
+        if (all) {
 #pragma unroll
-        for (int j = 0; j < M::CH / 2; ++j) {
-          const int row = (lane + WAVE * j) / M::CH, at = (lane + WAVE * j) % M::CH;
-          const int ck = at ^ few_k<M::CH>(row), cv = at ^ few_v<M::CH>(row);
-          const int h = WAVE * j / M::CH / 16;
-          const char *pk = kb[h] + 2 * ((row & 15) * a.c.k_slot + 8 * ck);
-          const char *pv = vb[h] + 2 * ((row & 15) * a.c.v_slot + 8 * cv);
-          if (!all) {
-            const bool in = k0 + row >= lo && k0 + row < hi;
-            pk = in && 8 * ck < a.D ? pk : zero;
-            pv = in && 8 * cv < a.D ? pv : zero;
+          for (int j = 0; j < M::CH / 2; ++j) {
+            const int h = WAVE * j / M::CH / 16;
+            glb_to_lds(kb[h], ko[j], st + j * 1024);
+            glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
           }
-          glb_to_lds(pk, st + j * 1024);
-          glb_to_lds(pv, st + TK * M::ROWB + j * 1024);
+        } else {
+          // a step at the end of what is seen, or heads shorter than DP: zeros in the places
+          // of what is not there
+#pragma unroll 1
+          for (int j = 0; j < M::CH / 2; ++j) {
+            const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
+            const int ck = piece ^ few_k<M::CH>(row), cv = piece ^ few_v<M::CH>(row);
+            const bool h = row >= 16, in = k0 + row >= lo && k0 + row < hi;
+            const char *pk = (h ? kb[1] : kb[0]) + 2 * ((row & 15) * a.c.k_slot + 8 * ck);
+            const char *pv = (h ? vb[1] : vb[0]) + 2 * ((row & 15) * a.c.v_slot + 8 * cv);
+            glb_to_lds(in && 8 * ck < a.D ? pk : zero, st + j * 1024);
+            glb_to_lds(in && 8 * cv < a.D ? pv : zero, st + TK * M::ROWB + j * 1024);
+          }
         }
       };
-      if (i0 < i1) {
-        fetch_pages(i0);
-        issue(i0);
-      }
-      if (i0 + 1 < i1) issue(i0 + 1);
-      for (int i = i0; i < i1; ++i) {
+      if (i0 < i1) fetch_pages(i0);
+      mask_queries();
+      for (int i = i0 - 2; i < i1; ++i) {
+        if (i < i0) {
+          if (i + 2 < i1) issue(i + 2);
+          continue;
+        }
         if (i + 1 < i1) wait_vm<M::LOADS>();
         else wait_vm<0>();
         const char *st = ring + (i & 1) * M::STAGE, *sv = st + TK * M::ROWB;
@@ -227,7 +263,7 @@ void k_attn_few(AttnArgs a) {
             const bf16x8 kv = *reinterpret_cast<const bf16x8 *>(
                 st + row * M::ROWB + (((4 * q + g) ^ few_k<M::CH>(row)) * 16));
             s[0][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[0][q]), s[0][b]);
-            if (nr > 1) s[1][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[1][q]), s[1][b]);
+            if (nr > 1) s[NR - 1][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[NR - 1][q]), s[NR - 1][b]);
           }
         bf16x8 p[NR];
 #pragma unroll
@@ -248,13 +284,14 @@ void k_attn_few(AttnArgs a) {
           const bf16x4 v0 = read_tr(at), v1 = read_tr(at + 16 * M::ROWB);
           const bf16x8 vv = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
           acc[0][t] = mfma16(vv, p[0], acc[0][t]);
-          if (nr > 1) acc[1][t] = mfma16(vv, p[1], acc[1][t]);
+          if (nr > 1) acc[NR - 1][t] = mfma16(vv, p[NR - 1], acc[NR - 1][t]);
         }
         // this stage's reads are done before its next rows are requested
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (i + 2 < i1) issue(i + 2);
       }
     } else {
+      mask_queries();
       for (int i = i0; i < i1; ++i) {
         const int k0 = key0(i);
         const long long page = attn_page(a, work.s, k0), slot = k0 & ((1 << a.c.shift) - 1);
@@ -339,7 +376,7 @@ void k_attn_few(AttnArgs a) {
           part[R * DP + R + r] = sum;
         }
       } else {
-        const int pr = sg.r0 + r, tok = pr / a.G, head = sg.hk * a.G + pr - tok * a.G;
+        const int pr = sg.r0 + r, tok = over(pr, a.by_G), head = sg.hk * a.G + pr - tok * a.G;
         const long long row = work.q.first + tok;
         const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
 #pragma unroll
@@ -384,6 +421,14 @@ void k_attn_many(AttnArgs a) {
   const int wave = wave_id_u(), lane = lane_id(), n = lane % 32, h = lane / 32;
   const int w = a.W % N_XCD ? blockIdx.x : blockIdx.x % N_XCD * (a.W / N_XCD) + blockIdx.x / N_XCD;
   const char *zero = reinterpret_cast<const char *>(g_zero);
+  auto row0 = [&](int j) { return (wave + M::WAVES * j) * WAVE / CH; };   // of load j
+  uint32_t ko[M::PI], vo[M::PI];                                          // the lane's places in it
+#pragma unroll
+  for (int j = 0; j < M::PI; ++j) {
+    const int row = row0(j) + lane / CH;
+    ko[j] = 2 * (lane / CH * (uint32_t)a.c.k_slot + 8 * (lane % CH ^ many_k<CH>(row)));
+    vo[j] = 2 * (lane / CH * (uint32_t)a.c.v_slot + 8 * (lane % CH ^ many_v<CH>(row)));
+  }
   const float scale = a.scale != 0.0f ? fabsf(a.scale) : 1.0f;
   const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
   AttnPart begun{};
@@ -391,24 +436,20 @@ void k_attn_many(AttnArgs a) {
   typename AttnWork<R, BK>::Segment sg;
   while (work.next(sg, begun)) {
     const int lo = sg.keys.lo, hi = sg.keys.hi;
-    const int r = 32 * wave + n, pr = sg.r0 + min(r, sg.n - 1), tok = pr / a.G;
+    const int r = 32 * wave + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
     const bool mine = 32 * wave < sg.n;
     const int pos = r < sg.n ? work.q.pos0 + tok : -1;
     // positions of the wavefront's first and last row
     const int wlast = min(32 * wave + 31, sg.n - 1);
-    const int pmin = work.q.pos0 + (sg.r0 + 32 * wave) / a.G, pmax = work.q.pos0 + (sg.r0 + wlast) / a.G;
-    bf16x8 qv[QS];
+    const int pmin = work.q.pos0 + over(sg.r0 + 32 * wave, a.by_G), pmax = work.q.pos0 + over(sg.r0 + max(wlast, 0), a.by_G);
+    u32x4 qv[QS];
     {
       const uint16_t *p = (const uint16_t *)a.q.p + (long long)(work.q.first + tok) * a.q.row +
                           (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
         const int d = 16 * s + 8 * h;
-        const u32x4 v = reinterpret_cast<const Any16H *>(p + min(d, a.D - 8))->v;
-        // a negative scale is taken over by the queries' signs, 0 by queries of 0: the
-        // scaled maximum is then the maximum scaled
-        const uint32_t keep = a.scale != 0.0f && d < a.D ? ~0u : 0u;
-        qv[s] = __builtin_bit_cast(bf16x8, (v ^ flip) & keep);
+        qv[s] = reinterpret_cast<const Any16H *>(p + min(d, a.D - 8))->v;
       }
     }
     f32x16 acc[DT];
@@ -421,7 +462,6 @@ void k_attn_many(AttnArgs a) {
     // the pages of 64 / PI blocks at a time: lane e has that of load e % PI of block
     // from + e / PI
     int from = sg.k0, pages = 0;
-    auto row0 = [&](int j) { return (wave + M::WAVES * j) * WAVE / CH; };   // of load j
     auto fetch_pages = [&](int i) {
       from = i;
       const int key = (i + lane / M::PI) * BK + (wave + M::WAVES * (lane % M::PI)) * WAVE / CH;
@@ -435,27 +475,31 @@ void k_attn_many(AttnArgs a) {
 #pragma unroll
       for (int j = 0; j < M::PI; ++j) {
         const long long page = __builtin_amdgcn_readlane(pages, M::PI * (i - from) + j);
-        const int row = row0(j) + lane / CH, piece = lane % CH;
         const long long slot = (k0 + row0(j)) & ((1 << a.c.shift) - 1);
-        const char *kb = (const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head);
-        const char *vb = (const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head);
-        const int ck = piece ^ many_k<CH>(row), cv = piece ^ many_v<CH>(row);
-        const char *pk = kb + 2 * (lane / CH * a.c.k_slot + 8 * ck);
-        const char *pv = vb + 2 * (lane / CH * a.c.v_slot + 8 * cv);
-        if (!all) {
+        const char *kb = uni_at((const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head));
+        const char *vb = uni_at((const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head));
+        const uint32_t to = st + row0(j) * M::ROWB;
+        if (all) {
+          glb_to_lds(kb, ko[j], to);
+          glb_to_lds(vb, vo[j], to + M::HALF);
+        } else {
+          const int row = row0(j) + lane / CH, ck = lane % CH ^ many_k<CH>(row), cv = lane % CH ^ many_v<CH>(row);
           const bool in = k0 + row >= lo && k0 + row < hi;
-          pk = in && 8 * ck < a.D ? pk : zero;
-          pv = in && 8 * cv < a.D ? pv : zero;
+          glb_to_lds(in && 8 * ck < a.D ? kb + ko[j] : zero, to);
+          glb_to_lds(in && 8 * cv < a.D ? vb + vo[j] : zero, to + M::HALF);
         }
-        glb_to_lds(pk, st + row0(j) * M::ROWB);
-        glb_to_lds(pv, st + M::HALF + row0(j) * M::ROWB);
       }
     };
     const int k1 = hi > 0 ? sg.k1 : sg.k0;
-    if (sg.k0 < k1) {
-      fetch_pages(sg.k0);
-      issue(sg.k0, 0);
+    if (sg.k0 < k1) fetch_pages(sg.k0);
+    // a negative scale is taken over by the queries' signs, 0 by queries of 0: the scaled
+    // maximum is then the maximum scaled
+#pragma unroll
+    for (int s = 0; s < QS; ++s) {
+      const uint32_t keep = a.scale != 0.0f && 16 * s + 8 * h < a.D ? ~0u : 0u;
+      qv[s] = (qv[s] ^ flip) & keep;
     }
+    if (sg.k0 < k1) issue(sg.k0, 0);
     if (sg.k0 + 1 < k1) issue(sg.k0 + 1, 1);
     int at = 0;
     for (int i = sg.k0; i < k1; ++i) {
@@ -477,7 +521,7 @@ void k_attn_many(AttnArgs a) {
         for (int q = 0; q < QS; ++q) {
           const bf16x8 kv = *reinterpret_cast<const bf16x8 *>(
               sk + row * M::ROWB + (((2 * q + h) ^ many_k<CH>(row)) * 16));
-          s[b] = mfma32(kv, qv[q], s[b]);
+          s[b] = mfma32(kv, __builtin_bit_cast(bf16x8, qv[q]), s[b]);
         }
       }
       if (k0 + BK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window)) {
@@ -562,52 +606,130 @@ void k_attn_many(AttnArgs a) {
   if (threadIdx.x == 0) a.rec[w] = begun;
 }
 
-// The parts of a unit, in order: a wavefront a row
-template <typename T, int R, int DP>
-__global__ __launch_bounds__(256)
-void k_attn_join(AttnArgs a) {
-  const AttnPart p = a.rec[blockIdx.x];
-  const int r = blockIdx.y * 4 + wave_id_u(), lane = lane_id();
-  if (p.count == 0 || r >= p.n) return;
-  constexpr size_t F = attn_part_floats<R, DP>();
+// The parts of the units that lie in several workgroups' stretches, added in their order.
+// Workgroup b takes its share of the unit that goes on behind stretch b: a unit of count
+// parts has count - 1 workgroups.
+template <typename T>
+__device__ __forceinline__ void join_store(const AttnArgs &a, const AttnPart &p, int r, int at, float top,
+                                           float sum, float o) {
+  const int pr = p.r0 + r, tok = over(pr, a.by_G), head = p.head + pr - tok * a.G;
+  const long long row = p.token + tok;
+  const float v = sum > 0.0f ? o / sum : (sum == 0.0f ? 0.0f : sum);
+  T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
+  if (at < a.D) {
+    if constexpr (sizeof(T) == 2) out[at] = f32_to_bf16_any(v);
+    else out[at] = v;
+  }
+  if (a.lse && at == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+}
+// Sums of parts k0, k0 + step, .. (NB at a time, their loads together) of RB rows
+template <int R, int DP, int RB, int NB>
+__device__ __forceinline__ void join_sum(const AttnArgs &a, const AttnPart &p, int r0, int k0, int step,
+                                         float (&top)[RB], float (&sum)[RB], float (&o)[RB][DP / WAVE]) {
   constexpr int E = DP / WAVE;
-  auto part = [&](int k) { return a.part + (k == 0 ? p.slot : 2 * (p.w + k)) * F; };
-  float top = -INFINITY;
-  for (int k = lane; k < p.count; k += WAVE) top = fmaxf(top, part(k)[R * DP + r]);
-  top = fmaxf(top, xor_lane<32>(top));
-  top = fmaxf(top, xor_lane<16>(top));
-  top = fmaxf(top, xor_lane<8>(top));
-  top = fmaxf(top, xor_lane<4>(top));
-  top = fmaxf(top, xor_lane<2>(top));
-  top = fmaxf(top, xor_lane<1>(top));
-  const float mm = top == -INFINITY ? 0.0f : top;
-  float o[E], sum = 0.0f;
+  constexpr size_t F = attn_part_floats<R, DP>();
+  const int lane = lane_id();
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  for (int k0 = 0; k0 < p.count; k0 += WAVE) {
-    const int k = k0 + lane;
-    const float f = k < p.count ? __builtin_amdgcn_exp2f(part(min(k, p.count - 1))[R * DP + r] - mm) : 0.0f;
-    sum += wave_tree_sum(k < p.count ? f * part(k)[R * DP + R + r] : 0.0f);
-    const int left = min(WAVE, p.count - k0);
-#pragma unroll 8
-    for (int j = 0; j < left; ++j) {
-      const float fj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j));
-      const float *src = part(k0 + j) + r * DP + lane * E;
+  for (int b = 0; b < RB; ++b) {
+    top[b] = -INFINITY;
+    sum[b] = 0.0f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(fj, src[e], o[e]);
+    for (int e = 0; e < E; ++e) o[b][e] = 0.0f;
+  }
+  for (; k0 < p.count; k0 += NB * step) {
+    float m[NB][RB], l[NB][RB], x[NB][RB][E];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int k = min(k0 + j * step, p.count - 1);
+      const float *part = a.part + (k == 0 ? p.slot : 2 * (p.w + k)) * F;
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const int r = min(r0 + b, p.n - 1);
+        m[j][b] = part[R * DP + r];
+        l[j][b] = part[R * DP + R + r];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[j][b][e] = part[r * DP + WAVE * e + lane];
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      float to = top[b];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if (k0 + j * step >= p.count) m[j][b] = -INFINITY;
+        to = fmaxf(to, m[j][b]);
+      }
+      const float mm = to == -INFINITY ? 0.0f : to, f0 = __builtin_amdgcn_exp2f(top[b] - mm);
+      top[b] = to;
+      sum[b] *= f0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[b][e] *= f0;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const float f = __builtin_amdgcn_exp2f(m[j][b] - mm);   // 0 past the last part
+        if (k0 + j * step >= p.count) continue;
+        sum[b] = __builtin_fmaf(f, l[j][b], sum[b]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[b][e] = __builtin_fmaf(f, x[j][b][e], o[b][e]);
+      }
     }
   }
-  const int pr = p.r0 + r, tok = pr / a.G, head = p.head + pr - tok * a.G;
-  const long long row = p.token + tok;
-  const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
-  T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
+}
+template <typename T, int R, int DP>
+__global__ __launch_bounds__(R > 32 ? 1024 : 512)
+void k_attn_join(AttnArgs a) {
+  constexpr int WAVES = R > 32 ? 16 : 8, E = DP / WAVE;
+  __shared__ float ml[WAVES][2], os[WAVES][DP];
+  const AttnPart p = a.rec[blockIdx.x];
+  if (p.count == 0) return;
+  const int share = blockIdx.x - p.w, shares = p.count - 1, wave = wave_id_u(), lane = lane_id();
+  if (p.count <= 4) {   // a wavefront a row, several rows' loads together
+    constexpr int RB = R > 32 ? (DP == 256 ? 2 : 4) : 1;
+    for (int r0 = (share * WAVES + wave) * RB; r0 < p.n; r0 += shares * WAVES * RB) {
+      float top[RB], sum[RB], o[RB][E];
+      if (p.count == 2) join_sum<R, DP, RB, 2>(a, p, r0, 0, 1, top, sum, o);
+      else join_sum<R, DP, RB, 4>(a, p, r0, 0, 1, top, sum, o);
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if (lane * E + e >= a.D) continue;
-    if constexpr (sizeof(T) == 2) out[lane * E + e] = f32_to_bf16_any(o[e] * inv);
-    else out[lane * E + e] = o[e] * inv;
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (r0 + b < p.n) join_store<T>(a, p, r0 + b, WAVE * e + lane, top[b], sum[b], o[b][e]);
+    }
+    return;
   }
-  if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+  // `per` wavefronts a row, with every so-manieth part
+  int per = 2;
+  while (per < WAVES && per * 8 < p.count) per *= 2;
+  const int sub = wave & (per - 1), groups = WAVES / per, group = wave / per;
+  for (int r0 = share * groups; r0 < p.n; r0 += shares * groups) {
+    const int r = min(r0 + group, p.n - 1);
+    float top[1], sum[1], o[1][E];
+    join_sum<R, DP, 1, 8>(a, p, r, sub, per, top, sum, o);
+    if (lane == 0) {
+      ml[wave][0] = top[0];
+      ml[wave][1] = sum[0];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) os[wave][WAVE * e + lane] = o[0][e];
+    __syncthreads();
+    if (sub == 0 && r0 + group < p.n) {
+      float to = -INFINITY;
+      for (int v = 0; v < per; ++v) to = fmaxf(to, ml[wave + v][0]);
+      const float mm = to == -INFINITY ? 0.0f : to;
+      float t = 0.0f, x[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = 0.0f;
+      for (int v = 0; v < per; ++v) {
+        const float f = __builtin_amdgcn_exp2f(ml[wave + v][0] - mm);
+        t = __builtin_fmaf(f, ml[wave + v][1], t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, os[wave + v][WAVE * e + lane], x[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) join_store<T>(a, p, r, WAVE * e + lane, to, t, x[e]);
+    }
+    __syncthreads();
+  }
 }
 
 // The launches of a call.  Sequences of at most FEW_ROWS packed rows are k_attn_few's,
@@ -615,7 +737,7 @@ void k_attn_join(AttnArgs a) {
 // workspace of their own.
 constexpr int FEW_ROWS = 32;
 struct Launch {
-  int R, BK, W;             // W 0: none
+  int R, BK, W, coarse, least;   // W 0: none
   bool whole;
   size_t part, rec;         // in the workspace, bytes
 };
@@ -628,22 +750,24 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   Plan p{};
   p.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   const long long G = Hq / c.Hk, most = b.max_q * G;
-  auto shape = [&](Launch &l, int R, int BK, bool may_be_whole) {
+  auto shape = [&](Launch &l, int R, int BK, int occ, int least, bool may_be_whole) {
     l.R = R;
+    l.least = least;
     l.BK = BK;
     const long long blocks = (((long long)b.max_pages << c.shift) + BK - 1) / BK;
     const double units = (double)b.n_seq * c.Hk * ((most + R - 1) / R);
     l.whole = may_be_whole && blocks <= 2;
+    while (units * (double)((blocks >> l.coarse) + 1) > 1e9) ++l.coarse;
     const double want = l.whole ? (units < 65536 ? units : 65536) : units * blocks;
-    l.W = l.whole || want < n_cu ? (int)want : n_cu;
+    l.W = l.whole || want < occ * n_cu ? (int)want : occ * n_cu;
     l.part = p.bytes;
     if (!l.whole) p.bytes += 2 * (size_t)l.W * R * (p.dp + 2) * 4;
     l.rec = p.bytes = (p.bytes + 255) & ~(size_t)255;
     if (!l.whole) p.bytes += ((size_t)l.W * sizeof(AttnPart) + 255) & ~(size_t)255;
   };
   if (!bf16 || most <= FEW_ROWS || b.n_seq > 1)
-    shape(p.few, 32, !bf16 || p.dp == 256 ? 64 : 128, true);
-  if (bf16 && most > FEW_ROWS) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, false);
+    shape(p.few, p.dp == 256 || most <= 16 ? 16 : 32, 64, !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1, 1, true);
+  if (bf16 && most > FEW_ROWS) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, 6, false);
   if (p.bytes == 0) p.bytes = 256;
   return p;
 }
@@ -670,40 +794,50 @@ hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b,
   a.D = call.D;
   a.window = call.window;
   a.scale = call.scale * LOG2E;
-  const long long most = (long long)b.max_q * a.G;
+  a.by_G = divisor(a.G);
   auto use = [&](const Launch &l, int above, int upto) {
     a.above = above;
     a.upto = upto;
     a.W = l.W;
     a.whole = l.whole;
+    a.coarse = l.coarse;
+    a.by_W = divisor(l.W);
+    a.least = l.least;
     a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
     a.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);
-    return dim3((unsigned)l.W, (unsigned)(((most < l.R ? most : l.R) + 3) / 4));
   };
 #define BASE_MANY(DP)                                                                            \
   do {                                                                                           \
     launch_k(k_attn_many<DP>, dim3(p.many.W), dim3(ManyShape<DP>::THREADS), 0, st, a);           \
-    launch_k(k_attn_join<uint16_t, ManyShape<DP>::R, DP>, join, dim3(256), 0, st, a);            \
+    launch_k(k_attn_join<uint16_t, ManyShape<DP>::R, DP>, dim3(p.many.W), dim3(1024), 0, st, a); \
   } while (0)
-#define BASE_FEW(T, DP)                                                                          \
+#define BASE_FEW(T, DP, NR)                                                                      \
   do {                                                                                           \
-    launch_k(k_attn_few<T, DP>, dim3(p.few.W), dim3(FewShape<T, DP>::THREADS), 0, st, a);        \
-    if (!p.few.whole) launch_k(k_attn_join<T, 32, DP>, join, dim3(256), 0, st, a);               \
+    launch_k(k_attn_few<T, DP, NR>, dim3(p.few.W), dim3(FewShape<T, DP, NR>::THREADS), 0, st, a); \
+    if (!p.few.whole)                                                                            \
+      launch_k(k_attn_join<T, 16 * NR, DP>, dim3(p.few.W), dim3(512), 0, st, a);                 \
   } while (0)
+#define BASE_FEW_R(T, DP)                                                                        \
+  do { if (p.few.R == 16) BASE_FEW(T, DP, 1); else BASE_FEW(T, DP, 2); } while (0)
 #define BASE_FEW_D(T)                                                                            \
-  do { if (p.dp == 64) BASE_FEW(T, 64); else if (p.dp == 128) BASE_FEW(T, 128); else BASE_FEW(T, 256); } while (0)
+  do {                                                                                           \
+    if (p.dp == 64) BASE_FEW_R(T, 64);                                                           \
+    else if (p.dp == 128) BASE_FEW_R(T, 128);                                                    \
+    else BASE_FEW(T, 256, 1);                                                                    \
+  } while (0)
   if (p.many.W) {
-    const dim3 join = use(p.many, p.few.W ? FEW_ROWS : 0, 0x7FFFFFFF);
+    use(p.many, p.few.W ? FEW_ROWS : 0, 0x7FFFFFFF);
     if (p.dp == 64) BASE_MANY(64);
     else if (p.dp == 128) BASE_MANY(128);
     else BASE_MANY(256);
   }
   if (p.few.W) {
-    const dim3 join = use(p.few, 0, p.many.W ? FEW_ROWS : 0x7FFFFFFF);
+    use(p.few, 0, p.many.W ? FEW_ROWS : 0x7FFFFFFF);
     if (call.bf16) BASE_FEW_D(uint16_t);
     else BASE_FEW_D(float);
   }
 #undef BASE_FEW_D
+#undef BASE_FEW_R
 #undef BASE_FEW
 #undef BASE_MANY
   return hipGetLastError();

@@ -14,10 +14,36 @@ namespace basek {
 // (sequence, key head, tile) form one line of N blocks, and workgroup w of W takes the
 // stretch [w per, (w + 1) per), whatever the lengths are: a unit that lies in several
 // stretches is left in parts (the running maximum, the sum and the unnormalised output)
-// that k_attn_join adds in their order.
-struct AttnPart {
-  int token, head, r0, n, slot, count, w, pad;   // count parts: slot, then 2 (w + 1), 2 (w + 2), ..
+// that k_attn_join adds in their order.  A workgroup's parts lie at 2 w (its first
+// segment) and 2 w + 1.
+struct AttnPart {   // the unit that goes on behind a workgroup's stretch
+  int token, head, r0, n;
+  int slot, count, w, pad;   // count parts from workgroup w on: slot, 2 (w + 1), 2 (w + 2), ..
 };
+
+// x / by for 0 <= x < 2^31, by a product: by's m = floor(2^(31 + shift) / by) + 1 with
+// 2^shift >= by is too large by less than 2^-31 of itself (the host makes it)
+struct Divisor {
+  uint32_t m;
+  int shift;
+};
+inline Divisor divisor(uint32_t by) {
+  Divisor d{0, 0};
+  while ((1ull << d.shift) < by) ++d.shift;
+  d.m = (uint32_t)((1ull << (31 + d.shift)) / by + 1);
+  return d;
+}
+__device__ __forceinline__ int over(int x, Divisor d) {
+  return (int)(((uint64_t)(uint32_t)x * d.m) >> (31 + d.shift));
+}
+// x / y for 0 <= x < 2^31, 0 < y, with a quotient below 2^20
+__device__ __forceinline__ int quotient(int x, int y) {
+  int q = (int)((float)x * __builtin_amdgcn_rcpf((float)y));
+  int r = x - q * y;
+  if (r < 0) { --q; r += y; }
+  if (r >= y) ++q;
+  return q;
+}
 
 struct AttnArgs {
   HeadRows q, o;
@@ -25,27 +51,27 @@ struct AttnArgs {
   KvCache c;
   KvBatch b;
   int rows, Hq, G, D, window;
+  Divisor by_G, by_W;
   float scale;              // of the products, times log2 e
   int above, upto;          // sequences of more than `above` and at most `upto` packed rows
-  int W;                    // workgroups
+  int W, least;             // workgroups, and the least length of a stretch
+  int coarse;               // a cost is of 2^coarse blocks
   bool whole;               // every unit costs 1 and is done by one workgroup
   float *part;
-  AttnPart *rec;            // [W]: the unit that begins in workgroup w and ends in another
+  AttnPart *rec;            // [W]
 };
 
-// One sequence: its first row, new tokens (all, and those taken), keys, packed rows
+// One sequence: its first row, keys, new tokens taken, packed rows, and the first new
+// token's position (may be below 0)
 struct AttnSeq {
-  int first, n, kv, packed;
-  int pos0;                 // the first new token's position (may be below 0)
+  int first, kv, n, packed, pos0;
 };
-__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s) {
+// from its rows [begin, end) and keys, taken within their bounds
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int begin, int end, int kv) {
   AttnSeq q;
-  const int begin = min(max(a.b.q_start[s], 0), a.rows);
-  const int end = min(max(a.b.q_start[s + 1], begin), a.rows);
-  const long long room = (long long)a.b.max_pages << a.c.shift;
   q.first = begin;
-  q.kv = (int)min((long long)max(a.b.kv_len[s], 0), room);
-  q.pos0 = q.kv - (end - begin);
+  q.kv = kv;
+  q.pos0 = kv - (end - begin);
   q.n = min(end - begin, a.b.max_q);
   q.packed = q.n * a.G;
   if (q.packed <= a.above || q.packed > a.upto) q.packed = 0;
@@ -58,7 +84,7 @@ struct KeyRange {
 };
 __device__ __forceinline__ KeyRange attn_keys(const AttnArgs &a, const AttnSeq &q, int r0, int n) {
   KeyRange k;
-  const int p0 = q.pos0 + r0 / a.G, p1 = q.pos0 + (r0 + n - 1) / a.G;
+  const int p0 = q.pos0 + over(r0, a.by_G), p1 = q.pos0 + over(r0 + n - 1, a.by_G);
   k.hi = max(p1 + 1, 0);
   k.lo = a.window > 0 ? max(p0 - a.window + 1, 0) : 0;
   return k;
@@ -66,80 +92,79 @@ __device__ __forceinline__ KeyRange attn_keys(const AttnArgs &a, const AttnSeq &
 
 // a value that is the same in all lanes, known as such to the compiler
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ long long uni(long long v) {
-  return (long long)(((unsigned long long)(unsigned)uni((int)(v >> 32)) << 32) | (unsigned)uni((int)v));
-}
 
+// The walk of a workgroup over its stretch of the line (costs in units of 2^a.coarse
+// blocks, so that the line's length fits 31 bits).  Lane l holds sequence s0 + l.
 template <int R, int BK>
 struct AttnWork {
   const AttnArgs &a;
-  long long at, end;        // of this workgroup's stretch, what is left
-  long long per;
-  int w;
-  // where it stands: a sequence, its cost a head, the place inside it
-  int s;
+  int w, per, at, end;      // the stretch's rest
+  int s0, begin, stop, kv, cost;   // of the lane's sequence; cost: a head's
+  int s;                    // where it stands: the sequence, its cost a head, the place in it
   AttnSeq q;
-  int tiles;
-  long long head_cost, rem;
+  int head_cost, rem;
   bool first;
 
   __device__ int tile_cost(const AttnSeq &sq, int j) const {
     if (a.whole) return 1;
     const KeyRange k = attn_keys(a, sq, j * R, min(R, sq.packed - j * R));
-    const int c = (k.hi + BK - 1) / BK - k.lo / BK;
+    const int c = ((k.hi + BK - 1) / BK - k.lo / BK + (1 << a.coarse) - 1) >> a.coarse;
     return c > 1 ? c : 1;
   }
-  __device__ long long cost_a_head(const AttnSeq &sq) const {
+  __device__ void load(int from) {
+    s0 = from;
+    const int i = min(from + lane_id(), a.b.n_seq - 1);
+    begin = min(max(a.b.q_start[i], 0), a.rows);
+    stop = min(max(a.b.q_start[i + 1], begin), a.rows);
+    kv = min(max(a.b.kv_len[i], 0), a.b.max_pages << a.c.shift);
+    if (from + lane_id() >= a.b.n_seq) stop = begin;
+    const AttnSeq sq = attn_seq(a, begin, stop, kv);
     const int t = (sq.packed + R - 1) / R;
-    if (a.whole) return t;
-    long long c = 0;
-    for (int j = 0; j < t; ++j) c += tile_cost(sq, j);
-    return c;
+    cost = 0;
+    if (a.whole) cost = t;
+    else
+      for (int j = 0; j < t; ++j) cost += tile_cost(sq, j);
   }
 
   __device__ AttnWork(const AttnArgs &args, int w_) : a(args), w(w_), first(true) {
     const int lane = lane_id();
-    long long c = 0, total = 0;
-    for (int s0 = 0; s0 < a.b.n_seq; s0 += WAVE) {
-      c = s0 + lane < a.b.n_seq ? cost_a_head(attn_seq(a, s0 + lane)) * a.c.Hk : 0;
-      total += c;
+    int total = 0, run = 0;
+    for (int from = 0; from < a.b.n_seq; from += WAVE) {
+      load(from);
+      total += cost;
     }
+    total *= a.c.Hk;
 #pragma unroll
     for (int h = 1; h < WAVE; h *= 2) total += __shfl_xor(total, h, WAVE);
     total = uni(total);
-    per = (total + a.W - 1) / a.W;
-    if (per < 1) per = 1;
-    at = w * per;
-    end = at + per < total ? at + per : total;
-    s = a.b.n_seq;
-    rem = 0;
+    per = max(over(total + a.W - 1, a.by_W), a.least);
+    at = min(w * (long long)per, (long long)total);
+    end = min(at + per, total);
     if (at >= end) return;
-    long long run = 0;
-    for (int s0 = 0; s0 < a.b.n_seq; s0 += WAVE) {
-      if (a.b.n_seq > WAVE) c = s0 + lane < a.b.n_seq ? cost_a_head(attn_seq(a, s0 + lane)) * a.c.Hk : 0;
-      long long incl = c;
+    for (int from = 0; from < a.b.n_seq; from += WAVE) {
+      if (a.b.n_seq > WAVE) load(from);
+      int incl = cost * a.c.Hk;
 #pragma unroll
       for (int h = 1; h < WAVE; h *= 2) {
-        const long long o = __shfl_up(incl, h, WAVE);
+        const int o = __shfl_up(incl, h, WAVE);
         if (lane >= h) incl += o;
       }
       const unsigned long long hit = __ballot(run + incl > at);
       if (hit) {
         const int l = __ffsll(hit) - 1;
-        s = s0 + l;
-        rem = at - run - __shfl(incl - c, l, WAVE);
+        rem = at - run - __builtin_amdgcn_readlane(incl - cost * a.c.Hk, l);
+        enter(from + l);
         break;
       }
-      run += __shfl(incl, WAVE - 1, WAVE);
+      run += __builtin_amdgcn_readlane(incl, WAVE - 1);
     }
-    s = uni(s);
-    rem = uni(rem);
-    enter();
   }
-  __device__ void enter() {
-    q = attn_seq(a, s);
-    tiles = (q.packed + R - 1) / R;
-    head_cost = cost_a_head(q);
+  __device__ void enter(int i) {
+    s = i;
+    const int l = i - s0;
+    q = attn_seq(a, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(stop, l),
+                 __builtin_amdgcn_readlane(kv, l));
+    head_cost = __builtin_amdgcn_readlane(cost, l);
   }
 
   // The next segment: blocks [k0, k1) of a unit whose rows are r0 .. r0 + n - 1 of the
@@ -151,13 +176,17 @@ struct AttnWork {
   };
   __device__ bool next(Segment &g, AttnPart &begun) {
     if (at >= end) return false;
-    while (rem >= head_cost * a.c.Hk) {
-      ++s;
+    while (rem >= head_cost * a.c.Hk) {   // on to the next sequence that has work
       rem = 0;
-      enter();
+      unsigned long long more = __ballot(cost > 0) & (s - s0 == WAVE - 1 ? 0ull : ~0ull << (s - s0 + 1));
+      while (!more) {
+        load(s0 + WAVE);
+        more = __ballot(cost > 0);
+      }
+      enter(s0 + __ffsll(more) - 1);
     }
-    g.hk = (int)(rem / head_cost);
-    int left = (int)(rem - g.hk * head_cost), j = 0, c;
+    g.hk = quotient(rem, head_cost);
+    int left = rem - g.hk * head_cost, j = 0, c;
     while (left >= (c = tile_cost(q, j))) {
       left -= c;
       ++j;
@@ -165,20 +194,15 @@ struct AttnWork {
     g.r0 = j * R;
     g.n = min(R, q.packed - g.r0);
     g.keys = attn_keys(a, q, g.r0, g.n);
-    const int base = a.whole ? 0 : g.keys.lo / BK;
-    const int take = (int)min((long long)(c - left), end - at);
-    g.k0 = base + left;
-    g.k1 = g.k0 + take;
+    const int take = min(c - left, end - at), b0 = g.keys.lo / BK, b1 = (g.keys.hi + BK - 1) / BK;
+    g.k0 = a.whole ? b0 : b0 + (left << a.coarse);
+    g.k1 = take == c - left ? b1 : b0 + ((left + take) << a.coarse);
     g.slot = -1;
-    if (a.whole) {
-      g.k0 = g.keys.lo / BK;
-      g.k1 = (g.keys.hi + BK - 1) / BK;
-    } else if (take < c) {
-      g.slot = 2 * w + (first ? 0 : 1);
-      if (left == 0) {   // the unit begins here and goes on
-        const int last = (int)((at + c - 1) / per);
-        begun = {q.first, g.hk * a.G, g.r0, g.n, g.slot, last - w + 1, w, 0};
-      }
+    if (take < c) g.slot = 2 * w + (first ? 0 : 1);
+    if (left + take < c) {   // the unit goes on in the next workgroup
+      const int from = at - left, w0 = quotient(from, per);
+      begun = {q.first, g.hk * a.G, g.r0, g.n, 2 * w0 + (from == w0 * per ? 0 : 1),
+               quotient(from + c - 1, per) - w0 + 1, w0, 0};
     }
     first = false;
     at += take;

@@ -23,7 +23,7 @@ def rope(**kw):
 
 
 def heads(p=FAKE, row=4096, head=128):
-    return bd.base_heads(p, row, head)
+    return p, row, head
 
 
 def cache(**kw):
@@ -43,17 +43,17 @@ def ref(x):
 
 def turn(lib, R=rope(), rows=4, pos=FAKE, Hq=32, q=heads(), qo=heads(FAKE << 1), Hk=4, k=heads(FAKE << 2),
          ko=heads(FAKE << 3)):
-    return lib.base_head_rope(ref(R), rows, pos, Hq, ref(q), ref(qo), Hk, ref(k), ref(ko), None)
+    return lib.base_head_rope(ref(R), rows, pos, Hq, *q, *qo, Hk, *k, *ko, None)
 
 
 def append(lib, R=rope(), C=cache(), S=batch(), rows=4, pos=None, Hq=32, q=heads(), qo=heads(FAKE << 1),
            k=heads(FAKE << 2), v=heads(FAKE << 3)):
-    return lib.base_kv_append(ref(R), ref(C), ref(S), rows, pos, Hq, ref(q), ref(qo), ref(k), ref(v), None)
+    return lib.base_kv_append(ref(R), ref(C), ref(S), rows, pos, Hq, *q, *qo, *k, *v, None)
 
 
 def attend(lib, C=cache(), S=batch(), rows=4, Hq=32, q=heads(), out=heads(FAKE << 1), lse=None, scale=0.1, window=0,
            ws=FAKE, n=1 << 40):
-    return lib.base_paged_attention(ref(C), ref(S), rows, Hq, ref(q), ref(out), lse, scale, window, ws, n, None)
+    return lib.base_paged_attention(ref(C), ref(S), rows, Hq, *q, *out, lse, scale, window, ws, n, None)
 
 
 BAD_ROPE = [(dict(D=4), SHAPE), (dict(D=264), SHAPE), (dict(D=124), SHAPE), (dict(rot=-2), SHAPE),
@@ -74,7 +74,7 @@ def test_head_rope_arguments(lib):
         assert turn(lib, rows=rows) == SHAPE
     assert turn(lib, Hq=0, Hk=0) == SHAPE and turn(lib, Hq=-1) == SHAPE and turn(lib, Hk=1025) == SHAPE
     for f in ("q", "qo", "k", "ko"):
-        assert turn(lib, **{f: None}) == NULL and turn(lib, **{f: heads(0)}) == NULL
+        assert turn(lib, **{f: heads(0)}) == NULL
         assert turn(lib, **{f: heads(FAKE + 1)}) == ALIGN
         assert turn(lib, rope(dtype=0), **{f: heads(FAKE + 2)}) == ALIGN
         for bad in (heads(row=-1), heads(head=-8), heads(row=BIG), heads(head=BIG)):
@@ -86,7 +86,7 @@ def test_head_rope_arguments(lib):
 BAD_CACHE = [(dict(Hk=0), SHAPE), (dict(Hk=1025), SHAPE), (dict(D=4), SHAPE), (dict(D=260), SHAPE),
              (dict(dtype=-1), DTYPE), (dict(page_size=8), SHAPE), (dict(page_size=48), SHAPE),
              (dict(page_size=131072), SHAPE), (dict(n_pages=0), SHAPE), (dict(k=0), NULL), (dict(v=0), NULL),
-             (dict(k=FAKE + 8), ALIGN), (dict(v=FAKE + 2), ALIGN), (dict(k_page=-8), SHAPE), (dict(k_slot=BIG), SHAPE),
+             (dict(k=FAKE + 8), ALIGN), (dict(v=FAKE + 2), ALIGN), (dict(k_page=-8), SHAPE), (dict(k_slot=BIG), SHAPE), (dict(v_slot=(1 << 25) + 8), SHAPE),
              (dict(k_head=4), ALIGN), (dict(v_page=BIG), SHAPE), (dict(v_slot=132), ALIGN), (dict(v_head=-1), SHAPE)]
 BAD_BATCH = [(dict(n_seq=0), SHAPE), (dict(n_seq=65537), SHAPE), (dict(max_pages=0), SHAPE),
              (dict(max_pages=(1 << 26) + 1), SHAPE), (dict(table_ld=19), SHAPE), (dict(table_ld=BIG), SHAPE),
@@ -110,7 +110,7 @@ def test_append_arguments(lib):
     assert append(lib, rows=0) == SHAPE and append(lib, Hq=0) == SHAPE and append(lib, Hq=1025) == SHAPE
     assert append(lib, pos=FAKE + 2) == ALIGN
     for f in ("q", "qo", "k", "v"):
-        assert append(lib, **{f: None}) == NULL and append(lib, **{f: heads(FAKE + 1)}) == ALIGN
+        assert append(lib, **{f: heads(0)}) == NULL and append(lib, **{f: heads(FAKE + 1)}) == ALIGN
         assert append(lib, **{f: heads(row=BIG)}) == SHAPE
     assert append(lib, qo=heads(row=4104)) == FLAGS
 
@@ -124,7 +124,7 @@ def test_attention_arguments(lib):
     assert attend(lib, S=batch(max_q=1 << 30)) == SHAPE            # packed rows past 32 bits
     assert attend(lib, scale=NAN) == SHAPE and attend(lib, scale=INF) == SHAPE and attend(lib, window=-1) == SHAPE
     for f in ("q", "out"):
-        assert attend(lib, **{f: None}) == NULL and attend(lib, **{f: heads(FAKE + 1)}) == ALIGN
+        assert attend(lib, **{f: heads(0)}) == NULL and attend(lib, **{f: heads(FAKE + 1)}) == ALIGN
         assert attend(lib, **{f: heads(head=-1)}) == SHAPE
     assert attend(lib, out=heads(head=136)) == FLAGS and attend(lib, lse=FAKE + 2) == ALIGN
     assert attend(lib, ws=None) == NULL and attend(lib, ws=FAKE + 128) == ALIGN
