@@ -79,28 +79,30 @@ struct FewShape {
   static constexpr int WAVES = BF ? 2 : 4, THREADS = WAVES * WAVE, BK = WAVES * TK;
   static constexpr int CH = DP / 8;                        // 16-byte pieces of a 16-bit row
   static constexpr int ROWB = DP * 2, STAGE = 2 * TK * ROWB, RING = 2, LOADS = CH;
-  static constexpr int JOIN = WAVES * R * (DP + 2) * 4;
-  static constexpr int LDS = BF && WAVES * RING * STAGE > JOIN ? WAVES * RING * STAGE : JOIN;
+  static constexpr int STATE = DP * 64 + 512;              // 16 rows of a wavefront's state
+  static constexpr int AREA = (WAVES - 1) * STATE, LDS = (BF ? WAVES * RING * STAGE : 0) + AREA;
   static constexpr int OCC = BF ? (DP == 64 ? 4 : DP == 128 ? 2 : 1) : DP == 64 ? 2 : 1;   // workgroups a CU
   static constexpr int WPE = OCC * WAVES >= 4 ? OCC * WAVES / 4 : 1;
+  static_assert(OCC * LDS <= 160 * 1024, "LDS of a CU");
 };
 
 // pieces' places in a row of the ring: K's row r at piece ^ few_k(r), V's at piece ^ few_v(r)
 template <int CH> __device__ __forceinline__ int few_k(int r) { return CH == 8 ? (r >> 1) & 7 : r & 15; }
 template <int CH> __device__ __forceinline__ int few_v(int r) { return CH == 8 ? 2 * ((r >> 1) & 3) : 2 * (r & 7); }
 
-template <typename T, int DP, int NR_>
-__global__ __launch_bounds__((FewShape<T, DP, NR_>::THREADS), (FewShape<T, DP, NR_>::WPE))
+template <typename T, int DP, int NR>
+__global__ __launch_bounds__((FewShape<T, DP, NR>::THREADS), (FewShape<T, DP, NR>::WPE))
 void k_attn_few(AttnArgs a) {
-  using M = FewShape<T, DP, NR_>;
+  using M = FewShape<T, DP, NR>;
   constexpr bool BF = M::BF;
-  constexpr int R = M::R, NR = M::NR, TK = M::TK;
+  constexpr int R = M::R, TK = M::TK;
   constexpr int DT = DP / 16;                     // accumulator tiles
   constexpr int QS = BF ? DP / 32 : DP / 16;      // operand pieces of 16 bytes
+  using Work = AttnWork<R, M::BK>;
   __shared__ __attribute__((aligned(256))) char lds[M::LDS];
   const int wave = wave_id_u(), lane = lane_id(), n = lane % 16, g = lane / 16;
-  const int w = blockIdx.x;
   const char *zero = reinterpret_cast<const char *>(g_zero);
+  char *const area = lds + M::LDS - M::AREA;
   // the lane's places in the loads of a step (piece j of 64 16-byte pieces)
   uint32_t ko[BF ? M::CH / 2 : 1], vo[BF ? M::CH / 2 : 1];
   if constexpr (BF) {
@@ -111,18 +113,34 @@ void k_attn_few(AttnArgs a) {
       vo[j] = 2 * ((row & 15) * (uint32_t)a.c.v_slot + 8 * (piece ^ few_v<M::CH>(row)));
     }
   }
-  AttnPart begun{};
-  AttnWork<R, M::BK> work(a, w);
-  typename AttnWork<R, M::BK>::Segment sg;
-  while (work.next(sg, begun)) {
-    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1;
-    int pos[NR];
-    u32x4 qv[NR][QS];
+  char *const ring = lds + wave * M::RING * M::STAGE;
+  const uint32_t ring_at = lds_addr(ring);
+
+  // A segment as the wavefront has it: its steps i0 .. i1 - 1 (keys key0(i) .. + TK - 1),
+  // the next one to request, and the pages of 32 steps, two a step (16 keys lie in one
+  // page): lane e has those of step from + e / 2
+  struct Seg {
+    typename Work::Segment g;
+    int i0, i1, ask, from, pages;
+  };
+  auto key0 = [&](int i) { return i * M::BK + wave * TK; };
+  auto fetch_pages = [&](Seg &z, int i) {
+    z.from = i;
+    const int key = key0(i + lane / 2) + 16 * (lane & 1);
+    z.pages = attn_page(a, z.g.s, max(min(key, z.g.keys.hi - 1), 0));
+  };
+  auto steps = [&](Seg &z) {
+    z.i0 = z.g.k0;
+    z.i1 = z.g.k1;
+    while (z.i0 < z.i1 && key0(z.i0) + TK <= z.g.keys.lo) ++z.i0;
+    while (z.i1 > z.i0 && key0(z.i1 - 1) >= z.g.keys.hi) --z.i1;
+    z.ask = z.i0;
+  };
+  auto queries = [&](const typename Work::Segment &sg, u32x4 (&qv)[NR][QS]) {
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
       const int r = 16 * c + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
-      pos[c] = r < sg.n ? work.q.pos0 + tok : -1;
-      const T *p = (const T *)a.q.p + (long long)(work.q.first + tok) * a.q.row +
+      const T *p = (const T *)a.q.p + (long long)(sg.q.first + tok) * a.q.row +
                    (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
@@ -132,17 +150,90 @@ void k_attn_few(AttnArgs a) {
         else qv[c][s] = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
       }
     }
-    // (behind the pages' load, so that the two are waited for together)
-    auto mask_queries = [&] {
+  };
+  // the segment's next step into the stage given
+  auto issue = [&](Seg &z, int stage) {
+    const int i = z.ask++, k0 = key0(i), lo = z.g.keys.lo, hi = z.g.keys.hi;
+    if (i - z.from >= 32) fetch_pages(z, i);
+    const uint32_t st = ring_at + stage * M::STAGE;
+    const char *kb[2], *vb[2];
 #pragma unroll
-      for (int c = 0; c < NR; ++c)
+    for (int h = 0; h < 2; ++h) {
+      const long long page = __builtin_amdgcn_readlane(z.pages, 2 * (i - z.from) + h);
+      const long long slot = (k0 + 16 * h) & ((1 << a.c.shift) - 1);
+      kb[h] = uni_at((const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + z.g.hk * a.c.k_head));
+      vb[h] = uni_at((const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + z.g.hk * a.c.v_head));
+    }
+    if (k0 >= lo && k0 + TK <= hi && a.D == DP) {
 #pragma unroll
-        for (int s = 0; s < QS; ++s) {
-          const uint32_t keep = (BF ? 32 * s + 8 * g : 16 * s + 4 * g) < a.D ? ~0u : 0u;
-          qv[c][s] = qv[c][s] & keep;
-        }
-    };
-    const int pmin = work.q.pos0 + over(sg.r0, a.by_G), pmax = work.q.pos0 + over(sg.r0 + sg.n - 1, a.by_G);
+      for (int j = 0; j < M::CH / 2; ++j) {
+        const int h = WAVE * j / M::CH / 16;
+        glb_to_lds(kb[h], ko[j], st + j * 1024);
+        glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
+      }
+    } else {
+      // a step at the end of what is seen, or heads shorter than DP: zeros in the places
+      // of what is not there
+#pragma unroll 1
+      for (int j = 0; j < M::CH / 2; ++j) {
+        const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
+        const int ck = piece ^ few_k<M::CH>(row), cv = piece ^ few_v<M::CH>(row);
+        const bool h = row >= 16, in = k0 + row >= lo && k0 + row < hi;
+        const char *pk = (h ? kb[1] : kb[0]) + 2 * ((row & 15) * a.c.k_slot + 8 * ck);
+        const char *pv = (h ? vb[1] : vb[0]) + 2 * ((row & 15) * a.c.v_slot + 8 * cv);
+        glb_to_lds(in && 8 * ck < a.D ? pk : zero, st + j * 1024);
+        glb_to_lds(in && 8 * cv < a.D ? pv : zero, st + TK * M::ROWB + j * 1024);
+      }
+    }
+  };
+
+  AttnPart begun{};
+  Work work(a, blockIdx.x);
+  Seg z, ahead;
+  u32x4 qv[NR][QS], qn[NR][QS];
+  int asked = 0, used = 0;   // steps requested and used, of all segments: the ring's places
+  bool more = work.next(z.g, begun);
+  if (more) {
+    steps(z);
+    queries(z.g, qn);
+    if (BF) fetch_pages(z, z.i0);
+  }
+  while (more) {
+    const typename Work::Segment &sg = z.g;
+    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1;
+#pragma unroll
+    for (int c = 0; c < NR; ++c)
+#pragma unroll
+      for (int s = 0; s < QS; ++s) {
+        const uint32_t keep = (BF ? 32 * s + 8 * g : 16 * s + 4 * g) < a.D ? ~0u : 0u;
+        qv[c][s] = qn[c][s] & keep;
+      }
+    if constexpr (BF)
+      while (z.ask < z.i1 && z.ask < z.i0 + M::RING) issue(z, asked++ & 1);
+    // the next segment's queries and pages, and its first steps behind this one's last:
+    // between segments the memory is not left waiting
+    more = work.next(ahead.g, begun);
+    if (more) {
+      steps(ahead);
+      queries(ahead.g, qn);
+      if constexpr (BF) {
+        fetch_pages(ahead, ahead.i0);
+        // waited for here, where what is in flight besides has been for long: the compiler's
+        // wait at their first use would be for the steps requested since, too
+#pragma unroll
+        for (int c = 0; c < NR; ++c)
+#pragma unroll
+          for (int s = 0; s < QS; ++s) asm volatile("" ::"v"(qn[c][s]));
+        asm volatile("" ::"v"(ahead.pages));
+      }
+    }
+    int pos[NR];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const int r = 16 * c + n;
+      pos[c] = r < sg.n ? sg.q.pos0 + over(sg.r0 + min(r, sg.n - 1), a.by_G) : -1;
+    }
+    const int pmin = sg.q.pos0 + over(sg.r0, a.by_G), pmax = sg.q.pos0 + over(sg.r0 + sg.n - 1, a.by_G);
     f32x4 acc[NR][DT];
     float m[NR], l[NR];
 #pragma unroll
@@ -153,13 +244,7 @@ void k_attn_few(AttnArgs a) {
       for (int t = 0; t < DT; ++t) acc[c][t] = f32x4{0, 0, 0, 0};
     }
 
-    // the wavefront's steps: keys key0(i) .. + TK - 1 with a key in [lo, hi)
-    auto key0 = [&](int i) { return i * M::BK + wave * TK; };
-    int i0 = sg.k0, i1 = sg.k1;
-    while (i0 < i1 && key0(i0) + TK <= lo) ++i0;
-    while (i1 > i0 && key0(i1 - 1) >= hi) --i1;
-
-    // p (rounded for the second product) from the products of a step, and m, l, acc's scale
+    // p (for the second product) from the products of a step, and m, l, acc's scale
     auto soften = [&](int c, int k0, float (&x)[TK / 4]) {
       const bool cut = k0 + TK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window) || c * 16 + 16 > sg.n;
       float top = -INFINITY;
@@ -194,64 +279,12 @@ void k_attn_few(AttnArgs a) {
       }
     };
 
-    if constexpr (BF) {
-      char *ring = lds + wave * M::RING * M::STAGE;
-      const uint32_t ring_at = lds_addr(ring);
-      // the pages of 32 steps at a time, two a step (16 keys lie in one page): lane l has
-      // those of step from + l / 2
-      int from = i0, pages = 0;
-      auto fetch_pages = [&](int i) {
-        from = i;
-        const int key = key0(i + lane / 2) + 16 * (lane & 1);
-        pages = attn_page(a, work.s, min(key, hi - 1));
-      };
-      auto issue = [&](int i) {
-        if (i - from >= 32) fetch_pages(i);
-        const int k0 = key0(i);
-        const uint32_t st = ring_at + (i & 1) * M::STAGE;
-        const bool all = k0 >= lo && k0 + TK <= hi && a.D == DP;
-        const char *kb[2], *vb[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int key = k0 + 16 * h;
-          const long long page = __builtin_amdgcn_readlane(pages, 2 * (i - from) + h);
-          const long long slot = key & ((1 << a.c.shift) - 1);
-          kb[h] = uni_at((const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head));
-          vb[h] = uni_at((const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head));
-        }
-        if (all) {
-#pragma unroll
-          for (int j = 0; j < M::CH / 2; ++j) {
-            const int h = WAVE * j / M::CH / 16;
-            glb_to_lds(kb[h], ko[j], st + j * 1024);
-            glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
-          }
-        } else {
-          // a step at the end of what is seen, or heads shorter than DP: zeros in the places
-          // of what is not there
-#pragma unroll 1
-          for (int j = 0; j < M::CH / 2; ++j) {
-            const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
-            const int ck = piece ^ few_k<M::CH>(row), cv = piece ^ few_v<M::CH>(row);
-            const bool h = row >= 16, in = k0 + row >= lo && k0 + row < hi;
-            const char *pk = (h ? kb[1] : kb[0]) + 2 * ((row & 15) * a.c.k_slot + 8 * ck);
-            const char *pv = (h ? vb[1] : vb[0]) + 2 * ((row & 15) * a.c.v_slot + 8 * cv);
-            glb_to_lds(in && 8 * ck < a.D ? pk : zero, st + j * 1024);
-            glb_to_lds(in && 8 * cv < a.D ? pv : zero, st + TK * M::ROWB + j * 1024);
-          }
-        }
-      };
-      if (i0 < i1) fetch_pages(i0);
-      mask_queries();
-      for (int i = i0 - 2; i < i1; ++i) {
-        if (i < i0) {
-          if (i + 2 < i1) issue(i + 2);
-          continue;
-        }
-        if (i + 1 < i1) wait_vm<M::LOADS>();
+    for (int i = z.i0; i < z.i1; ++i) {
+      const int k0 = key0(i);
+      if constexpr (BF) {
+        if (asked - used > 1) wait_vm<M::LOADS>();
         else wait_vm<0>();
-        const char *st = ring + (i & 1) * M::STAGE, *sv = st + TK * M::ROWB;
-        const int k0 = key0(i);
+        const char *st = ring + (used++ & 1) * M::STAGE, *sv = st + TK * M::ROWB;
         f32x4 s[NR][2];
 #pragma unroll
         for (int c = 0; c < NR; ++c) s[c][0] = s[c][1] = f32x4{0, 0, 0, 0};
@@ -265,7 +298,9 @@ void k_attn_few(AttnArgs a) {
             s[0][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[0][q]), s[0][b]);
             if (nr > 1) s[NR - 1][b] = mfma16(kv, __builtin_bit_cast(bf16x8, qv[NR - 1][q]), s[NR - 1][b]);
           }
-        bf16x8 p[NR];
+        // p as a bf16 and the bf16 of what that leaves: the second product is not what
+        // bounds the kernel, and the output's error stays its own rounding's
+        bf16x8 p[NR], pl[NR];
 #pragma unroll
         for (int c = 0; c < NR; ++c) {
           if (c < nr) {
@@ -274,7 +309,10 @@ void k_attn_few(AttnArgs a) {
             for (int e = 0; e < 8; ++e) x[e] = s[c][e / 4][e % 4];
             soften(c, k0, x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[c][e] = (__bf16)x[e];
+            for (int e = 0; e < 8; ++e) {
+              p[c][e] = (__bf16)x[e];
+              pl[c][e] = (__bf16)(x[e] - (float)p[c][e]);
+            }
           }
         }
 #pragma unroll
@@ -284,17 +322,18 @@ void k_attn_few(AttnArgs a) {
           const bf16x4 v0 = read_tr(at), v1 = read_tr(at + 16 * M::ROWB);
           const bf16x8 vv = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
           acc[0][t] = mfma16(vv, p[0], acc[0][t]);
-          if (nr > 1) acc[NR - 1][t] = mfma16(vv, p[NR - 1], acc[NR - 1][t]);
+          acc[0][t] = mfma16(vv, pl[0], acc[0][t]);
+          if (nr > 1) {
+            acc[NR - 1][t] = mfma16(vv, p[NR - 1], acc[NR - 1][t]);
+            acc[NR - 1][t] = mfma16(vv, pl[NR - 1], acc[NR - 1][t]);
+          }
         }
         // this stage's reads are done before its next rows are requested
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (i + 2 < i1) issue(i + 2);
-      }
-    } else {
-      mask_queries();
-      for (int i = i0; i < i1; ++i) {
-        const int k0 = key0(i);
-        const long long page = attn_page(a, work.s, k0), slot = k0 & ((1 << a.c.shift) - 1);
+        if (z.ask < z.i1) issue(z, asked++ & 1);
+        else if (more && ahead.ask < ahead.i1) issue(ahead, asked++ & 1);
+      } else {
+        const long long page = attn_page(a, sg.s, k0), slot = k0 & ((1 << a.c.shift) - 1);
         const float *kb = (const float *)a.c.k + page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head;
         const float *vb = (const float *)a.c.v + page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head;
         const float *zf = reinterpret_cast<const float *>(zero);
@@ -334,60 +373,67 @@ void k_attn_few(AttnArgs a) {
       }
     }
 
-    // the wavefronts' states, joined in their order
-    float *join = reinterpret_cast<float *>(lds), *ml = join + M::WAVES * R * DP;
-    __syncthreads();
+    // the wavefronts' states, added to the first one's in their order, 16 rows at a time
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
       if (c >= nr) continue;
-      float t = l[c];
-      t = t + xor_lane<16>(t);
-      t = t + xor_lane<32>(t);
-      const int row = wave * R + 16 * c + n;
+      l[c] = l[c] + xor_lane<16>(l[c]);
+      l[c] = l[c] + xor_lane<32>(l[c]);
+      lds_barrier();   // the area is free
+      if (wave > 0) {
+        char *to = area + (wave - 1) * M::STATE;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)   // pieces of 16 bytes permuted: a row is 2 to 8 times all banks
-        *reinterpret_cast<f32x4 *>(join + row * DP + 4 * ((4 * d + g) ^ n)) = acc[c][d];
-      if (g == 0) {
-        ml[2 * row] = m[c];
-        ml[2 * row + 1] = t;
+        for (int t = 0; t < DT; ++t) reinterpret_cast<f32x4 *>(to)[t * WAVE + lane] = acc[c][t];
+        reinterpret_cast<float *>(to + DP * 64)[lane] = lane < 32 ? m[c] : l[c];   // (the same 16 twice)
       }
-    }
-    __syncthreads();
-    for (int u = threadIdx.x; u < sg.n * (DP / 4); u += M::THREADS) {
-      const int r = u / (DP / 4), piece = u % (DP / 4);
-      float top = -INFINITY, sum = 0.0f;
+      lds_barrier();
+      if (wave > 0) continue;
+      float top = m[c];
 #pragma unroll
-      for (int v = 0; v < M::WAVES; ++v) top = fmaxf(top, ml[2 * (v * R + r)]);
-      const float mm = top == -INFINITY ? 0.0f : top;
-      f32x4 o = {0, 0, 0, 0};
+      for (int v = 1; v < M::WAVES; ++v)
+        top = fmaxf(top, reinterpret_cast<const float *>(area + (v - 1) * M::STATE + DP * 64)[n]);
+      const float mm = top == -INFINITY ? 0.0f : top, f0 = __builtin_amdgcn_exp2f(m[c] - mm);
+      float sum = l[c] * f0;
 #pragma unroll
-      for (int v = 0; v < M::WAVES; ++v) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * (v * R + r)] - mm);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(join + (v * R + r) * DP + 4 * (piece ^ (r & 15)));
-        sum = __builtin_fmaf(f, ml[2 * (v * R + r) + 1], sum);
+      for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
+        for (int e = 0; e < 4; ++e) acc[c][t][e] *= f0;
+#pragma unroll
+      for (int v = 1; v < M::WAVES; ++v) {
+        const char *of = area + (v - 1) * M::STATE;
+        const float f = __builtin_amdgcn_exp2f(reinterpret_cast<const float *>(of + DP * 64)[n] - mm);
+        sum = __builtin_fmaf(f, reinterpret_cast<const float *>(of + DP * 64)[32 + n], sum);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          const f32x4 x = reinterpret_cast<const f32x4 *>(of)[t * WAVE + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[c][t][e] = __builtin_fmaf(f, x[e], acc[c][t][e]);
+        }
       }
+      const int r = 16 * c + n;
+      if (r >= sg.n) continue;
       if (sg.slot >= 0) {
         float *part = a.part + sg.slot * attn_part_floats<R, DP>();
-        *reinterpret_cast<f32x4 *>(part + r * DP + 4 * piece) = o;
-        if (piece == 0) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(part + r * DP + 16 * t + 4 * g) = acc[c][t];
+        if (g == 0) {
           part[R * DP + r] = top;
           part[R * DP + R + r] = sum;
         }
       } else {
         const int pr = sg.r0 + r, tok = over(pr, a.by_G), head = sg.hk * a.G + pr - tok * a.G;
-        const long long row = work.q.first + tok;
+        const long long row = sg.q.first + tok;
         const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+        T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= inv;
-        if (4 * piece < a.D) put4((T *)a.o.p + row * a.o.row + head * a.o.head + 4 * piece, o);
-        if (a.lse && piece == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+        for (int t = 0; t < DT; ++t)
+          if (16 * t + 4 * g < a.D) put4(out + 16 * t + 4 * g, acc[c][t] * inv);
+        if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
       }
     }
-    __syncthreads();
+    z = ahead;
   }
-  if (!a.whole && threadIdx.x == 0) a.rec[w] = begun;
+  if (!a.whole && threadIdx.x == 0) a.rec[blockIdx.x] = begun;
 }
 
 // ------------------------------------------------------------- chunks --
@@ -438,13 +484,13 @@ void k_attn_many(AttnArgs a) {
     const int lo = sg.keys.lo, hi = sg.keys.hi;
     const int r = 32 * wave + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
     const bool mine = 32 * wave < sg.n;
-    const int pos = r < sg.n ? work.q.pos0 + tok : -1;
+    const int pos = r < sg.n ? sg.q.pos0 + tok : -1;
     // positions of the wavefront's first and last row
     const int wlast = min(32 * wave + 31, sg.n - 1);
-    const int pmin = work.q.pos0 + over(sg.r0 + 32 * wave, a.by_G), pmax = work.q.pos0 + over(sg.r0 + max(wlast, 0), a.by_G);
+    const int pmin = sg.q.pos0 + over(sg.r0 + 32 * wave, a.by_G), pmax = sg.q.pos0 + over(sg.r0 + max(wlast, 0), a.by_G);
     u32x4 qv[QS];
     {
-      const uint16_t *p = (const uint16_t *)a.q.p + (long long)(work.q.first + tok) * a.q.row +
+      const uint16_t *p = (const uint16_t *)a.q.p + (long long)(sg.q.first + tok) * a.q.row +
                           (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
@@ -465,7 +511,7 @@ void k_attn_many(AttnArgs a) {
     auto fetch_pages = [&](int i) {
       from = i;
       const int key = (i + lane / M::PI) * BK + (wave + M::WAVES * (lane % M::PI)) * WAVE / CH;
-      pages = attn_page(a, work.s, min(key, hi - 1));
+      pages = attn_page(a, sg.s, min(key, hi - 1));
     };
     auto issue = [&](int i, int at) {
       if (i - from >= WAVE / M::PI) fetch_pages(i);
@@ -588,7 +634,7 @@ void k_attn_many(AttnArgs a) {
         }
       } else {
         const int head = sg.hk * a.G + pr - tok * a.G;
-        const long long row = work.q.first + tok;
+        const long long row = sg.q.first + tok;
         const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
         uint16_t *out = (uint16_t *)a.o.p + row * a.o.row + head * a.o.head;
 #pragma unroll

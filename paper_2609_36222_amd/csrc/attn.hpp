@@ -171,7 +171,8 @@ struct AttnWork {
   // sequence q and key head hk; `slot` is the part's place, -1 where the segment is all
   // of the unit
   struct Segment {
-    int hk, r0, n, k0, k1, slot;
+    int s, hk, r0, n, k0, k1, slot;
+    AttnSeq q;
     KeyRange keys;
   };
   __device__ bool next(Segment &g, AttnPart &begun) {
@@ -185,6 +186,8 @@ struct AttnWork {
       }
       enter(s0 + __ffsll(more) - 1);
     }
+    g.s = s;
+    g.q = q;
     g.hk = quotient(rem, head_cost);
     int left = rem - g.hk * head_cost, j = 0, c;
     while (left >= (c = tile_cost(q, j))) {
