@@ -670,23 +670,24 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, fast=32.0, slo
     return (inv * (1 - far) + inv / factor * far).float(), 0.1 * math.log(factor) + 1.0
 
 
-def _heads(t, what, dtype, dev, shape):
-    """(pointer, row stride, head stride) of a tensor [rows, H, D] with adjacent elements in
-    a head."""
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
-        raise ValueError(f"{what}: {dtype} {list(shape)} on the current GPU")
-    row, head, one = t.stride()
-    if one != 1 and shape[2] > 1:
-        raise ValueError(f"{what}: adjacent elements in a head")
+def _heads(t, what, dtype, dev, n, H, D):
+    """(pointer, row stride, head stride) of a tensor [n, H, D] with adjacent elements in a
+    head."""
+    try:
+        rows, heads, size = t.shape
+        row, head, one = t.stride()
+    except ValueError:
+        rows = -1
+    if rows != n or heads != H or size != D or one != 1 or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what}: {dtype} {[n, H, D]}, adjacent elements in a head, on the current GPU")
     # (a single row or head has no stride to speak of)
-    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+    return t.data_ptr(), row if n > 1 else 0, head if H > 1 else 0
 
 
-def _head_shape(t, what, D):
-    shape = t.shape
-    if len(shape) != 3 or shape[2] != D:
-        raise ValueError(f"{what}: [rows, heads, {D}]")
-    return shape
+def _stream_on(stream, dev):
+    """_stream, where the current device is known."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _ints(t, what, dev, shape=None):
@@ -768,23 +769,27 @@ _NO_HEADS = (0, None, 0, 0, None, 0, 0)
 def base_head_rope(rope: Rope, positions, q, k, q_out, k_out, stream=None):
     """q_out and k_out [rows, heads, D] from q and k (either pair None) at int32 positions
     [rows] (None where nothing rotates)."""
-    dev, dt, args, n = _device(), rope.torch_dtype, (), None
-    for t, out, what in ((q, q_out, "q"), (k, k_out, "k")):
-        if t is None or out is None:
-            if t is not None or out is not None:
-                raise ValueError(f"{what} and {what}_out: both or neither")
-            args += _NO_HEADS
-            continue
-        shape = _head_shape(t, what, rope.D)
-        if n is not None and shape[0] != n:
-            raise ValueError(f"{what}: q's rows")
-        n = shape[0]
-        args += (shape[1], *_heads(t, what, dt, dev, shape), *_heads(out, what + "_out", dt, dev, shape))
-    if n is None:
-        raise ValueError("q or k")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
+        raise ValueError("q and q_out, k and k_out: both or neither, and one of the two")
+    dev, dt, D = _device(), rope.torch_dtype, rope.D
+    qa = ka = _NO_HEADS
+    n = None
+    if q is not None:
+        n, H = q.size(0), q.size(1)
+        qa = (H, *_heads(q, "q", dt, dev, n, H, D), *_heads(q_out, "q_out", dt, dev, n, H, D))
+    if k is not None:
+        n, H = k.size(0) if n is None else n, k.size(1)
+        ka = (H, *_heads(k, "k", dt, dev, n, H, D), *_heads(k_out, "k_out", dt, dev, n, H, D))
     if positions is not None:
-        positions = _flat(positions, "positions", dev, (n,)).data_ptr()
-    _check(load().base_head_rope(rope.desc, n, positions, *args, _stream(stream)))
+        positions = _positions(positions, n, dev)
+    _check(load().base_head_rope(rope.desc, n, positions, *qa, *ka, _stream_on(stream, dev)))
+
+
+def _positions(t, n, dev):
+    import torch
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"positions: int32, {n} adjacent elements, on the current GPU")
+    return t.data_ptr()
 
 
 def head_rope(rope: Rope, positions, q, k=None, stream=None):
@@ -799,15 +804,14 @@ def base_kv_append(rope: Rope, cache: KVCache, batch: KVBatch, q, k, v, q_out, p
     [rows, Hq, D] the same to q_out.  positions: int32 [rows], or None: the tokens' numbers
     in their sequences."""
     dev, dt = _device(), rope.torch_dtype
-    shape = _head_shape(q, "q", rope.D)
-    n = shape[0]
+    D, Hk = rope.D, cache.Hk
+    n, Hq = q.size(0), q.size(1)
     if positions is not None:
-        positions = _flat(positions, "positions", dev, (n,)).data_ptr()
-    new = (n, cache.Hk, rope.D)
+        positions = _positions(positions, n, dev)
     _check(load().base_kv_append(
-        rope.desc, cache.desc, batch.desc, n, positions, shape[1], *_heads(q, "q", dt, dev, shape),
-        *_heads(q_out, "q_out", dt, dev, shape), *_heads(k, "k", dt, dev, new), *_heads(v, "v", dt, dev, new),
-        _stream(stream)))
+        rope.desc, cache.desc, batch.desc, n, positions, Hq, *_heads(q, "q", dt, dev, n, Hq, D),
+        *_heads(q_out, "q_out", dt, dev, n, Hq, D), *_heads(k, "k", dt, dev, n, Hk, D),
+        *_heads(v, "v", dt, dev, n, Hk, D), _stream_on(stream, dev)))
 
 
 def attention_workspace_bytes(cache: KVCache, batch: KVBatch, rows, Hq) -> int:
@@ -822,8 +826,8 @@ def base_paged_attention(cache: KVCache, batch: KVBatch, q, out, ws, scale=None,
     """out [rows, Hq, D] (and lse [rows, Hq] fp32) of q over the cache; scale None: 1 /
     sqrt(D); ws: a uint8 tensor of attention_workspace_bytes."""
     dev, dt = _device(), cache.torch_dtype
-    shape = _head_shape(q, "q", cache.D)
-    n, Hq, _ = shape
+    D = cache.D
+    n, Hq = q.size(0), q.size(1)
     if lse is not None:
         import torch
         if (lse.dtype is not torch.float32 or lse.shape != (n, Hq) or not lse.is_contiguous()
@@ -833,8 +837,8 @@ def base_paged_attention(cache: KVCache, batch: KVBatch, q, out, ws, scale=None,
     if ws.get_device() != dev or not ws.is_contiguous():
         raise ValueError("ws: contiguous, on the current GPU")
     _check(load().base_paged_attention(
-        cache.desc, batch.desc, n, Hq, *_heads(q, "q", dt, dev, shape), *_heads(out, "out", dt, dev, shape),
-        lse, cache.D ** -0.5 if scale is None else scale, window, ws.data_ptr(), ws.nbytes, _stream(stream)))
+        cache.desc, batch.desc, n, Hq, *_heads(q, "q", dt, dev, n, Hq, D), *_heads(out, "out", dt, dev, n, Hq, D),
+        lse, D ** -0.5 if scale is None else scale, window, ws.data_ptr(), ws.nbytes, _stream_on(stream, dev)))
 
 
 def paged_attention(q, cache: KVCache, batch: KVBatch, scale=None, window=0, return_lse=False, stream=None):

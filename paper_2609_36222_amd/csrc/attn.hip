@@ -45,9 +45,22 @@ __device__ __forceinline__ void glb_to_lds(const char *base, uint32_t off, uint3
                "s"(__builtin_amdgcn_readfirstlane(lds))
                : "memory");
 }
-__device__ __forceinline__ const char *uni_at(const char *p) {
-  const uintptr_t v = (uintptr_t)p;
-  return (const char *)(((uintptr_t)(uint32_t)uni((int)(v >> 32)) << 32) | (uint32_t)uni((int)v));
+// The addresses of K's and V's rows from a token on (16-bit), one token a lane: made for many
+// steps at once, and read lane by lane (in scalar registers their 64-bit products took 1100
+// of a block's 6000 cycles in k_attn_many).  A page that is not in the cache is read as its
+// first: in bounds.
+struct RowAt {
+  uint32_t klo, khi, vlo, vhi;
+};
+__device__ __forceinline__ RowAt row_at(const AttnArgs &a, int s, int hk, int key) {
+  const long long page = attn_page(a, s, key), slot = key & ((1 << a.c.shift) - 1);
+  const uint64_t k = (uint64_t)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + hk * a.c.k_head);
+  const uint64_t v = (uint64_t)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + hk * a.c.v_head);
+  return {(uint32_t)k, (uint32_t)(k >> 32), (uint32_t)v, (uint32_t)(v >> 32)};
+}
+__device__ __forceinline__ const char *lane_at(uint32_t lo, uint32_t hi, int l) {
+  return (const char *)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, l) << 32) |
+                        (uint32_t)__builtin_amdgcn_readlane((int)lo, l));
 }
 // Four 16-bit elements a lane, transposed in groups of 16 lanes: lane 4 r + c gives the
 // address of elements 4 c .. + 3 of row r, and lane i gets element i of the rows 0 .. 3
@@ -58,6 +71,14 @@ __device__ __forceinline__ bf16x4 read_tr(const char *p) {
 struct __attribute__((packed, aligned(2))) Any16H { u32x4 v; };
 struct __attribute__((packed, aligned(4))) Any16F { f32x4 v; };
 struct __attribute__((packed, aligned(2))) Any8H { u32x2 v; };
+
+// The same value, of which the compiler knows nothing: what follows from it is not computed
+// in front of the loop (the masks and addresses of a unit's queries would hold 60 registers
+// through the loop over the keys)
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
 
 __device__ __forceinline__ void put4(uint16_t *p, f32x4 v) {
   u32x2 q;
@@ -117,17 +138,18 @@ void k_attn_few(AttnArgs a) {
   const uint32_t ring_at = lds_addr(ring);
 
   // A segment as the wavefront has it: its steps i0 .. i1 - 1 (keys key0(i) .. + TK - 1),
-  // the next one to request, and the pages of 32 steps, two a step (16 keys lie in one
+  // the next one to request, and the addresses of 32 steps, two a step (16 keys lie in one
   // page): lane e has those of step from + e / 2
   struct Seg {
     typename Work::Segment g;
-    int i0, i1, ask, from, pages;
+    int i0, i1, ask, from;
+    RowAt at;
   };
   auto key0 = [&](int i) { return i * M::BK + wave * TK; };
-  auto fetch_pages = [&](Seg &z, int i) {
+  auto fetch_rows = [&](Seg &z, int i) {
     z.from = i;
     const int key = key0(i + lane / 2) + 16 * (lane & 1);
-    z.pages = attn_page(a, z.g.s, max(min(key, z.g.keys.hi - 1), 0));
+    z.at = row_at(a, z.g.s, z.g.hk, max(min(key, (z.g.keys.hi - 1) & ~15), 0));
   };
   auto steps = [&](Seg &z) {
     z.i0 = z.g.k0;
@@ -137,6 +159,7 @@ void k_attn_few(AttnArgs a) {
     z.ask = z.i0;
   };
   auto queries = [&](const typename Work::Segment &sg, u32x4 (&qv)[NR][QS]) {
+    const int D = here(a.D);
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
       const int r = 16 * c + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
@@ -145,7 +168,7 @@ void k_attn_few(AttnArgs a) {
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
         const int d = BF ? 32 * s + 8 * g : 16 * s + 4 * g;
-        const T *at = p + min(d, a.D - (BF ? 8 : 4));
+        const T *at = p + min(d, D - (BF ? 8 : 4));
         if constexpr (BF) qv[c][s] = reinterpret_cast<const Any16H *>(at)->v;
         else qv[c][s] = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
       }
@@ -154,15 +177,13 @@ void k_attn_few(AttnArgs a) {
   // the segment's next step into the stage given
   auto issue = [&](Seg &z, int stage) {
     const int i = z.ask++, k0 = key0(i), lo = z.g.keys.lo, hi = z.g.keys.hi;
-    if (i - z.from >= 32) fetch_pages(z, i);
+    if (i - z.from >= 32) fetch_rows(z, i);
     const uint32_t st = ring_at + stage * M::STAGE;
     const char *kb[2], *vb[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const long long page = __builtin_amdgcn_readlane(z.pages, 2 * (i - z.from) + h);
-      const long long slot = (k0 + 16 * h) & ((1 << a.c.shift) - 1);
-      kb[h] = uni_at((const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + z.g.hk * a.c.k_head));
-      vb[h] = uni_at((const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + z.g.hk * a.c.v_head));
+      kb[h] = lane_at(z.at.klo, z.at.khi, 2 * (i - z.from) + h);
+      vb[h] = lane_at(z.at.vlo, z.at.vhi, 2 * (i - z.from) + h);
     }
     if (k0 >= lo && k0 + TK <= hi && a.D == DP) {
 #pragma unroll
@@ -196,16 +217,16 @@ void k_attn_few(AttnArgs a) {
   if (more) {
     steps(z);
     queries(z.g, qn);
-    if (BF) fetch_pages(z, z.i0);
+    if (BF) fetch_rows(z, z.i0);
   }
   while (more) {
     const typename Work::Segment &sg = z.g;
-    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1;
+    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1, D = here(a.D);
 #pragma unroll
     for (int c = 0; c < NR; ++c)
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
-        const uint32_t keep = (BF ? 32 * s + 8 * g : 16 * s + 4 * g) < a.D ? ~0u : 0u;
+        const uint32_t keep = (BF ? 32 * s + 8 * g : 16 * s + 4 * g) < D ? ~0u : 0u;
         qv[c][s] = qn[c][s] & keep;
       }
     if constexpr (BF)
@@ -217,14 +238,14 @@ void k_attn_few(AttnArgs a) {
       steps(ahead);
       queries(ahead.g, qn);
       if constexpr (BF) {
-        fetch_pages(ahead, ahead.i0);
+        fetch_rows(ahead, ahead.i0);
         // waited for here, where what is in flight besides has been for long: the compiler's
         // wait at their first use would be for the steps requested since, too
 #pragma unroll
         for (int c = 0; c < NR; ++c)
 #pragma unroll
           for (int s = 0; s < QS; ++s) asm volatile("" ::"v"(qn[c][s]));
-        asm volatile("" ::"v"(ahead.pages));
+        asm volatile("" ::"v"(ahead.at.klo));
       }
     }
     int pos[NR];
@@ -342,7 +363,7 @@ void k_attn_few(AttnArgs a) {
 #pragma unroll
         for (int q = 0; q < QS; ++q) {
           const int d = 16 * q + 4 * g;
-          kv[q] = *reinterpret_cast<const f32x4 *>(kin && d < a.D ? kb + n * a.c.k_slot + d : zf);
+          kv[q] = *reinterpret_cast<const f32x4 *>(kin && d < D ? kb + n * a.c.k_slot + d : zf);
         }
         float vv[4][DT];
 #pragma unroll
@@ -351,7 +372,7 @@ void k_attn_few(AttnArgs a) {
           const bool vin = key >= lo && key < hi;
 #pragma unroll
           for (int t = 0; t < DT; ++t)
-            vv[e][t] = *(vin && 16 * t + n < a.D ? vb + (4 * g + e) * a.c.v_slot + 16 * t + n : zf);
+            vv[e][t] = *(vin && 16 * t + n < D ? vb + (4 * g + e) * a.c.v_slot + 16 * t + n : zf);
         }
 #pragma unroll
         for (int c = 0; c < NR; ++c) {
@@ -427,7 +448,7 @@ void k_attn_few(AttnArgs a) {
         T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
-          if (16 * t + 4 * g < a.D) put4(out + 16 * t + 4 * g, acc[c][t] * inv);
+          if (16 * t + 4 * g < D) put4(out + 16 * t + 4 * g, acc[c][t] * inv);
         if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
       }
     }
@@ -438,12 +459,15 @@ void k_attn_few(AttnArgs a) {
 
 // ------------------------------------------------------------- chunks --
 // k_attn_many: tiles of 32 packed rows a wavefront on 32x32x16 products, the workgroup's
-// wavefronts on the same block of BK keys, whose rows they bring to a ring of three in LDS
-// together; one barrier a block.
+// wavefronts on the same block of BK keys, whose rows they bring to a ring in LDS together.
+// The products and the softmax between them take a SIMD about as long as each other, so
+// its two wavefronts take turns: in phase 2 t the first half of the workgroup makes the
+// products of block t (S = K Q^T) and of block t - 1 (O += V^T P^T), and the second half
+// the softmax of block t - 1; in phase 2 t + 1 the other way round.
 template <int DP_>
 struct ManyShape {
   static constexpr int DP = DP_, WAVES = DP == 256 ? 4 : 8, THREADS = WAVES * WAVE, R = 32 * WAVES;
-  static constexpr int BK = DP == 256 ? 32 : 64, CH = DP / 8, ROWB = DP * 2, RING = 3;
+  static constexpr int BK = DP == 256 ? 32 : 64, CH = DP / 8, ROWB = DP * 2, RING = 4;
   static constexpr int HALF = BK * ROWB, STAGE = 2 * HALF, LDS = RING * STAGE;
   static constexpr int PI = HALF / 1024 / WAVES;   // loads of K, and of V, a wavefront and block
   static constexpr int WPE = DP == 256 ? 1 : 2;
@@ -457,6 +481,22 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// N products, each operand read from LDS AHEAD products before it (left to itself the
+// compiler reads each in front of its product and waits for it: twice the time)
+template <int N, int AHEAD, typename Read, typename Mul>
+__device__ __forceinline__ void fed(Read read, Mul mul) {
+  bf16x8 v[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) v[i] = read(i);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    mul(i, v[i % AHEAD]);
+    if (i + AHEAD < N) v[i % AHEAD] = read(i + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 template <int DP>
 __global__ __launch_bounds__((ManyShape<DP>::THREADS), (ManyShape<DP>::WPE))
 void k_attn_many(AttnArgs a) {
@@ -467,6 +507,8 @@ void k_attn_many(AttnArgs a) {
   const int wave = wave_id_u(), lane = lane_id(), n = lane % 32, h = lane / 32;
   const int w = a.W % N_XCD ? blockIdx.x : blockIdx.x % N_XCD * (a.W / N_XCD) + blockIdx.x / N_XCD;
   const char *zero = reinterpret_cast<const char *>(g_zero);
+  // (one wavefront a SIMD has nobody to take turns with)
+  const int half = M::WPE > 1 ? wave / (M::WAVES / 2) : 0;
   auto row0 = [&](int j) { return (wave + M::WAVES * j) * WAVE / CH; };   // of load j
   uint32_t ko[M::PI], vo[M::PI];                                          // the lane's places in it
 #pragma unroll
@@ -481,6 +523,7 @@ void k_attn_many(AttnArgs a) {
   AttnWork<R, BK> work(a, w);
   typename AttnWork<R, BK>::Segment sg;
   while (work.next(sg, begun)) {
+    const int D = here(a.D);
     const int lo = sg.keys.lo, hi = sg.keys.hi;
     const int r = 32 * wave + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
     const bool mine = 32 * wave < sg.n;
@@ -495,7 +538,7 @@ void k_attn_many(AttnArgs a) {
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
         const int d = 16 * s + 8 * h;
-        qv[s] = reinterpret_cast<const Any16H *>(p + min(d, a.D - 8))->v;
+        qv[s] = reinterpret_cast<const Any16H *>(p + min(d, D - 8))->v;
       }
     }
     f32x16 acc[DT];
@@ -505,119 +548,150 @@ void k_attn_many(AttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[t][e] = 0.0f;
 
-    // the pages of 64 / PI blocks at a time: lane e has that of load e % PI of block
+    // the addresses of 64 / PI blocks at a time: lane e has that of load e % PI of block
     // from + e / PI
-    int from = sg.k0, pages = 0;
-    auto fetch_pages = [&](int i) {
+    int from = sg.k0;
+    RowAt rows{};
+    auto fetch_rows = [&](int i) {
       from = i;
       const int key = (i + lane / M::PI) * BK + (wave + M::WAVES * (lane % M::PI)) * WAVE / CH;
-      pages = attn_page(a, sg.s, min(key, hi - 1));
+      const int most = (hi - 1) / (WAVE / CH) * (WAVE / CH);
+      rows = row_at(a, sg.s, sg.hk, min(key, most));
     };
-    auto issue = [&](int i, int at) {
-      if (i - from >= WAVE / M::PI) fetch_pages(i);
-      const int k0 = i * BK;
-      const uint32_t st = ring_at + at * M::STAGE;
-      const bool all = k0 >= lo && k0 + BK <= hi && a.D == DP;
+    // blocks whose keys are all there
+    const int full0 = a.D == DP ? (lo + BK - 1) / BK : 0x7FFFFFFF, full1 = hi / BK;
+    auto issue = [&](int i) {
+      if (i - from >= WAVE / M::PI) fetch_rows(i);
+      const uint32_t st = ring_at + (i & (M::RING - 1)) * M::STAGE;
+      const bool all = i >= full0 && i < full1;
 #pragma unroll
       for (int j = 0; j < M::PI; ++j) {
-        const long long page = __builtin_amdgcn_readlane(pages, M::PI * (i - from) + j);
-        const long long slot = (k0 + row0(j)) & ((1 << a.c.shift) - 1);
-        const char *kb = uni_at((const char *)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head));
-        const char *vb = uni_at((const char *)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + sg.hk * a.c.v_head));
+        const char *kb = lane_at(rows.klo, rows.khi, M::PI * (i - from) + j);
+        const char *vb = lane_at(rows.vlo, rows.vhi, M::PI * (i - from) + j);
         const uint32_t to = st + row0(j) * M::ROWB;
         if (all) {
           glb_to_lds(kb, ko[j], to);
           glb_to_lds(vb, vo[j], to + M::HALF);
         } else {
           const int row = row0(j) + lane / CH, ck = lane % CH ^ many_k<CH>(row), cv = lane % CH ^ many_v<CH>(row);
-          const bool in = k0 + row >= lo && k0 + row < hi;
+          const bool in = i * BK + row >= lo && i * BK + row < hi;
           glb_to_lds(in && 8 * ck < a.D ? kb + ko[j] : zero, to);
           glb_to_lds(in && 8 * cv < a.D ? vb + vo[j] : zero, to + M::HALF);
         }
       }
     };
-    const int k1 = hi > 0 ? sg.k1 : sg.k0;
-    if (sg.k0 < k1) fetch_pages(sg.k0);
+    const int blocks = hi > 0 ? sg.k1 - sg.k0 : 0;
+    if (blocks > 0) fetch_rows(sg.k0);
     // a negative scale is taken over by the queries' signs, 0 by queries of 0: the scaled
     // maximum is then the maximum scaled
 #pragma unroll
     for (int s = 0; s < QS; ++s) {
-      const uint32_t keep = a.scale != 0.0f && 16 * s + 8 * h < a.D ? ~0u : 0u;
+      const uint32_t keep = a.scale != 0.0f && 16 * s + 8 * h < D ? ~0u : 0u;
       qv[s] = (qv[s] ^ flip) & keep;
     }
-    if (sg.k0 < k1) issue(sg.k0, 0);
-    if (sg.k0 + 1 < k1) issue(sg.k0 + 1, 1);
-    int at = 0;
-    for (int i = sg.k0; i < k1; ++i) {
-      if (i + 1 < k1) wait_vm<2 * M::PI>();
+    if (blocks > 0) issue(sg.k0);
+    if (blocks > 1) issue(sg.k0 + 1);
+    if (blocks > 1) wait_vm<2 * M::PI>();
+    else wait_vm<0>();
+    lds_barrier();
+    // blocks that some row of the wavefront sees
+    auto seen_block = [&](int t) {
+      const int k0 = (sg.k0 + t) * BK;
+      return t >= 0 && t < blocks && mine && k0 <= pmax && !(a.window > 0 && k0 + BK - 1 <= pmin - a.window);
+    };
+    // the stage of block t + 1 is there (all wavefronts': each waits for its own loads)
+    auto wait_next = [&](int t) {
+      if (t + 2 < blocks) wait_vm<2 * M::PI>();
       else wait_vm<0>();
+    };
+    f32x16 s[KB];
+    bf16x8 p[2 * KB];
+    // the second half runs one phase behind; both request block t + 2 in phase 2 t, when
+    // the stage's last readers have passed
+    if (half) {
+      if (blocks > 2) issue(sg.k0 + 2);
       lds_barrier();
-      if (i + 2 < k1) issue(i + 2, at == 0 ? 2 : at - 1);
-      const int k0 = i * BK;
-      const char *sk = lds + at * M::STAGE, *sv = sk + M::HALF;
-      at = at == 2 ? 0 : at + 1;
-      if (!mine || k0 > pmax || (a.window > 0 && k0 + BK - 1 <= pmin - a.window)) continue;
-      f32x16 s[KB];
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
-        const int row = 32 * b + n;
-#pragma unroll
-        for (int q = 0; q < QS; ++q) {
-          const bf16x8 kv = *reinterpret_cast<const bf16x8 *>(
-              sk + row * M::ROWB + (((2 * q + h) ^ many_k<CH>(row)) * 16));
-          s[b] = mfma32(kv, __builtin_bit_cast(bf16x8, qv[q]), s[b]);
-        }
+    }
+    for (int t = 0; t <= blocks; ++t) {
+      const int late = here(half);   // (one loop for both halves, not one each)
+      if (!late && t + 2 < blocks) issue(sg.k0 + t + 2);
+      __builtin_amdgcn_s_setprio(1);
+      if (seen_block(t - 1)) {
+        const char *sv = lds + ((sg.k0 + t - 1) & (M::RING - 1)) * M::STAGE + M::HALF;
+        const int row = 4 * h + (lane % 16) / 4;   // of 16 (many_v(row) is that of row + 8)
+        fed<2 * KB * DT, 4>(
+            [&](int i) {
+              const int ks = i / DT, piece = 4 * (i % DT) + (lane / 16 & 1) * 2 + (lane & 3) / 2;
+              const char *at = sv + (16 * ks + row) * M::ROWB + ((piece ^ many_v<CH>(row)) * 16) + (lane & 1) * 8;
+              const bf16x4 v0 = read_tr(at), v1 = read_tr(at + 8 * M::ROWB);
+              return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            },
+            [&](int i, bf16x8 v) { acc[i % DT] = mfma32(v, p[i / DT], acc[i % DT]); });
       }
-      if (k0 + BK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window)) {
+      if (seen_block(t)) {
+        const char *sk = lds + ((sg.k0 + t) & (M::RING - 1)) * M::STAGE;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+        fed<QS * KB, 4>(
+            [&](int i) {
+              const int row = 32 * (i % KB) + n;
+              return *reinterpret_cast<const bf16x8 *>(sk + row * M::ROWB +
+                                                       (((2 * (i / KB) + h) ^ many_k<CH>(row)) * 16));
+            },
+            [&](int i, bf16x8 v) {
+              s[i % KB] = mfma32(v, __builtin_bit_cast(bf16x8, qv[i / KB]), s[i % KB]);
+            });
+      }
+      __builtin_amdgcn_s_setprio(0);
+      if (late) wait_next(t);
+      lds_barrier();
+      if (late && t + 3 < blocks) issue(sg.k0 + t + 3);
+      if (seen_block(t)) {
+        const int k0 = (sg.k0 + t) * BK;
+        if (k0 + BK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window)) {
+          // (key <= pos and > pos - window, the block's and the lane's part on one side)
+          const int last = pos - k0 - 4 * h, first = a.window > 0 ? last - a.window : -0x40000000;
+#pragma unroll
+          for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int key = 32 * b + 8 * (e / 4) + e % 4;
+              s[b][e] = key <= last && key > first ? s[b][e] : -INFINITY;
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+        top = fmaxf(top, xor_lane<32>(top)) * scale;
+        if (__any(top > m + LAG)) {
+          const float to = fmaxf(m, top), f = m == to ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+          m = to;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[d][e] *= f;
+        }
+        const float mm = m == -INFINITY ? 0.0f : m;
+        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int key = k0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4;
-            const bool seen = key <= pos && (a.window == 0 || key > pos - a.window);
-            s[b][e] = seen ? s[b][e] : -INFINITY;
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale, -mm));
+            sums[e % 4] += x;
+            p[2 * b + e / 8][e % 8] = (__bf16)x;
           }
+        l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
       }
-      float top = s[0][0];
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
-      top = fmaxf(top, xor_lane<32>(top)) * scale;
-      if (__any(top > m + LAG)) {
-        const float to = fmaxf(m, top), f = m == to ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-        m = to;
-        l *= f;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[t][e] *= f;
-      }
-      const float mm = m == -INFINITY ? 0.0f : m;
-      bf16x8 p[2 * KB];
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale, -mm));
-          l += x;
-          p[2 * b + e / 8][e % 8] = (__bf16)x;
-        }
-#pragma unroll
-      for (int ks = 0; ks < 2 * KB; ++ks)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) {
-          const int row = 16 * ks + 4 * h + (lane % 16) / 4;
-          const int piece = 4 * t + (lane / 16 & 1) * 2 + (lane & 3) / 2;
-          const char *p0 = sv + row * M::ROWB + ((piece ^ many_v<CH>(row)) * 16) + (lane & 1) * 8;
-          const char *p1 = sv + (row + 8) * M::ROWB + ((piece ^ many_v<CH>(row + 8)) * 16) + (lane & 1) * 8;
-          const bf16x4 v0 = read_tr(p0), v1 = read_tr(p1);
-          const bf16x8 vv = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-          acc[t] = mfma32(vv, p[ks], acc[t]);
-        }
+      if (!late) wait_next(t);
+      lds_barrier();
     }
+    if (!half) lds_barrier();
     l = l + xor_lane<32>(l);
     if (r < sg.n) {
       if (sg.slot >= 0) {
@@ -641,13 +715,12 @@ void k_attn_many(AttnArgs a) {
         for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int e = 0; e < 16; e += 4)
-            if (32 * t + 2 * e + 4 * h < a.D)
+            if (32 * t + 2 * e + 4 * h < D)
               put4(out + 32 * t + 2 * e + 4 * h,
                    f32x4{acc[t][e] * inv, acc[t][e + 1] * inv, acc[t][e + 2] * inv, acc[t][e + 3] * inv});
         if (a.lse && h == 0) a.lse[row * a.Hq + head] = l > 0.0f ? (m + __log2f(l)) * LN2 : -INFINITY;
       }
     }
-    __syncthreads();   // the ring is free for the next segment
   }
   if (threadIdx.x == 0) a.rec[w] = begun;
 }
