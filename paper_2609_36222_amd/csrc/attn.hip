@@ -72,14 +72,6 @@ struct __attribute__((packed, aligned(2))) Any16H { u32x4 v; };
 struct __attribute__((packed, aligned(4))) Any16F { f32x4 v; };
 struct __attribute__((packed, aligned(2))) Any8H { u32x2 v; };
 
-// The same value, of which the compiler knows nothing: what follows from it is not computed
-// in front of the loop (the masks and addresses of a unit's queries would hold 60 registers
-// through the loop over the keys)
-__device__ __forceinline__ int here(int v) {
-  asm volatile("" : "+s"(v));
-  return v;
-}
-
 __device__ __forceinline__ void put4(uint16_t *p, f32x4 v) {
   u32x2 q;
   q[0] = (uint32_t)f32_to_bf16_any(v[0]) | ((uint32_t)f32_to_bf16_any(v[1]) << 16);
@@ -281,8 +273,7 @@ void k_attn_few(AttnArgs a) {
       }
 #pragma unroll
       for (int e = 0; e < TK / 4; ++e) top = fmaxf(top, x[e]);
-      top = fmaxf(top, xor_lane<16>(top));
-      top = fmaxf(top, xor_lane<32>(top));
+      top = max_lane<32>(max_lane<16>(top));
       if (__any(top > m[c] + LAG)) {
         const float to = fmaxf(m[c], top), f = m[c] == to ? 1.0f : __builtin_amdgcn_exp2f(m[c] - to);
         m[c] = to;
@@ -398,8 +389,7 @@ void k_attn_few(AttnArgs a) {
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
       if (c >= nr) continue;
-      l[c] = l[c] + xor_lane<16>(l[c]);
-      l[c] = l[c] + xor_lane<32>(l[c]);
+      l[c] = add_lane<32>(add_lane<16>(l[c]));
       lds_barrier();   // the area is free
       if (wave > 0) {
         char *to = area + (wave - 1) * M::STATE;
@@ -436,7 +426,7 @@ void k_attn_few(AttnArgs a) {
       if (sg.slot >= 0) {
         float *part = a.part + sg.slot * attn_part_floats<R, DP>();
 #pragma unroll
-        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(part + r * DP + 16 * t + 4 * g) = acc[c][t];
+        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(part + ((c * DT + t) * WAVE + lane) * 4) = acc[c][t];
         if (g == 0) {
           part[R * DP + r] = top;
           part[R * DP + R + r] = sum;
@@ -537,7 +527,7 @@ void k_attn_many(AttnArgs a) {
                           (long long)(sg.hk * a.G + pr - tok * a.G) * a.q.head;
 #pragma unroll
       for (int s = 0; s < QS; ++s) {
-        const int d = 16 * s + 8 * h;
+        const int d = 16 * s + 8 * lane_here(h);
         qv[s] = reinterpret_cast<const Any16H *>(p + min(d, D - 8))->v;
       }
     }
@@ -561,22 +551,28 @@ void k_attn_many(AttnArgs a) {
     // blocks whose keys are all there
     const int full0 = a.D == DP ? (lo + BK - 1) / BK : 0x7FFFFFFF, full1 = hi / BK;
     auto issue = [&](int i) {
-      if (i - from >= WAVE / M::PI) fetch_rows(i);
+      if (__builtin_expect(i - from >= WAVE / M::PI, 0)) fetch_rows(i);
       const uint32_t st = ring_at + (i & (M::RING - 1)) * M::STAGE;
-      const bool all = i >= full0 && i < full1;
+      const uint32_t to = st + row0(0) * M::ROWB;
+      const char *kb[M::PI], *vb[M::PI];
 #pragma unroll
       for (int j = 0; j < M::PI; ++j) {
-        const char *kb = lane_at(rows.klo, rows.khi, M::PI * (i - from) + j);
-        const char *vb = lane_at(rows.vlo, rows.vhi, M::PI * (i - from) + j);
-        const uint32_t to = st + row0(j) * M::ROWB;
-        if (all) {
-          glb_to_lds(kb, ko[j], to);
-          glb_to_lds(vb, vo[j], to + M::HALF);
-        } else {
+        kb[j] = lane_at(rows.klo, rows.khi, M::PI * (i - from) + j);
+        vb[j] = lane_at(rows.vlo, rows.vhi, M::PI * (i - from) + j);
+      }
+      if (__builtin_expect(i >= full0 && i < full1, 1)) {
+#pragma unroll
+        for (int j = 0; j < M::PI; ++j) {
+          glb_to_lds(kb[j], ko[j], to + j * M::WAVES * 1024);
+          glb_to_lds(vb[j], vo[j], to + j * M::WAVES * 1024 + M::HALF);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < M::PI; ++j) {
           const int row = row0(j) + lane / CH, ck = lane % CH ^ many_k<CH>(row), cv = lane % CH ^ many_v<CH>(row);
           const bool in = i * BK + row >= lo && i * BK + row < hi;
-          glb_to_lds(in && 8 * ck < a.D ? kb + ko[j] : zero, to);
-          glb_to_lds(in && 8 * cv < a.D ? vb + vo[j] : zero, to + M::HALF);
+          glb_to_lds(in && 8 * ck < a.D ? kb[j] + ko[j] : zero, to + j * M::WAVES * 1024);
+          glb_to_lds(in && 8 * cv < a.D ? vb[j] + vo[j] : zero, to + j * M::WAVES * 1024 + M::HALF);
         }
       }
     };
@@ -586,7 +582,7 @@ void k_attn_many(AttnArgs a) {
     // maximum is then the maximum scaled
 #pragma unroll
     for (int s = 0; s < QS; ++s) {
-      const uint32_t keep = a.scale != 0.0f && 16 * s + 8 * h < D ? ~0u : 0u;
+      const uint32_t keep = a.scale != 0.0f && 16 * s + 8 * lane_here(h) < D ? ~0u : 0u;
       qv[s] = (qv[s] ^ flip) & keep;
     }
     if (blocks > 0) issue(sg.k0);
@@ -594,11 +590,10 @@ void k_attn_many(AttnArgs a) {
     if (blocks > 1) wait_vm<2 * M::PI>();
     else wait_vm<0>();
     lds_barrier();
-    // blocks that some row of the wavefront sees
-    auto seen_block = [&](int t) {
-      const int k0 = (sg.k0 + t) * BK;
-      return t >= 0 && t < blocks && mine && k0 <= pmax && !(a.window > 0 && k0 + BK - 1 <= pmin - a.window);
-    };
+    // blocks ta .. tb - 1: those that some row of the wavefront sees
+    const int ta = a.window > 0 ? max(0, (max(pmin - a.window + 1, 0)) / BK - sg.k0) : 0;
+    const int tb = mine ? min(blocks, (max(pmax, -1) + BK) / BK - sg.k0) : 0;
+    auto seen_block = [&](int t) { return t >= ta && t < tb; };
     // the stage of block t + 1 is there (all wavefronts': each waits for its own loads)
     auto wait_next = [&](int t) {
       if (t + 2 < blocks) wait_vm<2 * M::PI>();
@@ -606,49 +601,46 @@ void k_attn_many(AttnArgs a) {
     };
     f32x16 s[KB];
     bf16x8 p[2 * KB];
-    // the second half runs one phase behind; both request block t + 2 in phase 2 t, when
-    // the stage's last readers have passed
+    // operands of the products of block t: V^T of the keys 16 ks .., elements 32 d ..; K of
+    // the keys 32 b .., elements 16 q ..  (many_v(row) is that of row + 8)
+    const int vrow = 4 * h + (lane % 16) / 4;
+    auto read_v = [&](int t, int i) {
+      const char *sv = lds + ((sg.k0 + t) & (M::RING - 1)) * M::STAGE + M::HALF;
+      const int ks = i / DT, piece = 4 * (i % DT) + (lane / 16 & 1) * 2 + (lane & 3) / 2;
+      const char *at = sv + (16 * ks + vrow) * M::ROWB + ((piece ^ many_v<CH>(vrow)) * 16) + (lane & 1) * 8;
+      const bf16x4 v0 = read_tr(at), v1 = read_tr(at + 8 * M::ROWB);
+      return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+    };
+    auto read_k = [&](int t, int i) {
+      const char *sk = lds + ((sg.k0 + t) & (M::RING - 1)) * M::STAGE;
+      const int row = 32 * (i % KB) + n;
+      return *reinterpret_cast<const bf16x8 *>(sk + row * M::ROWB + (((2 * (i / KB) + h) ^ many_k<CH>(row)) * 16));
+    };
+    auto mul_v = [&](int i, bf16x8 v) { acc[i % DT] = mfma32(v, p[i / DT], acc[i % DT]); };
+    auto mul_k = [&](int i, bf16x8 v) {
+      if (i < KB)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[i][e] = 0.0f;
+      s[i % KB] = mfma32(v, __builtin_bit_cast(bf16x8, qv[i / KB]), s[i % KB]);
+    };
+    constexpr int NV = 2 * KB * DT, NK = QS * KB;
+    // the second half runs one phase behind; each requests rows in its softmax's phase: those
+    // of the block after next, whose stage's last readers have passed
     if (half) {
       if (blocks > 2) issue(sg.k0 + 2);
       lds_barrier();
     }
     for (int t = 0; t <= blocks; ++t) {
       const int late = here(half);   // (one loop for both halves, not one each)
-      if (!late && t + 2 < blocks) issue(sg.k0 + t + 2);
+      const bool old = seen_block(t - 1), now = seen_block(t);
       __builtin_amdgcn_s_setprio(1);
-      if (seen_block(t - 1)) {
-        const char *sv = lds + ((sg.k0 + t - 1) & (M::RING - 1)) * M::STAGE + M::HALF;
-        const int row = 4 * h + (lane % 16) / 4;   // of 16 (many_v(row) is that of row + 8)
-        fed<2 * KB * DT, 4>(
-            [&](int i) {
-              const int ks = i / DT, piece = 4 * (i % DT) + (lane / 16 & 1) * 2 + (lane & 3) / 2;
-              const char *at = sv + (16 * ks + row) * M::ROWB + ((piece ^ many_v<CH>(row)) * 16) + (lane & 1) * 8;
-              const bf16x4 v0 = read_tr(at), v1 = read_tr(at + 8 * M::ROWB);
-              return bf16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            },
-            [&](int i, bf16x8 v) { acc[i % DT] = mfma32(v, p[i / DT], acc[i % DT]); });
-      }
-      if (seen_block(t)) {
-        const char *sk = lds + ((sg.k0 + t) & (M::RING - 1)) * M::STAGE;
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
-        fed<QS * KB, 4>(
-            [&](int i) {
-              const int row = 32 * (i % KB) + n;
-              return *reinterpret_cast<const bf16x8 *>(sk + row * M::ROWB +
-                                                       (((2 * (i / KB) + h) ^ many_k<CH>(row)) * 16));
-            },
-            [&](int i, bf16x8 v) {
-              s[i % KB] = mfma32(v, __builtin_bit_cast(bf16x8, qv[i / KB]), s[i % KB]);
-            });
-      }
+      if (old) fed<NV, 4>([&](int i) { return read_v(t - 1, i); }, mul_v);
+      if (now) fed<NK, 4>([&](int i) { return read_k(t, i); }, mul_k);
       __builtin_amdgcn_s_setprio(0);
       if (late) wait_next(t);
       lds_barrier();
-      if (late && t + 3 < blocks) issue(sg.k0 + t + 3);
-      if (seen_block(t)) {
+      if (t + 2 + late < blocks) issue(sg.k0 + t + 2 + late);
+      if (now) {
         const int k0 = (sg.k0 + t) * BK;
         if (k0 + BK - 1 > pmin || (a.window > 0 && k0 <= pmax - a.window)) {
           // (key <= pos and > pos - window, the block's and the lane's part on one side)
@@ -666,7 +658,7 @@ void k_attn_many(AttnArgs a) {
         for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
-        top = fmaxf(top, xor_lane<32>(top)) * scale;
+        top = max_lane<32>(top) * scale;
         if (__any(top > m + LAG)) {
           const float to = fmaxf(m, top), f = m == to ? 1.0f : __builtin_amdgcn_exp2f(m - to);
           m = to;
@@ -692,7 +684,8 @@ void k_attn_many(AttnArgs a) {
       lds_barrier();
     }
     if (!half) lds_barrier();
-    l = l + xor_lane<32>(l);
+    l = add_lane<32>(l);
+    const int d0 = lane_here(4 * h);   // the lane's first element
     if (r < sg.n) {
       if (sg.slot >= 0) {
         float *part = a.part + sg.slot * attn_part_floats<R, DP>();
@@ -700,7 +693,7 @@ void k_attn_many(AttnArgs a) {
         for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<f32x4 *>(part + r * DP + 32 * t + 2 * e + 4 * h) =
+            *reinterpret_cast<f32x4 *>(part + (((wave * DT + t) * 4 + e / 4) * WAVE + lane) * 4) =
                 f32x4{acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]};
         if (h == 0) {
           part[R * DP + r] = m;
@@ -715,8 +708,8 @@ void k_attn_many(AttnArgs a) {
         for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int e = 0; e < 16; e += 4)
-            if (32 * t + 2 * e + 4 * h < D)
-              put4(out + 32 * t + 2 * e + 4 * h,
+            if (32 * t + 2 * e + d0 < D)
+              put4(out + 32 * t + 2 * e + d0,
                    f32x4{acc[t][e] * inv, acc[t][e + 1] * inv, acc[t][e + 2] * inv, acc[t][e + 3] * inv});
         if (a.lse && h == 0) a.lse[row * a.Hq + head] = l > 0.0f ? (m + __log2f(l)) * LN2 : -INFINITY;
       }
@@ -728,124 +721,113 @@ void k_attn_many(AttnArgs a) {
 // The parts of the units that lie in several workgroups' stretches, added in their order.
 // Workgroup b takes its share of the unit that goes on behind stretch b: a unit of count
 // parts has count - 1 workgroups.
-template <typename T>
-__device__ __forceinline__ void join_store(const AttnArgs &a, const AttnPart &p, int r, int at, float top,
-                                           float sum, float o) {
-  const int pr = p.r0 + r, tok = over(pr, a.by_G), head = p.head + pr - tok * a.G;
+template <typename T, int ROWS, int DP>
+__device__ __forceinline__ void join_store(const AttnArgs &a, const AttnPart &p, int r, int q, float top,
+                                           float sum, f32x4 o) {
+  if (r >= p.n) return;
+  const int pr = p.r0 + r, tok = over(pr, a.by_G), head = p.head + pr - tok * a.G, at = attn_at<ROWS, DP>(q, lane_id());
   const long long row = p.token + tok;
-  const float v = sum > 0.0f ? o / sum : (sum == 0.0f ? 0.0f : sum);
-  T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
-  if (at < a.D) {
-    if constexpr (sizeof(T) == 2) out[at] = f32_to_bf16_any(v);
-    else out[at] = v;
-  }
+  const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+  if (at < a.D) put4((T *)a.o.p + row * a.o.row + head * a.o.head + at, o * inv);
   if (a.lse && at == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
 }
-// Sums of parts k0, k0 + step, .. (NB at a time, their loads together) of RB rows
-template <int R, int DP, int RB, int NB>
-__device__ __forceinline__ void join_sum(const AttnArgs &a, const AttnPart &p, int r0, int k0, int step,
-                                         float (&top)[RB], float (&sum)[RB], float (&o)[RB][DP / WAVE]) {
-  constexpr int E = DP / WAVE;
+// Sums of parts k0, k0 + step, .. (NB at a time, their loads together) of the pieces q0 ..
+// q0 + PB - 1, which are of the same rows; r: the lane's
+template <int R, int DP, int PB, int NB>
+__device__ __forceinline__ void join_sum(const AttnArgs &a, const AttnPart &p, int r, int q0, int k0, int step,
+                                         float &top, float &sum, f32x4 (&o)[PB]) {
   constexpr size_t F = attn_part_floats<R, DP>();
   const int lane = lane_id();
+  top = -INFINITY;
+  sum = 0.0f;
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    top[b] = -INFINITY;
-    sum[b] = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[b][e] = 0.0f;
-  }
+  for (int b = 0; b < PB; ++b) o[b] = f32x4{0, 0, 0, 0};
   for (; k0 < p.count; k0 += NB * step) {
-    float m[NB][RB], l[NB][RB], x[NB][RB][E];
+    float m[NB], l[NB];
+    f32x4 x[NB][PB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int k = min(k0 + j * step, p.count - 1);
       const float *part = a.part + (k == 0 ? p.slot : 2 * (p.w + k)) * F;
+      m[j] = part[R * DP + r];
+      l[j] = part[R * DP + R + r];
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        const int r = min(r0 + b, p.n - 1);
-        m[j][b] = part[R * DP + r];
-        l[j][b] = part[R * DP + R + r];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[j][b][e] = part[r * DP + WAVE * e + lane];
-      }
+      for (int b = 0; b < PB; ++b) x[j][b] = *reinterpret_cast<const f32x4 *>(part + ((q0 + b) * WAVE + lane) * 4);
     }
+    float to = top;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      float to = top[b];
+    for (int j = 0; j < NB; ++j) {
+      if (k0 + j * step >= p.count) m[j] = -INFINITY;
+      to = fmaxf(to, m[j]);
+    }
+    const float mm = to == -INFINITY ? 0.0f : to, f0 = __builtin_amdgcn_exp2f(top - mm);
+    top = to;
+    sum *= f0;
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        if (k0 + j * step >= p.count) m[j][b] = -INFINITY;
-        to = fmaxf(to, m[j][b]);
-      }
-      const float mm = to == -INFINITY ? 0.0f : to, f0 = __builtin_amdgcn_exp2f(top[b] - mm);
-      top[b] = to;
-      sum[b] *= f0;
+    for (int b = 0; b < PB; ++b) o[b] *= f0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[b][e] *= f0;
+    for (int j = 0; j < NB; ++j) {
+      const float f = __builtin_amdgcn_exp2f(m[j] - mm);   // 0 past the last part
+      if (k0 + j * step >= p.count) continue;
+      sum = __builtin_fmaf(f, l[j], sum);
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const float f = __builtin_amdgcn_exp2f(m[j][b] - mm);   // 0 past the last part
-        if (k0 + j * step >= p.count) continue;
-        sum[b] = __builtin_fmaf(f, l[j][b], sum[b]);
+      for (int b = 0; b < PB; ++b)
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[b][e] = __builtin_fmaf(f, x[j][b][e], o[b][e]);
-      }
+        for (int e = 0; e < 4; ++e) o[b][e] = __builtin_fmaf(f, x[j][b][e], o[b][e]);
     }
   }
 }
 template <typename T, int R, int DP>
 __global__ __launch_bounds__(R > 32 ? 1024 : 512)
 void k_attn_join(AttnArgs a) {
-  constexpr int WAVES = R > 32 ? 16 : 8, E = DP / WAVE;
-  __shared__ float ml[WAVES][2], os[WAVES][DP];
+  constexpr int ROWS = R > 32 ? 32 : 16, WAVES = R > 32 ? 16 : 8, PER = ROWS * DP / 256, PB = PER < 4 ? PER : 4;
+  __shared__ float ml[WAVES][2][WAVE];
+  __shared__ f32x4 os[WAVES][WAVE];
   const AttnPart p = a.rec[blockIdx.x];
   if (p.count == 0) return;
   const int share = blockIdx.x - p.w, shares = p.count - 1, wave = wave_id_u(), lane = lane_id();
-  if (p.count <= 4) {   // a wavefront a row, several rows' loads together
-    constexpr int RB = R > 32 ? (DP == 256 ? 2 : 4) : 1;
-    for (int r0 = (share * WAVES + wave) * RB; r0 < p.n; r0 += shares * WAVES * RB) {
-      float top[RB], sum[RB], o[RB][E];
-      if (p.count == 2) join_sum<R, DP, RB, 2>(a, p, r0, 0, 1, top, sum, o);
-      else join_sum<R, DP, RB, 4>(a, p, r0, 0, 1, top, sum, o);
+  const int pieces = (p.n + ROWS - 1) / ROWS * PER;
+  // (a row of the part past the unit's holds something, which is not stored)
+  auto row = [&](int q) { return q / PER * ROWS + lane % ROWS; };
+  if (R > 32 && p.count <= 4) {   // a wavefront several pieces
+    for (int q0 = (share * WAVES + wave) * PB; q0 < pieces; q0 += shares * WAVES * PB) {
+      float top, sum;
+      f32x4 o[PB];
+      join_sum<R, DP, PB, 2>(a, p, row(q0), q0, 0, 1, top, sum, o);
 #pragma unroll
-      for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (r0 + b < p.n) join_store<T>(a, p, r0 + b, WAVE * e + lane, top[b], sum[b], o[b][e]);
+      for (int b = 0; b < PB; ++b) join_store<T, ROWS, DP>(a, p, row(q0), q0 + b, top, sum, o[b]);
     }
     return;
   }
-  // `per` wavefronts a row, with every so-manieth part
-  int per = 2;
+  // `per` wavefronts a piece, with every so-manieth part
+  int per = 1;
   while (per < WAVES && per * 8 < p.count) per *= 2;
   const int sub = wave & (per - 1), groups = WAVES / per, group = wave / per;
-  for (int r0 = share * groups; r0 < p.n; r0 += shares * groups) {
-    const int r = min(r0 + group, p.n - 1);
-    float top[1], sum[1], o[1][E];
-    join_sum<R, DP, 1, 8>(a, p, r, sub, per, top, sum, o);
-    if (lane == 0) {
-      ml[wave][0] = top[0];
-      ml[wave][1] = sum[0];
+  for (int p0 = share * groups; p0 < pieces; p0 += shares * groups) {
+    const int q = min(p0 + group, pieces - 1), r = row(q);
+    float top, sum;
+    f32x4 o[1];
+    join_sum<R, DP, 1, 8>(a, p, r, q, sub, per, top, sum, o);
+    if (per == 1) {
+      if (p0 + group < pieces) join_store<T, ROWS, DP>(a, p, r, q, top, sum, o[0]);
+      continue;
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) os[wave][WAVE * e + lane] = o[0][e];
+    ml[wave][0][lane] = top;
+    ml[wave][1][lane] = sum;
+    os[wave][lane] = o[0];
     __syncthreads();
-    if (sub == 0 && r0 + group < p.n) {
-      float to = -INFINITY;
-      for (int v = 0; v < per; ++v) to = fmaxf(to, ml[wave + v][0]);
+    if (sub == 0 && p0 + group < pieces) {
+      float to = -INFINITY, t = 0.0f;
+      for (int v = 0; v < per; ++v) to = fmaxf(to, ml[wave + v][0][lane]);
       const float mm = to == -INFINITY ? 0.0f : to;
-      float t = 0.0f, x[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = 0.0f;
+      f32x4 x = {0, 0, 0, 0};
       for (int v = 0; v < per; ++v) {
-        const float f = __builtin_amdgcn_exp2f(ml[wave + v][0] - mm);
-        t = __builtin_fmaf(f, ml[wave + v][1], t);
+        const float f = __builtin_amdgcn_exp2f(ml[wave + v][0][lane] - mm);
+        t = __builtin_fmaf(f, ml[wave + v][1][lane], t);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(f, os[wave + v][WAVE * e + lane], x[e]);
+        for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(f, os[wave + v][lane][e], x[e]);
       }
-#pragma unroll
-      for (int e = 0; e < E; ++e) join_store<T>(a, p, r, WAVE * e + lane, to, t, x[e]);
+      join_store<T, ROWS, DP>(a, p, r, q, to, t, x);
     }
     __syncthreads();
   }

@@ -93,6 +93,58 @@ __device__ __forceinline__ KeyRange attn_keys(const AttnArgs &a, const AttnSeq &
 // a value that is the same in all lanes, known as such to the compiler
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// The same value, of which the compiler knows nothing: what follows from it is not computed
+// in front of a loop (the masks and addresses of a unit's rows would hold 80 registers
+// through the loop over the keys)
+__device__ __forceinline__ int here(int v) {   // uniform
+  asm volatile("" : "+s"(v));
+  return v;
+}
+__device__ __forceinline__ int lane_here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// The value of lane ^ 16 or lane ^ 32 beside the lane's own, in one or the other order (an
+// exchange of rows of 16 lanes, or of the halves, between two copies: no way through LDS)
+template <int H>
+__device__ __forceinline__ void both_lanes(float v, float &x, float &y) {
+  static_assert(H == 16 || H == 32, "lane distance");
+  const unsigned u = __float_as_uint(v);
+  const auto r = H == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false)
+                         : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  x = __uint_as_float(r[0]);
+  y = __uint_as_float(r[1]);
+}
+template <int H>
+__device__ __forceinline__ float max_lane(float v) {
+  float x, y;
+  both_lanes<H>(v, x, y);
+  return fmaxf(x, y);
+}
+template <int H>
+__device__ __forceinline__ float add_lane(float v) {
+  float x, y;
+  both_lanes<H>(v, x, y);
+  return x + y;
+}
+
+__device__ __forceinline__ int wave_sum(int v) {
+  const int lane = lane_here(lane_id());
+#pragma unroll
+  for (int h = 1; h < WAVE; h *= 2) v += __builtin_amdgcn_ds_bpermute(4 * (lane ^ h), v);
+  return v;
+}
+__device__ __forceinline__ int wave_prefix(int v) {   // inclusive
+  const int lane = lane_here(lane_id());
+#pragma unroll
+  for (int h = 1; h < WAVE; h *= 2) {
+    const int o = __builtin_amdgcn_ds_bpermute(4 * (lane - h), v);
+    if (lane >= h) v += o;
+  }
+  return v;
+}
+
 // The walk of a workgroup over its stretch of the line (costs in units of 2^a.coarse
 // blocks, so that the line's length fits 31 bits).  Lane l holds sequence s0 + l.
 template <int R, int BK>
@@ -100,9 +152,9 @@ struct AttnWork {
   const AttnArgs &a;
   int w, per, at, end;      // the stretch's rest
   int s0, begin, stop, kv, cost;   // of the lane's sequence; cost: a head's
-  int s;                    // where it stands: the sequence, its cost a head, the place in it
+  int s, hk, j, left;       // where it stands: sequence, key head, tile, place in the tile
+  int tiles;
   AttnSeq q;
-  int head_cost, rem;
   bool first;
 
   __device__ int tile_cost(const AttnSeq &sq, int j) const {
@@ -111,60 +163,82 @@ struct AttnWork {
     const int c = ((k.hi + BK - 1) / BK - k.lo / BK + (1 << a.coarse) - 1) >> a.coarse;
     return c > 1 ? c : 1;
   }
+  __device__ AttnSeq lane_seq(int l) const {
+    return attn_seq(a, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(stop, l),
+                    __builtin_amdgcn_readlane(kv, l));
+  }
   __device__ void load(int from) {
     s0 = from;
-    const int i = min(from + lane_id(), a.b.n_seq - 1);
+    const int lane = lane_id(), i = min(from + lane, a.b.n_seq - 1);
     begin = min(max(a.b.q_start[i], 0), a.rows);
     stop = min(max(a.b.q_start[i + 1], begin), a.rows);
     kv = min(max(a.b.kv_len[i], 0), a.b.max_pages << a.c.shift);
-    if (from + lane_id() >= a.b.n_seq) stop = begin;
+    if (from + lane >= a.b.n_seq) stop = begin;
     const AttnSeq sq = attn_seq(a, begin, stop, kv);
     const int t = (sq.packed + R - 1) / R;
-    cost = 0;
-    if (a.whole) cost = t;
-    else
-      for (int j = 0; j < t; ++j) cost += tile_cost(sq, j);
+    cost = a.whole ? t : t == 1 ? tile_cost(sq, 0) : 0;
+    // a sequence of several tiles: a tile a lane
+    unsigned long long more = a.whole ? 0 : __ballot(t > 1);
+    while (more) {
+      const int l = __ffsll(more) - 1;
+      more &= more - 1;
+      const AttnSeq one = lane_seq(l);
+      const int n = (one.packed + R - 1) / R;
+      int c = 0;
+      for (int t0 = lane; t0 < n; t0 += WAVE) c += tile_cost(one, t0);
+      c = wave_sum(c);
+      if (lane == l) cost = c;
+    }
   }
 
   __device__ AttnWork(const AttnArgs &args, int w_) : a(args), w(w_), first(true) {
-    const int lane = lane_id();
-    int total = 0, run = 0;
+    int total = 0, run = 0, incl = 0;
     for (int from = 0; from < a.b.n_seq; from += WAVE) {
       load(from);
-      total += cost;
+      incl = wave_prefix(cost * a.c.Hk);
+      total += __builtin_amdgcn_readlane(incl, WAVE - 1);
     }
-    total *= a.c.Hk;
-#pragma unroll
-    for (int h = 1; h < WAVE; h *= 2) total += __shfl_xor(total, h, WAVE);
-    total = uni(total);
     per = max(over(total + a.W - 1, a.by_W), a.least);
     at = min(w * (long long)per, (long long)total);
     end = min(at + per, total);
     if (at >= end) return;
     for (int from = 0; from < a.b.n_seq; from += WAVE) {
-      if (a.b.n_seq > WAVE) load(from);
-      int incl = cost * a.c.Hk;
-#pragma unroll
-      for (int h = 1; h < WAVE; h *= 2) {
-        const int o = __shfl_up(incl, h, WAVE);
-        if (lane >= h) incl += o;
+      if (a.b.n_seq > WAVE) {
+        load(from);
+        incl = wave_prefix(cost * a.c.Hk);
       }
+      const int mine = cost * a.c.Hk;
       const unsigned long long hit = __ballot(run + incl > at);
-      if (hit) {
-        const int l = __ffsll(hit) - 1;
-        rem = at - run - __builtin_amdgcn_readlane(incl - cost * a.c.Hk, l);
-        enter(from + l);
-        break;
+      if (!hit) {
+        run += __builtin_amdgcn_readlane(incl, WAVE - 1);
+        continue;
       }
-      run += __builtin_amdgcn_readlane(incl, WAVE - 1);
+      const int l = __ffsll(hit) - 1, head = __builtin_amdgcn_readlane(cost, l);
+      int rest = at - run - __builtin_amdgcn_readlane(incl - mine, l);
+      enter(from + l);
+      hk = quotient(rest, head);
+      rest -= hk * head;
+      // the tile with that place, 64 tiles at a time
+      for (int j0 = 0; tiles > 1; j0 += WAVE) {
+        const int c = j0 + lane_id() < tiles ? tile_cost(q, j0 + lane_id()) : 0, upto = wave_prefix(c);
+        const unsigned long long in = __ballot(upto > rest);
+        if (in) {
+          const int m = __ffsll(in) - 1;
+          j = j0 + m;
+          rest -= __builtin_amdgcn_readlane(upto - c, m);
+          break;
+        }
+        rest -= __builtin_amdgcn_readlane(upto, WAVE - 1);
+      }
+      left = rest;
+      break;
     }
   }
   __device__ void enter(int i) {
     s = i;
-    const int l = i - s0;
-    q = attn_seq(a, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(stop, l),
-                 __builtin_amdgcn_readlane(kv, l));
-    head_cost = __builtin_amdgcn_readlane(cost, l);
+    q = lane_seq(i - s0);
+    tiles = (q.packed + R - 1) / R;
+    hk = j = left = 0;
   }
 
   // The next segment: blocks [k0, k1) of a unit whose rows are r0 .. r0 + n - 1 of the
@@ -177,8 +251,11 @@ struct AttnWork {
   };
   __device__ bool next(Segment &g, AttnPart &begun) {
     if (at >= end) return false;
-    while (rem >= head_cost * a.c.Hk) {   // on to the next sequence that has work
-      rem = 0;
+    if (j == tiles) {
+      j = 0;
+      ++hk;
+    }
+    if (hk == a.c.Hk) {   // on to the next sequence that has work
       unsigned long long more = __ballot(cost > 0) & (s - s0 == WAVE - 1 ? 0ull : ~0ull << (s - s0 + 1));
       while (!more) {
         load(s0 + WAVE);
@@ -186,35 +263,39 @@ struct AttnWork {
       }
       enter(s0 + __ffsll(more) - 1);
     }
+    const int c = tile_cost(q, j);
     g.s = s;
     g.q = q;
-    g.hk = quotient(rem, head_cost);
-    int left = rem - g.hk * head_cost, j = 0, c;
-    while (left >= (c = tile_cost(q, j))) {
-      left -= c;
-      ++j;
-    }
+    g.hk = hk;
     g.r0 = j * R;
     g.n = min(R, q.packed - g.r0);
     g.keys = attn_keys(a, q, g.r0, g.n);
     const int take = min(c - left, end - at), b0 = g.keys.lo / BK, b1 = (g.keys.hi + BK - 1) / BK;
     g.k0 = a.whole ? b0 : b0 + (left << a.coarse);
     g.k1 = take == c - left ? b1 : b0 + ((left + take) << a.coarse);
-    g.slot = -1;
-    if (take < c) g.slot = 2 * w + (first ? 0 : 1);
+    g.slot = take < c ? 2 * w + (first ? 0 : 1) : -1;
     if (left + take < c) {   // the unit goes on in the next workgroup
       const int from = at - left, w0 = quotient(from, per);
-      begun = {q.first, g.hk * a.G, g.r0, g.n, 2 * w0 + (from == w0 * per ? 0 : 1),
+      begun = {q.first, hk * a.G, g.r0, g.n, 2 * w0 + (from == w0 * per ? 0 : 1),
                quotient(from + c - 1, per) - w0 + 1, w0, 0};
     }
     first = false;
     at += take;
-    rem += take;
+    left = 0;
+    ++j;
     return true;
   }
 };
 
-// A part: R rows of DP floats, then R maxima (of the products times scale log2 e) and R sums
+// A part: pieces of 64 lanes times four floats as the accumulators lie, ROWS rows' (32 in
+// k_attn_many, 16 in k_attn_few) after another's, R DP floats in all; then R maxima (of the
+// products times scale log2 e) and R sums.  Piece q of lane l holds row ROWS (q / per) + l %
+// ROWS, per = ROWS DP / 256, and four elements from attn_at on.
+template <int ROWS, int DP>
+__device__ __forceinline__ int attn_at(int q, int lane) {
+  const int in = q % (ROWS * DP / 256);
+  return ROWS == 32 ? 8 * in + 4 * (lane / 32) : 16 * in + 4 * (lane / 16);
+}
 template <int R, int DP>
 __host__ __device__ constexpr size_t attn_part_floats() { return (size_t)R * (DP + 2); }
 
