@@ -144,10 +144,11 @@ void k_attn_few(AttnArgs a) {
     z.at = row_at(a, z.g.s, z.g.hk, max(min(key, (z.g.keys.hi - 1) & ~15), 0));
   };
   auto steps = [&](Seg &z) {
-    z.i0 = z.g.k0;
-    z.i1 = z.g.k1;
+    z.i0 = max(z.g.k0, (z.g.keys.lo - wave * TK) / M::BK);
+    z.i1 = min(z.g.k1, (z.g.keys.hi - wave * TK + M::BK - 1) / M::BK);
+    // (a quotient rounds to zero, where the bound above or below holds)
     while (z.i0 < z.i1 && key0(z.i0) + TK <= z.g.keys.lo) ++z.i0;
-    while (z.i1 > z.i0 && key0(z.i1 - 1) >= z.g.keys.hi) --z.i1;
+    z.i1 = max(z.i1, z.i0);
     z.ask = z.i0;
   };
   auto queries = [&](const typename Work::Segment &sg, u32x4 (&qv)[NR][QS]) {
@@ -165,6 +166,16 @@ void k_attn_few(AttnArgs a) {
         else qv[c][s] = __builtin_bit_cast(u32x4, reinterpret_cast<const Any16F *>(at)->v);
       }
     }
+  };
+  auto take_queries = [&](u32x4 (&to)[NR][QS], const u32x4 (&raw)[NR][QS]) {
+    const int D = here(a.D);
+#pragma unroll
+    for (int c = 0; c < NR; ++c)
+#pragma unroll
+      for (int s = 0; s < QS; ++s) {
+        const uint32_t keep = (BF ? 32 * s + 8 * lane_here(g) : 16 * s + 4 * lane_here(g)) < D ? ~0u : 0u;
+        to[c][s] = raw[c][s] & keep;
+      }
   };
   // the segment's next step into the stage given
   auto issue = [&](Seg &z, int stage) {
@@ -202,44 +213,44 @@ void k_attn_few(AttnArgs a) {
 
   AttnPart begun{};
   Work work(a, blockIdx.x);
-  Seg z, ahead;
-  u32x4 qv[NR][QS], qn[NR][QS];
+  // z: the segment at hand, ahead: the next one, whose queries and addresses are loaded (16-bit) and
+  // whose first steps are requested behind z's last, so that between segments the memory is
+  // not left waiting; src: the one whose steps are being requested
+  Seg z, ahead, src;
+  u32x4 qv[NR][QS], qn[NR][BF ? QS : 1];
   int asked = 0, used = 0;   // steps requested and used, of all segments: the ring's places
-  bool more = work.next(z.g, begun);
-  if (more) {
-    steps(z);
-    queries(z.g, qn);
-    if (BF) fetch_rows(z, z.i0);
-  }
-  while (more) {
-    const typename Work::Segment &sg = z.g;
-    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1, D = here(a.D);
-#pragma unroll
-    for (int c = 0; c < NR; ++c)
-#pragma unroll
-      for (int s = 0; s < QS; ++s) {
-        const uint32_t keep = (BF ? 32 * s + 8 * g : 16 * s + 4 * g) < D ? ~0u : 0u;
-        qv[c][s] = qn[c][s] & keep;
-      }
-    if constexpr (BF)
-      while (z.ask < z.i1 && z.ask < z.i0 + M::RING) issue(z, asked++ & 1);
-    // the next segment's queries and pages, and its first steps behind this one's last:
-    // between segments the memory is not left waiting
-    more = work.next(ahead.g, begun);
+  bool have = false, more = true, early = false;   // early: src is ahead
+  while (true) {
     if (more) {
-      steps(ahead);
-      queries(ahead.g, qn);
-      if constexpr (BF) {
-        fetch_rows(ahead, ahead.i0);
-        // waited for here, where what is in flight besides has been for long: the compiler's
-        // wait at their first use would be for the steps requested since, too
+      more = work.next(ahead.g, begun);
+      if (more) {
+        steps(ahead);
+        if constexpr (BF) {
+          queries(ahead.g, qn);
+          fetch_rows(ahead, ahead.i0);
+          // waited for here, where what is in flight besides has been for long: the compiler's
+          // wait at their first use would be for the steps requested since, too
 #pragma unroll
-        for (int c = 0; c < NR; ++c)
+          for (int c = 0; c < NR; ++c)
 #pragma unroll
-          for (int s = 0; s < QS; ++s) asm volatile("" ::"v"(qn[c][s]));
-        asm volatile("" ::"v"(ahead.at.klo));
+            for (int s = 0; s < QS; ++s) asm volatile("" ::"v"(qn[c][s]));
+          asm volatile("" ::"v"(ahead.at.klo));
+        }
       }
     }
+    if (!have) {
+      if (!more) break;
+      have = true;
+      z = src = ahead;
+      if constexpr (BF) take_queries(qv, qn);
+      continue;
+    }
+    const typename Work::Segment &sg = z.g;
+    if constexpr (!BF) {   // (nothing is requested ahead here, and there are no registers to spare)
+      queries(sg, qv);
+      take_queries(qv, qv);
+    }
+    const int lo = sg.keys.lo, hi = sg.keys.hi, nr = NR > 1 && sg.n > 16 ? 2 : 1, D = here(a.D);
     int pos[NR];
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
@@ -294,6 +305,14 @@ void k_attn_few(AttnArgs a) {
     for (int i = z.i0; i < z.i1; ++i) {
       const int k0 = key0(i);
       if constexpr (BF) {
+        while (asked - used < M::RING) {
+          if (src.ask == src.i1 && !early && more) {
+            src = ahead;
+            early = true;
+          }
+          if (src.ask == src.i1) break;
+          issue(src, asked++ & 1);
+        }
         if (asked - used > 1) wait_vm<M::LOADS>();
         else wait_vm<0>();
         const char *st = ring + (used++ & 1) * M::STAGE, *sv = st + TK * M::ROWB;
@@ -342,8 +361,6 @@ void k_attn_few(AttnArgs a) {
         }
         // this stage's reads are done before its next rows are requested
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (z.ask < z.i1) issue(z, asked++ & 1);
-        else if (more && ahead.ask < ahead.i1) issue(ahead, asked++ & 1);
       } else {
         const long long page = attn_page(a, sg.s, k0), slot = k0 & ((1 << a.c.shift) - 1);
         const float *kb = (const float *)a.c.k + page * a.c.k_page + slot * a.c.k_slot + sg.hk * a.c.k_head;
@@ -442,7 +459,11 @@ void k_attn_few(AttnArgs a) {
         if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
       }
     }
+    if (!more) break;
     z = ahead;
+    if (!early) src = ahead;
+    early = false;
+    if constexpr (BF) take_queries(qv, qn);
   }
   if (!a.whole && threadIdx.x == 0) a.rec[blockIdx.x] = begun;
 }
@@ -737,7 +758,10 @@ template <int R, int DP, int PB, int NB>
 __device__ __forceinline__ void join_sum(const AttnArgs &a, const AttnPart &p, int r, int q0, int k0, int step,
                                          float &top, float &sum, f32x4 (&o)[PB]) {
   constexpr size_t F = attn_part_floats<R, DP>();
-  const int lane = lane_id();
+  // (a lane whose row is not there reads the last row's: nothing more from memory)
+  constexpr int ROWS = R > 32 ? 32 : 16;
+  const int past = max(r - (p.n - 1), 0), lane = lane_id() - past;
+  r -= past;
   top = -INFINITY;
   sum = 0.0f;
 #pragma unroll

@@ -192,46 +192,53 @@ struct AttnWork {
   }
 
   __device__ AttnWork(const AttnArgs &args, int w_) : a(args), w(w_), first(true) {
+    // the line's length, then the place of the stretch's begin in it: the second pass needs
+    // no loads where one chunk of 64 holds all sequences
     int total = 0, run = 0, incl = 0;
-    for (int from = 0; from < a.b.n_seq; from += WAVE) {
-      load(from);
-      incl = wave_prefix(cost * a.c.Hk);
-      total += __builtin_amdgcn_readlane(incl, WAVE - 1);
-    }
-    per = max(over(total + a.W - 1, a.by_W), a.least);
-    at = min(w * (long long)per, (long long)total);
-    end = min(at + per, total);
-    if (at >= end) return;
-    for (int from = 0; from < a.b.n_seq; from += WAVE) {
-      if (a.b.n_seq > WAVE) {
+    bool placed = false;
+    at = 0;
+    for (int from = 0;;) {
+      if (!placed || a.b.n_seq > WAVE) {
         load(from);
         incl = wave_prefix(cost * a.c.Hk);
       }
-      const int mine = cost * a.c.Hk;
+      const int sum = __builtin_amdgcn_readlane(incl, WAVE - 1);
+      if (!placed) {
+        total += sum;
+        from += WAVE;
+        if (from < a.b.n_seq) continue;
+        per = max(over(total + a.W - 1, a.by_W), a.least);
+        at = min(w * (long long)per, (long long)total);
+        end = min(at + per, total);
+        if (at >= end) return;
+        placed = true;
+        from = 0;
+        if (a.b.n_seq > WAVE) continue;
+      }
       const unsigned long long hit = __ballot(run + incl > at);
-      if (!hit) {
-        run += __builtin_amdgcn_readlane(incl, WAVE - 1);
-        continue;
+      if (hit) {
+        const int l = __ffsll(hit) - 1, head = __builtin_amdgcn_readlane(cost, l);
+        left = at - run - __builtin_amdgcn_readlane(incl, l) + head * a.c.Hk;
+        const int rest = left;
+        enter(from + l);
+        hk = quotient(rest, head);
+        left = rest - hk * head;
+        break;
       }
-      const int l = __ffsll(hit) - 1, head = __builtin_amdgcn_readlane(cost, l);
-      int rest = at - run - __builtin_amdgcn_readlane(incl - mine, l);
-      enter(from + l);
-      hk = quotient(rest, head);
-      rest -= hk * head;
-      // the tile with that place, 64 tiles at a time
-      for (int j0 = 0; tiles > 1; j0 += WAVE) {
-        const int c = j0 + lane_id() < tiles ? tile_cost(q, j0 + lane_id()) : 0, upto = wave_prefix(c);
-        const unsigned long long in = __ballot(upto > rest);
-        if (in) {
-          const int m = __ffsll(in) - 1;
-          j = j0 + m;
-          rest -= __builtin_amdgcn_readlane(upto - c, m);
-          break;
-        }
-        rest -= __builtin_amdgcn_readlane(upto, WAVE - 1);
+      run += sum;
+      from += WAVE;
+    }
+    // the tile with that place, 64 tiles at a time
+    for (int j0 = 0; tiles > 1; j0 += WAVE) {
+      const int c = j0 + lane_id() < tiles ? tile_cost(q, j0 + lane_id()) : 0, upto = wave_prefix(c);
+      const unsigned long long in = __ballot(upto > left);
+      if (in) {
+        const int m = __ffsll(in) - 1;
+        j = j0 + m;
+        left -= __builtin_amdgcn_readlane(upto - c, m);
+        break;
       }
-      left = rest;
-      break;
+      left -= __builtin_amdgcn_readlane(upto, WAVE - 1);
     }
   }
   __device__ void enter(int i) {

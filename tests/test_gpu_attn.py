@@ -260,3 +260,15 @@ def test_bad_device_data_stays_in_bounds(bd):
     batch.tensors[1].copy_(torch.tensor([0, 1, -3, 2 ** 31 - 1], dtype=torch.int32))
     bd.paged_attention(q.cuda(), cache, batch)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q", [1, 6])
+def test_several_units_a_workgroup(bd, dtype, D, q):
+    """More work than workgroups: each goes through parts and wholes of several units."""
+    g = np.random.default_rng(D + q)
+    lens = [(int(g.integers(1, q + 1)), int(g.integers(q, 400))) for _ in range(90)]
+    b = U.Batch(lens, 9, D, 16, dtype, seed=D)
+    b.fill()
+    check(bd, b, 36)
