@@ -118,16 +118,27 @@ void k_attn_few(AttnArgs a) {
   char *const area = lds + M::LDS - M::AREA;
   // the lane's places in the loads of a step (piece j of 64 16-byte pieces)
   uint32_t ko[BF ? M::CH / 2 : 1], vo[BF ? M::CH / 2 : 1];
+  uint32_t kin = 0, vin = 0;   // bit j: the piece is one of the head's D elements
   if constexpr (BF) {
 #pragma unroll
     for (int j = 0; j < M::CH / 2; ++j) {
       const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
       ko[j] = 2 * ((row & 15) * (uint32_t)a.c.k_slot + 8 * (piece ^ few_k<M::CH>(row)));
       vo[j] = 2 * ((row & 15) * (uint32_t)a.c.v_slot + 8 * (piece ^ few_v<M::CH>(row)));
+      if (8 * (piece ^ few_k<M::CH>(row)) < a.D) kin |= 1u << j;
+      if (8 * (piece ^ few_v<M::CH>(row)) < a.D) vin |= 1u << j;
     }
   }
   char *const ring = lds + wave * M::RING * M::STAGE;
   const uint32_t ring_at = lds_addr(ring);
+  // heads shorter than DP: K's places past D, which no load of a whole step writes, are zeros
+  // from here on (V's hold anything: they are sums of their own, which nobody stores)
+  if (BF && a.D < DP) {
+#pragma unroll 1
+    for (int j = 0; j < M::CH / 2 * M::RING; ++j)
+      *reinterpret_cast<u32x4 *>(ring + j / (M::CH / 2) * M::STAGE + j % (M::CH / 2) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
 
   // A segment as the wavefront has it: its steps i0 .. i1 - 1 (keys key0(i) .. + TK - 1),
   // the next one to request, and the addresses of 32 steps, two a step (16 keys lie in one
@@ -188,16 +199,24 @@ void k_attn_few(AttnArgs a) {
       kb[h] = lane_at(z.at.klo, z.at.khi, 2 * (i - z.from) + h);
       vb[h] = lane_at(z.at.vlo, z.at.vhi, 2 * (i - z.from) + h);
     }
-    if (k0 >= lo && k0 + TK <= hi && a.D == DP) {
+    if (k0 >= lo && k0 + TK <= hi) {
+      if (a.D == DP) {
 #pragma unroll
-      for (int j = 0; j < M::CH / 2; ++j) {
-        const int h = WAVE * j / M::CH / 16;
-        glb_to_lds(kb[h], ko[j], st + j * 1024);
-        glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
+        for (int j = 0; j < M::CH / 2; ++j) {
+          const int h = WAVE * j / M::CH / 16;
+          glb_to_lds(kb[h], ko[j], st + j * 1024);
+          glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
+        }
+      } else {   // (some lanes of each load have a piece: all are issued, as wait_vm counts)
+#pragma unroll
+        for (int j = 0; j < M::CH / 2; ++j) {
+          const int h = WAVE * j / M::CH / 16;
+          if (kin >> j & 1) glb_to_lds(kb[h], ko[j], st + j * 1024);
+          if (vin >> j & 1) glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
+        }
       }
     } else {
-      // a step at the end of what is seen, or heads shorter than DP: zeros in the places
-      // of what is not there
+      // a step at the end of what is seen: zeros in the places of what is not there
 #pragma unroll 1
       for (int j = 0; j < M::CH / 2; ++j) {
         const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
@@ -521,12 +540,21 @@ void k_attn_many(AttnArgs a) {
   // (one wavefront a SIMD has nobody to take turns with)
   const int half = M::WPE > 1 ? wave / (M::WAVES / 2) : 0;
   auto row0 = [&](int j) { return (wave + M::WAVES * j) * WAVE / CH; };   // of load j
-  uint32_t ko[M::PI], vo[M::PI];                                          // the lane's places in it
+  uint32_t ko[M::PI], vo[M::PI], kin = 0, vin = 0;                        // the lane's places in it, and which there are
 #pragma unroll
   for (int j = 0; j < M::PI; ++j) {
     const int row = row0(j) + lane / CH;
     ko[j] = 2 * (lane / CH * (uint32_t)a.c.k_slot + 8 * (lane % CH ^ many_k<CH>(row)));
     vo[j] = 2 * (lane / CH * (uint32_t)a.c.v_slot + 8 * (lane % CH ^ many_v<CH>(row)));
+    if (8 * (lane % CH ^ many_k<CH>(row)) < a.D) kin |= 1u << j;
+    if (8 * (lane % CH ^ many_v<CH>(row)) < a.D) vin |= 1u << j;
+  }
+  // as in k_attn_few: K's places past D are zeros, V's anything
+  if (a.D < DP) {
+#pragma unroll 1
+    for (int j = 0; j < M::PI * M::RING; ++j)
+      *reinterpret_cast<u32x4 *>(lds + j / M::PI * M::STAGE + (j % M::PI * M::WAVES + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    lds_barrier();
   }
   const float scale = a.scale != 0.0f ? fabsf(a.scale) : 1.0f;
   const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
@@ -570,7 +598,7 @@ void k_attn_many(AttnArgs a) {
       rows = row_at(a, sg.s, sg.hk, min(key, most));
     };
     // blocks whose keys are all there
-    const int full0 = a.D == DP ? (lo + BK - 1) / BK : 0x7FFFFFFF, full1 = hi / BK;
+    const int full0 = (lo + BK - 1) / BK, full1 = hi / BK;
     auto issue = [&](int i) {
       if (__builtin_expect(i - from >= WAVE / M::PI, 0)) fetch_rows(i);
       const uint32_t st = ring_at + (i & (M::RING - 1)) * M::STAGE;
@@ -582,10 +610,18 @@ void k_attn_many(AttnArgs a) {
         vb[j] = lane_at(rows.vlo, rows.vhi, M::PI * (i - from) + j);
       }
       if (__builtin_expect(i >= full0 && i < full1, 1)) {
+        if (__builtin_expect(a.D == DP, 1)) {
 #pragma unroll
-        for (int j = 0; j < M::PI; ++j) {
-          glb_to_lds(kb[j], ko[j], to + j * M::WAVES * 1024);
-          glb_to_lds(vb[j], vo[j], to + j * M::WAVES * 1024 + M::HALF);
+          for (int j = 0; j < M::PI; ++j) {
+            glb_to_lds(kb[j], ko[j], to + j * M::WAVES * 1024);
+            glb_to_lds(vb[j], vo[j], to + j * M::WAVES * 1024 + M::HALF);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < M::PI; ++j) {
+            if (kin >> j & 1) glb_to_lds(kb[j], ko[j], to + j * M::WAVES * 1024);
+            if (vin >> j & 1) glb_to_lds(vb[j], vo[j], to + j * M::WAVES * 1024 + M::HALF);
+          }
         }
       } else {
 #pragma unroll
@@ -801,15 +837,19 @@ __device__ __forceinline__ void join_sum(const AttnArgs &a, const AttnPart &p, i
     }
   }
 }
-template <typename T, int R, int DP>
-__global__ __launch_bounds__(R > 32 ? 1024 : 512)
-void k_attn_join(AttnArgs a) {
-  constexpr int ROWS = R > 32 ? 32 : 16, WAVES = R > 32 ? 16 : 8, PER = ROWS * DP / 256, PB = PER < 4 ? PER : 4;
-  __shared__ float ml[WAVES][2][WAVE];
-  __shared__ f32x4 os[WAVES][WAVE];
-  const AttnPart p = a.rec[blockIdx.x];
+template <int WAVES>
+struct JoinLds {
+  float ml[WAVES][2][WAVE];
+  f32x4 os[WAVES][WAVE];
+};
+template <typename T, int R, int DP, int WAVES>
+__device__ __forceinline__ void join(const AttnArgs &a, int b, JoinLds<WAVES> &lds) {
+  constexpr int ROWS = R > 32 ? 32 : 16, PER = ROWS * DP / 256, PB = PER < 4 ? PER : 4;
+  auto &ml = lds.ml;
+  auto &os = lds.os;
+  const AttnPart p = a.rec[b];
   if (p.count == 0) return;
-  const int share = blockIdx.x - p.w, shares = p.count - 1, wave = wave_id_u(), lane = lane_id();
+  const int share = b - p.w, shares = p.count - 1, wave = wave_id_u(), lane = lane_id();
   const int pieces = (p.n + ROWS - 1) / ROWS * PER;
   // (a row of the part past the unit's holds something, which is not stored)
   auto row = [&](int q) { return q / PER * ROWS + lane % ROWS; };
@@ -856,11 +896,32 @@ void k_attn_join(AttnArgs a) {
     __syncthreads();
   }
 }
+template <typename T, int R, int DP>
+__global__ __launch_bounds__(R > 32 ? 1024 : 512)
+void k_attn_join(AttnArgs a) {
+  __shared__ JoinLds<(R > 32 ? 16 : 8)> lds;
+  join<T, R, DP>(a, blockIdx.x, lds);
+}
+// both kernels' in one launch
+template <int RF, int RM, int DP>
+__global__ __launch_bounds__(1024)
+void k_attn_join_both(AttnArgs few, AttnArgs many) {
+  __shared__ JoinLds<16> lds;
+  if ((int)blockIdx.x < many.W) join<uint16_t, RM, DP>(many, blockIdx.x, lds);
+  else join<uint16_t, RF, DP>(few, blockIdx.x - many.W, lds);
+}
 
 // The launches of a call.  Sequences of at most FEW_ROWS packed rows are k_attn_few's,
 // longer ones (16-bit) k_attn_many's; where there may be both, both run, on parts of the
-// workspace of their own.
+// workspace of their own, and one launch joins the units of both.  Calls whose products
+// come to at most FEW_FLOPS are k_attn_few's alone, however long their sequences are: a
+// unit of k_attn_many takes 9 us (its rows go through eight wavefronts' ring), and each
+// launch about 4.  Measured at D 128, 96 or 64, k_attn_few alone against both: 0.15 GFLOP
+// 15.9 against 36.7 us, 0.02 GFLOP 13.4 against 38.1, 2.1 GFLOP 26.7 against 28.8, 2.9
+// GFLOP 29.8 against 33.6; 6.5 GFLOP 69.8 against 62.5; at D 256, where its tiles are of 16
+// rows, 2.3 GFLOP 45 against 39.5.
 constexpr int FEW_ROWS = 32;
+constexpr double FEW_FLOPS = 3e9;
 struct Launch {
   int R, BK, W, coarse, least;   // W 0: none
   bool whole;
@@ -871,7 +932,7 @@ struct Plan {
   Launch few, many;
   size_t bytes;
 };
-Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows, int n_cu) {
+Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows, int window, int n_cu) {
   Plan p{};
   p.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   const long long G = Hq / c.Hk, most = b.max_q * G;
@@ -890,9 +951,13 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
     l.rec = p.bytes = (p.bytes + 255) & ~(size_t)255;
     if (!l.whole) p.bytes += ((size_t)l.W * sizeof(AttnPart) + 255) & ~(size_t)255;
   };
-  if (!bf16 || most <= FEW_ROWS || b.n_seq > 1)
+  // (the lengths are on the device: this is the most that the products can come to)
+  const double keys = (double)((long long)b.max_pages << c.shift), span = window > 0 ? window + b.max_q : keys;
+  const double flops = 4.0 * p.dp * Hq * rows * (span < keys ? span : keys);
+  const bool small = !bf16 || most <= FEW_ROWS || flops <= (p.dp == 256 ? FEW_FLOPS / 3 : FEW_FLOPS);
+  if (small || b.n_seq > 1)
     shape(p.few, p.dp == 256 || most <= 16 ? 16 : 32, 64, !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1, 1, true);
-  if (bf16 && most > FEW_ROWS) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, 6, false);
+  if (!small) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, 6, false);
   if (p.bytes == 0) p.bytes = 256;
   return p;
 }
@@ -901,12 +966,14 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
 
 size_t attn_ws_bytes(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long long rows,
                      int n_cu) {
-  return plan(bf16, D, Hq, c, b, rows, n_cu).bytes;
+  // (of any window: none, and the least)
+  const size_t all = plan(bf16, D, Hq, c, b, rows, 0, n_cu).bytes, one = plan(bf16, D, Hq, c, b, rows, 1, n_cu).bytes;
+  return all > one ? all : one;
 }
 
 hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b, void *ws, int n_cu,
                        hipStream_t st) {
-  const Plan p = plan(call.bf16, call.D, call.Hq, c, b, call.rows, n_cu);
+  const Plan p = plan(call.bf16, call.D, call.Hq, c, b, call.rows, call.window, n_cu);
   AttnArgs a{};
   a.q = call.q;
   a.o = call.o;
@@ -920,44 +987,49 @@ hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b,
   a.window = call.window;
   a.scale = call.scale * LOG2E;
   a.by_G = divisor(a.G);
-  auto use = [&](const Launch &l, int above, int upto) {
-    a.above = above;
-    a.upto = upto;
-    a.W = l.W;
-    a.whole = l.whole;
-    a.coarse = l.coarse;
-    a.by_W = divisor(l.W);
-    a.least = l.least;
-    a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
-    a.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);
+  AttnArgs af = a, am = a;
+  auto use = [&](AttnArgs &to, const Launch &l, int above, int upto) {
+    to.above = above;
+    to.upto = upto;
+    to.W = l.W;
+    to.whole = l.whole;
+    to.coarse = l.coarse;
+    to.by_W = divisor(l.W);
+    to.least = l.least;
+    to.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
+    to.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);
   };
-#define BASE_MANY(DP)                                                                            \
-  do {                                                                                           \
-    launch_k(k_attn_many<DP>, dim3(p.many.W), dim3(ManyShape<DP>::THREADS), 0, st, a);           \
-    launch_k(k_attn_join<uint16_t, ManyShape<DP>::R, DP>, dim3(p.many.W), dim3(1024), 0, st, a); \
+  if (p.many.W) use(am, p.many, p.few.W ? FEW_ROWS : 0, 0x7FFFFFFF);
+  if (p.few.W) use(af, p.few, 0, p.many.W ? FEW_ROWS : 0x7FFFFFFF);
+#define BASE_MANY(DP)                                                                             \
+  do {                                                                                            \
+    launch_k(k_attn_many<DP>, dim3(p.many.W), dim3(ManyShape<DP>::THREADS), 0, st, am);           \
+    if (!p.few.W || p.few.whole)                                                                  \
+      launch_k(k_attn_join<uint16_t, ManyShape<DP>::R, DP>, dim3(p.many.W), dim3(1024), 0, st, am); \
   } while (0)
-#define BASE_FEW(T, DP, NR)                                                                      \
-  do {                                                                                           \
-    launch_k(k_attn_few<T, DP, NR>, dim3(p.few.W), dim3(FewShape<T, DP, NR>::THREADS), 0, st, a); \
-    if (!p.few.whole)                                                                            \
-      launch_k(k_attn_join<T, 16 * NR, DP>, dim3(p.few.W), dim3(512), 0, st, a);                 \
+#define BASE_FEW(T, DP, NR)                                                                       \
+  do {                                                                                            \
+    launch_k(k_attn_few<T, DP, NR>, dim3(p.few.W), dim3(FewShape<T, DP, NR>::THREADS), 0, st, af); \
+    if (p.few.whole) break;                                                                       \
+    if (p.many.W)                                                                                 \
+      launch_k(k_attn_join_both<16 * NR, ManyShape<DP>::R, DP>, dim3(p.few.W + p.many.W), dim3(1024), 0, st, af, am); \
+    else                                                                                          \
+      launch_k(k_attn_join<T, 16 * NR, DP>, dim3(p.few.W), dim3(512), 0, st, af);                 \
   } while (0)
-#define BASE_FEW_R(T, DP)                                                                        \
+#define BASE_FEW_R(T, DP)                                                                         \
   do { if (p.few.R == 16) BASE_FEW(T, DP, 1); else BASE_FEW(T, DP, 2); } while (0)
-#define BASE_FEW_D(T)                                                                            \
-  do {                                                                                           \
-    if (p.dp == 64) BASE_FEW_R(T, 64);                                                           \
-    else if (p.dp == 128) BASE_FEW_R(T, 128);                                                    \
-    else BASE_FEW(T, 256, 1);                                                                    \
+#define BASE_FEW_D(T)                                                                             \
+  do {                                                                                            \
+    if (p.dp == 64) BASE_FEW_R(T, 64);                                                            \
+    else if (p.dp == 128) BASE_FEW_R(T, 128);                                                     \
+    else BASE_FEW(T, 256, 1);                                                                     \
   } while (0)
   if (p.many.W) {
-    use(p.many, p.few.W ? FEW_ROWS : 0, 0x7FFFFFFF);
     if (p.dp == 64) BASE_MANY(64);
     else if (p.dp == 128) BASE_MANY(128);
     else BASE_MANY(256);
   }
   if (p.few.W) {
-    use(p.few, 0, p.many.W ? FEW_ROWS : 0x7FFFFFFF);
     if (call.bf16) BASE_FEW_D(uint16_t);
     else BASE_FEW_D(float);
   }

@@ -154,8 +154,10 @@ struct AttnWork {
   int s0, begin, stop, kv, cost;   // of the lane's sequence; cost: a head's
   int s, hk, j, left;       // where it stands: sequence, key head, tile, place in the tile
   int tiles;
+  int q0, q1, len;          // of the lane's sequence of the next 64, as they are in memory
   AttnSeq q;
   bool first;
+  static constexpr int LANE_TILES = 16;
 
   __device__ int tile_cost(const AttnSeq &sq, int j) const {
     if (a.whole) return 1;
@@ -167,18 +169,32 @@ struct AttnWork {
     return attn_seq(a, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(stop, l),
                     __builtin_amdgcn_readlane(kv, l));
   }
+  __device__ void fetch(int from) {   // the sequences from .. from + 63, for load
+    const int i = min(from + lane_id(), a.b.n_seq - 1);
+    q0 = a.b.q_start[i];
+    q1 = a.b.q_start[i + 1];
+    len = a.b.kv_len[i];
+  }
+  // (the next 64 are fetched while these are taken: in a batch of 256 a workgroup would wait
+  // eight times for memory before its first key)
   __device__ void load(int from) {
     s0 = from;
-    const int lane = lane_id(), i = min(from + lane, a.b.n_seq - 1);
-    begin = min(max(a.b.q_start[i], 0), a.rows);
-    stop = min(max(a.b.q_start[i + 1], begin), a.rows);
-    kv = min(max(a.b.kv_len[i], 0), a.b.max_pages << a.c.shift);
+    const int lane = lane_id();
+    begin = min(max(q0, 0), a.rows);
+    stop = min(max(q1, begin), a.rows);
+    kv = min(max(len, 0), a.b.max_pages << a.c.shift);
     if (from + lane >= a.b.n_seq) stop = begin;
+    if (a.b.n_seq > WAVE) fetch(from + WAVE < a.b.n_seq ? from + WAVE : 0);
     const AttnSeq sq = attn_seq(a, begin, stop, kv);
     const int t = (sq.packed + R - 1) / R;
-    cost = a.whole ? t : t == 1 ? tile_cost(sq, 0) : 0;
-    // a sequence of several tiles: a tile a lane
-    unsigned long long more = a.whole ? 0 : __ballot(t > 1);
+    if (a.whole) {
+      cost = t;
+      return;
+    }
+    // a lane the tiles of its sequence, or where they are many, all lanes those of one
+    cost = 0;
+    for (int i = 0; i < t && t <= LANE_TILES; ++i) cost += tile_cost(sq, i);
+    unsigned long long more = __ballot(t > LANE_TILES);
     while (more) {
       const int l = __ffsll(more) - 1;
       more &= more - 1;
@@ -197,6 +213,7 @@ struct AttnWork {
     int total = 0, run = 0, incl = 0;
     bool placed = false;
     at = 0;
+    fetch(0);
     for (int from = 0;;) {
       if (!placed || a.b.n_seq > WAVE) {
         load(from);
