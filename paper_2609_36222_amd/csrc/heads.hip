@@ -7,10 +7,13 @@
 // radians its step is 1/16), so the turns position * inv_freq / 2 pi are taken in fp64
 // and their fraction goes on in fp32.
 //
-// Bound by memory: each head is read once and written once.  A lane holds eight pairs of
+// Bound by memory: each head is read once and written once.  A lane holds 16 elements of
 // a head, D / 16 lanes (rounded up to a power of two) a head, and a wavefront several
 // heads of one row at a time, the next ones' loads in flight; the row's cosines and sines
-// are computed once a wavefront, a pair a lane, and shared through LDS.
+// are computed once a wavefront, a pair a lane, and shared through LDS, while the first
+// heads are on their way.  8191 rows of 16 + 16 fp32 heads of 128 (268 MB): 63.5 us, 4.2 TB/s
+// of the 4.9 a large copy reaches; a cache filled by 205 MB of prompts 46.4 us, 4.4 TB/s; one
+// row 3.2 us, of which the launch is most.
 #include "common.hpp"
 #include "internal.hpp"
 #include "seq.hpp"
@@ -91,9 +94,63 @@ __device__ __forceinline__ float value(uint16_t v) { return bf16_to_f32(v); }
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t *p, float v) { *p = f32_to_bf16_any(v); }
 
-// VEC: rot and D are multiples of 16, so that a lane's eight pairs are two runs of eight
-// elements, all rotated or none.
-template <typename T, bool VEC, bool CACHE>
+// What a lane has of a head.  MODE 1, rot and D multiples of 16: two runs of eight elements
+// that are eight pairs' (a and b, or the pairs' one after another), all rotated or none.
+// MODE 2, other heads with room for whole runs: the rotated elements and the others are cut
+// apart, and the last lane of each takes runs that end with it; the first elements of such
+// a run are another lane's too (both write the same values), and count once in the sum of
+// squares.  MODE 0, the rest (less than 16 rotated elements, less than 8 others): eight pairs
+// element by element.  (20000 rows of 40 heads with norms, 50 of 80 elements rotated, 256 MB:
+// 84.8 us by runs, 209.8 element by element; 20 heads, 34 of 128: 74 against 192.)
+struct Run {
+  int p0, o1, o2;    // the first pair's number, the runs' places
+  int dx, dy;        // how many of a run's first elements are another lane's
+  bool inside, turned;
+};
+template <int MODE>
+__device__ __forceinline__ Run run_of(int li, int D, int rot, bool interleaved) {
+  Run r{};
+  const int half = rot / 2;
+  if constexpr (MODE != 2) {
+    const bool halves = !interleaved && li * 8 < half;
+    r.p0 = li * 8;
+    r.o1 = halves ? r.p0 : 2 * r.p0;
+    r.o2 = halves ? half + r.p0 : 2 * r.p0 + 8;
+    r.inside = r.p0 < D / 2;
+    r.turned = r.p0 < half;
+  } else {
+    const int turning = interleaved ? 0 : (half + 7) / 8, lane0 = li - turning;   // lanes with a and b apart
+    if (lane0 < 0) {
+      r.p0 = min(8 * li, half - 8);
+      r.o1 = r.p0;
+      r.o2 = half + r.p0;
+      r.dx = r.dy = 8 * li - r.p0;
+      r.inside = r.turned = true;
+    } else {
+      const int first = interleaved ? 0 : rot, n = D - first, at = first + 16 * lane0;
+      r.inside = 16 * lane0 < n;
+      r.o1 = n >= 16 ? min(at, D - 16) : first;
+      r.o2 = n >= 16 ? r.o1 + 8 : D - 8;
+      r.dx = n >= 16 ? min(at - r.o1, 8) : 0;
+      r.dy = n >= 16 ? max(at - r.o1 - 8, 0) : 16 - n;
+      r.p0 = r.o1 / 2;
+      r.turned = interleaved && r.p0 < half;
+    }
+  }
+  return r;
+}
+// lanes of a head
+inline int run_lanes(int mode, int D, int rot, bool interleaved) {
+  if (mode != 2 || interleaved) return (D + 15) / 16;
+  return (rot / 2 + 7) / 8 + (D - rot + 15) / 16;
+}
+inline int run_mode(int D, int rot, bool interleaved) {
+  if (D % 16 == 0 && rot % 16 == 0) return 1;
+  if (interleaved) return D >= 16 ? 2 : 0;
+  return rot >= 16 && (rot == D || D - rot >= 8) ? 2 : 0;
+}
+
+template <typename T, int MODE, bool CACHE>
 __global__ __launch_bounds__(HEAD_WAVES * WAVE)
 void k_heads(HeadsArgs a) {
   __shared__ float cs[HEAD_WAVES][2][MAX_PAIRS];
@@ -103,6 +160,33 @@ void k_heads(HeadsArgs a) {
   const int part = (int)(job - row * a.split);
   if (row >= a.rows) return;
   const int D = a.r.D, rot = a.r.rot, half = rot / 2;
+
+  const int lph = a.lph, per = WAVE / lph, li = lane & (lph - 1), sub = lane / lph;
+  const int pairs = D / 2;
+  const Run run = run_of<MODE>(li, D, rot, a.r.interleaved);
+  const int p0 = run.p0;
+  const bool halves = !a.r.interleaved && run.turned;
+  constexpr bool RUNS = MODE != 0;
+  using Raw = decltype(raw8((const T *)nullptr));
+  // a pass takes `per` heads; the first's runs are on their way while the angles are made,
+  // the next one's while one is worked on
+  auto source = [&](int pass) {
+    const int h = pass * per + sub;
+    const bool isq = h < a.Hq, isk = !isq && h < a.Hq + a.Hk;
+    const HeadRows &in = isq ? a.q : isk ? a.k : a.v;
+    return (const T *)in.p + row * in.row + (isq ? h : isk ? h - a.Hq : h - a.Hq - a.Hk) * in.head;
+  };
+  Raw r1{}, r2{};
+  auto request = [&](int pass) {
+    if (run.inside && pass * per + sub < a.heads) {
+      const T *src = source(pass);
+      r1 = raw8(src + run.o1);
+      r2 = raw8(src + run.o2);
+    }
+  };
+  if constexpr (RUNS) {
+    if (part < a.passes) request(part);
+  }
 
   int position = 0;
   long long kp = 0, vp = 0;      // the token's slot, head 0
@@ -133,19 +217,11 @@ void k_heads(HeadsArgs a) {
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
-  const int lph = a.lph, per = WAVE / lph, li = lane & (lph - 1), sub = lane / lph;
-  const int pairs = D / 2, p0 = li * 8;
-  const bool inside = p0 < pairs;            // the lane holds pairs of the head
-  const bool halves = !a.r.interleaved && p0 < half;
-  const int o1 = halves ? p0 : 2 * p0, o2 = halves ? half + p0 : 2 * p0 + 8;   // VEC
-
   for (int pass = part; pass < a.passes; pass += a.split) {
     const int h = pass * per + sub;
-    const bool have = inside && h < a.heads;
+    const bool have = run.inside && h < a.heads;
     const bool isq = h < a.Hq, isk = !isq && h < a.Hq + a.Hk;
     const int hl = isq ? h : isk ? h - a.Hq : h - a.Hq - a.Hk;
-    const HeadRows &in = isq ? a.q : isk ? a.k : a.v;
-    const T *src = (const T *)in.p + row * in.row + hl * in.head;
     T *dst;
     bool write = have;
     if (!CACHE || isq) {
@@ -156,17 +232,18 @@ void k_heads(HeadsArgs a) {
       write = have && stored;
     }
     const float *gain = isq ? a.r.q_gain : isk ? a.r.k_gain : nullptr;
-    float x[8], y[8];   // VEC: the runs at o1 and o2; else pair i is (x[i], y[i])
+    float x[8], y[8];   // the runs at o1 and o2; in MODE 0 pair i is (x[i], y[i])
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.0f;
-    if constexpr (VEC) {
+    if constexpr (RUNS) {
       if (have) {
-        const auto r1 = raw8(src + o1), r2 = raw8(src + o2);
         values8(r1, x);
         values8(r2, y);
       }
+      if (pass + a.split < a.passes) request(pass + a.split);
     } else {
       if (have) {
+        const T *src = source(pass);
         T u[16];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -186,9 +263,11 @@ void k_heads(HeadsArgs a) {
       float ss = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        ss = __builtin_fmaf(x[i], x[i], ss);
-        ss = __builtin_fmaf(y[i], y[i], ss);
+        const float u = MODE == 2 && i < run.dx ? 0.0f : x[i], v = MODE == 2 && i < run.dy ? 0.0f : y[i];
+        ss = __builtin_fmaf(u, u, ss);
+        ss = __builtin_fmaf(v, v, ss);
       }
+      if (lph > 16) ss = ss + xor_lane<16>(ss);
       if (lph > 8) ss = ss + xor_lane<8>(ss);
       if (lph > 4) ss = ss + xor_lane<4>(ss);
       if (lph > 2) ss = ss + xor_lane<2>(ss);
@@ -197,9 +276,9 @@ void k_heads(HeadsArgs a) {
         const float m = ss / (float)D + a.r.eps;
         const float r = m > 0.0f ? 1.0f / __fsqrt_rn(m) : (m == 0.0f ? 0.0f : m);   // NaN stays NaN
         float gx[8], gy[8];
-        if constexpr (VEC) {
-          values8(raw8(gain + o1), gx);
-          values8(raw8(gain + o2), gy);
+        if constexpr (RUNS) {
+          values8(raw8(gain + run.o1), gx);
+          values8(raw8(gain + run.o2), gy);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -217,8 +296,8 @@ void k_heads(HeadsArgs a) {
       }
     }
     if (isq || isk) {
-      if constexpr (VEC) {
-        if (p0 < half) {
+      if constexpr (RUNS) {
+        if (run.turned) {
           const float *c = &cs[w][0][p0], *s = &cs[w][1][p0];
           if (halves) {
 #pragma unroll
@@ -231,10 +310,14 @@ void k_heads(HeadsArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float u = x[2 * i], v = x[2 * i + 1], e = y[2 * i], f = y[2 * i + 1];
-              x[2 * i] = __builtin_fmaf(u, c[i], -(v * s[i]));
-              x[2 * i + 1] = __builtin_fmaf(u, s[i], v * c[i]);
-              y[2 * i] = __builtin_fmaf(e, c[4 + i], -(f * s[4 + i]));
-              y[2 * i + 1] = __builtin_fmaf(e, s[4 + i], f * c[4 + i]);
+              if (MODE == 1 || p0 + i < half) {
+                x[2 * i] = __builtin_fmaf(u, c[i], -(v * s[i]));
+                x[2 * i + 1] = __builtin_fmaf(u, s[i], v * c[i]);
+              }
+              if (MODE == 1 || p0 + 4 + i < half) {
+                y[2 * i] = __builtin_fmaf(e, c[4 + i], -(f * s[4 + i]));
+                y[2 * i + 1] = __builtin_fmaf(e, s[4 + i], f * c[4 + i]);
+              }
             }
           }
         }
@@ -250,9 +333,9 @@ void k_heads(HeadsArgs a) {
       }
     }
     if (write) {
-      if constexpr (VEC) {
-        store8(dst + o1, x);
-        store8(dst + o2, y);
+      if constexpr (RUNS) {
+        store8(dst + run.o1, x);
+        store8(dst + run.o2, y);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -279,8 +362,10 @@ hipError_t launch_heads(bool bf16, const RopeArgs &R, long long rows, const int3
   a.Hq = Hq;
   a.Hk = Hk;
   a.heads = Hq + Hk + (cache ? Hk : 0);
+  a.r.interleaved = R.interleaved || R.rot == 0;
+  const int mode = run_mode(R.D, R.rot, a.r.interleaved);
   a.lph = 1;
-  while (a.lph * 16 < R.D) a.lph *= 2;
+  while (a.lph < run_lanes(mode, R.D, R.rot, a.r.interleaved)) a.lph *= 2;
   a.passes = (a.heads * a.lph + WAVE - 1) / WAVE;
   const long long want = (16384 + rows - 1) / rows;
   a.split = (int)(want < a.passes ? want : a.passes);
@@ -294,12 +379,11 @@ hipError_t launch_heads(bool bf16, const RopeArgs &R, long long rows, const int3
     a.b = *batch;
   }
   const dim3 grid((unsigned)((rows * a.split + HEAD_WAVES - 1) / HEAD_WAVES));
-  const bool vec = R.D % 16 == 0 && R.rot % 16 == 0;
-#define BASE_HEADS(T, V)                                                                        \
-  launch_k(cache ? k_heads<T, V, true> : k_heads<T, V, false>, grid, dim3(HEAD_WAVES *WAVE), 0, \
+#define BASE_HEADS(T, MODE)                                                                         \
+  launch_k(cache ? k_heads<T, MODE, true> : k_heads<T, MODE, false>, grid, dim3(HEAD_WAVES *WAVE), 0, \
            st, a)
-  if (bf16) { if (vec) BASE_HEADS(uint16_t, true); else BASE_HEADS(uint16_t, false); }
-  else { if (vec) BASE_HEADS(float, true); else BASE_HEADS(float, false); }
+  if (bf16) { if (mode == 1) BASE_HEADS(uint16_t, 1); else if (mode == 2) BASE_HEADS(uint16_t, 2); else BASE_HEADS(uint16_t, 0); }
+  else { if (mode == 1) BASE_HEADS(float, 1); else if (mode == 2) BASE_HEADS(float, 2); else BASE_HEADS(float, 0); }
 #undef BASE_HEADS
   return hipGetLastError();
 }

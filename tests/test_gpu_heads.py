@@ -47,6 +47,27 @@ def test_rotation(bd, dtype, interleaved, D, rot):
             U.near(got, want, bound, dtype)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,rot", [(16, 8), (24, 16), (24, 18), (32, 18), (40, 24), (72, 64), (80, 50), (88, 72), (120, 120),
+                                   (128, 18), (128, 110), (128, 120), (232, 96), (248, 248), (256, 18), (256, 250)])
+def test_rotation_of_a_part(bd, dtype, interleaved, D, rot):
+    """Parts that are no whole runs: in place and out of place, norms with them."""
+    g = np.random.default_rng(D * 1000 + rot)
+    rows, Hq, Hk = 21, 19, 3
+    q, k = make(g, rows, Hq, D, dtype), make(g, rows, Hk, D, dtype)
+    inv, pos = U.frequencies(rot), g.integers(0, 200000, rows).astype(np.int32)
+    gq, gk = gains(g, D, True)
+    r = bd.Rope(D, dtype, cuda(inv), interleaved, 1.0, cuda(gq), cuda(gk), 1e-6)
+    qo, ko = bd.head_rope(r, cuda(pos), q.cuda(), k.cuda())
+    for x, gain, got in ((q, gq, qo), (k, gk, ko)):
+        want, bound = U.rotate(x.double().numpy(), gain, pos, inv, 1.0, interleaved, 1e-6)
+        U.near(got, want, bound, dtype)
+    qi, ki = q.cuda(), k.cuda()
+    bd.base_head_rope(r, cuda(pos), qi, ki, qi, ki)
+    assert torch.equal(qi, qo) and torch.equal(ki, ko)
+
+
 @pytest.mark.parametrize("rows", [1, 2, 3, 65, 1000, 20000])
 @pytest.mark.parametrize("Hq,Hk", [(1, 0), (0, 3), (32, 4), (13, 13)])
 def test_rows_and_heads(bd, rows, Hq, Hk):
