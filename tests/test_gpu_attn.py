@@ -272,3 +272,168 @@ def test_several_units_a_workgroup(bd, dtype, D, q):
     b = U.Batch(lens, 9, D, 16, dtype, seed=D)
     b.fill()
     check(bd, b, 36)
+
+
+# A table wide enough that a call counts as a large one (the host knows the table's width, not
+# the lengths): these go through the kernels of many rows, with short sequences.
+def wide(lens, Hk, D, ps, Hq, **kw):
+    rows = sum(n for n, _ in lens)
+    shape = 64 if D <= 64 else 128 if D <= 128 else 256
+    return U.Batch(lens, Hk, D, ps, BF, extra=int(3.2e9 / (4 * shape * Hq * rows * ps)) + 1, **kw)
+
+
+@pytest.mark.parametrize("D", [8, 40, 64, 96, 128, 136, 160, 256])
+@pytest.mark.parametrize("n,kv", [(17, 17), (33, 100), (64, 64), (65, 300), (130, 130), (257, 700)])
+def test_wide_chunks(bd, D, n, kv):
+    b = wide([(n, kv)], 2, D, 16, 6, seed=D + n)
+    b.fill()
+    check(bd, b, 6)
+
+
+@pytest.mark.parametrize("Hq,Hk", [(1, 1), (3, 3), (12, 4), (32, 1), (66, 2)])
+def test_wide_head_layouts(bd, Hq, Hk):
+    b = wide([(1, 700), (40, 70), (35, 129)], Hk, 128, 32, Hq, seed=Hq, heads_first=False)
+    b.fill()
+    check(bd, b, Hq)
+
+
+@pytest.mark.parametrize("D", [64, 80, 128, 192])
+def test_wide_mixed_and_empty(bd, D):
+    lens = [(1, 77), (0, 0), (150, 150), (0, 40), (1, 1), (40, 1200), (9, 4), (2, 0), (200, 130), (1, 2000), (0, 0)]
+    b = wide(lens, 2, D, 64, 8, seed=D)
+    b.fill()
+    check(bd, b, 8, pad_rows=5)
+    check(bd, b, 8, pad_rows=5, max_q=1000)
+
+
+@pytest.mark.parametrize("scale", [1.0, -0.3, 0.0, 30.0])
+def test_wide_scales(bd, scale):
+    b = wide([(1, 600), (40, 111), (70, 333)], 2, 64, 16, 4, seed=9)
+    b.fill()
+    check(bd, b, 4, scale=scale)
+
+
+@pytest.mark.parametrize("D,window", [(64, 1), (64, 31), (128, 64), (128, 100), (128, 1000), (96, 37), (256, 50)])
+def test_large_windows(bd, D, window):
+    """Calls that are large by their rows; what a window leaves behind may hold anything."""
+    lens = [(1, 900), (7, 300), (730, 1401), (450, 450), (3, 3)]
+    b = U.Batch(lens, 1, D, 16, BF, seed=window)
+    lowest = [max(0, kv - n + 1 - window) for n, kv in lens]
+    b.fill(lowest)
+    for s, lo in enumerate(lowest):
+        b.table[s, :lo // 16] = -1
+    Hq = 16
+    shape = 64 if D <= 64 else 128 if D <= 128 else 256
+    assert 4 * shape * Hq * b.rows * (window + 730) > 3e9
+    check(bd, b, Hq, window=window)
+
+
+@pytest.mark.parametrize("lens,Hq", [([(1200, 1200), (3, 50), (700, 701)], 1), ([(2100, 2100)], 1), ([(90, 95)] * 70, 2)])
+def test_many_tiles(bd, lens, Hq):
+    """Sequences of more tiles than a lane counts by itself, of more than 64 tiles; more than
+    64 sequences of several."""
+    for dtype in (BF, F32):
+        b = U.Batch(lens, 1, 8, 16, dtype, seed=len(lens))
+        b.fill()
+        check(bd, b, Hq)
+    b = wide(lens, 1, 8, 16, Hq, seed=len(lens))
+    b.fill()
+    check(bd, b, Hq)
+
+
+def test_wide_many_tiles(bd):
+    for lens, Hq in (([(1030, 1040), (1, 9)], 16), ([(40, 60), (300, 300)] * 40, 4)):
+        b = wide(lens, 1, 16, 16, Hq, seed=3)
+        b.fill()
+        check(bd, b, Hq)
+
+
+def test_wide_every_key_counts(bd):
+    for n, kv in ((100, 1000), (300, 300)):
+        b = wide([(n, kv), (1, 5000)], 1, 64, 16, 4, seed=kv)
+        b.fill()
+        _, lse = check(bd, b, 4, q=torch.zeros(b.rows, 4, 64, dtype=BF))
+        seen = np.concatenate([kv - n + 1 + np.arange(n), [5000]])
+        assert (np.round(np.exp(lse.double().cpu().numpy())) == seen[:, None]).all()
+
+
+def test_wide_repeat_graphs_and_streams(bd):
+    """The same bits every time, with any workspace; two graphs of one workspace replayed in
+    turn, two calls at once with a workspace each, lengths that change between replays."""
+    lens = [(1, 3000), (90, 340), (64, 700), (1, 1), (130, 130)]
+    b = wide(lens, 2, 128, 16, 8, seed=13)
+    b.fill()
+    q = b.queries(8).cuda()
+    cache, batch = b.device(bd)
+    n = bd.attention_workspace_bytes(cache, batch, b.rows, 8)
+    ws = torch.full((n,), 0x7F, dtype=torch.uint8, device="cuda")
+
+    def call(w, window=0):
+        out = torch.full_like(q, 5.0)
+        bd.base_paged_attention(cache, batch, q, out, w, None, window)
+        return out
+    first = call(ws)
+    for fill in (0, 0xFF):
+        ws.fill_(fill)
+        assert torch.equal(call(ws), first)
+    outs, graphs = [torch.empty_like(q) for _ in range(2)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i, window in enumerate((0, 100)):
+            with torch.cuda.graph(graphs[i], stream=side):
+                bd.base_paged_attention(cache, batch, q, outs[i], ws, None, window)
+    torch.cuda.synchronize()
+    full = batch.tensors[2].clone()
+    for cut in (0, 17, 250, 0, 2999):
+        batch.tensors[2].copy_((full - cut).clamp_min(0))
+        for o in outs:
+            o.fill_(5.0)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        other = torch.empty_like(ws)
+        assert torch.equal(outs[0], call(other)) and torch.equal(outs[1], call(other, 100))
+        assert cut or torch.equal(outs[0], first)
+    batch.tensors[2].copy_(full)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    works = [torch.empty_like(ws) for _ in range(2)]
+    got = [[torch.empty_like(q) for _ in range(4)] for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i in range(4):
+        for s, w, o in zip(streams, works, got):
+            bd.base_paged_attention(cache, batch, q, o[i], w, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, first) for os in got for o in os)
+
+
+def test_wide_bad_device_data_stays_in_bounds(bd):
+    lens = [(60, 500), (70, 200), (1, 300)]
+    b = wide(lens, 2, 96, 16, 4, seed=15, fill=0.0)
+    b.fill()
+    q = b.queries(4)
+    want, bound, *_ = U.attend(b, q, 96 ** -0.5)
+    b.table[1, :] = np.resize(np.array([b.n_pages, -7, 1 << 30, -(1 << 31)], np.int64), b.width).astype(np.int32)
+    cache, batch = b.device(bd)
+    out = bd.paged_attention(q.cuda(), cache, batch)
+    U.near(out[:60], want[:60], bound[:60], BF)
+    U.near(out[130:], want[130:], bound[130:], BF)
+    batch.tensors[2].copy_(torch.tensor([500, 2 ** 31 - 1, -5], dtype=torch.int32))
+    out = bd.paged_attention(q.cuda(), cache, batch)
+    U.near(out[:60], want[:60], bound[:60], BF)
+    assert (out[130:] == 0).all()
+    batch.tensors[1].copy_(torch.tensor([0, 60, -3, 2 ** 31 - 1], dtype=torch.int32))
+    bd.paged_attention(q.cuda(), cache, batch)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("D,Hq", [(256, 64), (128, 96)])
+def test_large_calls_of_short_contexts(bd, D, Hq):
+    """Tables of two blocks of keys: a workgroup a unit in the kernel of few rows, no parts."""
+    lens = [(100, 100), (2, 60), (128, 128), (1, 1), (0, 0), (110, 128), (1, 128), (100, 128)]
+    b = U.Batch(lens, 32, D, 16, BF, seed=D, extra=0)
+    b.fill()
+    assert 4 * D * Hq * b.rows * b.width * 16 > 3e9 and b.width <= 8
+    check(bd, b, Hq)
