@@ -429,7 +429,7 @@ def test_wide_bad_device_data_stays_in_bounds(bd):
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("D,Hq", [(256, 64), (128, 96)])
+@pytest.mark.parametrize("D,Hq", [(256, 64), (128, 128)])
 def test_large_calls_of_short_contexts(bd, D, Hq):
     """Tables of two blocks of keys: a workgroup a unit in the kernel of few rows, no parts."""
     lens = [(100, 100), (2, 60), (128, 128), (1, 1), (0, 0), (110, 128), (1, 128), (100, 128)]
