@@ -88,6 +88,13 @@ def parse_args():
                    help="only time the predictor's calibration on the workload's layer")
     p.add_argument("--calib-tokens", type=int, default=8192)
     p.add_argument("--calib-batch", type=int, default=1024)
+    p.add_argument("--attention", type=int, default=0, metavar="KEYS",
+                   help="only time the attention in front of the workload's layer: its batch's "
+                        "new tokens' heads normed and rotated into a paged cache, and attention "
+                        "over KEYS keys a sequence")
+    p.add_argument("--attention-heads", default="32,4,128",
+                   help="query heads, key heads, elements of a head")
+    p.add_argument("--attention-window", type=int, default=0)
     p.add_argument("--working-set-probe", action="store_true",
                    help="only measure the streaming-read rate by working-set size")
     p.add_argument("--copy-probe", action="store_true",
@@ -369,6 +376,72 @@ def bench_calibrate(args, shape, np, torch, W, bd):
     print(json.dumps(out), flush=True)
 
 
+def bench_attention(args, shape, np, torch, bd):
+    """A decode step's attention over a paged cache: one token a sequence of the workload's
+    batch, base_kv_append (norms, rotation, the cache's rows) and base_paged_attention,
+    captured together and replayed; every sequence holds --attention keys, the new one
+    among them, on pages of 16 in random order."""
+    dev = torch.device("cuda", 0)
+    Hq, Hk, D = (int(v) for v in args.attention_heads.split(","))
+    B, keys, ps = shape.B, args.attention, 16
+    dt = torch.bfloat16 if shape.bf16 else torch.float32
+    pages = -(-keys // ps)
+    g = torch.Generator(device=dev)
+    g.manual_seed(7)
+    kc, vc = (torch.randn(B * pages, Hk, ps, D, generator=g, device=dev, dtype=dt).transpose(1, 2)
+              for _ in range(2))
+    table = torch.randperm(B * pages, generator=g, device=dev).int().view(B, pages)
+    cache = bd.KVCache(kc, vc)
+    batch = bd.KVBatch(table, torch.arange(B + 1, dtype=torch.int32, device=dev),
+                       torch.full((B,), keys, dtype=torch.int32, device=dev), 1)
+    gain = [torch.ones(D, device=dev) for _ in range(2)]
+    inv, scale = bd.rope_frequencies(D)
+    rope = bd.Rope(D, dt, inv.to(dev), rot_scale=scale, q_gain=gain[0], k_gain=gain[1])
+    q, k, v = (torch.randn(B, H, D, generator=g, device=dev, dtype=dt) for H in (Hq, Hk, Hk))
+    qr, out = torch.empty_like(q), torch.empty_like(q)
+    ws = torch.empty(bd.attention_workspace_bytes(cache, batch, B, Hq), dtype=torch.uint8, device=dev)
+
+    def append():
+        bd.base_kv_append(rope, cache, batch, q, k, v, qr)
+
+    def attend():
+        bd.base_paged_attention(cache, batch, qr, out, ws, None, args.attention_window)
+
+    hip = hip_runtime()
+    sptr = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    t0, t1 = new_event(hip), new_event(hip)
+
+    def us(calls):
+        graph = torch.cuda.CUDAGraph()
+        for c in calls:
+            c()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            for c in calls:
+                c()
+        for _ in range(args.warmup):
+            graph.replay()
+        torch.cuda.synchronize()
+        hip.hipEventRecord(t0, sptr)
+        for _ in range(args.steps):
+            graph.replay()
+        hip.hipEventRecord(t1, sptr)
+        torch.cuda.synchronize()
+        return elapsed_ms(hip, t0, t1) * 1e3 / args.steps
+
+    step, parts = us((append, attend)), {"append_us": us((append,)), "attention_us": us((attend,))}
+    seen = min(keys, args.attention_window) if args.attention_window else keys
+    n = B * (2 * seen * Hk + 2 * Hq) * D * q.element_size()
+    print(json.dumps({
+        "metric": "attention of a decode step over a paged cache", "value": round(step, 2), "unit": "us",
+        "higher_is_better": False, "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "dtype": "bf16" if shape.bf16 else "fp32", "data": "synthetic",
+        "config": {"batch": B, "keys": keys, "q_heads": Hq, "kv_heads": Hk, "head_dim": D,
+                   "page_size": ps, "window": args.attention_window},
+        **{k: round(t, 2) for k, t in parts.items()},
+        "attention_TB_s": round(n / parts["attention_us"] / 1e6, 2)}), flush=True)
+
+
 def bench_stack(args, shape, np, torch, W, bd):
     """One step = the whole stack of MoE layers (48 Qwen3-shaped layers at
     batch 128, B_e = 24 each), every layer's experts resident and distinct.
@@ -557,6 +630,9 @@ def main():
         args.budget = shape.budgets[0]
     if args.calibrate:
         bench_calibrate(args, shape, np, torch, W, bd)
+        return
+    if args.attention > 0:
+        bench_attention(args, shape, np, torch, bd)
         return
     if shape.layers > 1:
         bench_stack(args, shape, np, torch, W, bd)

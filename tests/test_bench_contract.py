@@ -22,6 +22,24 @@ def test_more_than_one_gpu_is_refused():
         assert r.stdout.strip() == ""        # no JSON line
 
 
+def test_attention_is_an_option_of_one_gpu():
+    bench = os.path.join(ROOT, "bench.py")
+    r = subprocess.run([sys.executable, bench, "--gpus", "2", "--attention", "1024"],
+                       capture_output=True, text=True, timeout=120)
+    assert r.returncode == 2 and "one GPU" in r.stderr and r.stdout.strip() == ""
+    sys.path.insert(0, ROOT)
+    import bench as module
+    old, sys.argv = sys.argv, ["bench.py"]
+    try:
+        args = module.parse_args()
+        assert args.attention == 0 and args.workload == "qwen3_b256"    # the default runs the layer
+        sys.argv = ["bench.py", "--attention", "77", "--attention-heads", "8,2,64"]
+        args = module.parse_args()
+        assert (args.attention, args.attention_heads, args.attention_window) == (77, "8,2,64", 0)
+    finally:
+        sys.argv = old
+
+
 def test_counter_summary_is_well_formed():
     path = os.path.join(ROOT, "profiles", "counters_ffn_gateup_qwen3_b256_be32.md")
     txt = open(path).read()
