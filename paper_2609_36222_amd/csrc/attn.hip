@@ -188,9 +188,10 @@ void k_attn_few(AttnArgs a) {
         to[c][s] = raw[c][s] & keep;
       }
   };
-  // the segment's next step into the stage given
+  // The segment's next step into the stage given.  Rows of it that no token sees are brought
+  // too: 16 keys lie in one page, and in place of a page that is not there another is read.
   auto issue = [&](Seg &z, int stage) {
-    const int i = z.ask++, k0 = key0(i), lo = z.g.keys.lo, hi = z.g.keys.hi;
+    const int i = z.ask++;
     if (i - z.from >= 32) fetch_rows(z, i);
     const uint32_t st = ring_at + stage * M::STAGE;
     const char *kb[2], *vb[2];
@@ -199,33 +200,19 @@ void k_attn_few(AttnArgs a) {
       kb[h] = lane_at(z.at.klo, z.at.khi, 2 * (i - z.from) + h);
       vb[h] = lane_at(z.at.vlo, z.at.vhi, 2 * (i - z.from) + h);
     }
-    if (k0 >= lo && k0 + TK <= hi) {
-      if (a.D == DP) {
+    if (a.D == DP) {
 #pragma unroll
-        for (int j = 0; j < M::CH / 2; ++j) {
-          const int h = WAVE * j / M::CH / 16;
-          glb_to_lds(kb[h], ko[j], st + j * 1024);
-          glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
-        }
-      } else {   // (some lanes of each load have a piece: all are issued, as wait_vm counts)
-#pragma unroll
-        for (int j = 0; j < M::CH / 2; ++j) {
-          const int h = WAVE * j / M::CH / 16;
-          if (kin >> j & 1) glb_to_lds(kb[h], ko[j], st + j * 1024);
-          if (vin >> j & 1) glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
-        }
-      }
-    } else {
-      // a step at the end of what is seen: zeros in the places of what is not there
-#pragma unroll 1
       for (int j = 0; j < M::CH / 2; ++j) {
-        const int row = (lane + WAVE * j) / M::CH, piece = (lane + WAVE * j) % M::CH;
-        const int ck = piece ^ few_k<M::CH>(row), cv = piece ^ few_v<M::CH>(row);
-        const bool h = row >= 16, in = k0 + row >= lo && k0 + row < hi;
-        const char *pk = (h ? kb[1] : kb[0]) + 2 * ((row & 15) * a.c.k_slot + 8 * ck);
-        const char *pv = (h ? vb[1] : vb[0]) + 2 * ((row & 15) * a.c.v_slot + 8 * cv);
-        glb_to_lds(in && 8 * ck < a.D ? pk : zero, st + j * 1024);
-        glb_to_lds(in && 8 * cv < a.D ? pv : zero, st + TK * M::ROWB + j * 1024);
+        const int h = WAVE * j / M::CH / 16;
+        glb_to_lds(kb[h], ko[j], st + j * 1024);
+        glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
+      }
+    } else {   // (some lanes of each load have a piece: all are issued, as wait_vm counts)
+#pragma unroll
+      for (int j = 0; j < M::CH / 2; ++j) {
+        const int h = WAVE * j / M::CH / 16;
+        if (kin >> j & 1) glb_to_lds(kb[h], ko[j], st + j * 1024);
+        if (vin >> j & 1) glb_to_lds(vb[h], vo[j], st + TK * M::ROWB + j * 1024);
       }
     }
   };
@@ -334,7 +321,16 @@ void k_attn_few(AttnArgs a) {
         }
         if (asked - used > 1) wait_vm<M::LOADS>();
         else wait_vm<0>();
-        const char *st = ring + (used++ & 1) * M::STAGE, *sv = st + TK * M::ROWB;
+        char *st = ring + (used++ & 1) * M::STAGE, *sv = st + TK * M::ROWB;
+        // V's rows that no token sees may hold anything: zeros (K's are masked as products)
+        if (k0 < lo || k0 + TK > hi) {
+#pragma unroll
+          for (int j = 0; j < M::CH / 2; ++j) {
+            const int key = k0 + (lane + WAVE * j) / M::CH;
+            if (key < lo || key >= hi) *reinterpret_cast<u32x4 *>(sv + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+          }
+          asm volatile("" ::: "memory");
+        }
         f32x4 s[NR][2];
 #pragma unroll
         for (int c = 0; c < NR; ++c) s[c][0] = s[c][1] = f32x4{0, 0, 0, 0};
@@ -922,8 +918,15 @@ void k_attn_join_both(AttnArgs few, AttnArgs many) {
 // rows, 2.3 GFLOP 45 against 39.5.
 constexpr int FEW_ROWS = 32;
 constexpr double FEW_FLOPS = 3e9;
+// Units go to one workgroup each, with no parts and no join, where splitting them over the
+// workgroups that there are would save few blocks of keys a workgroup: at tiles of 16 rows
+// 6, 4 and 2.5 of heads of 64, 128 and 256 elements (a block takes 0.9, 1.4 and 1.9 us, a
+// join 4 and the parts some), half as many at 32.  Of D 128, in parts and whole: 256 units of
+// four blocks 17.4 and 13.8 us, of eight 22.5 and 19.3; 2048 of two 35.5 and 33.0; 32 of four
+// 11.9 and 12.5, of eight (in parts by this rule) 12.0 and 18.0.
+constexpr long long WHOLE_BLOCKS = 8;
 struct Launch {
-  int R, BK, W, coarse, least;   // W 0: none
+  int R, BK, W, coarse;     // W 0: none
   bool whole;
   size_t part, rec;         // in the workspace, bytes
 };
@@ -936,16 +939,19 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   Plan p{};
   p.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   const long long G = Hq / c.Hk, most = b.max_q * G;
-  auto shape = [&](Launch &l, int R, int BK, int occ, int least, bool may_be_whole) {
+  auto shape = [&](Launch &l, int R, int BK, int occ, double whole) {
     l.R = R;
-    l.least = least;
     l.BK = BK;
     const long long blocks = (((long long)b.max_pages << c.shift) + BK - 1) / BK;
-    const double units = (double)b.n_seq * c.Hk * ((most + R - 1) / R);
-    l.whole = may_be_whole && blocks <= 2;
-    while (units * (double)((blocks >> l.coarse) + 1) > 1e9) ++l.coarse;
-    const double want = l.whole ? (units < 65536 ? units : 65536) : units * blocks;
-    l.W = l.whole || want < occ * n_cu ? (int)want : occ * n_cu;
+    // (whatever the starts on the device say, and where they are sound)
+    const double bound = (double)b.n_seq * c.Hk * ((most + R - 1) / R);
+    double units = ((double)b.n_seq + (double)rows * G / R) * c.Hk;
+    if (bound < units) units = bound;
+    const double slots = (double)occ * n_cu;
+    l.whole = blocks <= WHOLE_BLOCKS && blocks * (units < slots ? 1 - units / slots : 0) <= whole * 16 / R;
+    while (bound * (double)((blocks >> l.coarse) + 1) > 1e9) ++l.coarse;
+    const double want = l.whole ? units : units * blocks;
+    l.W = (int)(want < slots ? want : slots);
     l.part = p.bytes;
     if (!l.whole) p.bytes += 2 * (size_t)l.W * R * (p.dp + 2) * 4;
     l.rec = p.bytes = (p.bytes + 255) & ~(size_t)255;
@@ -958,8 +964,10 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   // (tiles of 16 rows hold a token's heads: beside k_attn_many few sequences have more than
   // one; 17 sequences, one of them of 509 tokens: 56.4 us against 58.9 with tiles of 32)
   if (small || b.n_seq > 1)
-    shape(p.few, p.dp == 256 || most <= 16 || (!small && bf16 && G <= 16) ? 16 : 32, 64, !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1, 1, true);
-  if (!small) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, 6, false);
+    shape(p.few, p.dp == 256 || most <= 16 || (!small && bf16 && G <= 16) ? 16 : 32, 64,
+          !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1,
+          p.dp == 64 ? 6.0 : p.dp == 128 ? 4.0 : 2.5);
+  if (!small) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, -1.0);
   if (p.bytes == 0) p.bytes = 256;
   return p;
 }
@@ -997,7 +1005,6 @@ hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b,
     to.whole = l.whole;
     to.coarse = l.coarse;
     to.by_W = divisor(l.W);
-    to.least = l.least;
     to.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
     to.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);
   };

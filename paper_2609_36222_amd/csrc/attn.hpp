@@ -54,7 +54,7 @@ struct AttnArgs {
   Divisor by_G, by_W;
   float scale;              // of the products, times log2 e
   int above, upto;          // sequences of more than `above` and at most `upto` packed rows
-  int W, least;             // workgroups, and the least length of a stretch
+  int W;                    // workgroups
   int coarse;               // a cost is of 2^coarse blocks
   bool whole;               // every unit costs 1 and is done by one workgroup
   float *part;
@@ -224,7 +224,7 @@ struct AttnWork {
         total += sum;
         from += WAVE;
         if (from < a.b.n_seq) continue;
-        per = max(over(total + a.W - 1, a.by_W), a.least);
+        per = max(over(total + a.W - 1, a.by_W), 1);
         at = min(w * (long long)per, (long long)total);
         end = min(at + per, total);
         if (at >= end) return;
