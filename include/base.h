@@ -401,6 +401,7 @@ typedef struct base_kv_batch {
 } base_kv_batch;
 #define BASE_MAX_SEQ 65536
 #define BASE_KV_MAX_SLOT (1LL << 25)
+#define BASE_MAX_HEAD_ROWS (1LL << 33)   /* rows * Hq of an attention call */
 
 /* The new tokens on their way into the cache: q (Hq heads) to q_out as base_head_rope,
  * k (the cache's Hk heads) the same into the cache, v unchanged beside it.
@@ -426,7 +427,7 @@ base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const bas
  * Keys that no new token of its sequence sees may hold anything.  Rows behind the last
  * sequence are left as they were.  Deterministic run to run.
  *   rows   of q, out and lse: 1 to BASE_HEAD_MAX_ROWS
- *   Hq     a multiple of C->Hk, at most BASE_MAX_HEADS
+ *   Hq     a multiple of C->Hk, at most BASE_MAX_HEADS; rows * Hq at most BASE_MAX_HEAD_ROWS
  *   out    may be q
  *   lse    [rows][Hq] fp32, or NULL
  *   scale  finite;  window >= 0 (0: none)

@@ -804,7 +804,8 @@ static base_status check_attention(const base_kv_cache *C, const base_kv_batch *
   BASE_TRY(check_cache(C, S, pointers));
   if (rows < 1 || rows > BASE_HEAD_MAX_ROWS || Hq < 1 || Hq > BASE_MAX_HEADS || Hq % C->Hk)
     return BASE_ERR_SHAPE;
-  // a sequence's packed rows are counted in 32 bits
+  // a sequence's packed rows are counted in 32 bits, all tiles' key blocks in 30
+  if (rows > BASE_MAX_HEAD_ROWS / Hq) return BASE_ERR_SHAPE;
   return S->max_q > 0x40000000 / (Hq / C->Hk) ? BASE_ERR_SHAPE : BASE_OK;
 }
 

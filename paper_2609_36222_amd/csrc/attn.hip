@@ -936,6 +936,7 @@ constexpr double FEW_FLOPS = 3e9;
 constexpr long long WHOLE_BLOCKS = 8;
 struct Launch {
   int R, BK, W, coarse;     // W 0: none
+  uint32_t limit;           // of the line's length
   bool whole;
   size_t part, rec;         // in the workspace, bytes
 };
@@ -952,13 +953,14 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
     l.R = R;
     l.BK = BK;
     const long long blocks = (((long long)b.max_pages << c.shift) + BK - 1) / BK;
-    // (whatever the starts on the device say, and where they are sound)
+    // (what the rows come to; starts on the device that say more are not followed, see AttnWork)
     const double bound = (double)b.n_seq * c.Hk * ((most + R - 1) / R);
     double units = ((double)b.n_seq + (double)rows * G / R) * c.Hk;
     if (bound < units) units = bound;
     const double slots = (double)occ * n_cu;
     l.whole = blocks <= WHOLE_BLOCKS && blocks * (units < slots ? 1 - units / slots : 0) <= whole * 16 / R;
-    while (bound * (double)((blocks >> l.coarse) + 1) > 1e9) ++l.coarse;
+    while (units * (double)((blocks >> l.coarse) + 1) > 1e9) ++l.coarse;
+    l.limit = (uint32_t)(l.whole ? units : units * (double)((blocks >> l.coarse) + 1)) + 1;
     const double want = l.whole ? units : units * blocks;
     l.W = (int)(want < slots ? want : slots);
     l.part = p.bytes;
@@ -1013,6 +1015,7 @@ hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b,
     to.W = l.W;
     to.whole = l.whole;
     to.coarse = l.coarse;
+    to.limit = l.limit;
     to.by_W = divisor(l.W);
     to.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
     to.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);

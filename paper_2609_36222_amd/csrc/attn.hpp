@@ -56,6 +56,7 @@ struct AttnArgs {
   int above, upto;          // sequences of more than `above` and at most `upto` packed rows
   int W;                    // workgroups
   int coarse;               // a cost is of 2^coarse blocks
+  uint32_t limit;           // the line is no longer
   bool whole;               // every unit costs 1 and is done by one workgroup
   float *part;
   AttnPart *rec;            // [W]
@@ -135,18 +136,21 @@ __device__ __forceinline__ int wave_sum(int v) {
   for (int h = 1; h < WAVE; h *= 2) v += __builtin_amdgcn_ds_bpermute(4 * (lane ^ h), v);
   return v;
 }
-__device__ __forceinline__ int wave_prefix(int v) {   // inclusive
+// inclusive, and 2^32 - 1 where it is more
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
   const int lane = lane_here(lane_id());
 #pragma unroll
   for (int h = 1; h < WAVE; h *= 2) {
-    const int o = __builtin_amdgcn_ds_bpermute(4 * (lane - h), v);
-    if (lane >= h) v += o;
+    const uint32_t o = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane - h), (int)v);
+    if (lane >= h) v = __builtin_elementwise_add_sat(v, o);
   }
   return v;
 }
 
 // The walk of a workgroup over its stretch of the line (costs in units of 2^a.coarse
-// blocks, so that the line's length fits 31 bits).  Lane l holds sequence s0 + l.
+// blocks, so that the line of `rows` rows is shorter than 2^30; starts on the device that
+// fall and rise again can make it longer than rows can, and then nothing is done).  Lane l
+// holds sequence s0 + l.
 template <int R, int BK>
 struct AttnWork {
   const AttnArgs &a;
@@ -210,32 +214,34 @@ struct AttnWork {
   __device__ AttnWork(const AttnArgs &args, int w_) : a(args), w(w_), first(true) {
     // the line's length, then the place of the stretch's begin in it: the second pass needs
     // no loads where one chunk of 64 holds all sequences
-    int total = 0, run = 0, incl = 0;
+    uint32_t total = 0, incl = 0;
+    int run = 0;
     bool placed = false;
-    at = 0;
+    at = end = 0;
     fetch(0);
     for (int from = 0;;) {
       if (!placed || a.b.n_seq > WAVE) {
         load(from);
         incl = wave_prefix(cost * a.c.Hk);
       }
-      const int sum = __builtin_amdgcn_readlane(incl, WAVE - 1);
+      const uint32_t sum = (uint32_t)__builtin_amdgcn_readlane((int)incl, WAVE - 1);
       if (!placed) {
-        total += sum;
+        total = __builtin_elementwise_add_sat(total, sum);
         from += WAVE;
         if (from < a.b.n_seq) continue;
-        per = max(over(total + a.W - 1, a.by_W), 1);
+        if (total > a.limit) return;
+        per = max(over((int)total + a.W - 1, a.by_W), 1);
         at = min(w * (long long)per, (long long)total);
-        end = min(at + per, total);
+        end = min(at + per, (int)total);
         if (at >= end) return;
         placed = true;
         from = 0;
         if (a.b.n_seq > WAVE) continue;
       }
-      const unsigned long long hit = __ballot(run + incl > at);
+      const unsigned long long hit = __ballot(run + (int)incl > at);
       if (hit) {
         const int l = __ffsll(hit) - 1, head = __builtin_amdgcn_readlane(cost, l);
-        left = at - run - __builtin_amdgcn_readlane(incl, l) + head * a.c.Hk;
+        left = at - run - __builtin_amdgcn_readlane((int)incl, l) + head * a.c.Hk;
         const int rest = left;
         enter(from + l);
         hk = quotient(rest, head);
@@ -247,7 +253,7 @@ struct AttnWork {
     }
     // the tile with that place, 64 tiles at a time
     for (int j0 = 0; tiles > 1; j0 += WAVE) {
-      const int c = j0 + lane_id() < tiles ? tile_cost(q, j0 + lane_id()) : 0, upto = wave_prefix(c);
+      const int c = j0 + lane_id() < tiles ? tile_cost(q, j0 + lane_id()) : 0, upto = (int)wave_prefix(c);
       const unsigned long long in = __ballot(upto > left);
       if (in) {
         const int m = __ffsll(in) - 1;

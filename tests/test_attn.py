@@ -122,6 +122,7 @@ def test_attention_arguments(lib):
     for Hq in (0, 3, 30, 1028):
         assert attend(lib, Hq=Hq) == SHAPE
     assert attend(lib, S=batch(max_q=1 << 30)) == SHAPE            # packed rows past 32 bits
+    assert attend(lib, rows=(1 << 28) + 1) == SHAPE                # rows * Hq past 2^33
     assert attend(lib, scale=NAN) == SHAPE and attend(lib, scale=INF) == SHAPE and attend(lib, window=-1) == SHAPE
     for f in ("q", "out"):
         assert attend(lib, **{f: heads(0)}) == NULL and attend(lib, **{f: heads(FAKE + 1)}) == ALIGN
@@ -137,6 +138,9 @@ def test_workspace(lib, kw):
         n = lib.base_attention_workspace_bytes(ref(C), ref(S), 4, 32)
         assert n > 0 and n % 256 == 0 and n < 2 << 30
         assert attend(lib, C, S, n=n - 1) == WS
+    # a max_q far beyond what the rows can hold, at the largest batches
+    S = batch(max_q=1 << 26, max_pages=1 << 20, table_ld=1 << 20, n_seq=65536)
+    assert 0 < lib.base_attention_workspace_bytes(ref(C), ref(S), 1 << 27, 32) < 2 << 30
     assert lib.base_attention_workspace_bytes(ref(cache(D=4)), ref(batch()), 4, 32) == 0
     assert lib.base_attention_workspace_bytes(ref(cache()), ref(batch()), 0, 32) == 0
     assert lib.base_attention_workspace_bytes(None, None, 4, 32) == 0

@@ -437,3 +437,23 @@ def test_large_calls_of_short_contexts(bd, D, Hq):
     b.fill()
     assert 4 * D * Hq * b.rows * b.width * 16 > 3e9 and b.width <= 8
     check(bd, b, Hq)
+
+
+def test_starts_that_fall_and_rise(bd):
+    """Starts that make more work than the rows can be: the call ends (what it writes is
+    nobody's), the next one with sound starts is right."""
+    lens = [(40, 60)] * 70
+    for b in (U.Batch(lens, 1, 64, 16, BF, seed=8, fill=0.0), wide(lens, 1, 64, 16, 4, seed=8, fill=0.0)):
+        b.fill()
+        q = b.queries(4)
+        cache, batch = b.device(bd, max_q=b.rows)
+        sound = batch.tensors[1].clone()
+        bad = torch.zeros_like(sound)
+        bad[1::2] = b.rows
+        batch.tensors[1].copy_(bad)
+        bd.paged_attention(q.cuda(), cache, batch)
+        torch.cuda.synchronize()
+        batch.tensors[1].copy_(sound)
+        out = bd.paged_attention(q.cuda(), cache, batch)
+        want, bound, *_ = U.attend(b, q, 0.125)
+        U.near(out, want, bound, BF)
