@@ -423,7 +423,8 @@ base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const bas
  *   out = sum_j e^(scale q.k_j - m) v_j / sum_j e^(scale q.k_j - m),  m the maximum,
  *   lse = m + log sum_j e^(scale q.k_j - m);
  * a token that sees no key gets zeros and -infinity.  Products' sums, maxima and sums in
- * fp32; with 16-bit heads the exponentials are rounded to bf16 for the product with v.
+ * fp32; with 16-bit heads the exponentials go into the product with v as bf16, in two
+ * parts (value and rest) in the kernel of few rows.
  * Keys that no new token of its sequence sees may hold anything.  Rows behind the last
  * sequence are left as they were.  Deterministic run to run.
  *   rows   of q, out and lse: 1 to BASE_HEAD_MAX_ROWS
