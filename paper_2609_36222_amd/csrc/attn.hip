@@ -934,8 +934,15 @@ constexpr double FEW_FLOPS = 3e9;
 // four blocks 17.4 and 13.8 us, of eight 22.5 and 19.3; 2048 of two 35.5 and 33.0; 32 of four
 // 11.9 and 12.5, of eight (in parts by this rule) 12.0 and 18.0.
 constexpr long long WHOLE_BLOCKS = 8;
+// What a unit costs besides its blocks (queries, the ring's filling, the state's way out), in
+// blocks, so that a workgroup with ends of three units has fewer blocks.  Without, and with
+// these: 64 sequences of up to 8192 keys 63.1 and 56.8 us, 128 of up to 600 36.9 and 28.1,
+// 200 of up to 1000 with heads of 256 153 and 97; chunks of 2048 tokens (32 heads on 8)
+// 101 and 63.5, of 1000 54.2 and 39.5, of 2048 over 8191 keys 240 and 238.  Half and twice
+// as much are within 5% of it, mostly slower.
+constexpr int FEW_PAD = 2, MANY_PAD = 4;
 struct Launch {
-  int R, BK, W, coarse;     // W 0: none
+  int R, BK, W, coarse, pad;   // W 0: none
   uint32_t limit;           // of the line's length
   bool whole;
   size_t part, rec;         // in the workspace, bytes
@@ -949,7 +956,7 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   Plan p{};
   p.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   const long long G = Hq / c.Hk, most = b.max_q * G;
-  auto shape = [&](Launch &l, int R, int BK, int occ, double whole) {
+  auto shape = [&](Launch &l, int R, int BK, int occ, int pad, double whole) {
     l.R = R;
     l.BK = BK;
     const long long blocks = (((long long)b.max_pages << c.shift) + BK - 1) / BK;
@@ -959,9 +966,11 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
     if (bound < units) units = bound;
     const double slots = (double)occ * n_cu;
     l.whole = blocks <= WHOLE_BLOCKS && blocks * (units < slots ? 1 - units / slots : 0) <= whole * 16 / R;
-    while (units * (double)((blocks >> l.coarse) + 1) > 1e9) ++l.coarse;
-    l.limit = (uint32_t)(l.whole ? units : units * (double)((blocks >> l.coarse) + 1)) + 1;
-    const double want = l.whole ? units : units * blocks;
+    const auto length = [&] { return units * (double)((blocks >> l.coarse) + 1 + (pad >> l.coarse)); };
+    while (length() > 1e9) ++l.coarse;
+    l.pad = l.whole ? 0 : pad >> l.coarse;
+    l.limit = (uint32_t)(l.whole ? units : length()) + 1;
+    const double want = l.whole ? units : units * (blocks + pad);
     l.W = (int)(want < slots ? want : slots);
     l.part = p.bytes;
     if (!l.whole) p.bytes += 2 * (size_t)l.W * R * (p.dp + 2) * 4;
@@ -976,9 +985,9 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   // one; 17 sequences, one of them of 509 tokens: 56.4 us against 58.9 with tiles of 32)
   if (small || b.n_seq > 1)
     shape(p.few, p.dp == 256 || most <= 16 || (!small && bf16 && G <= 16) ? 16 : 32, 64,
-          !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1,
+          !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1, FEW_PAD,
           p.dp == 64 ? 6.0 : p.dp == 128 ? 4.0 : 2.5);
-  if (!small) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, -1.0);
+  if (!small) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, MANY_PAD, -1.0);
   if (p.bytes == 0) p.bytes = 256;
   return p;
 }
@@ -1016,6 +1025,7 @@ hipError_t launch_attn(const AttnCall &call, const KvCache &c, const KvBatch &b,
     to.whole = l.whole;
     to.coarse = l.coarse;
     to.limit = l.limit;
+    to.pad = l.pad;
     to.by_W = divisor(l.W);
     to.part = reinterpret_cast<float *>(static_cast<char *>(ws) + l.part);
     to.rec = reinterpret_cast<AttnPart *>(static_cast<char *>(ws) + l.rec);

@@ -10,7 +10,8 @@ namespace basek {
 // A unit is a tile of R packed rows of one sequence and key head: packed row r is the
 // query head hk G + r % G of the sequence's new token r / G, so that the G query heads
 // that share a key head go through the matrix instructions together.  Its cost is the
-// number of blocks of BK keys its rows see (at least 1).  All units in the order
+// number of blocks of BK keys its rows see (at least 1) and a pad in front of them, for
+// what a change of units costs.  All units in the order
 // (sequence, key head, tile) form one line of N blocks, and workgroup w of W takes the
 // stretch [w per, (w + 1) per), whatever the lengths are: a unit that lies in several
 // stretches is left in parts (the running maximum, the sum and the unnormalised output)
@@ -57,6 +58,7 @@ struct AttnArgs {
   int W;                    // workgroups
   int coarse;               // a cost is of 2^coarse blocks
   uint32_t limit;           // the line is no longer
+  int pad;                  // what a unit costs besides its blocks
   bool whole;               // every unit costs 1 and is done by one workgroup
   float *part;
   AttnPart *rec;            // [W]
@@ -167,7 +169,7 @@ struct AttnWork {
     if (a.whole) return 1;
     const KeyRange k = attn_keys(a, sq, j * R, min(R, sq.packed - j * R));
     const int c = ((k.hi + BK - 1) / BK - k.lo / BK + (1 << a.coarse) - 1) >> a.coarse;
-    return c > 1 ? c : 1;
+    return a.pad + (c > 1 ? c : 1);
   }
   __device__ AttnSeq lane_seq(int l) const {
     return attn_seq(a, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(stop, l),
@@ -294,6 +296,12 @@ struct AttnWork {
       enter(s0 + __ffsll(more) - 1);
     }
     const int c = tile_cost(q, j);
+    if (left < a.pad) {   // the unit's blocks begin behind its pad, if in this stretch at all
+      const int skip = min(a.pad - left, end - at);
+      at += skip;
+      left += skip;
+      if (at >= end) return false;
+    }
     g.s = s;
     g.q = q;
     g.hk = hk;
@@ -301,12 +309,12 @@ struct AttnWork {
     g.n = min(R, q.packed - g.r0);
     g.keys = attn_keys(a, q, g.r0, g.n);
     const int take = min(c - left, end - at), b0 = g.keys.lo / BK, b1 = (g.keys.hi + BK - 1) / BK;
-    g.k0 = a.whole ? b0 : b0 + (left << a.coarse);
-    g.k1 = take == c - left ? b1 : b0 + ((left + take) << a.coarse);
-    g.slot = take < c ? 2 * w + (first ? 0 : 1) : -1;
+    g.k0 = a.whole ? b0 : b0 + ((left - a.pad) << a.coarse);
+    g.k1 = take == c - left ? b1 : b0 + ((left - a.pad + take) << a.coarse);
+    g.slot = take < c - a.pad ? 2 * w + (first ? 0 : 1) : -1;
     if (left + take < c) {   // the unit goes on in the next workgroup
-      const int from = at - left, w0 = quotient(from, per);
-      begun = {q.first, hk * a.G, g.r0, g.n, 2 * w0 + (from == w0 * per ? 0 : 1),
+      const int from = at - left, w0 = quotient(from + a.pad, per);
+      begun = {q.first, hk * a.G, g.r0, g.n, 2 * w0 + (from <= w0 * per ? 0 : 1),
                quotient(from + c - 1, per) - w0 + 1, w0, 0};
     }
     first = false;
