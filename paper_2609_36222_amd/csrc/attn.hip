@@ -920,19 +920,21 @@ void k_attn_join_both(AttnArgs few, AttnArgs many) {
 // longer ones (16-bit) k_attn_many's; where there may be both, both run, on parts of the
 // workspace of their own, and one launch joins the units of both.  Calls whose products
 // come to at most FEW_FLOPS are k_attn_few's alone, however long their sequences are: a
-// unit of k_attn_many takes 9 us (its rows go through eight wavefronts' ring), and each
-// launch about 4.  Measured at D 128, 96 or 64, k_attn_few alone against both: 0.15 GFLOP
-// 15.9 against 36.7 us, 0.02 GFLOP 13.4 against 38.1, 2.1 GFLOP 26.7 against 28.8, 2.9
-// GFLOP 29.8 against 33.6; 6.5 GFLOP 69.8 against 62.5; at D 256, where its tiles are of 16
-// rows, 2.3 GFLOP 45 against 39.5.
+// unit of k_attn_many takes 9 us before its first block (its rows go through eight
+// wavefronts' ring), and each launch about 4.  Measured, k_attn_few alone against
+// k_attn_many or both, by what the products can come to: one sequence 1.6 GFLOP 23.4 against
+// 25.8 us, 2.2 28.8 against 23.8; several 0.2 GFLOP 16.3 against 32.3, 1.4 23.7 against 34.6,
+// 3.1 26.9 against 27.9, 10 67 against 45.6; at D 256, where its tiles are of 16 rows, one of
+// 1.0 21.5 against 25.3, of 2.1 34.5 against 28.3.
 constexpr int FEW_ROWS = 32;
-constexpr double FEW_FLOPS = 3e9;
+constexpr double FEW_FLOPS = 3e9, FEW_FLOPS_ONE = 2e9, FEW_FLOPS_256 = 1e9;
 // Units go to one workgroup each, with no parts and no join, where splitting them over the
 // workgroups that there are would save few blocks of keys a workgroup: at tiles of 16 rows
 // 6, 4 and 2.5 of heads of 64, 128 and 256 elements (a block takes 0.9, 1.4 and 1.9 us, a
 // join 4 and the parts some), half as many at 32.  Of D 128, in parts and whole: 256 units of
-// four blocks 17.4 and 13.8 us, of eight 22.5 and 19.3; 2048 of two 35.5 and 33.0; 32 of four
-// 11.9 and 12.5, of eight (in parts by this rule) 12.0 and 18.0.
+// four blocks 18.6 and 13.9 us, of eight 22.9 and 19.3; 2048 of two 36.8 and 34.2; 32 of four
+// 11.5 and 12.2, of eight (in parts by this rule) 12.4 and 17.7.  More units than workgroups
+// only up to two blocks: 2048 of up to six (ragged) 38.8 and 53.
 constexpr long long WHOLE_BLOCKS = 8;
 // What a unit costs besides its blocks (queries, the ring's filling, the state's way out), in
 // blocks, so that a workgroup with ends of three units has fewer blocks.  Without, and with
@@ -965,7 +967,8 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
     double units = ((double)b.n_seq + (double)rows * G / R) * c.Hk;
     if (bound < units) units = bound;
     const double slots = (double)occ * n_cu;
-    l.whole = blocks <= WHOLE_BLOCKS && blocks * (units < slots ? 1 - units / slots : 0) <= whole * 16 / R;
+    l.whole = units <= slots ? blocks <= WHOLE_BLOCKS && blocks * (1 - units / slots) <= whole * 16 / R
+                             : whole > 0 && blocks <= 2;
     const auto length = [&] { return units * (double)((blocks >> l.coarse) + 1 + (pad >> l.coarse)); };
     while (length() > 1e9) ++l.coarse;
     l.pad = l.whole ? 0 : pad >> l.coarse;
@@ -980,7 +983,7 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   // (the lengths are on the device: this is the most that the products can come to)
   const double keys = (double)((long long)b.max_pages << c.shift), span = window > 0 ? window + b.max_q : keys;
   const double flops = 4.0 * p.dp * Hq * rows * (span < keys ? span : keys);
-  const bool small = !bf16 || most <= FEW_ROWS || flops <= (p.dp == 256 ? FEW_FLOPS / 3 : FEW_FLOPS);
+  const bool small = !bf16 || most <= FEW_ROWS || flops <= (p.dp == 256 ? FEW_FLOPS_256 : b.n_seq == 1 ? FEW_FLOPS_ONE : FEW_FLOPS);
   // (tiles of 16 rows hold a token's heads: beside k_attn_many few sequences have more than
   // one; 17 sequences, one of them of 509 tokens: 56.4 us against 58.9 with tiles of 32)
   if (small || b.n_seq > 1)
