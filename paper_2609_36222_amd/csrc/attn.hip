@@ -88,6 +88,12 @@ __device__ __forceinline__ void put4(float *p, f32x4 v) { reinterpret_cast<Any16
 // accumulators are rescaled only when the maximum has risen by more
 constexpr float LAG = 8.0f;
 
+// Workgroups a CU of k_attn_few.  16-bit: what its LDS holds.  fp32: with 16 rows of 128
+// elements two have registers (10 sequences of 21974 keys 273 us, one workgroup 361); with 32
+// rows they would spill, and short calls lose (64 tokens of 2048 keys 37.5 us against 32.3)
+constexpr int few_occ(bool bf, int dp, int nr) {
+  return bf ? (dp == 64 ? 4 : dp == 128 ? 2 : 1) : dp * nr <= 128 ? 2 : 1;
+}
 template <typename T, int DP_, int NR_>
 struct FewShape {
   static constexpr bool BF = sizeof(T) == 2;
@@ -98,7 +104,7 @@ struct FewShape {
   static constexpr int ROWB = DP * 2, STAGE = 2 * TK * ROWB, RING = 2, LOADS = CH;
   static constexpr int STATE = DP * 64 + 512;              // 16 rows of a wavefront's state
   static constexpr int AREA = (WAVES - 1) * STATE, LDS = (BF ? WAVES * RING * STAGE : 0) + AREA;
-  static constexpr int OCC = BF ? (DP == 64 ? 4 : DP == 128 ? 2 : 1) : DP == 64 ? 2 : 1;   // workgroups a CU
+  static constexpr int OCC = few_occ(BF, DP, NR);
   static constexpr int WPE = OCC * WAVES >= 4 ? OCC * WAVES / 4 : 1;
   static_assert(OCC * LDS <= 160 * 1024, "LDS of a CU");
 };
@@ -986,10 +992,10 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
   const bool small = !bf16 || most <= FEW_ROWS || flops <= (p.dp == 256 ? FEW_FLOPS_256 : b.n_seq == 1 ? FEW_FLOPS_ONE : FEW_FLOPS);
   // (tiles of 16 rows hold a token's heads: beside k_attn_many few sequences have more than
   // one; 17 sequences, one of them of 509 tokens: 56.4 us against 58.9 with tiles of 32)
-  if (small || b.n_seq > 1)
-    shape(p.few, p.dp == 256 || most <= 16 || (!small && bf16 && G <= 16) ? 16 : 32, 64,
-          !bf16 ? (p.dp == 64 ? 2 : 1) : p.dp == 64 ? 4 : p.dp == 128 ? 2 : 1, FEW_PAD,
-          p.dp == 64 ? 6.0 : p.dp == 128 ? 4.0 : 2.5);
+  if (small || b.n_seq > 1) {
+    const int R = p.dp == 256 || most <= 16 || (!small && bf16 && G <= 16) ? 16 : 32;
+    shape(p.few, R, 64, few_occ(bf16, p.dp, R / 16), FEW_PAD, p.dp == 64 ? 6.0 : p.dp == 128 ? 4.0 : 2.5);
+  }
   if (!small) shape(p.many, p.dp == 256 ? 128 : 256, p.dp == 256 ? 32 : 64, 1, MANY_PAD, -1.0);
   if (p.bytes == 0) p.bytes = 256;
   return p;
