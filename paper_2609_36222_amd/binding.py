@@ -673,20 +673,31 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, fast=32.0, slo
 def _heads(t, what, dtype, dev, n, H, D):
     """(pointer, row stride, head stride) of a tensor [n, H, D] with adjacent elements in a
     head."""
-    try:
-        rows, heads, size = t.shape
+    if t.shape == (n, H, D):
         row, head, one = t.stride()
+        if one == 1 and t.dtype is dtype and t.get_device() == dev:
+            # (a single row or head has no stride to speak of)
+            return t.data_ptr(), row if n > 1 else 0, head if H > 1 else 0
+    raise ValueError(f"{what}: {dtype} {[n, H, D]}, adjacent elements in a head, on the current GPU")
+
+
+def _rows_heads(t, what):
+    """Rows and heads of a tensor [n, H, D]."""
+    try:
+        n, H, _ = t.shape
     except ValueError:
-        rows = -1
-    if rows != n or heads != H or size != D or one != 1 or t.dtype is not dtype or t.get_device() != dev:
-        raise ValueError(f"{what}: {dtype} {[n, H, D]}, adjacent elements in a head, on the current GPU")
-    # (a single row or head has no stride to speak of)
-    return t.data_ptr(), row if n > 1 else 0, head if H > 1 else 0
+        raise ValueError(f"{what}: [rows, heads, D]") from None
+    return n, H
 
 
-def _stream_on(stream, dev):
-    """_stream, where the current device is known."""
+def _here():
+    """(the library, torch, the current GPU): what a call on heads looks up once."""
     import torch
+    return load(), torch, torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+
+
+def _stream_on(torch, stream, dev):
+    """_stream, where the current device is known."""
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
@@ -771,23 +782,24 @@ def base_head_rope(rope: Rope, positions, q, k, q_out, k_out, stream=None):
     [rows] (None where nothing rotates)."""
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q and q_out, k and k_out: both or neither, and one of the two")
-    dev, dt, D = _device(), rope.torch_dtype, rope.D
+    lib, torch, dev = _here()
+    dt, D = rope.torch_dtype, rope.D
     qa = ka = _NO_HEADS
     n = None
     if q is not None:
-        n, H = q.size(0), q.size(1)
+        n, H = _rows_heads(q, "q")
         qa = (H, *_heads(q, "q", dt, dev, n, H, D), *_heads(q_out, "q_out", dt, dev, n, H, D))
     if k is not None:
-        n, H = k.size(0) if n is None else n, k.size(1)
+        rows, H = _rows_heads(k, "k")
+        n = rows if n is None else n
         ka = (H, *_heads(k, "k", dt, dev, n, H, D), *_heads(k_out, "k_out", dt, dev, n, H, D))
     if positions is not None:
-        positions = _positions(positions, n, dev)
-    _check(load().base_head_rope(rope.desc, n, positions, *qa, *ka, _stream_on(stream, dev)))
+        positions = _positions(torch, positions, n, dev)
+    _check(lib.base_head_rope(rope.desc, n, positions, *qa, *ka, _stream_on(torch, stream, dev)))
 
 
-def _positions(t, n, dev):
-    import torch
-    if t.dtype is not torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+def _positions(torch, t, n, dev):
+    if t.dtype is not torch.int32 or t.shape != (n,) or (t.stride(0) != 1 and n > 1) or t.get_device() != dev:
         raise ValueError(f"positions: int32, {n} adjacent elements, on the current GPU")
     return t.data_ptr()
 
@@ -803,15 +815,15 @@ def base_kv_append(rope: Rope, cache: KVCache, batch: KVBatch, q, k, v, q_out, p
     """The new tokens' k [rows, Hk, D], normalised and rotated, and v into the cache; q
     [rows, Hq, D] the same to q_out.  positions: int32 [rows], or None: the tokens' numbers
     in their sequences."""
-    dev, dt = _device(), rope.torch_dtype
-    D, Hk = rope.D, cache.Hk
-    n, Hq = q.size(0), q.size(1)
+    lib, torch, dev = _here()
+    dt, D, Hk = rope.torch_dtype, rope.D, cache.Hk
+    n, Hq = _rows_heads(q, "q")
     if positions is not None:
-        positions = _positions(positions, n, dev)
-    _check(load().base_kv_append(
+        positions = _positions(torch, positions, n, dev)
+    _check(lib.base_kv_append(
         rope.desc, cache.desc, batch.desc, n, positions, Hq, *_heads(q, "q", dt, dev, n, Hq, D),
         *_heads(q_out, "q_out", dt, dev, n, Hq, D), *_heads(k, "k", dt, dev, n, Hk, D),
-        *_heads(v, "v", dt, dev, n, Hk, D), _stream_on(stream, dev)))
+        *_heads(v, "v", dt, dev, n, Hk, D), _stream_on(torch, stream, dev)))
 
 
 def attention_workspace_bytes(cache: KVCache, batch: KVBatch, rows, Hq) -> int:
@@ -825,20 +837,19 @@ def base_paged_attention(cache: KVCache, batch: KVBatch, q, out, ws, scale=None,
                          stream=None):
     """out [rows, Hq, D] (and lse [rows, Hq] fp32) of q over the cache; scale None: 1 /
     sqrt(D); ws: a uint8 tensor of attention_workspace_bytes."""
-    dev, dt = _device(), cache.torch_dtype
-    D = cache.D
-    n, Hq = q.size(0), q.size(1)
+    lib, torch, dev = _here()
+    dt, D = cache.torch_dtype, cache.D
+    n, Hq = _rows_heads(q, "q")
     if lse is not None:
-        import torch
         if (lse.dtype is not torch.float32 or lse.shape != (n, Hq) or not lse.is_contiguous()
                 or lse.get_device() != dev):
             raise ValueError(f"lse: contiguous fp32 {[n, Hq]} on the current GPU")
         lse = lse.data_ptr()
     if ws.get_device() != dev or not ws.is_contiguous():
         raise ValueError("ws: contiguous, on the current GPU")
-    _check(load().base_paged_attention(
+    _check(lib.base_paged_attention(
         cache.desc, batch.desc, n, Hq, *_heads(q, "q", dt, dev, n, Hq, D), *_heads(out, "out", dt, dev, n, Hq, D),
-        lse, D ** -0.5 if scale is None else scale, window, ws.data_ptr(), ws.nbytes, _stream_on(stream, dev)))
+        lse, D ** -0.5 if scale is None else scale, window, ws.data_ptr(), ws.nbytes, _stream_on(torch, stream, dev)))
 
 
 def paged_attention(q, cache: KVCache, batch: KVBatch, scale=None, window=0, return_lse=False, stream=None):
