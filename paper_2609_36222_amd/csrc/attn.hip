@@ -90,7 +90,8 @@ constexpr float LAG = 8.0f;
 
 // Workgroups a CU of k_attn_few.  16-bit: what its LDS holds.  fp32: with 16 rows of 128
 // elements two have registers (10 sequences of 21974 keys 273 us, one workgroup 361); with 32
-// rows they would spill, and short calls lose (64 tokens of 2048 keys 37.5 us against 32.3)
+// rows short calls lose by the parts of twice the workgroups (64 tokens of 2048 keys 35.7 us
+// against 29.9, 300 of 1000 36.2 against 30.8; 13 of 21974, 28 heads on 7, 602 against 672)
 constexpr int few_occ(bool bf, int dp, int nr) {
   return bf ? (dp == 64 ? 4 : dp == 128 ? 2 : 1) : dp * nr <= 128 ? 2 : 1;
 }
@@ -399,15 +400,19 @@ void k_attn_few(AttnArgs a) {
           const int d = 16 * q + 4 * g;
           kv[q] = *reinterpret_cast<const f32x4 *>(kin && d < D ? kb + n * a.c.k_slot + d : zf);
         }
-        float vv[4][DT];
+        // (Which elements the tiles have is free: a lane's of four tiles adjoin, one load for
+        // four.  64 sequences of 1000 keys, heads of 256: 240 us with a load each, 195.)
+        f32x4 vv[4][DT / 4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = k0 + 4 * g + e;
           const bool vin = key >= lo && key < hi;
 #pragma unroll
-          for (int t = 0; t < DT; ++t)
-            vv[e][t] = *(vin && 16 * t + n < D ? vb + (4 * g + e) * a.c.v_slot + 16 * t + n : zf);
+          for (int j = 0; j < DT / 4; ++j)
+            vv[e][j] = *reinterpret_cast<const f32x4 *>(
+                vin && 64 * j + 4 * n < D ? vb + (4 * g + e) * a.c.v_slot + 64 * j + 4 * n : zf);
         }
+        __builtin_amdgcn_sched_barrier(0);   // (left to itself the compiler moves them behind the first product)
 #pragma unroll
         for (int c = 0; c < NR; ++c) {
           if (c >= nr) continue;
@@ -423,11 +428,17 @@ void k_attn_few(AttnArgs a) {
           for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int t = 0; t < DT; ++t)
-              acc[c][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[e][t], x[e], acc[c][t], 0, 0, 0);
+              acc[c][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[e][t / 4][t % 4], x[e], acc[c][t], 0, 0, 0);
         }
       }
     }
 
+    // four adjoining elements of the lane's row: 16-bit a tile's, fp32 one of each of four tiles
+    auto piece = [&](int c, int t) {
+      if constexpr (BF) return acc[c][t];
+      const int j = t / 4 * 4, e = t % 4;
+      return f32x4{acc[c][j][e], acc[c][j + 1][e], acc[c][j + 2][e], acc[c][j + 3][e]};
+    };
     // the wavefronts' states, added to the first one's in their order, 16 rows at a time
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
@@ -469,7 +480,7 @@ void k_attn_few(AttnArgs a) {
       if (sg.slot >= 0) {
         float *part = a.part + sg.slot * attn_part_floats<R, DP>();
 #pragma unroll
-        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(part + ((c * DT + t) * WAVE + lane) * 4) = acc[c][t];
+        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(part + ((c * DT + t) * WAVE + lane) * 4) = piece(c, t);
         if (g == 0) {
           part[R * DP + r] = top;
           part[R * DP + R + r] = sum;
@@ -480,8 +491,10 @@ void k_attn_few(AttnArgs a) {
         const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
         T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-          if (16 * t + 4 * g < D) put4(out + 16 * t + 4 * g, acc[c][t] * inv);
+        for (int t = 0; t < DT; ++t) {
+          const int at = attn_at<T, 16, DP>(t, lane);
+          if (at < D) put4(out + at, piece(c, t) * inv);
+        }
         if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
       }
     }
@@ -793,7 +806,7 @@ template <typename T, int ROWS, int DP>
 __device__ __forceinline__ void join_store(const AttnArgs &a, const AttnPart &p, int r, int q, float top,
                                            float sum, f32x4 o) {
   if (r >= p.n) return;
-  const int pr = p.r0 + r, tok = over(pr, a.by_G), head = p.head + pr - tok * a.G, at = attn_at<ROWS, DP>(q, lane_id());
+  const int pr = p.r0 + r, tok = over(pr, a.by_G), head = p.head + pr - tok * a.G, at = attn_at<T, ROWS, DP>(q, lane_id());
   const long long row = p.token + tok;
   const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
   if (at < a.D) put4((T *)a.o.p + row * a.o.row + head * a.o.head + at, o * inv);

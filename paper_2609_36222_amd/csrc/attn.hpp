@@ -325,13 +325,14 @@ struct AttnWork {
   }
 };
 
-// A part: pieces of 64 lanes times four floats as the accumulators lie, ROWS rows' (32 in
-// k_attn_many, 16 in k_attn_few) after another's, R DP floats in all; then R maxima (of the
-// products times scale log2 e) and R sums.  Piece q of lane l holds row ROWS (q / per) + l %
-// ROWS, per = ROWS DP / 256, and four elements from attn_at on.
-template <int ROWS, int DP>
+// A part: pieces of 64 lanes times four adjoining elements as the accumulators lie, ROWS rows'
+// (32 in k_attn_many, 16 in k_attn_few) after another's, R DP floats in all; then R maxima (of
+// the products times scale log2 e) and R sums.  Piece q of lane l holds row ROWS (q / per) + l
+// % ROWS, per = ROWS DP / 256, and four elements from attn_at on.
+template <typename T, int ROWS, int DP>
 __device__ __forceinline__ int attn_at(int q, int lane) {
   const int in = q % (ROWS * DP / 256);
+  if (sizeof(T) == 4) return 64 * (in / 4) + 16 * (lane / 16) + 4 * (in % 4);
   return ROWS == 32 ? 8 * in + 4 * (lane / 32) : 16 * in + 4 * (lane / 16);
 }
 template <int R, int DP>
