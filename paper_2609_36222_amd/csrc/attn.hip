@@ -26,29 +26,9 @@ namespace {
 // 16 bytes of zeros: what a lane reads in the place of a key or element that is not there
 __device__ __attribute__((aligned(16))) uint32_t g_zero[4];
 
-typedef __attribute__((address_space(3))) void *lds_p;
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) bf16x4 *lds_b4;
 
-// 16 bytes per lane from global memory to LDS, lane l's at lds + 16 l (lds uniform).  The
-// compiler's builtin makes every transposed read wait for all such loads, those of the
-// steps ahead among them; here the reader waits for its own (wait_vm).  No register is
-// written; a wait of the compiler's for a load of its own is only the longer for these.
-// (m0 holds nothing that the compiler keeps: it sets it in front of each use.)
-__device__ __forceinline__ uint32_t lds_addr(const void *p) {
-  return (uint32_t)(uintptr_t)(lds_p)p;
-}
-__device__ __forceinline__ void glb_to_lds(const char *p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
-               "s"(__builtin_amdgcn_readfirstlane(lds))
-               : "memory");
-}
-// the same from a uniform address and a lane's offset
-__device__ __forceinline__ void glb_to_lds(const char *base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
-               "s"(__builtin_amdgcn_readfirstlane(lds))
-               : "memory");
-}
 // The addresses of K's and V's rows from a token on (16-bit), one token a lane: made for many
 // steps at once, and read lane by lane (in scalar registers their 64-bit products took 1100
 // of a block's 6000 cycles in k_attn_many).  A page that is not in the cache is read as its
@@ -61,10 +41,6 @@ __device__ __forceinline__ RowAt row_at(const AttnArgs &a, int s, int hk, int ke
   const uint64_t k = (uint64_t)a.c.k + 2 * (page * a.c.k_page + slot * a.c.k_slot + hk * a.c.k_head);
   const uint64_t v = (uint64_t)a.c.v + 2 * (page * a.c.v_page + slot * a.c.v_slot + hk * a.c.v_head);
   return {(uint32_t)k, (uint32_t)(k >> 32), (uint32_t)v, (uint32_t)(v >> 32)};
-}
-__device__ __forceinline__ const char *lane_at(uint32_t lo, uint32_t hi, int l) {
-  return (const char *)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, l) << 32) |
-                        (uint32_t)__builtin_amdgcn_readlane((int)lo, l));
 }
 // Four 16-bit elements a lane, transposed in groups of 16 lanes: lane 4 r + c gives the
 // address of elements 4 c .. + 3 of row r, and lane i gets element i of the rows 0 .. 3
