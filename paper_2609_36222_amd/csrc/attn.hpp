@@ -350,14 +350,13 @@ typedef __attribute__((address_space(3))) void *lds_p;
 // compiler's builtin makes every transposed read wait for all such loads, those of the
 // steps ahead among them; here the reader waits for its own (wait_vm).  No register is
 // written; a wait of the compiler's for a load of its own is only the longer for these.
-// (m0 holds nothing that the compiler keeps: it sets it in front of each use.)
 __device__ __forceinline__ uint32_t lds_addr(const void *p) {
   return (uint32_t)(uintptr_t)(lds_p)p;
 }
 __device__ __forceinline__ void glb_to_lds(const char *p, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
                "s"(__builtin_amdgcn_readfirstlane(lds))
-               : "memory");
+               : "memory", "m0");
 }
 // the same from a uniform address and a lane's offset.  The address may come out of a
 // vector register right in front of this (lane_at, or a spilled scalar's reload), and a
@@ -367,7 +366,7 @@ __device__ __forceinline__ void glb_to_lds(const char *p, uint32_t lds) {
 __device__ __forceinline__ void glb_to_lds(const char *base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
                "s"(__builtin_amdgcn_readfirstlane(lds))
-               : "memory");
+               : "memory", "m0");
 }
 // the address in lane l's registers
 __device__ __forceinline__ const char *lane_at(uint32_t lo, uint32_t hi, int l) {

@@ -1,7 +1,7 @@
 """The loads from global memory to LDS that are written in assembly hold by themselves: the
 wait states between a scalar address that a vector instruction writes and the load that
-reads it.  Read from the compiler's assembly of a small kernel that puts the least between
-the two (no GPU)."""
+reads it, and m0 named as written.  Read from the compiler's assembly of small kernels that
+put the least between the two (no GPU)."""
 import os
 import re
 import subprocess
@@ -21,6 +21,15 @@ __global__ void near(const uint32_t *at, int l, uint32_t *out) {
   wait_vm<0>();
   out[threadIdx.x] = lds[threadIdx.x];
 }
+// m0 holds the same before and behind
+__global__ void between(const char *p, const char *q, uint32_t *out) {
+  __shared__ __attribute__((aligned(256))) uint32_t lds[1024];
+  load_lds(make_rsrc(p, 1 << 20), lds, threadIdx.x * 16, 0);
+  glb_to_lds(q + threadIdx.x * 16, lds_addr(lds + 512));
+  load_lds(make_rsrc(p, 1 << 20), lds, threadIdx.x * 16, 4096);
+  wait_vm<0>();
+  out[threadIdx.x] = lds[threadIdx.x] + lds[512 + threadIdx.x];
+}
 """
 
 
@@ -38,7 +47,7 @@ def functions(tmp_path_factory):
     found, name = {}, None
     for line in (at / "k.s").read_text().splitlines():
         line = line.split(";")[0].strip()
-        m = re.match(r"_Z\d+(near)", line)
+        m = re.match(r"_Z\d+(near|between)", line)
         if m and line.endswith(":"):
             name = m[1]
         elif line.startswith("s_endpgm"):
@@ -69,3 +78,12 @@ def test_wait_states_before_a_scalar_address_is_read(functions):
     else:
         pytest.fail("no lane's read in front of the load")
     assert states >= 5
+
+
+def test_m0_is_named(functions):
+    """Each of the three loads has m0 set in front of it, the last one again to what it was."""
+    sets = 0
+    for s in functions["between"]:
+        if re.match(r"s_\w+ m0,", s):
+            sets += 1
+    assert sets == 3
