@@ -648,8 +648,9 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, fast=32.0, slo
     for contexts `factor` times as long as the trained one.  trained None: every angle is
     divided by the factor (rot_scale 1).  Else, with the trained length: pairs that turn
     more than `fast` times over it keep their angle, pairs that turn less than `slow`
-    times have it divided, those between a mixture linear in the pair's number; rot_scale
-    = 0.1 ln(factor) + 1."""
+    times have it divided, those between a mixture linear in the pair's number from the last
+    whole one with `fast` turns (or 0) to the first with `slow` (or rot - 1: it may lie behind
+    the last pair); rot_scale = 0.1 ln(factor) + 1."""
     import math
 
     import torch
@@ -665,8 +666,9 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, fast=32.0, slo
         raise ValueError("fast > slow > 0, trained >= 1 and base > 1")
     # the pair that turns n times over the trained length
     pair = lambda n: rot * math.log(trained / (n * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
-    lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot // 2 - 1)
+    lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot - 1)
     far = ((i - lo) / max(hi - lo, 0.001)).clamp(0, 1)
+    far[i > pair(slow)] = 1.0   # (pair 0 too, where none turns so often)
     return (inv * (1 - far) + inv / factor * far).float(), 0.1 * math.log(factor) + 1.0
 
 

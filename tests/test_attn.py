@@ -173,3 +173,26 @@ def test_frequencies_by_parts():
     assert abs(s - (0.1 * np.log(4) + 1)) < 1e-12
     assert np.allclose(ratio[turns > 40], 1) and np.allclose(ratio[turns < 0.8], 0.25)
     assert (np.diff(ratio) <= 1e-6).all() and ((ratio > 0.26) & (ratio < 0.99)).any()
+
+
+@pytest.mark.parametrize("rot,base,factor,trained,fast,slow", [
+    (128, 1e4, 4.0, 131072, 32.0, 1.0),        # the last pair turns 2.4 times: between the two
+    (64, 1e4, 8.0, 200000, 32.0, 1.0), (128, 500.0, 2.0, 65536, 32.0, 1.0),
+    (128, 1e6, 4.0, 32768, 32.0, 1.0), (64, 1e4, 40.0, 4096, 32.0, 1.0), (8, 10.0, 4.0, 3000, 32.0, 1.0),
+    (128, 1e4, 4.0, 100, 32.0, 1.0), (64, 1e4, 4.0, 5, 32.0, 1.0), (2, 1e4, 4.0, 100, 32.0, 1.0)])
+def test_frequencies_of_any_trained_length(rot, base, factor, trained, fast, slow):
+    """Pairs that turn more than `fast` times keep their angle, those that turn less than
+    `slow` times have it divided, also where no pair, or every one, is beyond a border; the
+    mixture between is linear in the pair's number and ends where `slow` turns are, whether
+    or not a pair is there."""
+    np = pytest.importorskip("numpy")
+    got = bd.rope_frequencies(rot, base, factor, trained, fast, slow)[0].double().numpy()
+    plain = base ** (-2.0 * np.arange(rot // 2) / rot)
+    turns = trained * plain / (2 * np.pi)
+    # the pair's number at which n turns are: base^(-2 i / rot) trained / 2 pi = n
+    at = [rot / 2 * np.log(trained / (2 * np.pi * n)) / np.log(base) for n in (fast, slow)]
+    lo, hi = max(np.floor(at[0]), 0), min(np.ceil(at[1]), rot - 1)
+    far = np.where(turns < slow, 1, np.clip((np.arange(rot // 2) - lo) / max(hi - lo, 1e-3), 0, 1))
+    assert np.allclose(got, plain * (1 - far) + plain / factor * far, rtol=2.0 ** -22, atol=0)
+    assert np.allclose(got[turns < slow], plain[turns < slow] / factor, rtol=2.0 ** -22, atol=0)
+    assert np.allclose(got[turns > fast], plain[turns > fast], rtol=2.0 ** -22, atol=0)
