@@ -431,7 +431,7 @@ base_status base_kv_append(const base_rope *R, const base_kv_cache *C, const bas
  *   Hq     a multiple of C->Hk, at most BASE_MAX_HEADS; rows * Hq at most BASE_MAX_HEAD_ROWS
  *   out    may be q
  *   lse    [rows][Hq] fp32, or NULL
- *   scale  finite;  window >= 0 (0: none)
+ *   scale  finite;  window >= 0 (0, or as many tokens as a row of the table holds: none)
  *   ws     at least base_attention_workspace_bytes of the same cache, batch (its n_seq,
  *          max_pages and max_q), rows and Hq; 256-B aligned.  Nothing in it needs a
  *          value; calls that overlap need one each. */

@@ -830,7 +830,9 @@ base_status base_paged_attention(const base_kv_cache *C, const base_kv_batch *S,
   const KvCache c = kv_cache(C);
   const KvBatch b = kv_batch(S);
   const int n_cu = device_cus();
-  const AttnCall a{C->dtype == BASE_BF16, C->D, Hq, window, scale, rows, hq, ho, lse};
+  // a window that no sequence can fill is none (and the kernels' differences stay in 32 bits)
+  const int seen = window >= S->max_pages * C->page_size ? 0 : window;
+  const AttnCall a{C->dtype == BASE_BF16, C->D, Hq, seen, scale, rows, hq, ho, lse};
   if (ws_bytes < attn_ws_bytes(a.bf16, a.D, Hq, c, b, rows, n_cu)) return BASE_ERR_WORKSPACE;
   HIP_TRY(launch_attn(a, c, b, ws, n_cu, (hipStream_t)stream));
   return BASE_OK;

@@ -248,7 +248,7 @@ void k_attn_few(AttnArgs a) {
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
       const int r = 16 * c + n;
-      pos[c] = r < sg.n ? sg.q.pos0 + over(sg.r0 + min(r, sg.n - 1), a.by_G) : -1;
+      pos[c] = r < sg.n ? max(sg.q.pos0 + over(sg.r0 + min(r, sg.n - 1), a.by_G), -1) : -1;
     }
     const int pmin = sg.q.pos0 + over(sg.r0, a.by_G), pmax = sg.q.pos0 + over(sg.r0 + sg.n - 1, a.by_G);
     f32x4 acc[NR][DT];
@@ -566,7 +566,7 @@ void k_attn_many(AttnArgs a) {
     const int lo = sg.keys.lo, hi = sg.keys.hi;
     const int r = 32 * wave + n, pr = sg.r0 + min(r, sg.n - 1), tok = over(pr, a.by_G);
     const bool mine = 32 * wave < sg.n;
-    const int pos = r < sg.n ? sg.q.pos0 + tok : -1;
+    const int pos = r < sg.n ? max(sg.q.pos0 + tok, -1) : -1;
     // positions of the wavefront's first and last row
     const int wlast = min(32 * wave + 31, sg.n - 1);
     const int pmin = sg.q.pos0 + over(sg.r0 + 32 * wave, a.by_G), pmax = sg.q.pos0 + over(sg.r0 + max(wlast, 0), a.by_G);
@@ -648,7 +648,7 @@ void k_attn_many(AttnArgs a) {
     else wait_vm<0>();
     lds_barrier();
     // blocks ta .. tb - 1: those that some row of the wavefront sees
-    const int ta = a.window > 0 ? max(0, (max(pmin - a.window + 1, 0)) / BK - sg.k0) : 0;
+    const int ta = a.window > 0 ? max(0, max(max(pmin, 0) - a.window + 1, 0) / BK - sg.k0) : 0;
     const int tb = mine ? min(blocks, (max(pmax, -1) + BK) / BK - sg.k0) : 0;
     auto seen_block = [&](int t) { return t >= ta && t < tb; };
     // the stage of block t + 1 is there (all wavefronts': each waits for its own loads)
@@ -976,7 +976,7 @@ Plan plan(bool bf16, int D, int Hq, const KvCache &c, const KvBatch &b, long lon
     if (!l.whole) p.bytes += ((size_t)l.W * sizeof(AttnPart) + 255) & ~(size_t)255;
   };
   // (the lengths are on the device: this is the most that the products can come to)
-  const double keys = (double)((long long)b.max_pages << c.shift), span = window > 0 ? window + b.max_q : keys;
+  const double keys = (double)((long long)b.max_pages << c.shift), span = window > 0 ? (double)window + b.max_q : keys;
   const double flops = 4.0 * p.dp * Hq * rows * (span < keys ? span : keys);
   const bool small = !bf16 || most <= FEW_ROWS || flops <= (p.dp == 256 ? FEW_FLOPS_256 : b.n_seq == 1 ? FEW_FLOPS_ONE : FEW_FLOPS);
   // (tiles of 16 rows hold a token's heads: beside k_attn_many few sequences have more than

@@ -89,7 +89,7 @@ __device__ __forceinline__ KeyRange attn_keys(const AttnArgs &a, const AttnSeq &
   KeyRange k;
   const int p0 = q.pos0 + over(r0, a.by_G), p1 = q.pos0 + over(r0 + n - 1, a.by_G);
   k.hi = max(p1 + 1, 0);
-  k.lo = a.window > 0 ? max(p0 - a.window + 1, 0) : 0;
+  k.lo = a.window > 0 ? max(max(p0, 0) - a.window + 1, 0) : 0;
   return k;
 }
 

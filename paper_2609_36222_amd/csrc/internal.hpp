@@ -519,7 +519,7 @@ hipError_t launch_heads(bool bf16, const RopeArgs &R, long long rows, const int3
 // (attn.hip) attention of the batch's new tokens over the cache; scale: of the products
 struct AttnCall {
   bool bf16;
-  int D, Hq, window;   // window 0: none
+  int D, Hq, window;   // window 0: none; less than the table has tokens
   float scale;
   long long rows;
   HeadRows q, o;

@@ -457,3 +457,34 @@ def test_starts_that_fall_and_rise(bd):
         out = bd.paged_attention(q.cuda(), cache, batch)
         want, bound, *_ = U.attend(b, q, 0.125)
         U.near(out, want, bound, BF)
+
+
+def call(bd, b, q, cache, batch, window=0):
+    out, lse = bd.paged_attention(q, cache, batch, window=window, return_lse=True)
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 100, 2 ** 30])
+def test_windows_wider_than_any_table(bd, dtype, window):
+    """A window that no sequence can fill is none: the same bits, small calls and large ones,
+    with more new tokens than tokens among them."""
+    lens = [(9, 4), (200, 130), (1, 77), (40, 900), (2, 0)]
+    for b in [U.Batch(lens, 2, 64, 16, dtype, seed=17)] + ([wide(lens, 2, 128, 16, 8, seed=17)] if dtype is BF else []):
+        b.fill()
+        q = b.queries(8)
+        check(bd, b, 8, window=window, q=q)
+        cache, batch = b.device(bd)
+        for got, want in zip(call(bd, b, q.cuda(), cache, batch, window), call(bd, b, q.cuda(), cache, batch)):
+            assert torch.equal(got, want)
+
+
+def test_a_wide_window_takes_a_large_calls_kernel(bd):
+    """The kernel of a large call does not hang on how no window is said."""
+    b = U.Batch([(600, 700)], 2, 128, 16, BF, seed=18)
+    b.fill()
+    q = b.queries(16).cuda()
+    assert 4 * 128 * 16 * 600 * 700 > 2e9
+    cache, batch = b.device(bd)
+    for got, want in zip(call(bd, b, q, cache, batch, 2 ** 31 - 1), call(bd, b, q, cache, batch)):
+        assert torch.equal(got, want)
