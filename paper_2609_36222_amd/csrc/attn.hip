@@ -464,14 +464,14 @@ void k_attn_few(AttnArgs a) {
       } else {
         const int pr = sg.r0 + r, tok = over(pr, a.by_G), head = sg.hk * a.G + pr - tok * a.G;
         const long long row = sg.q.first + tok;
-        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+        const float inv = inverse(sum);
         T *out = (T *)a.o.p + row * a.o.row + head * a.o.head;
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
           const int at = attn_at<T, 16, DP>(t, lane);
           if (at < D) put4(out + at, piece(c, t) * inv);
         }
-        if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+        if (a.lse && g == 0) a.lse[row * a.Hq + head] = log_sum(top, sum);
       }
     }
     if (!more) break;
@@ -759,7 +759,7 @@ void k_attn_many(AttnArgs a) {
       } else {
         const int head = sg.hk * a.G + pr - tok * a.G;
         const long long row = sg.q.first + tok;
-        const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+        const float inv = inverse(l);
         uint16_t *out = (uint16_t *)a.o.p + row * a.o.row + head * a.o.head;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -768,7 +768,7 @@ void k_attn_many(AttnArgs a) {
             if (32 * t + 2 * e + d0 < D)
               put4(out + 32 * t + 2 * e + d0,
                    f32x4{acc[t][e] * inv, acc[t][e + 1] * inv, acc[t][e + 2] * inv, acc[t][e + 3] * inv});
-        if (a.lse && h == 0) a.lse[row * a.Hq + head] = l > 0.0f ? (m + __log2f(l)) * LN2 : -INFINITY;
+        if (a.lse && h == 0) a.lse[row * a.Hq + head] = log_sum(m, l);
       }
     }
   }
@@ -784,9 +784,9 @@ __device__ __forceinline__ void join_store(const AttnArgs &a, const AttnPart &p,
   if (r >= p.n) return;
   const int pr = p.r0 + r, tok = over(pr, a.by_G), head = p.head + pr - tok * a.G, at = attn_at<T, ROWS, DP>(q, lane_id());
   const long long row = p.token + tok;
-  const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+  const float inv = inverse(sum);
   if (at < a.D) put4((T *)a.o.p + row * a.o.row + head * a.o.head + at, o * inv);
-  if (a.lse && at == 0) a.lse[row * a.Hq + head] = sum > 0.0f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+  if (a.lse && at == 0) a.lse[row * a.Hq + head] = log_sum(top, sum);
 }
 // Sums of parts k0, k0 + step, .. (NB at a time, their loads together) of the pieces q0 ..
 // q0 + PB - 1, which are of the same rows; r: the lane's

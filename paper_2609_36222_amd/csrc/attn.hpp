@@ -376,4 +376,12 @@ __device__ __forceinline__ const char *lane_at(uint32_t lo, uint32_t hi, int l) 
 
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.44269504088896341f;
 
+// What a row's sum comes to: 0 and -infinity where it has no key, NaN where the sum is NaN
+__device__ __forceinline__ float inverse(float sum) {
+  return sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+}
+__device__ __forceinline__ float log_sum(float top, float sum) {
+  return sum > 0.0f ? (top + __log2f(sum)) * LN2 : (sum == 0.0f ? -INFINITY : sum);
+}
+
 }  // namespace basek

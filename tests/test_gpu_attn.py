@@ -488,3 +488,53 @@ def test_a_wide_window_takes_a_large_calls_kernel(bd):
     cache, batch = b.device(bd)
     for got, want in zip(call(bd, b, q, cache, batch, 2 ** 31 - 1), call(bd, b, q, cache, batch)):
         assert torch.equal(got, want)
+
+
+def paths(dtype):
+    """Batches whose units are done whole, in parts, and (16 bits) in the kernel of chunks."""
+    lens = [(1, 20), (3, 45), (1, 33)]
+    yield U.Batch(lens, 2, 64, 16, dtype, seed=21)
+    yield U.Batch([(1, 3000), (4, 1500), (1, 1)], 2, 64, 16, dtype, seed=22)
+    if dtype is BF:
+        yield wide([(70, 300), (64, 64), (1, 700)], 2, 64, 16, 8, seed=23)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("what", ["q", "k", "v", "q inf", "k inf"])
+def test_nan_and_infinity_where_tokens_see_them(bd, dtype, what):
+    """A row whose softmax is NaN says so in out and lse (-infinity is a row without keys); the
+    other rows keep their results (to the bit where no score changes: when a tile's maxima
+    are raised hangs on all its rows)."""
+    bad = float("inf") if "inf" in what else float("nan")
+    for b in paths(dtype):
+        b.fill()
+        q = b.queries(8)
+        cache, batch = b.device(bd)
+        clean, clean_lse = call(bd, b, q.cuda(), cache, batch)
+        want, bound, wl, lb = U.attend(b, q, 0.125)
+        n = b.lens[1][0]
+        hit = torch.zeros(b.rows, 8, dtype=torch.bool)        # rows and heads that see it
+        if what[0] == "q":
+            q[2, 5, 7] = bad
+            hit[2, 5] = True
+        else:
+            # the second sequence's first token, of the second key head
+            page, slot = b.slots(1, 0, 1)
+            t = cache.tensors["kv".index(what[0])]
+            t[page.cuda(), slot.cuda(), 1, 7] = bad
+            hit[b.starts[1]:b.starts[1] + n, 4:] = True
+        out, lse = call(bd, b, q.cuda(), cache, batch)
+        hit = hit.cuda()
+        keep = (~hit).cpu().numpy()
+        U.near(out[~hit], want[keep], bound[keep], dtype)
+        assert (np.abs(lse[~hit].double().cpu().numpy() - wl[keep]) <= lb[keep]).all()
+        if what == "v":
+            assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+            assert out[hit][:, 7].isnan().all() and torch.equal(lse[hit], clean_lse[hit])
+            assert torch.equal(out[hit][:, :7], clean[hit][:, :7]) and torch.equal(out[hit][:, 8:], clean[hit][:, 8:])
+        elif what == "q" or what == "k":
+            assert out[hit].isnan().all() and lse[hit].isnan().all()
+        else:
+            # an infinity's products are +inf (NaN) or -inf (no weight, or where all are, no keys)
+            assert torch.equal(out[hit].isnan().any(1), lse[hit].isnan())
+            assert lse[hit].isnan().any() and not (lse[hit] == float("inf")).any()
