@@ -4,6 +4,7 @@
 
 #include "common.hpp"
 #include "internal.hpp"
+#include "seq.hpp"
 
 namespace basek {
 
@@ -186,9 +187,10 @@ struct AttnWork {
   __device__ void load(int from) {
     s0 = from;
     const int lane = lane_id();
-    begin = min(max(q0, 0), a.rows);
-    stop = min(max(q1, begin), a.rows);
-    kv = min(max(len, 0), a.b.max_pages << a.c.shift);
+    const SeqRows rows = seq_rows(q0, q1, len, a.rows, a.b.max_pages << a.c.shift);
+    begin = rows.begin;
+    stop = rows.stop;
+    kv = rows.kv;
     if (from + lane >= a.b.n_seq) stop = begin;
     if (a.b.n_seq > WAVE) fetch(from + WAVE < a.b.n_seq ? from + WAVE : 0);
     const AttnSeq sq = attn_seq(a, begin, stop, kv);

@@ -194,10 +194,11 @@ void k_heads(HeadsArgs a) {
   if constexpr (CACHE) {
     const int s = seq_of_row(a.b, (int)row);
     if (s < 0) return;           // behind the last sequence
-    const int start = a.b.q_start[s], stop = a.b.q_start[s + 1], kv = a.b.kv_len[s];
-    const long long at = (long long)kv - stop + row;   // row - start new tokens before it
+    const SeqRows own = seq_rows(a.b.q_start[s], a.b.q_start[s + 1], a.b.kv_len[s], (int)a.rows,
+                                 a.b.max_pages << a.c.shift);
+    const long long at = (long long)own.kv - own.stop + row;   // (below 0: more new tokens than tokens)
     position = (int)at;
-    if (at >= 0 && at < kv && row >= start && (at >> a.c.shift) < a.b.max_pages) {
+    if (at >= 0 && at < own.kv && row >= own.begin) {   // (at < kv: within the table's row)
       const int page = a.b.table[s * a.b.table_ld + (at >> a.c.shift)];
       if ((unsigned)page < (unsigned)a.c.n_pages) {
         const long long slot = at & ((1LL << a.c.shift) - 1);

@@ -300,3 +300,38 @@ def test_whole_block(bd):
                                     method.Experts(inp["w13"], inp["w2"], True))
         step = h1.float().cpu().numpy() + ref["y"]
         assert np.abs(h2.float().cpu().numpy() - step).max() <= 2e-2 + 2.0 ** -8 * np.abs(step).max()
+
+
+@pytest.mark.parametrize("starts,lens,width", [
+    ([0, 5], [10], 2),                       # the last start beyond the rows (a padded batch)
+    ([-3, 2, 9], [6, 40], 3),                # and the first before them
+    ([0, 1, 4], [9, 50], 3),                 # a length beyond the table's row
+    ([0, 2, 4], [-4, 2 ** 31 - 1], 2), ([0, 2, 2 ** 31 - 1], [7, 2 ** 31 - 1], 2)])
+def test_starts_and_lengths_are_taken_within_their_bounds(bd, starts, lens, width):
+    """Append and attention take the same starts and lengths, those of 0 .. rows and 0 .. the
+    table's row: the calls give what they give with these written out."""
+    g = np.random.default_rng(5)
+    rows, D, ps = 4, 32, 16
+    n_seq = len(lens)
+    table = cuda(np.arange(n_seq * width, dtype=np.int32).reshape(n_seq, width))
+    r = bd.Rope(D, BF, cuda(U.frequencies(D)))
+    qkv = make(g, rows, 6, D, BF).cuda()
+    old = make(g, n_seq * width * 2 * ps, 1, D, BF).view(2, n_seq * width, ps, 1, D).cuda()
+    within = np.clip(starts, 0, rows)
+    got = []
+    for q_start, kv_len in ((starts, lens), (within, np.clip(lens, 0, width * ps))):
+        k, v = old.clone()
+        cache = bd.KVCache(k, v)
+        batch = bd.KVBatch(table, *(cuda(np.array(t, np.int64).astype(np.int32)) for t in (q_start, kv_len)), rows)
+        q = torch.full((rows, 4, D), 7.0, dtype=BF, device="cuda")
+        bd.base_kv_append(r, cache, batch, qkv[:, :4], qkv[:, 4:5], qkv[:, 5:], q)
+        out, lse = bd.paged_attention(q, cache, batch, return_lse=True)
+        got.append((q, k, v, out, lse))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    # and these are the tokens' places: the last of the sequence's new rows in its last slot
+    for s in range(n_seq):
+        kv, n = int(np.clip(lens[s], 0, width * ps)), int(within[s + 1] - within[s])
+        for i in range(max(n - kv, 0), n):
+            at = kv - n + i
+            assert torch.equal(got[0][2][s * width + at // ps, at % ps, 0], qkv[within[s] + i, 5])
