@@ -24,10 +24,12 @@ namespace {
 
 constexpr int HEAD_WAVES = 4;
 constexpr int MAX_PAIRS = MAX_HEAD_D / 2;
+// rows of a launch, a wavefront each: it has less than 2^32 work-items in all
+constexpr long long LAUNCH_ROWS = 1LL << 25;
 
 struct HeadsArgs {
   RopeArgs r;
-  long long rows;
+  long long rows, row0, row1;   // the call's; the launch's: row0 .. row1 - 1
   const int32_t *pos;
   int Hq, Hk, heads, lph, passes, split;   // heads: with the values; split: wavefronts a row
   HeadRows q, qo, k, ko, v;
@@ -155,10 +157,9 @@ __global__ __launch_bounds__(HEAD_WAVES * WAVE)
 void k_heads(HeadsArgs a) {
   __shared__ float cs[HEAD_WAVES][2][MAX_PAIRS];
   const int w = wave_id_u(), lane = lane_id();
-  const long long job = (long long)blockIdx.x * HEAD_WAVES + w;
-  const long long row = job / a.split;
-  const int part = (int)(job - row * a.split);
-  if (row >= a.rows) return;
+  const int job = blockIdx.x * HEAD_WAVES + w, at_row = job / a.split, part = job - at_row * a.split;
+  const long long row = a.row0 + at_row;
+  if (row >= a.row1) return;
   const int D = a.r.D, rot = a.r.rot, half = rot / 2;
 
   const int lph = a.lph, per = WAVE / lph, li = lane & (lph - 1), sub = lane / lph;
@@ -368,7 +369,7 @@ hipError_t launch_heads(bool bf16, const RopeArgs &R, long long rows, const int3
   a.lph = 1;
   while (a.lph < run_lanes(mode, R.D, R.rot, a.r.interleaved)) a.lph *= 2;
   a.passes = (a.heads * a.lph + WAVE - 1) / WAVE;
-  const long long want = (16384 + rows - 1) / rows;
+  const long long want = (16384 + rows - 1) / rows;   // (1 in calls of several launches)
   a.split = (int)(want < a.passes ? want : a.passes);
   a.q = q;
   a.qo = q_out;
@@ -379,14 +380,19 @@ hipError_t launch_heads(bool bf16, const RopeArgs &R, long long rows, const int3
     a.c = *cache;
     a.b = *batch;
   }
-  const dim3 grid((unsigned)((rows * a.split + HEAD_WAVES - 1) / HEAD_WAVES));
 #define BASE_HEADS(T, MODE)                                                                         \
   launch_k(cache ? k_heads<T, MODE, true> : k_heads<T, MODE, false>, grid, dim3(HEAD_WAVES *WAVE), 0, \
            st, a)
-  if (bf16) { if (mode == 1) BASE_HEADS(uint16_t, 1); else if (mode == 2) BASE_HEADS(uint16_t, 2); else BASE_HEADS(uint16_t, 0); }
-  else { if (mode == 1) BASE_HEADS(float, 1); else if (mode == 2) BASE_HEADS(float, 2); else BASE_HEADS(float, 0); }
+  for (a.row0 = 0; a.row0 < rows; a.row0 = a.row1) {
+    a.row1 = a.row0 + LAUNCH_ROWS < rows ? a.row0 + LAUNCH_ROWS : rows;
+    const dim3 grid((unsigned)(((a.row1 - a.row0) * a.split + HEAD_WAVES - 1) / HEAD_WAVES));
+    if (bf16) { if (mode == 1) BASE_HEADS(uint16_t, 1); else if (mode == 2) BASE_HEADS(uint16_t, 2); else BASE_HEADS(uint16_t, 0); }
+    else { if (mode == 1) BASE_HEADS(float, 1); else if (mode == 2) BASE_HEADS(float, 2); else BASE_HEADS(float, 0); }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
 #undef BASE_HEADS
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace basek

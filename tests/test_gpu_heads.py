@@ -335,3 +335,56 @@ def test_starts_and_lengths_are_taken_within_their_bounds(bd, starts, lens, widt
         for i in range(max(n - kv, 0), n):
             at = kv - n + i
             assert torch.equal(got[0][2][s * width + at // ps, at % ps, 0], qkv[within[s] + i, 5])
+
+
+MANY = (1 << 26) + 5      # a wavefront a row: more than one launch can have
+
+
+def test_more_rows_than_a_launch_has(bd):
+    """The rows of one call against the same in parts that a launch holds."""
+    inv = cuda(U.frequencies(8))
+    r = bd.Rope(8, BF, inv)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    q = torch.randn(MANY, 1, 8, generator=gen, dtype=BF, device="cuda")
+    pos = torch.arange(MANY, dtype=torch.int32, device="cuda")
+    got = torch.zeros_like(q)
+    bd.base_head_rope(r, pos, q, None, got, None)
+    step = 1 << 24
+    for at in range(0, MANY, step):
+        part = slice(at, min(at + step, MANY))
+        want = bd.head_rope(r, pos[part], q[part])[0]
+        assert torch.equal(got[part], want), at
+    want, bound = U.rotate(q[-7:].double().cpu().numpy(), None, pos[-7:].cpu().numpy(), U.frequencies(8), 1.0, False, 1e-6)
+    # (a turn's fraction of 2^26 positions: fp64, as near as any)
+    U.near(got[-7:], want, bound, BF)
+
+
+def test_append_of_more_rows_than_a_launch_has(bd):
+    """Three sequences, the second over the launches' border; most of its tokens have negative
+    numbers and stay out of the cache.  Rows of no sequence are left."""
+    r = bd.Rope(8, BF, cuda(U.frequencies(8)))
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    qkv = torch.randn(MANY, 3, 8, generator=gen, dtype=BF, device="cuda")
+    q, k, v = qkv[:, :1], qkv[:, 1:2], qkv[:, 2:]
+    starts, lens = [5, 8, (1 << 26) + 1, MANY - 1], [3, 100, 50]
+    kc, vc = (torch.full((3 * 7, 16, 1, 8), 3.0, dtype=BF, device="cuda") for _ in range(2))
+    table = torch.arange(21, dtype=torch.int32, device="cuda").view(3, 7)
+    batch = bd.KVBatch(table, cuda(np.array(starts, np.int32)), cuda(np.array(lens, np.int32)), 1 << 26)
+    got = torch.full((MANY, 1, 8), 7.0, dtype=BF, device="cuda")
+    bd.base_kv_append(r, bd.KVCache(kc, vc), batch, q, k, v, got)
+    assert (got[:5] == 7).all() and (got[-1] == 7).all()
+    pos = torch.cat([torch.arange(n - (b - a), n, dtype=torch.int32) for a, b, n in zip(starts, starts[1:], lens)]).cuda()
+    step = 1 << 24
+    for at in range(5, MANY - 1, step):
+        part = slice(at, min(at + step, MANY - 1))
+        assert torch.equal(got[part], bd.head_rope(r, pos[at - 5:part.stop - 5], q[part])[0]), at
+    for s, (stop, n) in enumerate(zip(starts[1:], lens)):
+        rows = slice(max(stop - n, starts[s]), stop)
+        new = rows.stop - rows.start
+        turned = bd.head_rope(r, pos[rows.start - 5:rows.stop - 5], k[rows])[0]
+        for c, want in ((kc, turned), (vc, v[rows])):
+            have = c.view(3, 112, 1, 8)[s]
+            assert torch.equal(have[n - new:n], want)
+            assert (have[:n - new] == 3).all() and (have[n:] == 3).all()
