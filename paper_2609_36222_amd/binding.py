@@ -692,10 +692,15 @@ def _rows_heads(t, what):
     return n, H
 
 
-def _here():
-    """(the library, torch, the current GPU): what a call on heads looks up once."""
+def _here(*made):
+    """(the library, torch, the current GPU): what a call on heads looks up once.  made: its
+    Rope, KVCache and KVBatch, whose tensors have to lie there."""
     import torch
-    return load(), torch, torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+    for m in made:
+        if m.dev != dev:
+            raise ValueError(f"{type(m).__name__}: made on GPU {m.dev}, the current one is {dev}")
+    return load(), torch, dev
 
 
 def _stream_on(torch, stream, dev):
@@ -725,7 +730,7 @@ class Rope:
         import torch
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise ValueError("dtype: fp32 or bf16")
-        dev = _device()
+        self.dev = dev = _device()
         rot = 0 if inv_freq is None else 2 * inv_freq.numel()
         for t, n, what in ((inv_freq, rot // 2, "inv_freq"), (q_gain, D, "q_gain"), (k_gain, D, "k_gain")):
             if t is not None and (t.dtype is not torch.float32 or t.shape != (n,) or not t.is_contiguous()
@@ -745,7 +750,7 @@ class KVCache:
 
     def __init__(self, k, v):
         import torch
-        dev = _device()
+        self.dev = dev = _device()
         for t, what in ((k, "k"), (v, "v")):
             if (t.dim() != 4 or t.shape != k.shape or t.dtype is not k.dtype or t.get_device() != dev
                     or t.dtype not in (torch.bfloat16, torch.float32) or t.stride(3) != 1):
@@ -765,7 +770,7 @@ class KVBatch:
     contents may change between calls."""
 
     def __init__(self, table, q_start, kv_len, max_q):
-        dev = _device()
+        self.dev = dev = _device()
         n = kv_len.shape[0] if kv_len.dim() == 1 else -1
         if table.dim() != 2 or table.shape[0] != n or (table.stride(1) != 1 and table.shape[1] > 1):
             raise ValueError("table: int32 [n_seq, pages], adjacent entries")
@@ -784,7 +789,7 @@ def base_head_rope(rope: Rope, positions, q, k, q_out, k_out, stream=None):
     [rows] (None where nothing rotates)."""
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q and q_out, k and k_out: both or neither, and one of the two")
-    lib, torch, dev = _here()
+    lib, torch, dev = _here(rope)
     dt, D = rope.torch_dtype, rope.D
     qa = ka = _NO_HEADS
     n = None
@@ -817,7 +822,7 @@ def base_kv_append(rope: Rope, cache: KVCache, batch: KVBatch, q, k, v, q_out, p
     """The new tokens' k [rows, Hk, D], normalised and rotated, and v into the cache; q
     [rows, Hq, D] the same to q_out.  positions: int32 [rows], or None: the tokens' numbers
     in their sequences."""
-    lib, torch, dev = _here()
+    lib, torch, dev = _here(rope, cache, batch)
     dt, D, Hk = rope.torch_dtype, rope.D, cache.Hk
     n, Hq = _rows_heads(q, "q")
     if positions is not None:
@@ -839,7 +844,7 @@ def base_paged_attention(cache: KVCache, batch: KVBatch, q, out, ws, scale=None,
                          stream=None):
     """out [rows, Hq, D] (and lse [rows, Hq] fp32) of q over the cache; scale None: 1 /
     sqrt(D); ws: a uint8 tensor of attention_workspace_bytes."""
-    lib, torch, dev = _here()
+    lib, torch, dev = _here(cache, batch)
     dt, D = cache.torch_dtype, cache.D
     n, Hq = _rows_heads(q, "q")
     if lse is not None:

@@ -196,3 +196,28 @@ def test_frequencies_of_any_trained_length(rot, base, factor, trained, fast, slo
     assert np.allclose(got, plain * (1 - far) + plain / factor * far, rtol=2.0 ** -22, atol=0)
     assert np.allclose(got[turns < slow], plain[turns < slow] / factor, rtol=2.0 ** -22, atol=0)
     assert np.allclose(got[turns > fast], plain[turns > fast], rtol=2.0 ** -22, atol=0)
+
+
+def test_handles_of_another_gpu():
+    """A rotation, cache or batch whose tensors lie on another GPU than the current one is
+    refused before anything is enqueued: the kernels would read that GPU's addresses here."""
+    torch = pytest.importorskip("torch")
+
+    def made(cls, dev):
+        m = cls.__new__(cls)
+        m.dev, m.D, m.Hk, m.torch_dtype, m.desc = dev, 64, 2, torch.bfloat16, None
+        return m
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    x = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    kinds = (bd.Rope, bd.KVCache, bd.KVBatch)
+    for other in kinds:
+        r, c, b = (made(k, here + (k is other)) for k in kinds)
+        said = f"{other.__name__}: made on GPU {here + 1}, the current one is {here}"
+        with pytest.raises(ValueError, match=said):
+            bd.base_kv_append(r, c, b, x, x, x, x)
+        if other is bd.Rope:
+            with pytest.raises(ValueError, match=said):
+                bd.base_head_rope(r, None, x, None, x, None)
+        else:
+            with pytest.raises(ValueError, match=said):
+                bd.base_paged_attention(c, b, x, x, x)
