@@ -555,3 +555,45 @@ def test_few_rows_keep_their_exponentials_in_two_parts(bd, lens, D, window):
     want, bound, *_ = U.attend(b, q, D ** -0.5, window)
     b.dtype = BF
     U.near(out, want, bound + 2.0 ** -16 * max(float(v.abs().max()) for v in b.v), BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_largest_table(bd, dtype):
+    """A table of 2^30 tokens a sequence: the units' costs are counted in several blocks."""
+    ps, width = 65536, 1 << 14
+    g = np.random.default_rng(31)
+    lens = [(int(g.integers(0, 4)), int(g.integers(4, 700))) for _ in range(30)] + [(60, 5000), (1, 3333), (300, 300)]
+    b = U.Batch(lens, 4, 8, ps, dtype, seed=31, extra=width - 1)
+    assert b.width == width and len(lens) * 4 * (1 << 30) // 64 > 10 ** 9
+    b.fill()
+    check(bd, b, 8)
+
+
+@pytest.mark.parametrize("width", [2, 40])
+def test_the_most_sequences(bd, width):
+    """65536 sequences, of one or no new token."""
+    n = 65536
+    lens = [(int(i % 3 != 1), 1 + i % 17) for i in range(n)]
+    b = U.Batch(lens, 1, 8, 16, BF, seed=32, extra=width - 2)
+    b.fill()
+    check(bd, b, 1)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout", ["pages", "tokens", "heads"])
+def test_views_of_one_cache_and_of_a_wider_table(bd, dtype, layout):
+    """Keys and values side by side in one tensor (page by page, token by token, head by head),
+    the table a view of a wider one's first entries."""
+    b = U.Batch([(1, 700), (40, 130), (3, 33)], 2, 72, 32, dtype, seed=33)
+    b.fill()
+    q = b.queries(6)
+    at = {"pages": 1, "tokens": 2, "heads": 3}[layout]
+    both = torch.stack([b.kc, b.vc], at).contiguous().cuda()
+    k, v = both.unbind(at)
+    put = lambda t: torch.from_numpy(t).cuda()  # noqa: E731
+    table = np.full((3, 500), -1, np.int32)
+    table[:, :b.width] = b.table
+    batch = bd.KVBatch(put(table)[:, :b.width], put(b.starts), put(np.array([kv for _, kv in b.lens], np.int32)), 40)
+    out = bd.paged_attention(q.cuda(), bd.KVCache(k, v), batch)
+    want, bound, *_ = U.attend(b, q, 72 ** -0.5)
+    U.near(out, want, bound, dtype)

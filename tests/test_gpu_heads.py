@@ -388,3 +388,51 @@ def test_append_of_more_rows_than_a_launch_has(bd):
             have = c.view(3, 112, 1, 8)[s]
             assert torch.equal(have[n - new:n], want)
             assert (have[:n - new] == 3).all() and (have[n:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_captured_step(bd, dtype):
+    """Append and attention captured together and replayed token by token, the program writing
+    the next token's heads and the lengths between the replays, with eager work of its own."""
+    g = np.random.default_rng(41)
+    D, Hq, Hk, ps, n_seq, steps = 64, 8, 2, 16, 5, 20
+    r = bd.Rope(D, dtype, cuda(U.frequencies(D)), True, 1.0, *(cuda(t) for t in gains(g, D, True)))
+    start = np.array([0, 15, 16, 47, 130], np.int32)
+    pages = n_seq * 10
+    table = cuda(g.permutation(pages).astype(np.int32).reshape(n_seq, 10))
+    first = torch.randn(2, pages, ps, Hk, D, dtype=dtype, device="cuda")
+    runs = []
+    for captured in (False, True):
+        k, v = first.clone()
+        cache = bd.KVCache(k, v)
+        kv_len = cuda(start + 1)
+        batch = bd.KVBatch(table, torch.arange(n_seq + 1, dtype=torch.int32, device="cuda"), kv_len, 1)
+        qkv = torch.empty(n_seq, Hq + 2 * Hk, D, dtype=dtype, device="cuda")
+        q, out = (torch.empty(n_seq, Hq, D, dtype=dtype, device="cuda") for _ in range(2))
+        ws = torch.empty(bd.attention_workspace_bytes(cache, batch, n_seq, Hq), dtype=torch.uint8, device="cuda")
+
+        def step():
+            bd.base_kv_append(r, cache, batch, qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:], q)
+            bd.base_paged_attention(cache, batch, q, out, ws)
+        if captured:
+            qkv.zero_()
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+                step()
+            torch.cuda.synchronize()
+        h = np.random.default_rng(42)
+        got = []
+        for i in range(steps):
+            qkv.copy_(make(h, n_seq, Hq + 2 * Hk, D, dtype).cuda())
+            graph.replay() if captured else step()
+            got.append((out.clone(), q.clone()))
+            kv_len += 1
+            if i % 5 == 4:
+                torch.cuda.synchronize()
+        runs.append((got, k, v))
+    (eager, ke, ve), (replayed, kr, vr) = runs
+    for a, b in zip(eager, replayed):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert torch.equal(ke, kr) and torch.equal(ve, vr)
